@@ -17,6 +17,11 @@ C ABI:
     hc_aggregate  sum of sketches and OR of bitmaps over W workers (section 3)
     hc_decode     Algorithm 1 phase II: parallel peeling + median estimate
 
+and the training-side operators around them (include/hc_train.h, see train.py):
+
+    hc_embed, hc_embed_grad, hc_embed_grad_rows   embedding lookup and its gradient
+    hc_orthogonalise      Newton-Schulz orthogonalisation of a weight's update
+
 The library must be built (``python -m paper_2402_07529_amd.build``); there is
 no fallback: importing this package without libhc.so raises.
 """
@@ -356,3 +361,10 @@ def alloc_workspace(p: hc_params, max_support: int = 0, device="cuda"):
     import torch
     _, _, w = hc_sizes(p, max_support)
     return torch.empty(w, dtype=torch.uint8, device=device)
+
+
+from .train import (  # noqa: E402  (it takes this module's helpers)
+    FIXED_POINT, HC_T_BF16, HC_T_F16, HC_T_F32, HC_T_I32, MUON, TRAIN_EXPORTS,
+    alloc_embed_workspace, alloc_orthogonalise_workspace, hc_embed, hc_embed_grad,
+    hc_embed_grad_bytes, hc_embed_grad_rows, hc_embed_params, hc_orthogonalise,
+    hc_orthogonalise_bytes, hc_orthogonalise_params)

@@ -14,9 +14,9 @@
 
 namespace hc {
 
-namespace {
+static thread_local std::string g_last_error;
 
-thread_local std::string g_last_error;
+void clear_error() { g_last_error.clear(); }
 
 hc_status fail(hc_status s, const char* msg) {
     g_last_error = msg;
@@ -29,6 +29,8 @@ hc_status fail_hip(hipError_t e, const char* where) {
 }
 
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+
+namespace {
 
 // Validate the public params and convert them to the kernels' form.
 hc_status to_geo(const hc_params* p, Geo* g) {

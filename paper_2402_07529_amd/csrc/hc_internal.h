@@ -6,6 +6,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "../../include/hc.h"
+
 namespace hc {
 
 // Validated geometry in the form the kernels take it.
@@ -31,6 +33,13 @@ struct Geo {
     uint32_t bloom_rows;
     uint64_t bwords;
 };
+
+// The calling thread's error message: set by a failing call (fail returns its
+// status), cleared on entry to every call.
+hc_status fail(hc_status s, const char* msg);
+hc_status fail_hip(hipError_t e, const char* where);
+void clear_error();
+bool aligned(const void* p, uintptr_t a);  // a: a power of two
 
 struct DeviceInfo {
     int cus;          // compute units

@@ -138,11 +138,25 @@ def _check(status: int, where: str):
         raise HCError(status, where, (_lib.hc_last_error() or b"").decode())
 
 
+_current_stream = None
+
+
 def _stream(stream):
-    import torch
-    if stream is None:
-        stream = torch.cuda.current_stream()
-    return ctypes.c_void_p(stream.cuda_stream)
+    """The stream's handle (None: the current device's current stream, asked for without a
+    Stream object around it where torch offers that: 0.3 us a call instead of 2.7)."""
+    global _current_stream
+    if stream is not None:
+        return ctypes.c_void_p(stream.cuda_stream)
+    if _current_stream is None:
+        import torch
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        device = getattr(torch._C, "_cuda_getDevice", None)
+        if raw is not None and device is not None:
+            torch.cuda.init()
+            _current_stream = lambda: raw(device())  # noqa: E731
+        else:
+            _current_stream = lambda: torch.cuda.current_stream().cuda_stream  # noqa: E731
+    return ctypes.c_void_p(_current_stream())
 
 
 def _ptr(t, name, dtype=None, numel=None):

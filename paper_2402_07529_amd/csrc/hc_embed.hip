@@ -4,10 +4,12 @@
 // The gradient of out[i] = scale * W[t_i] is dW[v] = scale * sum over t_i = v of
 // dOut[i].  Sorting the pairs (t_i, i) by id, stably, puts the terms of one row
 // next to each other in token order.  The sorted list is cut into chunks of
-// equal length whatever the ids are, so a frequent id is shared by many
-// workgroups: a run that lies inside one chunk is summed and stored at once,
-// a run that crosses chunks leaves one partial sum per chunk and a second
-// launch joins those in chunk order.  Every order is fixed by the ids alone.
+// equal length whatever the ids are.  A run of equal ids is summed by the chunk
+// it begins in, which follows it into the next chunk; a run that goes on past
+// that (a frequent id) is shared by all chunks it reaches, one partial sum each,
+// and a second launch joins those in chunk order.  Every order is fixed by the
+// ids alone.  A dense gradient's zeros are written by workgroups of the sorting
+// launches that have no pairs to sort.
 #include "hc_device.h"
 #include "hc_internal.h"
 #include "hc_train_internal.h"
@@ -44,14 +46,14 @@ template <typename T> __device__ __forceinline__ void unpack(v4u w, float* v) {
 }
 
 // nv (1 .. kVec<T>) elements at p, the others 0
-template <typename T> __device__ __forceinline__ void load_vec(const T* p, int nv, float* v) {
-    if (nv == kVec<T>) {
-        const typename Wide<T>::V w = *reinterpret_cast<const typename Wide<T>::V*>(p);
-        unpack<T>((v4u)w, v);
-    } else {
+template <typename T> __device__ __forceinline__ v4u load_raw(const T* p, int nv) {
+    if (nv == kVec<T>) return *reinterpret_cast<const typename Wide<T>::V*>(p);
+    typedef T TV __attribute__((ext_vector_type(kVec<T>)));
+    TV t = {};
 #pragma unroll
-        for (int j = 0; j < kVec<T>; j++) v[j] = j < nv ? (float)p[j] : 0.0f;
-    }
+    for (int j = 0; j < kVec<T>; j++)
+        if (j < nv) t[j] = p[j];
+    return __builtin_bit_cast(v4u, t);
 }
 
 // ---- lookup ----------------------------------------------------------------------
@@ -61,9 +63,10 @@ __device__ __forceinline__ bool valid_id(ID id, uint32_t vocab) {
     return id >= 0 && (uint64_t)id < vocab;
 }
 
-// A group of g lanes (a power of two up to a wave) takes one token's row, or 64
-// lanes' worth of columns of it, one 16-byte vector a lane.
-template <typename T, typename ID>
+// A unit is one token's row, or 64 lanes' worth of columns of it; a group of g
+// lanes (a power of two up to a wave) takes U units, one 16-byte vector a lane
+// each, all loads before the first store.
+template <typename T, typename ID, int U>
 __global__ __launch_bounds__(kBlock) void embed_kernel(const T* __restrict__ table,
                                                        const ID* __restrict__ ids,
                                                        T* __restrict__ out, uint64_t units,
@@ -72,32 +75,52 @@ __global__ __launch_bounds__(kBlock) void embed_kernel(const T* __restrict__ tab
                                                        uint32_t log2g, uint32_t slabs,
                                                        float scale) {
     constexpr int VEC = kVec<T>;
-    const uint64_t first = ((uint64_t)blockIdx.x * kBlock + threadIdx.x) >> log2g;
-    const uint64_t step = ((uint64_t)gridDim.x * kBlock) >> log2g;
-    for (uint64_t unit = first; unit < units; unit += step) {
-        const uint64_t i = unit / slabs;
-        const uint32_t slab = (uint32_t)(unit - i * slabs);
-        const uint32_t col = ((slab << log2g) + (threadIdx.x & ((1u << log2g) - 1u))) * VEC;
-        if (col >= dim) continue;
-        const int nv = (int)min((uint32_t)VEC, dim - col);
-        const ID id = ids[i];
-        float v[VEC];
+    const uint32_t groups = kBlock >> log2g, group = threadIdx.x >> log2g;
+    const uint32_t lane_col = (threadIdx.x & ((1u << log2g) - 1u)) * VEC;
+    for (uint64_t base = (uint64_t)blockIdx.x * groups * U; base < units;
+         base += (uint64_t)gridDim.x * groups * U) {
+        ID id[U];
+        uint64_t row[U];
+        uint32_t col[U];
+        v4u w[U];
 #pragma unroll
-        for (int j = 0; j < VEC; j++) v[j] = 0.0f;
-        if (valid_id(id, vocab)) {
-            load_vec<T>(table + (uint64_t)id * table_ld + col, nv, v);
-#pragma unroll
-            for (int j = 0; j < VEC; j++) v[j] *= scale;
+        for (int u = 0; u < U; u++) {
+            const uint64_t unit = base + u * groups + group;
+            row[u] = slabs == 1 ? unit : unit / slabs;
+            col[u] = unit < units ? (((uint32_t)(unit - row[u] * slabs) << log2g) * VEC + lane_col) : dim;
+            id[u] = unit < units ? ids[row[u]] : (ID)-1;
         }
-        T* q = out + i * out_ld + col;
-        if (nv == VEC) {
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            w[u] = v4u{};
+            if (col[u] < dim && valid_id(id[u], vocab))
+                w[u] = load_raw<T>(table + (uint64_t)id[u] * table_ld + col[u],
+                                   (int)min((uint32_t)VEC, dim - col[u]));
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            if (col[u] >= dim) continue;
+            const bool valid = valid_id(id[u], vocab);
+            float v[VEC];
+            unpack<T>(w[u], v);
+            T* q = out + row[u] * out_ld + col[u];
+            const int nv = (int)min((uint32_t)VEC, dim - col[u]);
             typedef T TV __attribute__((ext_vector_type(VEC)));
             TV t;
 #pragma unroll
-            for (int j = 0; j < VEC; j++) t[j] = (T)v[j];
-            *reinterpret_cast<typename Wide<T>::V*>(q) = __builtin_bit_cast(v4u, t);
-        } else {
-            for (int j = 0; j < nv; j++) q[j] = (T)v[j];
+            for (int j = 0; j < VEC; j++) {
+                float y = valid ? v[j] * scale : 0.0f;
+                // the product in fp32 first: not fused with the rounding to fp16
+                if constexpr (sizeof(T) == 2) asm("" : "+v"(y));
+                t[j] = (T)y;
+            }
+            if (nv == VEC) {
+                *reinterpret_cast<typename Wide<T>::V*>(q) = __builtin_bit_cast(v4u, t);
+            } else {
+#pragma unroll
+                for (int j = 0; j < VEC; j++)
+                    if (j < nv) q[j] = t[j];
+            }
         }
     }
 }
@@ -118,24 +141,62 @@ hipError_t embed_typed(const hc_embed_params& p, const void* table, const void* 
     const uint64_t vectors = (p.dim + kVec<T> - 1) / kVec<T>;
     const uint32_t log2g = group_log2(vectors);
     const uint64_t slabs = (vectors + (1ull << log2g) - 1) >> log2g;
-    const uint64_t units = p.count * slabs;
-    const uint64_t per_block = kBlock >> log2g;
-    const uint64_t blocks = (units + per_block - 1) / per_block;
-    hipLaunchKernelGGL((embed_kernel<T, ID>), dim3((uint32_t)(blocks < kMaxGroups ? blocks : kMaxGroups)), dim3(kBlock), 0, s,
-                       static_cast<const T*>(table), static_cast<const ID*>(ids),
-                       static_cast<T*>(out), units, (uint32_t)p.vocab, (uint32_t)p.dim, p.table_ld,
-                       p.x_ld, log2g, (uint32_t)slabs, p.scale);
-    return hipGetLastError();
+    const uint64_t units = p.count * slabs, groups = kBlock >> log2g;
+    auto launch = [&](auto kernel, uint64_t per_block) {
+        const uint64_t blocks = (units + per_block - 1) / per_block;
+        hipLaunchKernelGGL(kernel, dim3((uint32_t)(blocks < kMaxGroups ? blocks : kMaxGroups)),
+                           dim3(kBlock), 0, s, static_cast<const T*>(table),
+                           static_cast<const ID*>(ids), static_cast<T*>(out), units,
+                           (uint32_t)p.vocab, (uint32_t)p.dim, p.table_ld, p.x_ld, log2g,
+                           (uint32_t)slabs, p.scale);
+        return hipGetLastError();
+    };
+    // four units a group once that still leaves every CU 16 workgroups
+    if (units >= groups * 4 * 4096) return launch(&embed_kernel<T, ID, 4>, groups * 4);
+    return launch(&embed_kernel<T, ID, 1>, groups);
 }
+
+// ---- gradient: zeros -------------------------------------------------------------
+
+// A dense gradient's zeros, cut into pieces of about 16 KiB, a workgroup each
+// (plain stores, short-lived workgroups: 7.9 TB/s on 200 MB, 6.0 on 4.3 GB; a
+// grid of 4096 striding workgroups 6.6 and 4.4, nontemporal stores 5.8 and 5.9).
+constexpr uint64_t kPieceBytes = 16384;
+
+struct Zeros {
+    char* dst;            // NULL: none
+    uint64_t rows;        // rows of row_bytes at ld_bytes; one where they lie back to back
+    uint64_t row_bytes, ld_bytes;
+    uint64_t per;         // rows a piece (rows > 1)
+    uint64_t pieces;
+    uint64_t first;       // this launch's: [first, first + its extra workgroups)
+};
+
+__device__ __forceinline__ void zero_bytes(char* p, uint64_t bytes, uint32_t at, uint32_t step) {
+    typedef uint32_t V __attribute__((ext_vector_type(4), aligned(2)));
+    const V zero = {};
+    for (uint64_t i = at; i < bytes / 16; i += step) reinterpret_cast<V*>(p)[i] = zero;
+    if (at < (bytes & 15) / 2) reinterpret_cast<uint16_t*>(p + (bytes & ~15ull))[at] = 0;
+}
+
+__device__ __forceinline__ void zero_piece(const Zeros& z, uint64_t piece) {
+    if (z.rows == 1) {
+        const uint64_t b = piece * kPieceBytes;
+        zero_bytes(z.dst + b, min(kPieceBytes, z.row_bytes - b), threadIdx.x, blockDim.x);
+        return;
+    }
+    const uint64_t r0 = piece * z.per, r1 = min(r0 + z.per, z.rows);
+    for (uint64_t r = r0 + (threadIdx.x >> 6); r < r1; r += blockDim.x >> 6)
+        zero_bytes(z.dst + r * z.ld_bytes, z.row_bytes, threadIdx.x & 63, 64);
+}
+
+__global__ __launch_bounds__(kBlock) void zero_kernel(Zeros z) { zero_piece(z, z.first + blockIdx.x); }
 
 // ---- gradient: sort --------------------------------------------------------------
 
-// Stable radix sort of the pairs (id, token) by id in digits of up to 9 bits:
-// per pass every workgroup counts its tile's digits, the counts are scanned per
-// digit over the workgroups, and every workgroup moves its tile's pairs to
-// their places.  Ids that add nothing get the key `vocab` and end up last.
+// Stable radix sort of the pairs (id, token) by id in digits of up to 9 bits.
+// Ids that add nothing get the key `vocab` and end up last.
 constexpr int kItems = 8;
-constexpr uint32_t kTile = kBlock * kItems;
 constexpr uint32_t kMaxBins = 512;
 
 struct Pair {
@@ -159,116 +220,208 @@ struct FromPairs {
     __device__ Pair get(uint32_t i) const { return pairs[i]; }
 };
 
-template <typename SRC>
-__global__ __launch_bounds__(kBlock) void digit_count_kernel(SRC src, uint32_t count,
-                                                             uint32_t shift, uint32_t bins,
-                                                             uint32_t* __restrict__ hist) {
-    __shared__ uint32_t s_cnt[kMaxBins];
-    for (uint32_t b = threadIdx.x; b < bins; b += kBlock) s_cnt[b] = 0;
-    lds_barrier();
-    const uint32_t base = blockIdx.x * kTile;
-#pragma unroll
-    for (int it = 0; it < kItems; it++) {
-        const uint32_t i = base + it * kBlock + threadIdx.x;
-        if (i < count) atomicAdd(&s_cnt[(src.get(i).key >> shift) & (bins - 1u)], 1u);
+// Rank of this lane's digit among the wave's earlier lanes and, by its running
+// counts `cnt`, the wave's earlier pairs, so that equal keys keep their order.
+// Equal digits among the lanes are found with one ballot per digit bit.
+__device__ __forceinline__ uint32_t wave_rank(volatile uint32_t* cnt, uint32_t digit, bool live,
+                                              uint32_t log2bins) {
+    uint64_t same = __ballot(live);
+    for (uint32_t b = 0; b < log2bins; b++) {
+        const bool bit = (digit >> b) & 1u;
+        const uint64_t m = __ballot(bit);
+        same &= bit ? m : ~m;
     }
+    const uint32_t before = lanes_below(same);
+    const uint32_t seen = live ? cnt[digit] : 0u;
+    __builtin_amdgcn_wave_barrier();
+    if (live && before == 0) cnt[digit] = seen + (uint32_t)__popcll(same);
+    __builtin_amdgcn_wave_barrier();
+    return seen + before;
+}
+
+// Up to kSmallCount ids: one launch.  A pair's place is the number of pairs
+// before it in the order, and every workgroup counts that for `own` pairs (a
+// power of two) against all keys, held in LDS: its lanes are `own` pairs times
+// 1024 / own interleaved slices of the keys.  4099 ids, 25-bit keys: 5 us, where
+// a radix sort by one workgroup took 23.  The other workgroups write zeros.
+constexpr uint32_t kSmallThreads = 1024, kSmallCount = 8192;
+
+struct SmallSort {
+    uint32_t count, groups, log2own;
+    Pair* out;
+    uint32_t* crossing_count;
+    Zeros zeros;
+};
+
+template <typename ID>
+__global__ __launch_bounds__(kSmallThreads) void small_sort_kernel(FromIds<ID> src, SmallSort a) {
+    extern __shared__ __align__(16) uint32_t s_key[];  // padded to a multiple of 4 keys
+    __shared__ uint32_t s_rank[64];
+    if (blockIdx.x >= a.groups) {
+        zero_piece(a.zeros, a.zeros.first + blockIdx.x - a.groups);
+        return;
+    }
+    const uint32_t quads = (a.count + 3) / 4;
+    uint32_t keys[kSmallCount / kSmallThreads];
+#pragma unroll
+    for (uint32_t u = 0; u < kSmallCount / kSmallThreads; u++) {
+        const uint32_t k = u * kSmallThreads + threadIdx.x;
+        keys[u] = k < a.count ? src.get(k).key : ~0u;
+    }
+#pragma unroll
+    for (uint32_t u = 0; u < kSmallCount / kSmallThreads; u++) {
+        const uint32_t k = u * kSmallThreads + threadIdx.x;
+        if (k < quads * 4) s_key[k] = keys[u];
+    }
+    const uint32_t own = 1u << a.log2own;
+    if (threadIdx.x < own) s_rank[threadIdx.x] = 0;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.crossing_count = 0;
     lds_barrier();
-    for (uint32_t b = threadIdx.x; b < bins; b += kBlock)
-        hist[(uint64_t)b * gridDim.x + blockIdx.x] = s_cnt[b];
+    const uint32_t i = (blockIdx.x << a.log2own) + (threadIdx.x & (own - 1u));
+    const uint32_t key = i < a.count ? s_key[i] : 0u;
+    uint32_t before = 0;
+    for (uint32_t q = threadIdx.x >> a.log2own; q < quads; q += kSmallThreads >> a.log2own) {
+        const v4u k = *reinterpret_cast<const v4u*>(s_key + 4 * q);
+#pragma unroll
+        for (uint32_t j = 0; j < 4; j++)  // keys are below 2^31
+            before += k[j] < key + (4 * q + j < i ? 1u : 0u) ? 1u : 0u;
+    }
+    for (uint32_t d = own; d < 64; d <<= 1) before += __shfl_xor(before, d);
+    if (lane_id() < own) atomicAdd(&s_rank[lane_id()], before);
+    lds_barrier();
+    if (threadIdx.x < own && i < a.count) a.out[s_rank[threadIdx.x]] = Pair{key, i};
+}
+
+// More ids: per pass every workgroup counts its tile's digits, the counts are
+// scanned per digit over the workgroups, and every workgroup moves its tile's
+// pairs to their places.  Each launch's workgroups past its own write zeros.
+template <uint32_t THREADS, typename SRC>
+__global__ __launch_bounds__(THREADS) void digit_count_kernel(SRC src, uint32_t count,
+                                                              uint32_t groups, uint32_t shift,
+                                                              uint32_t bins,
+                                                              uint32_t* __restrict__ hist,
+                                                              uint32_t* __restrict__ crossing_count,
+                                                              Zeros zeros) {
+    __shared__ uint32_t s_cnt[kMaxBins];
+    if (blockIdx.x >= groups) {
+        zero_piece(zeros, zeros.first + blockIdx.x - groups);
+        return;
+    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) *crossing_count = 0;
+    const uint32_t base = blockIdx.x * (THREADS * kItems) + threadIdx.x;
+    uint32_t key[kItems];
+#pragma unroll
+    for (int it = 0; it < kItems; it++)
+        key[it] = base + it * THREADS < count ? src.get(base + it * THREADS).key : 0u;
+    for (uint32_t b = threadIdx.x; b < bins; b += THREADS) s_cnt[b] = 0;
+    lds_barrier();
+#pragma unroll
+    for (int it = 0; it < kItems; it++)
+        if (base + it * THREADS < count) atomicAdd(&s_cnt[(key[it] >> shift) & (bins - 1u)], 1u);
+    lds_barrier();
+    for (uint32_t b = threadIdx.x; b < bins; b += THREADS)
+        hist[(uint64_t)b * groups + blockIdx.x] = s_cnt[b];
 }
 
 // One wave a digit: hist[digit][workgroup] becomes the count in earlier
 // workgroups, total[digit] the count in all.
 __global__ __launch_bounds__(kBlock) void digit_scan_kernel(uint32_t* __restrict__ hist,
                                                             uint32_t* __restrict__ total,
-                                                            uint32_t bins, uint32_t groups) {
+                                                            uint32_t bins, uint32_t groups,
+                                                            Zeros zeros) {
+    const uint32_t own = (bins + kBlock / 64 - 1) / (kBlock / 64);
+    if (blockIdx.x >= own) {
+        zero_piece(zeros, zeros.first + blockIdx.x - own);
+        return;
+    }
     const uint32_t bin = blockIdx.x * (kBlock / 64) + (threadIdx.x >> 6);
     if (bin >= bins) return;
     const uint32_t lane = lane_id();
     uint32_t* h = hist + (uint64_t)bin * groups;
     uint32_t before = 0;
-    for (uint32_t g0 = 0; g0 < groups; g0 += 64) {
-        const uint32_t g = g0 + lane;
-        const uint32_t v = g < groups ? h[g] : 0u;
-        uint32_t x = v;
+    for (uint32_t g0 = 0; g0 < groups; g0 += 256) {  // 4 consecutive workgroups a lane
+        uint32_t v[4], sum = 0;
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const uint32_t g = g0 + lane * 4 + j;
+            v[j] = g < groups ? h[g] : 0u;
+            sum += v[j];
+        }
+        uint32_t x = sum;
         for (int d = 1; d < 64; d <<= 1) {
             const uint32_t y = __shfl_up(x, d);
             if (lane >= (uint32_t)d) x += y;
         }
-        if (g < groups) h[g] = before + x - v;
+        uint32_t at = before + x - sum;
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const uint32_t g = g0 + lane * 4 + j;
+            if (g < groups) h[g] = at;
+            at += v[j];
+        }
         before += __shfl(x, 63);
     }
     if (lane == 0) total[bin] = before;
 }
 
-// A wave takes its pairs in order, 64 at a time; equal digits among the lanes
-// are found with one ballot per digit bit, and the wave's own running counts in
-// LDS give every pair its rank, so equal keys keep their order.
-template <typename SRC>
-__global__ __launch_bounds__(kBlock) void digit_move_kernel(SRC src, uint32_t count,
-                                                            uint32_t shift, uint32_t log2bins,
-                                                            const uint32_t* __restrict__ hist,
-                                                            const uint32_t* __restrict__ total,
-                                                            Pair* __restrict__ out) {
-    constexpr uint32_t kWaves = kBlock / 64;
+template <uint32_t THREADS, typename SRC>
+__global__ __launch_bounds__(THREADS) void digit_move_kernel(SRC src, uint32_t count,
+                                                             uint32_t groups, uint32_t shift,
+                                                             uint32_t log2bins,
+                                                             const uint32_t* __restrict__ hist,
+                                                             const uint32_t* __restrict__ total,
+                                                             Pair* __restrict__ out, Zeros zeros) {
+    constexpr uint32_t kWaves = THREADS / 64, kPer = kMaxBins / THREADS > 0 ? kMaxBins / THREADS : 1;
     __shared__ uint32_t s_cnt[kWaves][kMaxBins];
     __shared__ uint32_t s_tmp[kWaves];
+    if (blockIdx.x >= groups) {
+        zero_piece(zeros, zeros.first + blockIdx.x - groups);
+        return;
+    }
     const uint32_t bins = 1u << log2bins;
     const uint32_t wave = threadIdx.x >> 6, lane = lane_id();
-    for (uint32_t b = threadIdx.x; b < kWaves * kMaxBins; b += kBlock)
-        (&s_cnt[0][0])[b] = 0;
-    lds_barrier();
+    const uint32_t base = blockIdx.x * (THREADS * kItems) + wave * (64 * kItems) + lane;
     Pair p[kItems];
     uint32_t rank[kItems];
-    const uint32_t base = blockIdx.x * kTile + wave * (64 * kItems) + lane;
-    volatile uint32_t* cnt = s_cnt[wave];
 #pragma unroll
-    for (int it = 0; it < kItems; it++) {
-        const uint32_t i = base + it * 64;
-        const bool live = i < count;
-        p[it] = live ? src.get(i) : Pair{0, 0};
-        const uint32_t digit = (p[it].key >> shift) & (bins - 1u);
-        uint64_t same = __ballot(live);
-        for (uint32_t b = 0; b < log2bins; b++) {
-            const bool bit = (digit >> b) & 1u;
-            const uint64_t m = __ballot(bit);
-            same &= bit ? m : ~m;
-        }
-        const uint32_t before = lanes_below(same);
-        const uint32_t seen = live ? cnt[digit] : 0u;
-        rank[it] = seen + before;
-        __builtin_amdgcn_wave_barrier();
-        if (live && before == 0) cnt[digit] = seen + (uint32_t)__popcll(same);
-        __builtin_amdgcn_wave_barrier();
-    }
-    lds_barrier();
-    // per digit: where this workgroup's pairs of earlier waves end
-    uint32_t t[2], first = 0;
+    for (int it = 0; it < kItems; it++)
+        p[it] = base + it * 64 < count ? src.get(base + it * 64) : Pair{0, 0};
+    // per digit: its pairs in all, and in earlier workgroups
+    uint32_t t[kPer], h[kPer], sum = 0;
 #pragma unroll
-    for (int j = 0; j < 2; j++) {
-        const uint32_t b = threadIdx.x * 2 + j;
+    for (uint32_t j = 0; j < kPer; j++) {
+        const uint32_t b = threadIdx.x * kPer + j;
         t[j] = b < bins ? total[b] : 0u;
+        h[j] = b < bins ? hist[(uint64_t)b * groups + blockIdx.x] : 0u;
+        sum += t[j];
     }
-    uint32_t all;
-    first = block_exclusive_scan(t[0] + t[1], s_tmp, &all);
+    for (uint32_t b = threadIdx.x; b < kWaves * kMaxBins; b += THREADS) (&s_cnt[0][0])[b] = 0;
+    lds_barrier();
 #pragma unroll
-    for (int j = 0; j < 2; j++) {
-        const uint32_t b = threadIdx.x * 2 + j;
+    for (int it = 0; it < kItems; it++)
+        rank[it] = wave_rank(s_cnt[wave], (p[it].key >> shift) & (bins - 1u),
+                                       base + it * 64 < count, log2bins);
+    lds_barrier();
+    uint32_t all;
+    uint32_t first = block_exclusive_scan(sum, s_tmp, &all);
+#pragma unroll
+    for (uint32_t j = 0; j < kPer; j++) {
+        const uint32_t b = threadIdx.x * kPer + j;
         if (b < bins) {
-            uint32_t at = first + (j ? t[0] : 0u) + hist[(uint64_t)b * gridDim.x + blockIdx.x];
+            uint32_t at = first + h[j];
             for (uint32_t w = 0; w < kWaves; w++) {
                 const uint32_t c = s_cnt[w][b];
                 s_cnt[w][b] = at;
                 at += c;
             }
         }
+        first += t[j];
     }
     lds_barrier();
 #pragma unroll
-    for (int it = 0; it < kItems; it++) {
-        const uint32_t i = base + it * 64;
-        if (i < count) out[s_cnt[wave][(p[it].key >> shift) & (bins - 1u)] + rank[it]] = p[it];
-    }
+    for (int it = 0; it < kItems; it++)
+        if (base + it * 64 < count)
+            out[s_cnt[wave][(p[it].key >> shift) & (bins - 1u)] + rank[it]] = p[it];
 }
 
 // ---- gradient: rows --------------------------------------------------------------
@@ -276,43 +429,53 @@ __global__ __launch_bounds__(kBlock) void digit_move_kernel(SRC src, uint32_t co
 // First positions of runs per chunk of the sorted pairs.
 __global__ __launch_bounds__(kBlock) void head_count_kernel(const Pair* __restrict__ pairs,
                                                             uint32_t count, uint32_t chunk,
-                                                            uint32_t chunks, uint32_t vocab,
+                                                            uint32_t vocab,
                                                             uint32_t* __restrict__ heads) {
-    const uint32_t c = blockIdx.x * (kBlock / 64) + (threadIdx.x >> 6);
-    if (c >= chunks) return;
     const uint32_t lane = lane_id();
-    const uint32_t i = c * chunk + lane;
+    const uint32_t i = (blockIdx.x * (kBlock / 64) + (threadIdx.x >> 6)) * 64 + lane;
     bool head = false;
-    if (lane < chunk && i < count) {
+    if (i < count) {
         const uint32_t key = pairs[i].key;
         head = key != vocab && (i == 0 || pairs[i - 1].key != key);
     }
     const uint64_t m = __ballot(head);
-    if (lane == 0) heads[c] = (uint32_t)__popcll(m);
+    if (i < count && lane % chunk == 0)
+        heads[i / chunk] = (uint32_t)__popcll((m >> lane) & (~0ull >> (64 - chunk)));
 }
 
 // heads[c] becomes the number of runs that begin before chunk c; *touched the
-// number of runs.
+// number of runs.  One workgroup, 16 chunks a lane at a time.
 __global__ __launch_bounds__(1024) void head_scan_kernel(uint32_t* __restrict__ heads,
                                                          uint32_t chunks,
                                                          uint32_t* __restrict__ touched) {
+    constexpr int N = 16;
     __shared__ uint32_t s_tmp[16];
     uint32_t before = 0;
-    for (uint32_t c0 = 0; c0 < chunks; c0 += 4096) {
-        uint32_t v[4], sum = 0;
+    for (uint64_t c0 = 0; c0 < chunks; c0 += 1024 * N) {
+        uint32_t v[N], sum = 0;
 #pragma unroll
-        for (int j = 0; j < 4; j++) {
-            const uint32_t c = c0 + threadIdx.x * 4 + j;
-            v[j] = c < chunks ? heads[c] : 0u;
-            sum += v[j];
+        for (int j = 0; j < N; j += 4) {
+            const uint64_t c = c0 + threadIdx.x * N + j;
+            v4u w = {};
+            if (c < chunks) w = *reinterpret_cast<const v4u*>(heads + c);  // padded to 16
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                v[j + k] = c + k < chunks ? w[k] : 0u;
+                sum += v[j + k];
+            }
         }
         uint32_t total;
         uint32_t at = before + block_exclusive_scan(sum, s_tmp, &total);
 #pragma unroll
-        for (int j = 0; j < 4; j++) {
-            const uint32_t c = c0 + threadIdx.x * 4 + j;
-            if (c < chunks) heads[c] = at;
-            at += v[j];
+        for (int j = 0; j < N; j += 4) {
+            const uint64_t c = c0 + threadIdx.x * N + j;
+            v4u w;
+#pragma unroll
+            for (int k = 0; k < 4; k++) {
+                w[k] = at;
+                at += v[j + k];
+            }
+            if (c < chunks) *reinterpret_cast<v4u*>(heads + c) = w;
         }
         before += total;
     }
@@ -356,52 +519,85 @@ __device__ __forceinline__ void store_sum(TO* p, int nv, const typename Sum<TO>:
         for (int j = 0; j < VEC; j++) t[j] = o[j];
         *reinterpret_cast<TV*>(p) = t;
     } else {
-        for (int j = 0; j < nv; j++) p[j] = o[j];
+#pragma unroll
+        for (int j = 0; j < VEC; j++)
+            if (j < nv) p[j] = o[j];
     }
 }
 
 struct SumArgs {
     const Pair* pairs;
-    uint32_t count, chunk, chunks, vocab, dim;
+    uint32_t count, chunk, chunks, vocab, dim, dim8;
     uint64_t x_ld, dst_ld;
     uint32_t log2g, slabs;
     float scale, fixed;
     bool accumulate;
-    // rows
+    // by rows; heads: runs that begin before each chunk (NULL, for up to
+    // kSmallCount pairs: counted by the sums, which then set *touched)
     uint32_t* rows;
     const uint32_t* heads;
+    uint32_t* touched;
     uint64_t cap;
-    // runs that cross chunks: (chunk they begin in, rank), and their partial
-    // sums, two of dim elements a chunk: of the run it begins with, of the run
-    // it ends with
+    // shared runs: (chunk they begin in, rank), and their partial sums, two of
+    // dim8 (dim rounded up to 8) elements a chunk: of the run it begins with, of
+    // the run it ends with
     uint32_t* crossing_count;
     uint2* crossing;
     void* partial;
 };
 
-// One chunk's columns of one slab (a group of lanes).
+// One chunk's columns of one slab (a group of lanes).  A run of pairs covers
+// boundary c if it holds the pairs on both sides of chunk c's start.  A run that
+// covers two boundaries is shared by the chunks that it reaches; any other is
+// summed whole by the chunk it begins in.
 template <typename TI, typename TO, bool ROWS>
 __device__ __forceinline__ void sum_chunk(const SumArgs& a, const TI* __restrict__ x,
-                                          TO* __restrict__ dst, uint64_t unit) {
+                                          TO* __restrict__ dst, uint32_t c, uint32_t slab,
+                                          uint32_t heads) {
     typedef typename Sum<TO>::A A;
     constexpr int VEC = kVec<TI>;
-    constexpr int U = 4;
-    const uint32_t c = (uint32_t)(unit / a.slabs);
-    const uint32_t slab = (uint32_t)(unit - (uint64_t)c * a.slabs);
+    constexpr int U = 8;
     const uint32_t col = ((slab << a.log2g) + (threadIdx.x & ((1u << a.log2g) - 1u))) * VEC;
     if (col >= a.dim) return;
     const int nv = (int)min((uint32_t)VEC, a.dim - col);
-    const uint32_t start = c * a.chunk, end = min(start + a.chunk, a.count);
-    uint32_t cur = a.pairs[start].key;
+    const uint32_t C = a.chunk, n = a.count;
+    uint32_t start = c * C;
+    const uint32_t end = min(start + C, n);
+    // the keys around the chunk, all asked for at once
+    const uint32_t k_first = a.pairs[start].key, k_last = a.pairs[end - 1].key;
+    const uint32_t k_before = c > 0 ? a.pairs[start - 1].key : a.vocab;
+    const uint32_t k_earlier = c > 1 ? a.pairs[start - C - 1].key : a.vocab;
+    const uint32_t k_next = end < n ? a.pairs[end].key : a.vocab;
+    const uint32_t k_later = (uint64_t)end + C < n ? a.pairs[end + C].key : a.vocab;
+    if (k_first == a.vocab) return;
+    uint32_t rank = heads;
+    bool begins = k_before != k_first;
+    if (!begins) {
+        const bool shared = k_earlier == k_first || (end < n && k_next == k_first);
+        if (!shared) {  // an earlier chunk sums it: on to the next run
+            uint32_t lo = start, hi = end;  // first position with another key
+            while (lo < hi) {
+                const uint32_t mid = (lo + hi) / 2;
+                if (a.pairs[mid].key == k_first) lo = mid + 1; else hi = mid;
+            }
+            if (lo == end) return;
+            start = lo;
+            begins = true;
+        } else if constexpr (ROWS) {
+            rank--;
+        }
+    }
+    uint32_t cur = begins && start != c * C ? a.pairs[start].key : k_first;
     if (cur == a.vocab) return;
-    bool begins = start == 0 || a.pairs[start - 1].key != cur;
-    uint32_t rank = 0;
-    if constexpr (ROWS) rank = a.heads[c] - (begins ? 0u : 1u);
-    A* partial = static_cast<A*>(a.partial) + (uint64_t)c * 2 * a.dim + col;
+    // the last run goes on: shared if it covers the boundary after the next too,
+    // else followed to its end
+    const bool goes_on = end < n && k_next == k_last && k_last != a.vocab;
+    const bool covers = goes_on && (k_later == k_last || (k_first == k_last && !begins));
+    const uint32_t limit = goes_on && !covers ? min(end + C, n) : end;
+
     A acc[VEC];
 #pragma unroll
     for (int j = 0; j < VEC; j++) acc[j] = 0;
-
     auto flush = [&](bool finishes) {
         if (begins && finishes) {
             if constexpr (ROWS) {
@@ -413,36 +609,72 @@ __device__ __forceinline__ void sum_chunk(const SumArgs& a, const TI* __restrict
                 store_sum<TO, VEC>(dst + (uint64_t)cur * a.dst_ld + col, nv, acc, a.accumulate);
             }
         } else {
-            A* q = partial + (begins ? a.dim : 0u);
-            for (int j = 0; j < nv; j++) q[j] = acc[j];
+            A* q = static_cast<A*>(a.partial) + ((uint64_t)c * 2 + (begins ? 1 : 0)) * a.dim8 + col;
+#pragma unroll
+            for (int j = 0; j < VEC; j++) q[j] = acc[j];
             if (begins && col == 0) a.crossing[atomicAdd(a.crossing_count, 1u)] = make_uint2(c, rank);
         }
     };
-
-    for (uint32_t i = start; i < end; i += U) {
+    bool done = false;
+    for (uint32_t i = start; i < limit && !done; i += U) {
         Pair p[U];
-        float v[U][VEC];
-#pragma unroll
-        for (int u = 0; u < U; u++) p[u] = i + u < end ? a.pairs[i + u] : Pair{a.vocab, 0};
-#pragma unroll
-        for (int u = 0; u < U; u++)
-            if (p[u].key != a.vocab) load_vec<TI>(x + (uint64_t)p[u].pos * a.x_ld + col, nv, v[u]);
+        v4u w[U];
 #pragma unroll
         for (int u = 0; u < U; u++) {
-            if (p[u].key == a.vocab) break;
+            p[u] = i + u < limit ? a.pairs[i + u] : Pair{a.vocab, 0};
+            if (i + u >= end && p[u].key != k_last) p[u].key = a.vocab;
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++)
+            if (p[u].key != a.vocab) w[u] = load_raw<TI>(x + (uint64_t)p[u].pos * a.x_ld + col, nv);
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            if (p[u].key == a.vocab) {
+                done = true;
+                break;
+            }
             if (p[u].key != cur) {
                 flush(true);
                 cur = p[u].key;
                 begins = true;
-                rank++;
+                if constexpr (ROWS) rank++;
 #pragma unroll
                 for (int j = 0; j < VEC; j++) acc[j] = 0;
             }
+            float v[VEC];
+            unpack<TI>(w[u], v);
 #pragma unroll
-            for (int j = 0; j < VEC; j++) acc[j] += Sum<TO>::term(v[u][j], a.scale, a.fixed);
+            for (int j = 0; j < VEC; j++) acc[j] += Sum<TO>::term(v[j], a.scale, a.fixed);
         }
     }
-    flush(end == a.count || a.pairs[end].key != cur);
+    flush(!covers);
+}
+
+// Runs that begin at positions below `hi` (all lanes of a workgroup, at most
+// kSmallCount positions), added to *sum: two pairs a lane and load, 8 loads in
+// flight.
+__device__ __forceinline__ void count_begins(const SumArgs& a, uint32_t hi, uint32_t* sum) {
+    uint32_t found = 0;
+    for (uint32_t i0 = 0; i0 < hi; i0 += kBlock * 2 * 8) {
+        v4u w[8];
+        uint32_t before[8];
+#pragma unroll
+        for (uint32_t u = 0; u < 8; u++) {
+            const uint32_t i = i0 + (u * kBlock + threadIdx.x) * 2;  // the list is padded to 256 bytes
+            w[u] = i < hi ? *reinterpret_cast<const v4u*>(a.pairs + i) : v4u{};
+            before[u] = lane_id() == 0 && i > 0 && i < hi ? a.pairs[i - 1].key : a.vocab;
+        }
+#pragma unroll
+        for (uint32_t u = 0; u < 8; u++) {
+            const uint32_t i = i0 + (u * kBlock + threadIdx.x) * 2;
+            const uint32_t up = __shfl_up(w[u].z, 1);
+            const uint32_t prev = lane_id() == 0 ? before[u] : up;
+            if (i < hi && w[u].x != a.vocab && (i == 0 || prev != w[u].x)) found++;
+            if (i + 1 < hi && w[u].z != a.vocab && w[u].z != w[u].x) found++;
+        }
+    }
+    for (int d = 32; d > 0; d >>= 1) found += __shfl_xor(found, d);
+    if (lane_id() == 0 && found) atomicAdd(sum, found);
 }
 
 template <typename TI, typename TO, bool ROWS>
@@ -450,12 +682,40 @@ __global__ __launch_bounds__(kBlock) void segment_sum_kernel(SumArgs a, const TI
                                                              TO* __restrict__ dst) {
     const uint64_t units = (uint64_t)a.chunks * a.slabs;
     const uint64_t step = ((uint64_t)gridDim.x * kBlock) >> a.log2g;
-    for (uint64_t unit = ((uint64_t)blockIdx.x * kBlock + threadIdx.x) >> a.log2g; unit < units;
-         unit += step)
-        sum_chunk<TI, TO, ROWS>(a, x, dst, unit);
+    const uint64_t first = ((uint64_t)blockIdx.x * kBlock) >> a.log2g;
+    __shared__ uint32_t s_heads[kBlock + 1];  // before the workgroup's chunks, then in each
+    const bool count_heads = ROWS && a.heads == nullptr;  // then step covers all units
+    const uint32_t c0 = (uint32_t)(first / a.slabs);
+    if (count_heads) {
+        for (uint32_t i = threadIdx.x; i <= kBlock; i += kBlock) s_heads[i] = 0;
+        lds_barrier();
+        const uint32_t c1 = (uint32_t)(min(first + (kBlock >> a.log2g), units) - 1) / a.slabs;
+        const uint32_t lo = c0 * a.chunk, hi = min((c1 + 1) * a.chunk, a.count);
+        count_begins(a, lo, &s_heads[0]);
+        for (uint32_t i = lo + threadIdx.x; i < hi; i += kBlock) {
+            const uint32_t key = a.pairs[i].key;
+            if (key != a.vocab && (i == 0 || a.pairs[i - 1].key != key))
+                atomicAdd(&s_heads[1 + i / a.chunk - c0], 1u);
+        }
+        lds_barrier();
+        if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) {
+            uint32_t all = 0;
+            for (uint32_t k = 0; k <= c1 - c0 + 1; k++) all += s_heads[k];
+            *a.touched = all;
+        }
+    }
+    for (uint64_t unit = first + (threadIdx.x >> a.log2g); unit < units; unit += step) {
+        const uint32_t c = (uint32_t)(unit / a.slabs);
+        uint32_t heads = 0;
+        if (count_heads)
+            for (uint32_t k = 0; k <= c - c0; k++) heads += s_heads[k];
+        else if (ROWS)
+            heads = a.heads[c];
+        sum_chunk<TI, TO, ROWS>(a, x, dst, c, (uint32_t)(unit - (uint64_t)c * a.slabs), heads);
+    }
 }
 
-// Joins the partial sums of the runs that cross chunks: a workgroup takes one
+// Joins the partial sums of the shared runs: a workgroup takes one
 // run's columns, its groups of lanes a contiguous share of the run's chunks
 // each, in order, and the groups' sums are added in order.
 constexpr int kJoinBlock = 512;
@@ -496,14 +756,23 @@ __global__ __launch_bounds__(kJoinBlock) void segment_join_kernel(SumArgs a,
         A acc[VEC];
 #pragma unroll
         for (int j = 0; j < VEC; j++) acc[j] = 0;
-        const A* base = static_cast<const A*>(a.partial) + (uint64_t)c * 2 * a.dim + col;
-#pragma unroll 4
-        for (uint32_t k = lo; k < hi; k++) {
-            // item 0: what chunk c ends with; item k: what chunk c + k begins with
-            const A* q = base + (k == 0 ? (uint64_t)a.dim : (uint64_t)k * 2 * a.dim);
+        if (nv > 0) {
+            typedef A AV __attribute__((ext_vector_type(VEC)));
+            const A* base = static_cast<const A*>(a.partial) + (uint64_t)c * 2 * a.dim8 + col;
+            for (uint32_t k = lo; k < hi; k += 8) {
+                AV w[8];
 #pragma unroll
-            for (int j = 0; j < VEC; j++)
-                if (j < nv) acc[j] += q[j];
+                for (uint32_t u = 0; u < 8; u++)
+                    // item 0: what chunk c ends with; item k: what chunk c + k begins with
+                    if (k + u < hi)
+                        w[u] = *reinterpret_cast<const AV*>(
+                            base + (k + u == 0 ? (uint64_t)a.dim8 : (uint64_t)(k + u) * 2 * a.dim8));
+#pragma unroll
+                for (uint32_t u = 0; u < 8; u++)
+                    if (k + u < hi)
+#pragma unroll
+                        for (int j = 0; j < VEC; j++) acc[j] += w[u][j];
+            }
         }
 #pragma unroll
         for (int j = 0; j < VEC; j++) s_sum[threadIdx.x * VEC + j] = acc[j];
@@ -526,30 +795,7 @@ __global__ __launch_bounds__(kJoinBlock) void segment_join_kernel(SumArgs a,
     }
 }
 
-// ---- gradient: zeros -------------------------------------------------------------
-
-// rows x row_bytes zeros at a stride of ld_bytes (one row where the rows lie
-// back to back), 16 bytes a lane where everything is 16-byte aligned.
-template <typename V>
-__global__ __launch_bounds__(kBlock) void zero_rows_kernel(char* __restrict__ dst, uint64_t rows,
-                                                           uint64_t row_bytes, uint64_t ld_bytes) {
-    const uint64_t per = row_bytes / sizeof(V);
-    const V zero = {};
-    if (rows == 1) {
-        for (uint64_t i = (uint64_t)blockIdx.x * kBlock + threadIdx.x; i < per;
-             i += (uint64_t)gridDim.x * kBlock)
-            reinterpret_cast<V*>(dst)[i] = zero;
-        return;
-    }
-    for (uint64_t r = blockIdx.x; r < rows; r += gridDim.x)
-        for (uint64_t i = threadIdx.x; i < per; i += kBlock)
-            reinterpret_cast<V*>(dst + r * ld_bytes)[i] = zero;
-}
-
-__global__ void clear_word_kernel(uint32_t* a, uint32_t* b) {
-    if (a) *a = 0;
-    if (b) *b = 0;
-}
+__global__ void clear_word_kernel(uint32_t* a) { *a = 0; }
 
 // ---- layout and launches ---------------------------------------------------------
 
@@ -562,8 +808,21 @@ uint32_t chunk_for(const hc_embed_params& p) {
     return chunk;
 }
 
+// Digits of the keys 0 .. vocab.
+void digits_for(uint64_t vocab, uint32_t* passes, uint32_t* log2bins) {
+    uint32_t bits = 1;
+    while ((vocab >> bits) != 0) bits++;
+    *passes = (bits + 8) / 9;
+    *log2bins = (bits + *passes - 1) / *passes;
+}
+
+// Lanes of a sorting workgroup (8 pairs each): few enough pairs a workgroup to
+// spread them over the CUs, many enough that the counts stay few.
+uint32_t sort_threads(uint64_t count) { return count >= (1u << 19) ? 512 : 256; }
+
 struct GradLayout {
     uint32_t chunk, chunks, groups;
+    bool small;
     size_t pairs[2], hist, total, heads, crossing_count, crossing, partial, bytes;
 };
 
@@ -571,7 +830,9 @@ GradLayout grad_layout(const hc_embed_params& p) {
     GradLayout L;
     L.chunk = chunk_for(p);
     L.chunks = (uint32_t)((p.count + L.chunk - 1) / L.chunk);
-    L.groups = (uint32_t)((p.count + kTile - 1) / kTile);
+    const uint64_t tile = sort_threads(p.count) * kItems;
+    L.groups = (uint32_t)((p.count + tile - 1) / tile);
+    L.small = p.count <= kSmallCount;
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t o = at;
@@ -579,73 +840,114 @@ GradLayout grad_layout(const hc_embed_params& p) {
         return o;
     };
     L.pairs[0] = take(p.count * sizeof(Pair));
-    L.pairs[1] = take(p.count * sizeof(Pair));
-    L.hist = take((size_t)L.groups * kMaxBins * 4);
+    L.pairs[1] = take(L.small ? 0 : p.count * sizeof(Pair));
+    L.hist = take(L.small ? 0 : (size_t)L.groups * kMaxBins * 4);
     L.total = take(kMaxBins * 4);
     L.heads = take((size_t)L.chunks * 4);
     L.crossing_count = take(4);
     L.crossing = take((size_t)L.chunks * 8);
-    L.partial = take((size_t)L.chunks * 2 * p.dim * 8);
+    L.partial = take((size_t)L.chunks * 2 * ((p.dim + 7) / 8 * 8) * 8);
     L.bytes = at;
     return L;
 }
 
-hipError_t zero_rows(void* dst, uint64_t rows, uint64_t row_bytes, uint64_t ld_bytes, int cus,
-                     hipStream_t s) {
-    if (ld_bytes == row_bytes) {
-        row_bytes *= rows;
-        rows = 1;
+Zeros zeros_for(void* dst, uint64_t rows, uint64_t row_bytes, uint64_t ld_bytes) {
+    Zeros z = {};
+    z.dst = static_cast<char*>(dst);
+    if (ld_bytes == row_bytes || rows == 1) {
+        z.rows = 1;
+        z.row_bytes = rows * row_bytes;
+        z.pieces = (z.row_bytes + kPieceBytes - 1) / kPieceBytes;
+    } else {
+        z.rows = rows;
+        z.row_bytes = row_bytes;
+        z.ld_bytes = ld_bytes;
+        z.per = row_bytes >= kPieceBytes ? 1 : kPieceBytes / row_bytes;
+        z.pieces = (rows + z.per - 1) / z.per;
     }
-    const uint64_t want = rows == 1 ? (row_bytes / 16 + kBlock - 1) / kBlock : rows;
-    const uint32_t grid = (uint32_t)(want < 1 ? 1 : want < (uint64_t)cus * 16 ? want : cus * 16);
-    const uintptr_t al = reinterpret_cast<uintptr_t>(dst) | row_bytes | (rows > 1 ? ld_bytes : 0);
-    if (al % 16 == 0)
-        hipLaunchKernelGGL(zero_rows_kernel<v4u>, dim3(grid), dim3(kBlock), 0, s,
-                           static_cast<char*>(dst), rows, row_bytes, ld_bytes);
-    else if (al % 4 == 0)
-        hipLaunchKernelGGL(zero_rows_kernel<uint32_t>, dim3(grid), dim3(kBlock), 0, s,
-                           static_cast<char*>(dst), rows, row_bytes, ld_bytes);
-    else
-        hipLaunchKernelGGL(zero_rows_kernel<uint16_t>, dim3(grid), dim3(kBlock), 0, s,
-                           static_cast<char*>(dst), rows, row_bytes, ld_bytes);
+    return z;
+}
+
+// A launch's share of the pieces: workgroups beyond its own.  The grid's lanes
+// stay below 2^32, so what does not fit is written by launches of its own.
+constexpr uint64_t kMaxPieces = 1ull << 20;
+
+uint32_t share(Zeros* z, uint64_t launches_left) {
+    uint64_t n = z->pieces == 0 ? 0 : (z->pieces - z->first + launches_left - 1) / launches_left;
+    return (uint32_t)(n < kMaxPieces ? n : kMaxPieces);
+}
+
+hipError_t zero_rest(Zeros z, hipStream_t s) {
+    while (z.first < z.pieces) {
+        const uint32_t n = share(&z, 1);
+        hipLaunchKernelGGL(zero_kernel, dim3(n), dim3(kBlock), 0, s, z);
+        z.first += n;
+    }
     return hipGetLastError();
 }
 
-template <typename SRC>
-hipError_t radix_pass(const SRC& src, uint32_t count, uint32_t shift, uint32_t log2bins,
-                      const GradLayout& L, char* ws, Pair* out, hipStream_t s) {
+template <uint32_t THREADS, typename SRC>
+void radix_pass(const SRC& src, uint32_t count, uint32_t shift, uint32_t log2bins,
+                const GradLayout& L, char* ws, Pair* out, Zeros* z, uint32_t launches_left,
+                hipStream_t s) {
     const uint32_t bins = 1u << log2bins;
     uint32_t* hist = reinterpret_cast<uint32_t*>(ws + L.hist);
     uint32_t* total = reinterpret_cast<uint32_t*>(ws + L.total);
-    hipLaunchKernelGGL(digit_count_kernel<SRC>, dim3(L.groups), dim3(kBlock), 0, s, src, count,
-                       shift, bins, hist);
-    hipLaunchKernelGGL(digit_scan_kernel, dim3((bins + kBlock / 64 - 1) / (kBlock / 64)),
-                       dim3(kBlock), 0, s, hist, total, bins, L.groups);
-    hipLaunchKernelGGL(digit_move_kernel<SRC>, dim3(L.groups), dim3(kBlock), 0, s, src, count,
-                       shift, log2bins, hist, total, out);
-    return hipGetLastError();
+    uint32_t n = share(z, launches_left);
+    hipLaunchKernelGGL((digit_count_kernel<THREADS, SRC>), dim3(L.groups + n), dim3(THREADS), 0, s,
+                       src, count, L.groups, shift, bins, hist,
+                       reinterpret_cast<uint32_t*>(ws + L.crossing_count), *z);
+    z->first += n;
+    n = share(z, launches_left - 1);
+    hipLaunchKernelGGL(digit_scan_kernel, dim3((bins + kBlock / 64 - 1) / (kBlock / 64) + n),
+                       dim3(kBlock), 0, s, hist, total, bins, L.groups, *z);
+    z->first += n;
+    n = share(z, launches_left - 2);
+    hipLaunchKernelGGL((digit_move_kernel<THREADS, SRC>), dim3(L.groups + n), dim3(THREADS), 0, s,
+                       src, count, L.groups, shift, log2bins, hist, total, out, *z);
+    z->first += n;
+}
+
+template <uint32_t THREADS, typename ID>
+hipError_t sort_large(const hc_embed_params& p, const FromIds<ID>& ids, const GradLayout& L,
+                      char* ws, const Pair** sorted, Zeros z, hipStream_t s) {
+    uint32_t passes, log2bins;
+    digits_for(p.vocab, &passes, &log2bins);
+    Pair* buf[2] = {reinterpret_cast<Pair*>(ws + L.pairs[0]),
+                    reinterpret_cast<Pair*>(ws + L.pairs[1])};
+    for (uint32_t k = 0; k < passes; k++) {
+        const uint32_t left = 3 * (passes - k);
+        if (k == 0)
+            radix_pass<THREADS>(ids, (uint32_t)p.count, 0, log2bins, L, ws, buf[0], &z, left, s);
+        else
+            radix_pass<THREADS>(FromPairs{buf[(k - 1) & 1]}, (uint32_t)p.count, k * log2bins, log2bins,
+                                L, ws, buf[k & 1], &z, left, s);
+    }
+    *sorted = buf[(passes - 1) & 1];
+    return zero_rest(z, s);
 }
 
 template <typename ID>
 hipError_t sort_ids(const hc_embed_params& p, const void* ids, const GradLayout& L, char* ws,
-                    const Pair** sorted, hipStream_t s) {
-    uint32_t bits = 1;
-    while ((p.vocab >> bits) != 0) bits++;
-    const uint32_t passes = (bits + 8) / 9, width = (bits + passes - 1) / passes;
-    const uint32_t count = (uint32_t)p.count;
-    Pair* buf[2] = {reinterpret_cast<Pair*>(ws + L.pairs[0]),
-                    reinterpret_cast<Pair*>(ws + L.pairs[1])};
-    for (uint32_t k = 0; k < passes; k++) {
-        hipError_t e;
-        if (k == 0)
-            e = radix_pass(FromIds<ID>{static_cast<const ID*>(ids), (uint32_t)p.vocab, p.padding},
-                           count, 0, width, L, ws, buf[0], s);
-        else
-            e = radix_pass(FromPairs{buf[(k - 1) & 1]}, count, k * width, width, L, ws, buf[k & 1], s);
-        if (e != hipSuccess) return e;
+                    const Pair** sorted, Zeros z, hipStream_t s) {
+    const FromIds<ID> src = {static_cast<const ID*>(ids), (uint32_t)p.vocab, p.padding};
+    if (!L.small) {
+        if (sort_threads(p.count) == 512) return sort_large<512>(p, src, L, ws, sorted, z, s);
+        return sort_large<256>(p, src, L, ws, sorted, z, s);
     }
-    *sorted = buf[(passes - 1) & 1];
-    return hipSuccess;
+    SmallSort a = {};
+    a.count = (uint32_t)p.count;
+    a.log2own = a.count > 4096 ? 5 : 4;  // up to 256 workgroups
+    a.groups = (a.count + (1u << a.log2own) - 1) >> a.log2own;
+    a.out = reinterpret_cast<Pair*>(ws + L.pairs[0]);
+    a.crossing_count = reinterpret_cast<uint32_t*>(ws + L.crossing_count);
+    a.zeros = z;
+    const uint32_t n = share(&z, 1);
+    hipLaunchKernelGGL(small_sort_kernel<ID>, dim3(a.groups + n), dim3(kSmallThreads),
+                       (a.count + 3) / 4 * 16, s, src, a);
+    *sorted = a.out;
+    z.first += n;
+    return zero_rest(z, s);
 }
 
 template <typename TI, typename TO, bool ROWS>
@@ -711,30 +1013,27 @@ hipError_t launch_embed_grad(const hc_embed_params& p, hc_type x_type, const voi
     if (e != hipSuccess) return e;
     char* ws = static_cast<char*>(ws_);
     const GradLayout L = grad_layout(p);
-    uint32_t* crossing_count = reinterpret_cast<uint32_t*>(ws + L.crossing_count);
     const bool rows = out.by_rows;
+    Zeros z = {};
     if (!rows && !out.accumulate) {
         const uint64_t size = out.type == HC_T_I32 || out.type == HC_T_F32 ? 4 : 2;
-        e = zero_rows(out.dst, p.vocab, p.dim * size, p.table_ld * size, di.cus, s);
-        if (e != hipSuccess) return e;
+        z = zeros_for(out.dst, p.vocab, p.dim * size, p.table_ld * size);
     }
     if (p.count == 0) {
-        if (!rows) return hipSuccess;
-        hipLaunchKernelGGL(clear_word_kernel, dim3(1), dim3(1), 0, s, out.touched,
-                           static_cast<uint32_t*>(nullptr));
+        if (!rows) return zero_rest(z, s);
+        hipLaunchKernelGGL(clear_word_kernel, dim3(1), dim3(1), 0, s, out.touched);
         return hipGetLastError();
     }
-    hipLaunchKernelGGL(clear_word_kernel, dim3(1), dim3(1), 0, s, crossing_count,
-                       static_cast<uint32_t*>(nullptr));
     SumArgs a = {};
-    e = p.id_bits == 64 ? sort_ids<int64_t>(p, ids, L, ws, &a.pairs, s)
-                        : sort_ids<int32_t>(p, ids, L, ws, &a.pairs, s);
+    e = p.id_bits == 64 ? sort_ids<int64_t>(p, ids, L, ws, &a.pairs, z, s)
+                        : sort_ids<int32_t>(p, ids, L, ws, &a.pairs, z, s);
     if (e != hipSuccess) return e;
     a.count = (uint32_t)p.count;
     a.chunk = L.chunk;
     a.chunks = L.chunks;
     a.vocab = (uint32_t)p.vocab;
     a.dim = (uint32_t)p.dim;
+    a.dim8 = (a.dim + 7) / 8 * 8;
     a.x_ld = p.x_ld;
     a.dst_ld = p.table_ld;
     a.scale = p.scale;
@@ -742,17 +1041,20 @@ hipError_t launch_embed_grad(const hc_embed_params& p, hc_type x_type, const voi
     a.accumulate = out.accumulate;
     a.rows = out.rows;
     a.cap = out.cap;
-    a.crossing_count = crossing_count;
+    a.crossing_count = reinterpret_cast<uint32_t*>(ws + L.crossing_count);
     a.crossing = reinterpret_cast<uint2*>(ws + L.crossing);
     a.partial = ws + L.partial;
     if (!rows) return sum_from<false>(a, x_type, out.type, dout, out.dst, di.cus, s);
-    uint32_t* heads = reinterpret_cast<uint32_t*>(ws + L.heads);
-    a.heads = heads;
-    hipLaunchKernelGGL(head_count_kernel, dim3((L.chunks + kBlock / 64 - 1) / (kBlock / 64)),
-                       dim3(kBlock), 0, s, a.pairs, a.count, a.chunk, a.chunks, a.vocab, heads);
-    hipLaunchKernelGGL(head_scan_kernel, dim3(1), dim3(1024), 0, s, heads, a.chunks, out.touched);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
+    a.touched = out.touched;
+    if (!L.small) {
+        uint32_t* heads = reinterpret_cast<uint32_t*>(ws + L.heads);
+        a.heads = heads;
+        hipLaunchKernelGGL(head_count_kernel, dim3((uint32_t)((p.count + kBlock - 1) / kBlock)),
+                           dim3(kBlock), 0, s, a.pairs, a.count, a.chunk, a.vocab, heads);
+        hipLaunchKernelGGL(head_scan_kernel, dim3(1), dim3(1024), 0, s, heads, a.chunks, out.touched);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
     return sum_from<true>(a, x_type, out.type, dout, out.dst, di.cus, s);
 }
 

@@ -14,6 +14,8 @@ from __future__ import annotations
 
 import ctypes
 
+import torch
+
 from . import _check, _lib, _ptr, _stream, _u32
 
 HC_T_I32, HC_T_F32, HC_T_BF16, HC_T_F16 = range(4)
@@ -53,18 +55,16 @@ _lib.hc_orthogonalise.argtypes = [_OP, _P, _P, _P, _Z, _P]
 for _f in TRAIN_EXPORTS:
     getattr(_lib, _f).restype = ctypes.c_int
 
-_TYPES = None
+_TYPES = {torch.int32: HC_T_I32, torch.float32: HC_T_F32, torch.bfloat16: HC_T_BF16,
+          torch.float16: HC_T_F16}
+_ID_BITS = {torch.int32: 32, torch.int64: 64}
 
 
 def _type(t, name):
-    global _TYPES
-    if _TYPES is None:
-        import torch
-        _TYPES = {torch.int32: HC_T_I32, torch.float32: HC_T_F32, torch.bfloat16: HC_T_BF16,
-                  torch.float16: HC_T_F16}
-    if t.dtype not in _TYPES:
+    code = _TYPES.get(t.dtype)
+    if code is None:
         raise ValueError(f"{name} has dtype {t.dtype}, expected one of {tuple(_TYPES)}")
-    return _TYPES[t.dtype]
+    return code
 
 
 def _rows(t, name):
@@ -72,26 +72,32 @@ def _rows(t, name):
     contiguous and whose others are one stride apart (a matrix, or contiguous)."""
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
-    if t.dim() < 2:
+    shape = t.shape
+    if len(shape) < 2:
         raise ValueError(f"{name} needs two dimensions or more")
-    cols = t.shape[-1]
-    if t.dim() > 2 or t.is_contiguous():
-        if not t.is_contiguous():
-            raise ValueError(f"{name} must be a matrix or contiguous")
-        return ctypes.c_void_p(t.data_ptr()), t.numel() // cols if cols else 0, cols, cols
+    cols = shape[-1]
+    if t.is_contiguous():
+        rows = shape[0] if len(shape) == 2 else (t.numel() // cols if cols else 0)
+        return t.data_ptr(), rows, cols, cols
+    if len(shape) > 2:
+        raise ValueError(f"{name} must be a matrix or contiguous")
     if cols > 1 and t.stride(1) != 1:
         raise ValueError(f"{name}'s rows must be contiguous")
-    rows = t.shape[0]
+    rows = shape[0]
     if rows > 1 and t.stride(0) < cols:
         raise ValueError(f"{name}'s rows overlap")
-    return ctypes.c_void_p(t.data_ptr()), rows, cols, t.stride(0) if rows > 1 else cols
+    return t.data_ptr(), rows, cols, t.stride(0) if rows > 1 else cols
 
 
 def _ids(ids):
-    import torch
-    if ids.dtype not in (torch.int32, torch.int64):
+    bits = _ID_BITS.get(ids.dtype)
+    if bits is None:
         raise ValueError(f"ids has dtype {ids.dtype}, expected torch.int32 or torch.int64")
-    return _ptr(ids, "ids"), ids.numel(), 32 if ids.dtype == torch.int32 else 64
+    if not ids.is_cuda:
+        raise ValueError("ids must be a device tensor")
+    if not ids.is_contiguous():
+        raise ValueError("ids must be contiguous")
+    return ids.data_ptr(), ids.numel(), bits
 
 
 def hc_embed(table, ids, out, scale: float = 1.0, stream=None):
@@ -119,7 +125,6 @@ def hc_embed_grad_bytes(vocab: int, dim: int, count: int) -> int:
 
 def alloc_embed_workspace(vocab: int, dim: int, count: int, device="cuda"):
     """Workspace of hc_embed_grad and hc_embed_grad_rows for up to `count` ids."""
-    import torch
     return torch.empty(max(hc_embed_grad_bytes(vocab, dim, count), 256), dtype=torch.uint8,
                        device=device)
 
@@ -141,7 +146,6 @@ def hc_embed_grad(dout, ids, dtable, ws, scale: float = 1.0, fixed: float = FIXE
     """dtable[v] = scale * sum of dout[i] over ids[i] == v (or added to dtable).  dout [.., dim]
     float32, bfloat16 or float16; dtable [vocab, dim] one of them, or int32: fixed point with
     `fixed` units per 1.0.  Ids outside the table and `padding` add nothing."""
-    import torch
     p, xt, x, i, gt, d, _ = _grad_args(dout, ids, dtable.shape[0], dtable, "dtable", scale, fixed,
                                        padding)
     _check(_lib.hc_embed_grad(ctypes.byref(p), xt, x, i, gt, d, 1 if accumulate else 0,
@@ -154,7 +158,6 @@ def hc_embed_grad_rows(dout, ids, vocab: int, rows, values, touched, ws, scale: 
     """The touched rows alone: rows[u] ascending distinct ids, values[u] their sums (types as
     hc_embed_grad's dtable), touched[0] how many there are.  rows and values hold `cap` entries;
     what lies past touched is not written."""
-    import torch
     p, xt, x, i, gt, d, cap = _grad_args(dout, ids, vocab, values, "values", scale, fixed, padding)
     _check(_lib.hc_embed_grad_rows(ctypes.byref(p), xt, x, i, gt, _ptr(rows, "rows", _u32(), cap), d,
                                    cap, _ptr(touched, "touched", _u32(), 1),
@@ -175,7 +178,7 @@ def _matrices(t, name):
     if ld < n:
         raise ValueError(f"{name}'s rows overlap")
     batch = t.shape[0] if t.dim() == 3 else 1
-    return ctypes.c_void_p(t.data_ptr()), batch, m, n, ld, t.stride(0) if batch > 1 else m * ld
+    return t.data_ptr(), batch, m, n, ld, t.stride(0) if batch > 1 else m * ld
 
 
 def _ortho_params(x, out, steps, coeffs, eps, scale):
@@ -209,7 +212,6 @@ def hc_orthogonalise_bytes(x, steps: int = 5) -> int:
 
 def alloc_orthogonalise_workspace(x):
     """Workspace of hc_orthogonalise for matrices of x's shape and type."""
-    import torch
     return torch.empty(max(hc_orthogonalise_bytes(x), 256), dtype=torch.uint8, device=x.device)
 
 
@@ -218,7 +220,6 @@ def hc_orthogonalise(x, out, ws, steps: int = 5, coeffs=MUON, eps: float = 1e-7,
     """out = scale * X_steps, X_0 = x / (|x|_F + eps), X <- a X + (b A + c A^2) X with A = X X^T.
     x, out: [m, n] or [batch, m, n] float32 or bfloat16, rows contiguous; coeffs (a, b, c), or a
     triple for each step."""
-    import torch
     p, px, po = _ortho_params(x, out, steps, coeffs, eps, scale)
     _check(_lib.hc_orthogonalise(ctypes.byref(p), px, po, _ptr(ws, "ws", (torch.uint8,)), ws.numel(),
                                  _stream(stream)), "hc_orthogonalise")

@@ -187,6 +187,13 @@ struct Product {
     const _Float16 *p, *q;
     uint32_t inner;                  // length of l, a multiple of 64
     uint32_t tiles_i, tiles_j;       // tiles_j: of a result that is not symmetric
+    uint32_t tiles;                  // of one matrix
+    uint32_t batch;
+    // Streams: workgroups that share the steps of all tiles evenly, tile after
+    // tile, and leave the sums of tiles that they do only part of in `part` (two
+    // tiles a workgroup: of the one it begins inside, of the one it ends inside).
+    uint32_t streams;
+    float* part;
     size_t p_stride, q_stride;       // between matrices of the batch (stored values)
     float factor;                    // takes the sum to the result's unit
     float factor2;                   // SQUARE: takes the operand A to it; APPLY: a
@@ -208,15 +215,15 @@ struct Product {
 constexpr int kLine = 64;  // stored values of a tile's row in LDS: 128 bytes
 
 // A workgroup's tile: BM x BN, a wave's part WM x WN.
-template <int BM_, int BN_, int WM_, int WN_> struct Shape {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
+template <int BM_, int BN_, int WM_, int WN_, int STAGES_> struct Shape {
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, kStages = STAGES_;
     static constexpr int kWaves = (BM / WM) * (BN / WN);
     static constexpr int kThreads = kWaves * 64;
     static constexpr int kStageBytes = (BM + BN) * kLine * 2;
     // a wave's results pass through LDS in blocks of EM x EN
     static constexpr int EM = WM < 64 ? WM : 64, EN = WN < 64 ? WN : 64;
     static constexpr int kLdsBytes =
-        2 * kStageBytes > kWaves * EM * EN * 4 ? 2 * kStageBytes : kWaves * EM * EN * 4;
+        kStages * kStageBytes > kWaves * EM * EN * 4 ? kStages * kStageBytes : kWaves * EM * EN * 4;
 };
 
 // Result (i, j) of a block in LDS, [i][EN]: its 4-value group is turned by i so
@@ -233,6 +240,15 @@ __device__ __forceinline__ uint32_t swizzled(uint32_t row, uint32_t c) {
 
 typedef __attribute__((address_space(3))) void lds_void;
 
+// A barrier that keeps every instruction on its side.
+__device__ __forceinline__ void phase_barrier() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
 // Fragments and products of one 128-byte step l.  A lane holds row lane % 16 of a
 // fragment, 8 values from chunk 4 h + lane / 16.  The first operand of the
 // instruction gives a lane's 4 consecutive results: Q, so that they lie along j.
@@ -241,12 +257,23 @@ __device__ __forceinline__ void main_loop(f4 (&acc)[S::WM / 16][S::WN / 16], con
                                           const char* s_mem, uint32_t lines, uint32_t wi,
                                           uint32_t wj, uint32_t lane) {
     constexpr int FM = S::WM / 16, FN = S::WN / 16;
+    constexpr uint32_t N = S::kStages;
+    constexpr uint32_t kLoads = (S::BM + S::BN) / 8 / S::kWaves;  // of a wave and step
+#pragma unroll
+    for (uint32_t l = 1; l + 1 < N; l++)
+        if (l < lines) fetch(l, l);
+    uint32_t buf = 0;
     for (uint32_t l = 0; l < lines; l++) {
-        // this wave's loads have landed, then everybody's; and everybody is done
-        // reading the other buffer
-        __syncthreads();
-        if (l + 1 < lines) fetch(l + 1, (l + 1) & 1);
-        const _Float16* sp = reinterpret_cast<const _Float16*>(s_mem + (l & 1) * S::kStageBytes);
+        // this wave's loads of step l have landed (those of later steps may be on
+        // their way), then everybody's; and everybody is done with step l - 1
+        if (l + N - 2 < lines)
+            __builtin_amdgcn_s_waitcnt(0x0f70 | ((N - 2) * kLoads & 15) | ((N - 2) * kLoads >> 4) << 14);
+        else
+            __builtin_amdgcn_s_waitcnt(0x0f70);
+        phase_barrier();
+        if (l + N - 1 < lines) fetch(l + N - 1, buf == 0 ? N - 1 : buf - 1);
+        const _Float16* sp = reinterpret_cast<const _Float16*>(s_mem + buf * S::kStageBytes);
+        buf = buf + 1 == N ? 0 : buf + 1;
         const _Float16* sq = sp + S::BM * kLine;
         h8 fp[2][FM], fq[2][FN];
 #pragma unroll
@@ -276,15 +303,6 @@ __device__ __forceinline__ void main_loop(f4 (&acc)[S::WM / 16][S::WN / 16], con
                         acc[u][v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fq[t == 1][v], fp[t == 2][u], acc[u][v], 0, 0, 0);
         }
     }
-}
-
-// A barrier that keeps every instruction on its side.
-__device__ __forceinline__ void phase_barrier() {
-    __builtin_amdgcn_sched_barrier(0);
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
 }
 
 // Eight waves, two on each SIMD: a step is two halves, a half one phase of LDS
@@ -352,30 +370,65 @@ __device__ __forceinline__ void main_loop_paired(f4 (&acc)[S::WM / 16][S::WN / 1
     if (!second) phase_barrier();
 }
 
-template <Kind KIND, int PLANES, typename T, typename S>
-__global__ __launch_bounds__(S::kThreads) void product_kernel(Product g) {
-    constexpr int FM = S::WM / 16, FN = S::WN / 16;
-    extern __shared__ __align__(16) char s_mem[];
+// A tile's matrix and place.
+struct Tile {
+    uint32_t batch, ti, tj;
+};
+
+template <Kind KIND> __device__ __forceinline__ Tile tile_at(const Product& g, uint32_t t) {
+    Tile o;
+    o.batch = t / g.tiles;
+    t -= o.batch * g.tiles;
+    if constexpr (KIND == APPLY) {
+        // the shorter side (B's) first: neighbours share X^T's rows
+        if (g.tiles_i <= g.tiles_j) {
+            o.ti = t % g.tiles_i;
+            o.tj = t / g.tiles_i;
+        } else {
+            o.tj = t % g.tiles_j;
+            o.ti = t / g.tiles_j;
+        }
+    } else {
+        // the lower triangle in squares of 4 x 4 tiles, so that tiles near each
+        // other in the order share rows of both operands; row I of squares begins
+        // at 8 I^2 + 2 I
+        uint32_t I = (uint32_t)(sqrtf((float)t * 0.125f));
+        while (I > 0 && 8 * I * I + 2 * I > t) I--;
+        while (8 * (I + 1) * (I + 1) + 2 * (I + 1) <= t) I++;
+        uint32_t q = t - (8 * I * I + 2 * I);
+        const uint32_t h = min(4u, g.tiles_i - 4 * I);  // rows of this row of squares
+        if (q < I * 4 * h) {
+            const uint32_t J = q / (4 * h);
+            q -= J * 4 * h;
+            o.ti = 4 * I + q % h;
+            o.tj = 4 * J + q / h;
+        } else {
+            q -= I * 4 * h;
+            const uint32_t r = q < 1 ? 0 : q < 3 ? 1 : q < 6 ? 2 : 3;
+            o.ti = 4 * I + r;
+            o.tj = 4 * I + q - r * (r + 1) / 2;
+        }
+    }
+    return o;
+}
+
+// Workgroups go to the 8 XCDs in turn; each XCD takes a contiguous share of the
+// tiles, so that what neighbouring tiles read is shared in its L2.
+__device__ __forceinline__ uint32_t by_xcd(uint32_t block, uint32_t blocks) {
+    const uint32_t xcd = block & 7u, k = block >> 3, per = blocks >> 3, more = blocks & 7u;
+    return xcd * per + min(xcd, more) + k;
+}
+
+// Steps [l0, l1) of a tile, added to acc.
+template <int PLANES, typename S>
+__device__ __forceinline__ void accumulate(const Product& g, const Tile& tile, uint32_t l0,
+                                           uint32_t l1, char* s_mem,
+                                           f4 (&acc)[S::WM / 16][S::WN / 16]) {
     const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const uint32_t wi = wave / (S::BN / S::WN) * S::WM, wj = wave % (S::BN / S::WN) * S::WN;
-    const uint32_t batch = blockIdx.y;
-    uint32_t ti, tj;
-    if constexpr (KIND == APPLY) {
-        ti = blockIdx.x % g.tiles_i;
-        tj = blockIdx.x / g.tiles_i;
-    } else {
-        // row ti of the lower triangle begins at ti (ti + 1) / 2
-        ti = (uint32_t)((sqrtf(8.0f * (float)blockIdx.x + 1.0f) - 1.0f) * 0.5f);
-        while (ti * (ti + 1) / 2 > blockIdx.x) ti--;
-        while ((ti + 1) * (ti + 2) / 2 <= blockIdx.x) ti++;
-        tj = blockIdx.x - ti * (ti + 1) / 2;
-    }
-    const uint32_t i0 = ti * S::BM, j0 = tj * S::BN;
     const size_t line = (size_t)g.inner * PLANES;  // stored values of an operand's row
-    const _Float16* P = g.p + batch * g.p_stride + (size_t)i0 * line;
-    const _Float16* Q = g.q + batch * g.q_stride + (size_t)j0 * line;
-    const uint32_t lines = (uint32_t)(line / kLine);
-
+    const _Float16* P = g.p + tile.batch * g.p_stride + (size_t)tile.ti * S::BM * line;
+    const _Float16* Q = g.q + tile.batch * g.q_stride + (size_t)tile.tj * S::BN * line;
     // Tiles go from memory to LDS directly, 8 rows of 128 bytes an instruction:
     // lane l writes 16 bytes at 16 l, so it reads the chunk that belongs there.
     const __amdgpu_buffer_rsrc_t rp = buffer_rsrc(P, (uint32_t)(S::BM * line * 2));
@@ -389,117 +442,480 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Product g) {
             const uint32_t rows8 = wave * GP + u;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(
                 rp, (lds_void*)(base + rows8 * 1024), 16, voff,
-                (uint32_t)(rows8 * 8 * line * 2) + l * 128, 0, 0);
+                (uint32_t)(rows8 * 8 * line * 2) + (l0 + l) * 128, 0, 0);
         }
 #pragma unroll
         for (int u = 0; u < GQ; u++) {
             const uint32_t rows8 = wave * GQ + u;
             __builtin_amdgcn_raw_ptr_buffer_load_lds(
                 rq, (lds_void*)(base + S::BM * kLine * 2 + rows8 * 1024), 16, voff,
-                (uint32_t)(rows8 * 8 * line * 2) + l * 128, 0, 0);
+                (uint32_t)(rows8 * 8 * line * 2) + (l0 + l) * 128, 0, 0);
         }
     };
-
-    f4 acc[FM][FN] = {};
     fetch(0, 0);
     if constexpr (S::kWaves == 8)
-        main_loop_paired<PLANES, S>(acc, fetch, s_mem, lines, wi, wj, lane, wave);
+        main_loop_paired<PLANES, S>(acc, fetch, s_mem, l1 - l0, wi, wj, lane, wave);
     else
-        main_loop<PLANES, S>(acc, fetch, s_mem, lines, wi, wj, lane);
+        main_loop<PLANES, S>(acc, fetch, s_mem, l1 - l0, wi, wj, lane);
     __syncthreads();
+}
 
-    // Results: fragment (u, v) holds i = lane % 16, j = 4 (lane / 16) .. + 3.
+// What a tile's sums become, and where they go.
+template <Kind KIND, int PLANES, typename T, typename S> struct Results {
+    const Product& g;
+    size_t base;      // of the matrix
+    uint32_t batch;
+    bool turn;        // the transpose is stored too
+    bool first, last; // APPLY: x is read; the output is written
+    float inverse;
+
+    __device__ __forceinline__ Results(const Product& g_, const Tile& t)
+        : g(g_), base((size_t)t.batch * g_.rows * g_.cols), batch(t.batch),
+          turn(KIND == APPLY ? g_.out == nullptr : t.ti != t.tj),
+          first(KIND == APPLY && g_.x != nullptr), last(KIND == APPLY && g_.out != nullptr),
+          inverse(KIND == APPLY && g_.x != nullptr ? g_.inverse[t.batch] * g_.factor2 : 0.0f) {}
+
+    // Results (i, j .. j + 3) are stored, and returned for the transpose.
+    __device__ __forceinline__ f4 straight(uint32_t i, uint32_t j, f4 sum) const {
+        f4 w = sum * g.factor;
+        if constexpr (KIND == SQUARE) {
+            const _Float16* A = g.p + batch * g.p_stride + operand_at<PLANES>(i, g.inner, j);
+            const h4 hi = *reinterpret_cast<const h4*>(A);
+#pragma unroll
+            for (int e = 0; e < 4; e++) w[e] += (float)hi[e] * g.factor2;
+            if constexpr (PLANES == 2) {
+                const h4 lo = *reinterpret_cast<const h4*>(A + 32);
+#pragma unroll
+                for (int e = 0; e < 4; e++) w[e] += (float)lo[e] * g.factor2;
+            }
+        }
+        if constexpr (KIND == APPLY) {
+            typedef T T4 __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+            f4* mm = reinterpret_cast<f4*>(g.master + base + (size_t)i * g.cols + j);
+            if (first) {
+                const T* xr = static_cast<const T*>(g.x) + batch * g.x_stride + i * g.x_ld + j;
+                if (i < g.m && j + 3 < g.n) {
+                    const T4 v = *reinterpret_cast<const T4*>(xr);
+#pragma unroll
+                    for (int e = 0; e < 4; e++) w[e] += (float)v[e] * inverse;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; e++)
+                        if (i < g.m && j + e < g.n) w[e] += (float)xr[e] * inverse;
+                }
+            } else {
+                w += *mm * g.factor2;
+            }
+            if (last) {
+                w *= g.out_scale;
+                T* o = static_cast<T*>(g.out) + batch * g.out_stride + i * g.out_ld + j;
+                if (i < g.m && j + 3 < g.n) {
+                    T4 v;
+#pragma unroll
+                    for (int e = 0; e < 4; e++) v[e] = (T)w[e];
+                    *reinterpret_cast<T4*>(o) = v;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; e++)
+                        if (i < g.m && j + e < g.n) o[e] = (T)w[e];
+                }
+                return w;
+            }
+            *mm = w;
+            w *= g.next;
+        }
+        h4 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            _Float16 x, y = 0;
+            split<PLANES>(w[e], x, y);
+            hi[e] = x;
+            lo[e] = y;
+        }
+        _Float16* D = g.d + base * PLANES + operand_at<PLANES>(i, g.cols, j);
+        *reinterpret_cast<h4*>(D) = hi;
+        if constexpr (PLANES == 2) *reinterpret_cast<h4*>(D + 32) = lo;
+        return w;
+    }
+
+    // The transpose of a block in LDS: 8 consecutive i of one j a lane.  Lanes
+    // `at`, at + step, ... of the EM EN / 8.
+    __device__ __forceinline__ void turned(const float* stage, uint32_t ib, uint32_t jb, uint32_t at,
+                                           uint32_t step) const {
+        constexpr int kPer = S::EM / 8;  // lanes for one j
+        for (uint32_t q = at; q < S::EN * kPer; q += step) {
+            const uint32_t jj = q / kPer, ii = q % kPer * 8;
+            h8 hi, lo;
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                _Float16 x, y = 0;
+                split<PLANES>(stage[staged<S::EN>(ii + e, jj)], x, y);
+                hi[e] = x;
+                lo[e] = y;
+            }
+            _Float16* D = g.dt + base * PLANES + operand_at<PLANES>(jb + jj, g.rows, ib + ii);
+            *reinterpret_cast<h8*>(D) = hi;
+            if constexpr (PLANES == 2) *reinterpret_cast<h8*>(D + 32) = lo;
+        }
+    }
+};
+
+// A workgroup's sums of a whole tile become its results, a wave its own part:
+// fragment (u, v) of a lane holds i = lane % 16, j = 4 (lane / 16) .. + 3.
+template <Kind KIND, int PLANES, typename T, typename S>
+__device__ __forceinline__ void finish(const Product& g, const Tile& tile, char* s_mem,
+                                       f4 (&acc)[S::WM / 16][S::WN / 16]) {
     constexpr int EM = S::EM, EN = S::EN;
-    float* stage = reinterpret_cast<float*>(s_mem) + wave * EM * EN;
+    const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    const uint32_t i0 = tile.ti * S::BM + wave / (S::BN / S::WN) * S::WM;
+    const uint32_t j0 = tile.tj * S::BN + wave % (S::BN / S::WN) * S::WN;
     const uint32_t fi = lane & 15, fj = (lane >> 4) * 4;
-    const size_t base = (size_t)batch * g.rows * g.cols;
-    const bool last = KIND == APPLY && g.out != nullptr;
-    const bool first = KIND == APPLY && g.x != nullptr;
-    const float inverse = first ? g.inverse[batch] * g.factor2 : 0.0f;
+    float* stage = reinterpret_cast<float*>(s_mem) + wave * EM * EN;
+    const Results<KIND, PLANES, T, S> out(g, tile);
 #pragma unroll
     for (int eu = 0; eu < S::WM / EM; eu++)
 #pragma unroll
         for (int ev = 0; ev < S::WN / EN; ev++) {
-            const uint32_t ib = i0 + wi + eu * EM, jb = j0 + wj + ev * EN;
+            const uint32_t ib = i0 + eu * EM, jb = j0 + ev * EN;
 #pragma unroll
             for (int u = 0; u < EM / 16; u++)
 #pragma unroll
                 for (int v = 0; v < EN / 16; v++) {
-                    const uint32_t i = ib + 16 * u + fi, j = jb + 16 * v + fj;
-                    f4 w = acc[eu * (EM / 16) + u][ev * (EN / 16) + v] * g.factor;
-                    if constexpr (KIND == SQUARE) {
-                        const _Float16* A = g.p + batch * g.p_stride + operand_at<PLANES>(i, g.inner, j);
-                        const h4 hi = *reinterpret_cast<const h4*>(A);
-#pragma unroll
-                        for (int e = 0; e < 4; e++) w[e] += (float)hi[e] * g.factor2;
-                        if constexpr (PLANES == 2) {
-                            const h4 lo = *reinterpret_cast<const h4*>(A + 32);
-#pragma unroll
-                            for (int e = 0; e < 4; e++) w[e] += (float)lo[e] * g.factor2;
-                        }
-                    }
-                    if constexpr (KIND == APPLY) {
-                        f4* mm = reinterpret_cast<f4*>(g.master + base + (size_t)i * g.cols + j);
-                        if (first) {
-                            const T* xr = static_cast<const T*>(g.x) + batch * g.x_stride + i * g.x_ld + j;
-#pragma unroll
-                            for (int e = 0; e < 4; e++)
-                                if (i < g.m && j + e < g.n) w[e] += (float)xr[e] * inverse;
-                        } else {
-                            w += *mm * g.factor2;
-                        }
-                        if (!last) *mm = w;
-                        w *= last ? g.out_scale : g.next;
-                    }
-                    if (last) {
-                        T* o = static_cast<T*>(g.out) + batch * g.out_stride + i * g.out_ld + j;
-#pragma unroll
-                        for (int e = 0; e < 4; e++)
-                            if (i < g.m && j + e < g.n) o[e] = (T)w[e];
-                    } else {
-                        h4 hi, lo;
-#pragma unroll
-                        for (int e = 0; e < 4; e++) {
-                            _Float16 a, b = 0;
-                            split<PLANES>(w[e], a, b);
-                            hi[e] = a;
-                            lo[e] = b;
-                        }
-                        _Float16* D = g.d + base * PLANES + operand_at<PLANES>(i, g.cols, j);
-                        *reinterpret_cast<h4*>(D) = hi;
-                        if constexpr (PLANES == 2) *reinterpret_cast<h4*>(D + 32) = lo;
-                        *reinterpret_cast<f4*>(stage + staged<EN>(16 * u + fi, 16 * v + fj)) = w;
-                    }
+                    const f4 w = out.straight(ib + 16 * u + fi, jb + 16 * v + fj,
+                                              acc[eu * (EM / 16) + u][ev * (EN / 16) + v]);
+                    *reinterpret_cast<f4*>(stage + staged<EN>(16 * u + fi, 16 * v + fj)) = w;
                 }
-            if (last || (KIND != APPLY && ti == tj)) continue;
-            // the transpose: 8 consecutive i of one j a lane (only this wave's results)
+            if (!out.turn) continue;
+            // only this wave's results are read
             __builtin_amdgcn_s_waitcnt(0xc07f);
             __builtin_amdgcn_wave_barrier();
-            constexpr int kPer = EM / 8;  // lanes for one j
-#pragma unroll
-            for (int q = 0; q < EN * kPer / 64; q++) {
-                const uint32_t jj = q * (64 / kPer) + lane / kPer, ii = lane % kPer * 8;
-                h8 hi, lo;
-#pragma unroll
-                for (int e = 0; e < 8; e++) {
-                    _Float16 a, b = 0;
-                    split<PLANES>(stage[staged<EN>(ii + e, jj)], a, b);
-                    hi[e] = a;
-                    lo[e] = b;
-                }
-                _Float16* D = g.dt + base * PLANES + operand_at<PLANES>(jb + jj, g.rows, ib + ii);
-                *reinterpret_cast<h8*>(D) = hi;
-                if constexpr (PLANES == 2) *reinterpret_cast<h8*>(D + 32) = lo;
-            }
+            out.turned(stage, ib, jb, lane, 64);
             __builtin_amdgcn_wave_barrier();
         }
 }
 
+// First step of stream w, counted over all tiles.
+__device__ __forceinline__ uint64_t stream_begin(const Product& g, uint32_t lines, uint32_t w) {
+    return (uint64_t)w * g.tiles * g.batch * lines / g.streams;
+}
+
+// One tile a workgroup.
+template <Kind KIND, int PLANES, typename T, typename S>
+__global__ __launch_bounds__(S::kThreads) void product_kernel(Product g) {
+    extern __shared__ __align__(16) char s_mem[];
+    const Tile tile = tile_at<KIND>(g, by_xcd(blockIdx.x, gridDim.x));
+    f4 acc[S::WM / 16][S::WN / 16] = {};
+    accumulate<PLANES, S>(g, tile, 0, g.inner * PLANES / kLine, s_mem, acc);
+    finish<KIND, PLANES, T, S>(g, tile, s_mem, acc);
+}
+
+// An equal share of all tiles' steps a workgroup.
+template <Kind KIND, int PLANES, typename T, typename S>
+__global__ __launch_bounds__(S::kThreads) void stream_kernel(Product g) {
+    constexpr int FM = S::WM / 16, FN = S::WN / 16;
+    extern __shared__ __align__(16) char s_mem[];
+    const uint32_t lines = g.inner * PLANES / kLine;
+    const uint32_t stream = blockIdx.x;
+    uint64_t at = stream_begin(g, lines, stream);
+    const uint64_t end = stream_begin(g, lines, stream + 1);
+    while (at < end) {
+        const uint32_t t = (uint32_t)(at / lines), l0 = (uint32_t)(at - (uint64_t)t * lines);
+        const uint32_t l1 = (uint32_t)min((uint64_t)lines, l0 + (end - at));
+        const Tile tile = tile_at<KIND>(g, t);
+        f4 acc[FM][FN] = {};
+        accumulate<PLANES, S>(g, tile, l0, l1, s_mem, acc);
+        if (l1 - l0 == lines) {
+            finish<KIND, PLANES, T, S>(g, tile, s_mem, acc);
+        } else {
+            f4* part = reinterpret_cast<f4*>(g.part) +
+                       ((size_t)stream * 2 + (l0 > 0 ? 0 : 1)) * (S::BM * S::BN / 4);
+#pragma unroll
+            for (int u = 0; u < FM; u++)
+#pragma unroll
+                for (int v = 0; v < FN; v++) part[(u * FN + v) * S::kThreads + threadIdx.x] = acc[u][v];
+        }
+        at += l1 - l0;
+        __syncthreads();
+    }
+}
+
+// Tiles that several streams shared: their sums, in the streams' order.  A
+// workgroup takes an EM x EN block of a wave's part, a wave of it 16 rows.
+template <Kind KIND, int PLANES, typename T, typename S>
+__global__ __launch_bounds__(S::EM * 4) void join_kernel(Product g) {
+    constexpr int FN = S::WN / 16, EM = S::EM, EN = S::EN;
+    constexpr uint32_t kBlocks = S::kWaves * (S::WM / EM) * (S::WN / EN);  // of a tile
+    __shared__ __align__(16) float s_stage[EM * EN];
+    const uint32_t lines = g.inner * PLANES / kLine;
+    const uint32_t t = blockIdx.x / kBlocks, block = blockIdx.x - t * kBlocks;
+    const uint32_t wave = block % S::kWaves, sub = block / S::kWaves;
+    const uint32_t eu = sub / (S::WN / EN), ev = sub % (S::WN / EN);
+    const uint64_t first = (uint64_t)t * lines, last = first + lines;
+    uint32_t w = (uint32_t)(first * g.streams / ((uint64_t)g.tiles * g.batch * lines));
+    while (w > 0 && stream_begin(g, lines, w) > first) w--;
+    while (stream_begin(g, lines, w + 1) <= first) w++;
+    if (stream_begin(g, lines, w + 1) >= last) return;  // one stream did it all
+    const uint32_t lane = threadIdx.x & 63, u = threadIdx.x >> 6;
+    f4 acc[EN / 16] = {};
+    for (; w < g.streams; w++) {
+        const uint64_t begin = stream_begin(g, lines, w);
+        if (begin >= last) break;
+        const f4* part = reinterpret_cast<const f4*>(g.part) +
+                         ((size_t)w * 2 + (begin > first ? 0 : 1)) * (S::BM * S::BN / 4) +
+                         ((eu * (EM / 16) + u) * FN + ev * (EN / 16)) * S::kThreads + wave * 64 + lane;
+#pragma unroll
+        for (int v = 0; v < EN / 16; v++) acc[v] += part[v * S::kThreads];
+    }
+    const Tile tile = tile_at<KIND>(g, t);
+    const Results<KIND, PLANES, T, S> out(g, tile);
+    const uint32_t ib = tile.ti * S::BM + wave / (S::BN / S::WN) * S::WM + eu * EM;
+    const uint32_t jb = tile.tj * S::BN + wave % (S::BN / S::WN) * S::WN + ev * EN;
+    const uint32_t fi = 16 * u + (lane & 15), fj = (lane >> 4) * 4;
+#pragma unroll
+    for (int v = 0; v < EN / 16; v++)
+        *reinterpret_cast<f4*>(s_stage + staged<EN>(fi, 16 * v + fj)) =
+            out.straight(ib + fi, jb + 16 * v + fj, acc[v]);
+    if (!out.turn) return;
+    lds_barrier();
+    out.turned(s_stage, ib, jb, threadIdx.x, EM * 4);
+}
+
+// ---- thin matrices ---------------------------------------------------------------
+
+// A shorter side of at most 128: a step is one launch.  A workgroup owns columns
+// of X (along the longer side), 64 at a time.  It sums all workgroups' parts of
+// A = X X^T from the launch before, in order, squares A in LDS, multiplies its
+// columns by B, and leaves its part of the next A.  What bounds it is the chain
+// of latencies of a launch, so nothing but X and the parts of A goes to memory.
+//
+// A wave multiplies 16 of the 64 columns: a lane holds column lane % 16, rows
+// 16 u + 4 (lane / 16) .. + 3, which is what its product with B gives again, and
+// what the next takes as its second operand if B's columns are read in the same
+// order: chunk c of a line of 32 holds 4 c .. 4 c + 3 and 16 + 4 c .. + 3.  Two
+// planes always.
+struct Thin {
+    uint64_t m, n, x_ld, x_stride, out_ld, out_stride;
+    bool tall;
+    uint32_t slabs, per, parts;    // 64-column slabs, of a workgroup, workgroups
+    const void* x;
+    void* out;                     // last step
+    float* master;                 // X in fp32, in the lanes' order
+    const float* part_in;          // parts of A, [batch][parts][R][R]
+    float* part_out;
+    const double* norm;            // first launch
+    uint32_t norm_parts;
+    float eps, out_scale;
+    float a, sb, sc;               // step: a; factors of A and of its square in B
+    float x_unit, factor;          // unit of X's operands, factor of the sums of B X
+    float gram_x, gram;            // unit of the next X's operands, factor of their A
+};
+
+// Where 4 consecutive columns from l (a multiple of 4) of a row lie in a line.
+template <int R> __device__ __forceinline__ uint32_t thin_at(uint32_t row, uint32_t l, bool low) {
+    const uint32_t q = l & 31u;
+    return (l >> 5) * (R * kLine) + swizzled(row, ((q & 15u) >> 2) + (low ? 4u : 0u)) + (q >> 4) * 4;
+}
+
+__device__ __forceinline__ void split4(f4 w, h4& hi, h4& lo) {
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+        _Float16 x, y;
+        split<2>(w[e], x, y);
+        hi[e] = x;
+        lo[e] = y;
+    }
+}
+
+// high x high, low x high, high x low
+__device__ __forceinline__ f4 mfma3(h8 ah, h8 al, h8 bh, h8 bl, f4 c) {
+    c = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, bh, c, 0, 0, 0);
+    c = __builtin_amdgcn_mfma_f32_16x16x32_f16(al, bh, c, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, bl, c, 0, 0, 0);
+}
+
+template <typename T, int R, bool FIRST>
+__global__ __launch_bounds__(256) void thin_kernel(Thin g) {
+    constexpr int RT = R / 16, RS = R / 32;   // row tiles, lines of 32
+    constexpr int GT = RT / 4;                // row tiles of a wave in A and B
+    extern __shared__ __align__(16) char s_mem[];
+    _Float16* s_b = reinterpret_cast<_Float16*>(s_mem);  // A, then B: [RS][R][64]
+    _Float16* s_x = s_b + (FIRST ? 0 : RS * R * kLine);  // 64 columns of X: [2][R][64]
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t li = lane & 15, lg = lane >> 4;
+    const uint32_t batch = blockIdx.y;
+    float f = 0.0f;
+    if constexpr (FIRST) {
+        f = inverse_norm(g.norm + (uint64_t)batch * kNormParts, g.norm_parts, g.eps);
+    } else {
+        // A: the parts' sum
+        const f4* in = reinterpret_cast<const f4*>(g.part_in) + (size_t)batch * g.parts * (R * R / 4);
+        constexpr int N = R * R / 4 / 256;
+        f4 sum[N] = {};
+#pragma unroll 2
+        for (uint32_t w = 0; w < g.parts; w++)
+#pragma unroll
+            for (int k = 0; k < N; k++) sum[k] += in[(size_t)w * (R * R / 4) + k * 256 + threadIdx.x];
+#pragma unroll
+        for (int k = 0; k < N; k++) {
+            const uint32_t at = (k * 256 + threadIdx.x) * 4, i = at / R, j = at % R;
+            h4 hi, lo;
+            split4(sum[k], hi, lo);
+            *reinterpret_cast<h4*>(s_b + thin_at<R>(i, j, false)) = hi;
+            *reinterpret_cast<h4*>(s_b + thin_at<R>(i, j, true)) = lo;
+        }
+        lds_barrier();
+        // B = sb A + sc A A, rows 16 (GT wave + u) of it
+        f4 acc[GT][RT] = {};
+#pragma unroll
+        for (int s = 0; s < RS; s++) {
+            const _Float16* line = s_b + s * (R * kLine);
+            h8 ph[GT], pl[GT];
+#pragma unroll
+            for (int u = 0; u < GT; u++) {
+                const uint32_t row = 16 * (GT * wave + u) + li;
+                ph[u] = *reinterpret_cast<const h8*>(line + swizzled(row, lg));
+                pl[u] = *reinterpret_cast<const h8*>(line + swizzled(row, lg + 4));
+            }
+#pragma unroll
+            for (int v = 0; v < RT; v++) {
+                const h8 qh = *reinterpret_cast<const h8*>(line + swizzled(16 * v + li, lg));
+                const h8 ql = *reinterpret_cast<const h8*>(line + swizzled(16 * v + li, lg + 4));
+#pragma unroll
+                for (int u = 0; u < GT; u++) acc[u][v] = mfma3(qh, ql, ph[u], pl[u], acc[u][v]);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < GT; u++)
+#pragma unroll
+            for (int v = 0; v < RT; v++) {
+                const uint32_t i = 16 * (GT * wave + u) + li, j = 16 * v + 4 * lg;
+                const h4 hi = *reinterpret_cast<const h4*>(s_b + thin_at<R>(i, j, false));
+                const h4 lo = *reinterpret_cast<const h4*>(s_b + thin_at<R>(i, j, true));
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    acc[u][v][e] = acc[u][v][e] * g.sc + ((float)hi[e] + (float)lo[e]) * g.sb;
+            }
+        lds_barrier();
+#pragma unroll
+        for (int u = 0; u < GT; u++)
+#pragma unroll
+            for (int v = 0; v < RT; v++) {
+                const uint32_t i = 16 * (GT * wave + u) + li, j = 16 * v + 4 * lg;
+                h4 hi, lo;
+                split4(acc[u][v], hi, lo);
+                *reinterpret_cast<h4*>(s_b + thin_at<R>(i, j, false)) = hi;
+                *reinterpret_cast<h4*>(s_b + thin_at<R>(i, j, true)) = lo;
+            }
+        lds_barrier();
+    }
+    f4 gram[GT][RT] = {};
+    const bool last = !FIRST && g.out != nullptr;
+    const uint32_t slab0 = blockIdx.x * g.per, slab1 = min(slab0 + g.per, g.slabs);
+    for (uint32_t slab = slab0; slab < slab1; slab++) {
+        const uint32_t col = slab * 64 + wave * 16 + li;  // along the longer side
+        f4* master = reinterpret_cast<f4*>(g.master) +
+                     (((size_t)batch * g.slabs + slab) * 4 + wave) * (RT * 64) + lane;
+        f4 mine[RT];
+        if constexpr (FIRST) {
+            const T* x = static_cast<const T*>(g.x) + batch * g.x_stride;
+#pragma unroll
+            for (int u = 0; u < RT; u++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const uint32_t row = 16 * u + 4 * lg + e;
+                    const uint64_t i = g.tall ? col : row, j = g.tall ? row : col;
+                    mine[u][e] = i < g.m && j < g.n ? (float)x[i * g.x_ld + j] * f : 0.0f;
+                }
+        } else {
+#pragma unroll
+            for (int u = 0; u < RT; u++) mine[u] = master[u * 64];
+            h8 xh[RS], xl[RS];
+#pragma unroll
+            for (int s = 0; s < RS; s++)
+#pragma unroll
+                for (int q = 0; q < 2; q++)
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        _Float16 hi, lo;
+                        split<2>(mine[2 * s + q][e] * g.x_unit, hi, lo);
+                        xh[s][4 * q + e] = hi;
+                        xl[s][4 * q + e] = lo;
+                    }
+#pragma unroll
+            for (int u = 0; u < RT; u++) {
+                f4 sum = {};
+#pragma unroll
+                for (int s = 0; s < RS; s++) {
+                    const _Float16* line = s_b + s * (R * kLine);
+                    const h8 bh = *reinterpret_cast<const h8*>(line + swizzled(16 * u + li, lg));
+                    const h8 bl = *reinterpret_cast<const h8*>(line + swizzled(16 * u + li, lg + 4));
+                    sum = mfma3(bh, bl, xh[s], xl[s], sum);
+                }
+                mine[u] = mine[u] * g.a + sum * g.factor;
+            }
+        }
+        if (last) {
+            T* out = static_cast<T*>(g.out) + batch * g.out_stride;
+#pragma unroll
+            for (int u = 0; u < RT; u++)
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const uint32_t row = 16 * u + 4 * lg + e;
+                    const uint64_t i = g.tall ? col : row, j = g.tall ? row : col;
+                    if (i < g.m && j < g.n) out[i * g.out_ld + j] = (T)(mine[u][e] * g.out_scale);
+                }
+            continue;
+        }
+#pragma unroll
+        for (int u = 0; u < RT; u++) master[u * 64] = mine[u];
+        // the columns' part of the next A
+        _Float16* sx = s_x + (wave >> 1) * (R * kLine);
+        const uint32_t c = (wave & 1) * 16 + li;  // of 32 in a line
+        lds_barrier();                            // the last slab's are read
+#pragma unroll
+        for (int u = 0; u < RT; u++)
+#pragma unroll
+            for (int e = 0; e < 4; e++) {
+                const uint32_t row = 16 * u + 4 * lg + e;
+                _Float16 hi, lo;
+                split<2>(mine[u][e] * g.gram_x, hi, lo);
+                sx[swizzled(row, c >> 3) + (c & 7u)] = hi;
+                sx[swizzled(row, (c >> 3) + 4) + (c & 7u)] = lo;
+            }
+        lds_barrier();
+#pragma unroll
+        for (int s = 0; s < 2; s++) {
+            const _Float16* line = s_x + s * (R * kLine);
+            h8 ph[GT], pl[GT];
+#pragma unroll
+            for (int u = 0; u < GT; u++) {
+                const uint32_t row = 16 * (GT * wave + u) + li;
+                ph[u] = *reinterpret_cast<const h8*>(line + swizzled(row, lg));
+                pl[u] = *reinterpret_cast<const h8*>(line + swizzled(row, lg + 4));
+            }
+#pragma unroll
+            for (int v = 0; v < RT; v++) {
+                const h8 qh = *reinterpret_cast<const h8*>(line + swizzled(16 * v + li, lg));
+                const h8 ql = *reinterpret_cast<const h8*>(line + swizzled(16 * v + li, lg + 4));
+#pragma unroll
+                for (int u = 0; u < GT; u++) gram[u][v] = mfma3(qh, ql, ph[u], pl[u], gram[u][v]);
+            }
+        }
+    }
+    if (last) return;
+    f4* out = reinterpret_cast<f4*>(g.part_out) + ((size_t)batch * g.parts + blockIdx.x) * (R * R / 4);
+#pragma unroll
+    for (int u = 0; u < GT; u++)
+#pragma unroll
+        for (int v = 0; v < RT; v++)
+            out[((16 * (GT * wave + u) + li) * R + 16 * v + 4 * lg) / 4] = gram[u][v] * g.gram;
+}
+
 // ---- layout and launches ---------------------------------------------------------
 
-typedef Shape<256, 256, 128, 64> Large;
-typedef Shape<128, 128, 64, 64> Medium;
-typedef Shape<64, 64, 32, 32> Small;
+typedef Shape<256, 256, 128, 64, 2> Large;
+typedef Shape<128, 128, 64, 64, 2> Medium;
+typedef Shape<64, 64, 32, 32, 3> Small;
 
 // bf16 matrices with a side of at most this take two planes too: the rounding
 // of few entries does not average out (a 64-bit model of one plane's roundings:
@@ -507,29 +923,136 @@ typedef Shape<64, 64, 32, 32> Small;
 // sides are bound by launches, not by products.
 constexpr uint64_t kTwoPlaneSide = 256;
 
+// How a product runs: the tile, and the streams that share its steps (0: a
+// workgroup a tile).
+struct Way {
+    int tile;
+    uint32_t streams;
+};
+
+// Estimated time of a product in us, from measured ones: a step of 128 bytes
+// takes a workgroup `alone` on its CU, or `shared` by as many as fit; a tile's
+// first loads and its results take `ends`.  (One plane: a 4096 x 25088 Gram
+// product in 256-tiles, 136 of them, 574 us, its square 98; two planes, 6000 x
+// 1500: Gram 329, 159 and 94 us in tiles of 256, 128 and 64, square 101, 44 and
+// 30, apply 116, 113 and 133.)
+struct TileCost {
+    int tile, resident;
+    double alone, shared, ends;  // one plane
+    double alone2, shared2;      // two
+};
+constexpr TileCost kTileCosts[3] = {
+    {256, 1, 1.50, 1.50, 8.0, 2.20, 2.20},
+    {128, 2, 0.50, 0.86, 8.0, 0.70, 0.98},
+    {64, 4, 0.35, 0.70, 6.0, 0.45, 0.92},
+};
+// Streams (256-tiles only): a share's steps run at no common phase, so less of
+// what they read is shared, and partial sums go to memory and back in a launch
+// of its own.  Where the tiles fill most CUs this is slower than whole tiles:
+// 528 tiles of 128 on 512 places 911 us, 676 as whole tiles.
+constexpr double kStreamStep = 1.95, kStreamStep2 = 2.50, kStreamEnds = 36.0;
+constexpr uint32_t kLeastSteps = 8;
+
+double plain_cost(const TileCost& c, uint64_t tiles, uint32_t lines, int planes, int cus) {
+    const double alone = planes == 1 ? c.alone : c.alone2, shared = planes == 1 ? c.shared : c.shared2;
+    const uint64_t slots = (uint64_t)cus * c.resident, full = tiles / slots, rest = tiles % slots;
+    double t = (double)full * (lines * shared + c.ends);
+    if (rest) {
+        const double filled = c.resident == 1 || rest <= (uint64_t)cus
+                                  ? 0.0
+                                  : (double)(rest - cus) / (double)(slots - cus);
+        t += lines * (alone + filled * (shared - alone)) + c.ends;
+    }
+    return t;
+}
+
+double best_way(uint64_t tiles256, uint64_t tiles128, uint64_t tiles64, uint32_t lines, int planes,
+                int cus, Way* way) {
+    const uint64_t tiles[3] = {tiles256, tiles128, tiles64};
+    double best = 1e30;
+    for (int k = 0; k < 3; k++) {
+        if (tiles[k] == 0) continue;  // the sides are no multiples of this tile
+        const double t = plain_cost(kTileCosts[k], tiles[k], lines, planes, cus);
+        if (t < best) {
+            best = t;
+            *way = Way{kTileCosts[k].tile, 0};
+        }
+    }
+    if (tiles256 != 0 && tiles256 * 5 <= (uint64_t)cus * 3) {
+        const uint64_t most = tiles256 * lines / kLeastSteps;
+        const uint64_t streams = most < (uint64_t)cus ? most : (uint64_t)cus;
+        if (streams > tiles256) {
+            const double t = (double)(tiles256 * lines) / streams *
+                                 (planes == 1 ? kStreamStep : kStreamStep2) + kStreamEnds;
+            if (t < best) {
+                best = t;
+                *way = Way{256, (uint32_t)streams};
+            }
+        }
+    }
+    return best;
+}
+
+// CUs of the gfx950; a product is split over no more.
+constexpr int kMaxCus = 256;
+
+constexpr uint64_t kThinSide = 128;
+
 struct OrthoLayout {
     uint32_t rows, cols, r;  // padded m, n and their smaller
     int planes;
-    bool tall;
-    int tile;
-    size_t partial, inverse, master, x, xt[2], a, b, bytes;
+    bool tall, thin;
+    Way way[3];  // by Kind
+    uint32_t slabs, per, parts;  // thin
+    size_t partial, inverse, master, x, xt[2], a, b, part, bytes;
 };
 
-int tile_for(const hc_orthogonalise_params& p) {
-    const uint64_t r = p.m < p.n ? p.m : p.n;
-    return r > 1536 ? 256 : r > 64 ? 128 : 64;
+// Pads the sides to multiples of 64, 128 or 256 and picks every product's way,
+// for the least estimated time of a step.
+void plan_products(const hc_orthogonalise_params& p, int cus, OrthoLayout* L) {
+    double best = 1e30;
+    for (uint64_t pad = 64; pad <= 256; pad *= 2) {
+        const uint64_t rows = (p.m + pad - 1) / pad * pad, cols = (p.n + pad - 1) / pad * pad;
+        const uint64_t r = L->tall ? cols : rows, k = L->tall ? rows : cols;
+        uint64_t half[3] = {}, all[3] = {};  // tiles of 256, 128, 64
+        for (int s = 0; s < 3; s++) {
+            const uint64_t t = 256 >> s;
+            if (t > pad) continue;
+            half[s] = p.batch * (r / t) * (r / t + 1) / 2;
+            all[s] = p.batch * (r / t) * (k / t);
+        }
+        Way way[3];
+        const double t =
+            best_way(half[0], half[1], half[2], (uint32_t)(k * L->planes / kLine), L->planes, cus, &way[GRAM]) +
+            best_way(half[0], half[1], half[2], (uint32_t)(r * L->planes / kLine), L->planes, cus, &way[SQUARE]) +
+            best_way(all[0], all[1], all[2], (uint32_t)(r * L->planes / kLine), L->planes, cus, &way[APPLY]);
+        if (t < best) {
+            best = t;
+            L->rows = (uint32_t)rows;
+            L->cols = (uint32_t)cols;
+            for (int s = 0; s < 3; s++) L->way[s] = way[s];
+        }
+    }
 }
 
 OrthoLayout ortho_layout(const hc_orthogonalise_params& p) {
     OrthoLayout L;
     const uint64_t r = p.m < p.n ? p.m : p.n;
-    L.tile = tile_for(p);
-    const uint64_t t = L.tile;
-    L.rows = (uint32_t)((p.m + t - 1) / t * t);
-    L.cols = (uint32_t)((p.n + t - 1) / t * t);
     L.tall = p.m > p.n;
-    L.r = L.tall ? L.cols : L.rows;
+    L.thin = r <= kThinSide;
     L.planes = p.type == HC_T_F32 || r <= kTwoPlaneSide ? 2 : 1;
+    if (L.thin) {
+        // a workgroup reads all parts of A (16 KiB each with 64 rows, 64 KiB
+        // with 128), so they are kept few
+        const uint32_t most = r <= 64 ? 32 : 16;
+        L.r = r <= 64 ? 64 : 128;
+        L.slabs = (uint32_t)(((L.tall ? p.m : p.n) + 63) / 64);
+        L.per = (L.slabs + most - 1) / most;
+        L.parts = (L.slabs + L.per - 1) / L.per;
+    } else {
+        plan_products(p, kMaxCus, &L);
+        L.r = L.tall ? L.cols : L.rows;
+    }
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t o = at;
@@ -537,8 +1060,16 @@ OrthoLayout ortho_layout(const hc_orthogonalise_params& p) {
         return o;
     };
     const bool any = p.steps > 0;
-    const size_t xs = any ? p.batch * L.rows * L.cols : 0, as = any ? p.batch * L.r * L.r : 0;
     L.partial = take(p.batch * kNormParts * sizeof(double));
+    if (L.thin) {
+        const size_t part = any ? p.batch * L.parts * L.r * L.r * 4 : 0;
+        L.master = take(any ? p.batch * L.slabs * 64 * L.r * 4 : 0);
+        L.xt[0] = take(part);  // the parts of A, of this step and the next
+        L.xt[1] = take(part);
+        L.bytes = at;
+        return L;
+    }
+    const size_t xs = any ? p.batch * L.rows * L.cols : 0, as = any ? p.batch * L.r * L.r : 0;
     L.inverse = take(p.batch * 4);
     L.master = take(xs * 4);
     L.x = take(xs * 2 * L.planes);
@@ -546,27 +1077,93 @@ OrthoLayout ortho_layout(const hc_orthogonalise_params& p) {
     L.xt[1] = take(xs * 2 * L.planes);
     L.a = take(as * 2 * L.planes);
     L.b = take(as * 2 * L.planes);
+    uint32_t streams = 0;
+    for (const Way& w : L.way) streams = w.streams > streams ? w.streams : streams;
+    L.part = take(any ? (size_t)streams * 2 * 256 * 256 * 4 : 0);
     L.bytes = at;
     return L;
 }
 
 template <Kind KIND, int PLANES, typename T, typename S>
-hipError_t product_shape(Product g, uint32_t batch, hipStream_t s) {
-    const auto kernel = &product_kernel<KIND, PLANES, T, S>;
-    const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), S::kLdsBytes);
-    if (e != hipSuccess) return e;
+hipError_t product_shape(Product g, uint32_t batch, uint32_t streams, hipStream_t s) {
     g.tiles_i = g.rows / S::BM;
     g.tiles_j = g.cols / S::BN;
-    const uint32_t tiles = KIND == APPLY ? g.tiles_i * g.tiles_j : g.tiles_i * (g.tiles_i + 1) / 2;
-    hipLaunchKernelGGL(kernel, dim3(tiles, batch), dim3(S::kThreads), S::kLdsBytes, s, g);
-    return hipGetLastError();
+    g.tiles = KIND == APPLY ? g.tiles_i * g.tiles_j : g.tiles_i * (g.tiles_i + 1) / 2;
+    g.batch = batch;
+    g.streams = streams;
+    auto launch = [&](auto kernel, uint32_t groups) {
+        const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), S::kLdsBytes);
+        if (e != hipSuccess) return e;
+        hipLaunchKernelGGL(kernel, dim3(groups), dim3(S::kThreads), S::kLdsBytes, s, g);
+        return hipGetLastError();
+    };
+    if constexpr (S::BM == 256) {
+        if (streams) {
+            const hipError_t e = launch(&stream_kernel<KIND, PLANES, T, S>, streams);
+            if (e != hipSuccess) return e;
+            hipLaunchKernelGGL((join_kernel<KIND, PLANES, T, S>),
+                               dim3(g.tiles * batch * (S::BM / S::EM) * (S::BN / S::EN)),
+                               dim3(S::EM * 4), 0, s, g);
+            return hipGetLastError();
+        }
+    }
+    return launch(&product_kernel<KIND, PLANES, T, S>, g.tiles * batch);
 }
 
 template <Kind KIND, int PLANES, typename T>
-hipError_t product(const Product& g, int tile, uint32_t batch, hipStream_t s) {
-    if (tile == 256) return product_shape<KIND, PLANES, T, Large>(g, batch, s);
-    if (tile == 128) return product_shape<KIND, PLANES, T, Medium>(g, batch, s);
-    return product_shape<KIND, PLANES, T, Small>(g, batch, s);
+hipError_t product(const Product& g, const OrthoLayout& L, uint32_t batch, hipStream_t s) {
+    const Way w = L.way[KIND];
+    if (w.tile == 256) return product_shape<KIND, PLANES, T, Large>(g, batch, w.streams, s);
+    if (w.tile == 128) return product_shape<KIND, PLANES, T, Medium>(g, batch, 0, s);
+    return product_shape<KIND, PLANES, T, Small>(g, batch, 0, s);
+}
+
+template <typename T, int R>
+hipError_t thin_typed(const hc_orthogonalise_params& p, const OrthoLayout& L, const OrthoStep* steps,
+                      const void* x, void* out, uint32_t norm_parts, char* ws, hipStream_t s) {
+    constexpr int kFirstLds = 2 * R * kLine * 2, kStepLds = kFirstLds + R * R * 4;
+    hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(&thin_kernel<T, R, false>), kStepLds);
+    if (e != hipSuccess) return e;
+    float* parts[2] = {reinterpret_cast<float*>(ws + L.xt[0]), reinterpret_cast<float*>(ws + L.xt[1])};
+    Thin g = {};
+    g.m = p.m;
+    g.n = p.n;
+    g.x_ld = p.x_ld;
+    g.x_stride = p.x_stride;
+    g.out_ld = p.out_ld;
+    g.out_stride = p.out_stride;
+    g.tall = L.tall;
+    g.slabs = L.slabs;
+    g.per = L.per;
+    g.parts = L.parts;
+    g.x = x;
+    g.master = reinterpret_cast<float*>(ws + L.master);
+    g.norm = reinterpret_cast<const double*>(ws + L.partial);
+    g.norm_parts = norm_parts;
+    g.eps = p.eps;
+    g.out_scale = p.scale;
+    const dim3 grid(L.parts, (uint32_t)p.batch);
+    auto next = [&](const OrthoStep& st) {  // units of step st's X and A
+        g.gram_x = ldexpf(1.0f, st.ex);
+        g.gram = ldexpf(1.0f, st.ea - 2 * st.ex);
+    };
+    g.part_out = parts[0];
+    next(steps[0]);
+    hipLaunchKernelGGL((thin_kernel<T, R, true>), grid, dim3(256), kFirstLds, s, g);
+    for (uint32_t t = 0; t < p.steps; t++) {
+        const OrthoStep& st = steps[t];
+        g.part_in = parts[t & 1];
+        g.part_out = parts[(t + 1) & 1];
+        g.a = st.a;
+        g.sb = ldexpf(st.b, st.eb - st.ea);
+        g.sc = ldexpf(st.c, st.eb - 2 * st.ea);
+        g.x_unit = ldexpf(1.0f, st.ex);
+        g.factor = ldexpf(1.0f, -st.eb - st.ex);
+        if (t + 1 < p.steps) next(steps[t + 1]);
+        else g.out = out;
+        hipLaunchKernelGGL((thin_kernel<T, R, false>), grid, dim3(256), kStepLds, s, g);
+    }
+    return hipGetLastError();
 }
 
 template <typename T, int PLANES>
@@ -587,6 +1184,10 @@ hipError_t orthogonalise_typed(const hc_orthogonalise_params& p, const OrthoStep
                            partial, (uint32_t)parts);
         return hipGetLastError();
     }
+    if constexpr (PLANES == 2)
+        if (L.thin)
+            return L.r == 64 ? thin_typed<T, 64>(p, L, steps, x, out, (uint32_t)parts, ws, s)
+                             : thin_typed<T, 128>(p, L, steps, x, out, (uint32_t)parts, ws, s);
     _Float16* X = reinterpret_cast<_Float16*>(ws + L.x);  // by the shorter side's rows
     _Float16* XT[2] = {reinterpret_cast<_Float16*>(ws + L.xt[0]),
                        reinterpret_cast<_Float16*>(ws + L.xt[1])};
@@ -614,13 +1215,14 @@ hipError_t orthogonalise_typed(const hc_orthogonalise_params& p, const OrthoStep
     for (uint32_t t = 0; t < p.steps && e == hipSuccess; t++) {
         const OrthoStep& st = steps[t];
         Product g = {};
+        g.part = reinterpret_cast<float*>(ws + L.part);
         g.p = g.q = X;
         g.p_stride = g.q_stride = x_size;
         g.inner = L.tall ? L.rows : L.cols;
         g.factor = ldexpf(1.0f, st.ea - 2 * st.ex);
         g.rows = g.cols = L.r;
         g.d = g.dt = A;
-        e = product<GRAM, PLANES, T>(g, L.tile, batch, s);
+        e = product<GRAM, PLANES, T>(g, L, batch, s);
         if (e != hipSuccess) return e;
         g.p = g.q = A;
         g.p_stride = g.q_stride = a_size;
@@ -628,7 +1230,7 @@ hipError_t orthogonalise_typed(const hc_orthogonalise_params& p, const OrthoStep
         g.factor = ldexpf(st.c, st.eb - 2 * st.ea);
         g.factor2 = ldexpf(st.b, st.eb - st.ea);
         g.d = g.dt = B;
-        e = product<SQUARE, PLANES, T>(g, L.tile, batch, s);
+        e = product<SQUARE, PLANES, T>(g, L, batch, s);
         if (e != hipSuccess) return e;
         g.p = L.tall ? XT[t & 1] : B;
         g.q = L.tall ? B : XT[t & 1];
@@ -656,7 +1258,7 @@ hipError_t orthogonalise_typed(const hc_orthogonalise_params& p, const OrthoStep
             g.out_stride = p.out_stride;
             g.out_scale = p.scale;
         }
-        e = product<APPLY, PLANES, T>(g, L.tile, batch, s);
+        e = product<APPLY, PLANES, T>(g, L, batch, s);
     }
     return e;
 }

@@ -187,7 +187,8 @@ struct Product {
     const _Float16 *p, *q;
     uint32_t inner;                  // length of l, a multiple of 64
     uint32_t tiles_i, tiles_j;       // tiles_j: of a result that is not symmetric
-    uint32_t tiles;                  // of one matrix
+    uint32_t tiles;                  // of one matrix that this launch makes
+    uint32_t first;                  // APPLY: first of them along the longer side
     uint32_t batch;
     // Streams: workgroups that share the steps of all tiles evenly, tile after
     // tile, and leave the sums of tiles that they do only part of in `part` (two
@@ -380,14 +381,18 @@ template <Kind KIND> __device__ __forceinline__ Tile tile_at(const Product& g, u
     o.batch = t / g.tiles;
     t -= o.batch * g.tiles;
     if constexpr (KIND == APPLY) {
-        // the shorter side (B's) first: neighbours share X^T's rows
-        if (g.tiles_i <= g.tiles_j) {
-            o.ti = t % g.tiles_i;
-            o.tj = t / g.tiles_i;
-        } else {
-            o.tj = t % g.tiles_j;
-            o.ti = t / g.tiles_j;
-        }
+        // blocks of 8 tiles along the shorter side (B's) by 4 along the longer:
+        // the 32 tiles that an XCD works on then read 12 panels, not 18
+        const bool wide = g.tiles_i <= g.tiles_j;
+        const uint32_t across = wide ? g.tiles_i : g.tiles_j, along = g.tiles / across;
+        const uint32_t stripe = t / (4 * across);
+        t -= stripe * 4 * across;
+        const uint32_t w = min(4u, along - 4 * stripe), block = t / (8 * w);
+        t -= block * 8 * w;
+        const uint32_t h = min(8u, across - 8 * block);
+        const uint32_t r = 8 * block + t % h, k = g.first + 4 * stripe + t / h;
+        o.ti = wide ? r : k;
+        o.tj = wide ? k : r;
     } else {
         // the lower triangle in squares of 4 x 4 tiles, so that tiles near each
         // other in the order share rows of both operands; row I of squares begins
@@ -924,10 +929,13 @@ typedef Shape<64, 64, 32, 32, 3> Small;
 constexpr uint64_t kTwoPlaneSide = 256;
 
 // How a product runs: the tile, and the streams that share its steps (0: a
-// workgroup a tile).
+// workgroup a tile).  APPLY: `cut` values of the longer side in tiles of `tile`,
+// the rest in tiles of `rest`.
 struct Way {
     int tile;
     uint32_t streams;
+    uint32_t cut;
+    int rest;
 };
 
 // Estimated time of a product in us, from measured ones: a step of 128 bytes
@@ -975,7 +983,7 @@ double best_way(uint64_t tiles256, uint64_t tiles128, uint64_t tiles64, uint32_t
         const double t = plain_cost(kTileCosts[k], tiles[k], lines, planes, cus);
         if (t < best) {
             best = t;
-            *way = Way{kTileCosts[k].tile, 0};
+            *way = Way{kTileCosts[k].tile, 0, 0, 0};
         }
     }
     if (tiles256 != 0 && tiles256 * 5 <= (uint64_t)cus * 3) {
@@ -986,7 +994,7 @@ double best_way(uint64_t tiles256, uint64_t tiles128, uint64_t tiles64, uint32_t
                                  (planes == 1 ? kStreamStep : kStreamStep2) + kStreamEnds;
             if (t < best) {
                 best = t;
-                *way = Way{256, (uint32_t)streams};
+                *way = Way{256, (uint32_t)streams, 0, 0};
             }
         }
     }
@@ -995,6 +1003,39 @@ double best_way(uint64_t tiles256, uint64_t tiles128, uint64_t tiles64, uint32_t
 
 // CUs of the gfx950; a product is split over no more.
 constexpr int kMaxCus = 256;
+constexpr double kLaunch = 4.0;
+
+// APPLY, whose results are r x k: tiles of one size, or as many as fill whole
+// rounds of the CUs and smaller ones for the rest of the longer side.
+double best_apply(uint64_t batch, uint64_t r, uint64_t k, uint64_t pad, uint32_t lines, int planes,
+                  int cus, Way* way) {
+    double best = 1e30;
+    for (int c = 0; c < 3; c++) {
+        const TileCost& T = kTileCosts[c];
+        const uint64_t tile = T.tile;
+        if (tile > pad) continue;
+        const uint64_t across = batch * (r / tile), along = k / tile;
+        const double whole = plain_cost(T, across * along, lines, planes, cus);
+        if (whole < best) {
+            best = whole;
+            *way = Way{T.tile, 0, (uint32_t)k, 0};
+        }
+        const uint64_t slots = (uint64_t)cus * T.resident;
+        const uint64_t part = across * along / slots * slots / across;  // whole rounds
+        if (part == 0 || part == along) continue;
+        for (int d = c + 1; d < 3; d++) {
+            const uint64_t small = kTileCosts[d].tile;
+            const double t = plain_cost(T, across * part, lines, planes, cus) + kLaunch +
+                             plain_cost(kTileCosts[d], batch * (r / small) * ((k - part * tile) / small),
+                                        lines, planes, cus);
+            if (t < best) {
+                best = t;
+                *way = Way{T.tile, 0, (uint32_t)(part * tile), kTileCosts[d].tile};
+            }
+        }
+    }
+    return best;
+}
 
 constexpr uint64_t kThinSide = 128;
 
@@ -1014,18 +1055,17 @@ void plan_products(const hc_orthogonalise_params& p, int cus, OrthoLayout* L) {
     for (uint64_t pad = 64; pad <= 256; pad *= 2) {
         const uint64_t rows = (p.m + pad - 1) / pad * pad, cols = (p.n + pad - 1) / pad * pad;
         const uint64_t r = L->tall ? cols : rows, k = L->tall ? rows : cols;
-        uint64_t half[3] = {}, all[3] = {};  // tiles of 256, 128, 64
+        uint64_t half[3] = {};  // tiles of 256, 128, 64
         for (int s = 0; s < 3; s++) {
             const uint64_t t = 256 >> s;
             if (t > pad) continue;
             half[s] = p.batch * (r / t) * (r / t + 1) / 2;
-            all[s] = p.batch * (r / t) * (k / t);
         }
         Way way[3];
         const double t =
             best_way(half[0], half[1], half[2], (uint32_t)(k * L->planes / kLine), L->planes, cus, &way[GRAM]) +
             best_way(half[0], half[1], half[2], (uint32_t)(r * L->planes / kLine), L->planes, cus, &way[SQUARE]) +
-            best_way(all[0], all[1], all[2], (uint32_t)(r * L->planes / kLine), L->planes, cus, &way[APPLY]);
+            best_apply(p.batch, r, k, pad, (uint32_t)(r * L->planes / kLine), L->planes, cus, &way[APPLY]);
         if (t < best) {
             best = t;
             L->rows = (uint32_t)rows;
@@ -1084,22 +1124,32 @@ OrthoLayout ortho_layout(const hc_orthogonalise_params& p) {
     return L;
 }
 
+template <Kind KIND, int PLANES, typename T, typename S, typename K>
+hipError_t launch_tiles(K kernel, const Product& g, uint32_t groups, hipStream_t s) {
+    const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), S::kLdsBytes);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, dim3(groups), dim3(S::kThreads), S::kLdsBytes, s, g);
+    return hipGetLastError();
+}
+
+// [k0, k1) of the longer side (APPLY), or all of it.
 template <Kind KIND, int PLANES, typename T, typename S>
-hipError_t product_shape(Product g, uint32_t batch, uint32_t streams, hipStream_t s) {
+hipError_t product_shape(Product g, uint32_t batch, uint32_t streams, uint32_t k0, uint32_t k1,
+                         hipStream_t s) {
     g.tiles_i = g.rows / S::BM;
     g.tiles_j = g.cols / S::BN;
-    g.tiles = KIND == APPLY ? g.tiles_i * g.tiles_j : g.tiles_i * (g.tiles_i + 1) / 2;
+    if (KIND == APPLY) {
+        g.first = k0 / S::BM;
+        g.tiles = (g.tiles_i < g.tiles_j ? g.tiles_i : g.tiles_j) * ((k1 - k0) / S::BM);
+    } else {
+        g.tiles = g.tiles_i * (g.tiles_i + 1) / 2;
+    }
     g.batch = batch;
     g.streams = streams;
-    auto launch = [&](auto kernel, uint32_t groups) {
-        const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), S::kLdsBytes);
-        if (e != hipSuccess) return e;
-        hipLaunchKernelGGL(kernel, dim3(groups), dim3(S::kThreads), S::kLdsBytes, s, g);
-        return hipGetLastError();
-    };
-    if constexpr (S::BM == 256) {
+    if constexpr (S::BM == 256 && KIND != APPLY) {
         if (streams) {
-            const hipError_t e = launch(&stream_kernel<KIND, PLANES, T, S>, streams);
+            const hipError_t e =
+                launch_tiles<KIND, PLANES, T, S>(&stream_kernel<KIND, PLANES, T, S>, g, streams, s);
             if (e != hipSuccess) return e;
             hipLaunchKernelGGL((join_kernel<KIND, PLANES, T, S>),
                                dim3(g.tiles * batch * (S::BM / S::EM) * (S::BN / S::EN)),
@@ -1107,15 +1157,23 @@ hipError_t product_shape(Product g, uint32_t batch, uint32_t streams, hipStream_
             return hipGetLastError();
         }
     }
-    return launch(&product_kernel<KIND, PLANES, T, S>, g.tiles * batch);
+    return launch_tiles<KIND, PLANES, T, S>(&product_kernel<KIND, PLANES, T, S>, g, g.tiles * batch, s);
+}
+
+template <Kind KIND, int PLANES, typename T>
+hipError_t product_tiles(const Product& g, int tile, uint32_t batch, uint32_t streams, uint32_t k0,
+                         uint32_t k1, hipStream_t s) {
+    if (tile == 256) return product_shape<KIND, PLANES, T, Large>(g, batch, streams, k0, k1, s);
+    if (tile == 128) return product_shape<KIND, PLANES, T, Medium>(g, batch, 0, k0, k1, s);
+    return product_shape<KIND, PLANES, T, Small>(g, batch, 0, k0, k1, s);
 }
 
 template <Kind KIND, int PLANES, typename T>
 hipError_t product(const Product& g, const OrthoLayout& L, uint32_t batch, hipStream_t s) {
     const Way w = L.way[KIND];
-    if (w.tile == 256) return product_shape<KIND, PLANES, T, Large>(g, batch, w.streams, s);
-    if (w.tile == 128) return product_shape<KIND, PLANES, T, Medium>(g, batch, 0, s);
-    return product_shape<KIND, PLANES, T, Small>(g, batch, 0, s);
+    const hipError_t e = product_tiles<KIND, PLANES, T>(g, w.tile, batch, w.streams, 0, w.cut, s);
+    if (e != hipSuccess || w.rest == 0) return e;
+    return product_tiles<KIND, PLANES, T>(g, w.rest, batch, 0, w.cut, g.rows > g.cols ? g.rows : g.cols, s);
 }
 
 template <typename T, int R>

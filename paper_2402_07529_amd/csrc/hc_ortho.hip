@@ -182,6 +182,8 @@ __global__ __launch_bounds__(kPrepBlock) void normalise_kernel(hc_orthogonalise_
 // Of a symmetric result the tiles on and below the diagonal are computed and
 // the others mirrored.
 enum Kind { GRAM, SQUARE, APPLY };
+// APPLY's step: the first reads x itself, the last writes the output.
+enum Step { MIDDLE = 0, FIRST = 1, LAST = 2 };
 
 struct Product {
     const _Float16 *p, *q;
@@ -466,52 +468,61 @@ __device__ __forceinline__ void accumulate(const Product& g, const Tile& tile, u
 }
 
 // What a tile's sums become, and where they go.
-template <Kind KIND, int PLANES, typename T, typename S> struct Results {
+template <Kind KIND, int STEP, int PLANES, typename T, typename S> struct Results {
     const Product& g;
     size_t base;      // of the matrix
     uint32_t batch;
     bool turn;        // the transpose is stored too
-    bool first, last; // APPLY: x is read; the output is written
-    float inverse;
+    float addend_factor;
+    static constexpr bool first = KIND == APPLY && (STEP & FIRST), last = KIND == APPLY && (STEP & LAST);
 
     __device__ __forceinline__ Results(const Product& g_, const Tile& t)
         : g(g_), base((size_t)t.batch * g_.rows * g_.cols), batch(t.batch),
-          turn(KIND == APPLY ? g_.out == nullptr : t.ti != t.tj),
-          first(KIND == APPLY && g_.x != nullptr), last(KIND == APPLY && g_.out != nullptr),
-          inverse(KIND == APPLY && g_.x != nullptr ? g_.inverse[t.batch] * g_.factor2 : 0.0f) {}
+          turn(KIND == APPLY ? !last : t.ti != t.tj),
+          addend_factor(first ? g_.inverse[t.batch] * g_.factor2 : g_.factor2) {}
 
-    // Results (i, j .. j + 3) are stored, and returned for the transpose.
-    __device__ __forceinline__ f4 straight(uint32_t i, uint32_t j, f4 sum) const {
-        f4 w = sum * g.factor;
+    // What is added to the sums of (i, j .. j + 3).  Read for a whole block before
+    // its first store: the loads do not wait for each other.
+    __device__ __forceinline__ f4 addend(uint32_t i, uint32_t j) const {
+        f4 w = {};
         if constexpr (KIND == SQUARE) {
             const _Float16* A = g.p + batch * g.p_stride + operand_at<PLANES>(i, g.inner, j);
             const h4 hi = *reinterpret_cast<const h4*>(A);
 #pragma unroll
-            for (int e = 0; e < 4; e++) w[e] += (float)hi[e] * g.factor2;
+            for (int e = 0; e < 4; e++) w[e] = (float)hi[e];
             if constexpr (PLANES == 2) {
                 const h4 lo = *reinterpret_cast<const h4*>(A + 32);
 #pragma unroll
-                for (int e = 0; e < 4; e++) w[e] += (float)lo[e] * g.factor2;
+                for (int e = 0; e < 4; e++) w[e] += (float)lo[e];
             }
         }
         if constexpr (KIND == APPLY) {
-            typedef T T4 __attribute__((ext_vector_type(4), aligned(sizeof(T))));
-            f4* mm = reinterpret_cast<f4*>(g.master + base + (size_t)i * g.cols + j);
-            if (first) {
+            if constexpr (first) {
+                typedef T T4 __attribute__((ext_vector_type(4), aligned(sizeof(T))));
                 const T* xr = static_cast<const T*>(g.x) + batch * g.x_stride + i * g.x_ld + j;
                 if (i < g.m && j + 3 < g.n) {
                     const T4 v = *reinterpret_cast<const T4*>(xr);
 #pragma unroll
-                    for (int e = 0; e < 4; e++) w[e] += (float)v[e] * inverse;
+                    for (int e = 0; e < 4; e++) w[e] = (float)v[e];
                 } else {
 #pragma unroll
                     for (int e = 0; e < 4; e++)
-                        if (i < g.m && j + e < g.n) w[e] += (float)xr[e] * inverse;
+                        if (i < g.m && j + e < g.n) w[e] = (float)xr[e];
                 }
             } else {
-                w += *mm * g.factor2;
+                w = *reinterpret_cast<const f4*>(g.master + base + (size_t)i * g.cols + j);
             }
-            if (last) {
+        }
+        return w;
+    }
+
+    // Results (i, j .. j + 3) are stored, and returned for the transpose.
+    __device__ __forceinline__ f4 straight(uint32_t i, uint32_t j, f4 sum, f4 add) const {
+        f4 w = sum * g.factor;
+        if constexpr (KIND != GRAM) w += add * addend_factor;
+        if constexpr (KIND == APPLY) {
+            typedef T T4 __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+            if constexpr (last) {
                 w *= g.out_scale;
                 T* o = static_cast<T*>(g.out) + batch * g.out_stride + i * g.out_ld + j;
                 if (i < g.m && j + 3 < g.n) {
@@ -525,9 +536,10 @@ template <Kind KIND, int PLANES, typename T, typename S> struct Results {
                         if (i < g.m && j + e < g.n) o[e] = (T)w[e];
                 }
                 return w;
-            }
-            *mm = w;
+            } else {
+            *reinterpret_cast<f4*>(g.master + base + (size_t)i * g.cols + j) = w;
             w *= g.next;
+            }
         }
         h4 hi, lo;
 #pragma unroll
@@ -567,7 +579,7 @@ template <Kind KIND, int PLANES, typename T, typename S> struct Results {
 
 // A workgroup's sums of a whole tile become its results, a wave its own part:
 // fragment (u, v) of a lane holds i = lane % 16, j = 4 (lane / 16) .. + 3.
-template <Kind KIND, int PLANES, typename T, typename S>
+template <Kind KIND, int STEP, int PLANES, typename T, typename S>
 __device__ __forceinline__ void finish(const Product& g, const Tile& tile, char* s_mem,
                                        f4 (&acc)[S::WM / 16][S::WN / 16]) {
     constexpr int EM = S::EM, EN = S::EN;
@@ -576,18 +588,23 @@ __device__ __forceinline__ void finish(const Product& g, const Tile& tile, char*
     const uint32_t j0 = tile.tj * S::BN + wave % (S::BN / S::WN) * S::WN;
     const uint32_t fi = lane & 15, fj = (lane >> 4) * 4;
     float* stage = reinterpret_cast<float*>(s_mem) + wave * EM * EN;
-    const Results<KIND, PLANES, T, S> out(g, tile);
+    const Results<KIND, STEP, PLANES, T, S> out(g, tile);
 #pragma unroll
     for (int eu = 0; eu < S::WM / EM; eu++)
 #pragma unroll
         for (int ev = 0; ev < S::WN / EN; ev++) {
             const uint32_t ib = i0 + eu * EM, jb = j0 + ev * EN;
+            f4 add[EM / 16][EN / 16];
+#pragma unroll
+            for (int u = 0; u < EM / 16; u++)
+#pragma unroll
+                for (int v = 0; v < EN / 16; v++) add[u][v] = out.addend(ib + 16 * u + fi, jb + 16 * v + fj);
 #pragma unroll
             for (int u = 0; u < EM / 16; u++)
 #pragma unroll
                 for (int v = 0; v < EN / 16; v++) {
                     const f4 w = out.straight(ib + 16 * u + fi, jb + 16 * v + fj,
-                                              acc[eu * (EM / 16) + u][ev * (EN / 16) + v]);
+                                              acc[eu * (EM / 16) + u][ev * (EN / 16) + v], add[u][v]);
                     *reinterpret_cast<f4*>(stage + staged<EN>(16 * u + fi, 16 * v + fj)) = w;
                 }
             if (!out.turn) continue;
@@ -605,13 +622,13 @@ __device__ __forceinline__ uint64_t stream_begin(const Product& g, uint32_t line
 }
 
 // One tile a workgroup.
-template <Kind KIND, int PLANES, typename T, typename S>
+template <Kind KIND, int STEP, int PLANES, typename T, typename S>
 __global__ __launch_bounds__(S::kThreads) void product_kernel(Product g) {
     extern __shared__ __align__(16) char s_mem[];
     const Tile tile = tile_at<KIND>(g, by_xcd(blockIdx.x, gridDim.x));
     f4 acc[S::WM / 16][S::WN / 16] = {};
     accumulate<PLANES, S>(g, tile, 0, g.inner * PLANES / kLine, s_mem, acc);
-    finish<KIND, PLANES, T, S>(g, tile, s_mem, acc);
+    finish<KIND, STEP, PLANES, T, S>(g, tile, s_mem, acc);
 }
 
 // An equal share of all tiles' steps a workgroup.
@@ -630,7 +647,7 @@ __global__ __launch_bounds__(S::kThreads) void stream_kernel(Product g) {
         f4 acc[FM][FN] = {};
         accumulate<PLANES, S>(g, tile, l0, l1, s_mem, acc);
         if (l1 - l0 == lines) {
-            finish<KIND, PLANES, T, S>(g, tile, s_mem, acc);
+            finish<KIND, MIDDLE, PLANES, T, S>(g, tile, s_mem, acc);
         } else {
             f4* part = reinterpret_cast<f4*>(g.part) +
                        ((size_t)stream * 2 + (l0 > 0 ? 0 : 1)) * (S::BM * S::BN / 4);
@@ -672,14 +689,17 @@ __global__ __launch_bounds__(S::EM * 4) void join_kernel(Product g) {
         for (int v = 0; v < EN / 16; v++) acc[v] += part[v * S::kThreads];
     }
     const Tile tile = tile_at<KIND>(g, t);
-    const Results<KIND, PLANES, T, S> out(g, tile);
+    const Results<KIND, MIDDLE, PLANES, T, S> out(g, tile);
     const uint32_t ib = tile.ti * S::BM + wave / (S::BN / S::WN) * S::WM + eu * EM;
     const uint32_t jb = tile.tj * S::BN + wave % (S::BN / S::WN) * S::WN + ev * EN;
     const uint32_t fi = 16 * u + (lane & 15), fj = (lane >> 4) * 4;
+    f4 add[EN / 16];
+#pragma unroll
+    for (int v = 0; v < EN / 16; v++) add[v] = out.addend(ib + fi, jb + 16 * v + fj);
 #pragma unroll
     for (int v = 0; v < EN / 16; v++)
         *reinterpret_cast<f4*>(s_stage + staged<EN>(fi, 16 * v + fj)) =
-            out.straight(ib + fi, jb + 16 * v + fj, acc[v]);
+            out.straight(ib + fi, jb + 16 * v + fj, acc[v], add[v]);
     if (!out.turn) return;
     lds_barrier();
     out.turned(s_stage, ib, jb, threadIdx.x, EM * 4);
@@ -1124,7 +1144,7 @@ OrthoLayout ortho_layout(const hc_orthogonalise_params& p) {
     return L;
 }
 
-template <Kind KIND, int PLANES, typename T, typename S, typename K>
+template <typename S, typename K>
 hipError_t launch_tiles(K kernel, const Product& g, uint32_t groups, hipStream_t s) {
     const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), S::kLdsBytes);
     if (e != hipSuccess) return e;
@@ -1149,7 +1169,7 @@ hipError_t product_shape(Product g, uint32_t batch, uint32_t streams, uint32_t k
     if constexpr (S::BM == 256 && KIND != APPLY) {
         if (streams) {
             const hipError_t e =
-                launch_tiles<KIND, PLANES, T, S>(&stream_kernel<KIND, PLANES, T, S>, g, streams, s);
+                launch_tiles<S>(&stream_kernel<KIND, PLANES, T, S>, g, streams, s);
             if (e != hipSuccess) return e;
             hipLaunchKernelGGL((join_kernel<KIND, PLANES, T, S>),
                                dim3(g.tiles * batch * (S::BM / S::EM) * (S::BN / S::EN)),
@@ -1157,7 +1177,18 @@ hipError_t product_shape(Product g, uint32_t batch, uint32_t streams, uint32_t k
             return hipGetLastError();
         }
     }
-    return launch_tiles<KIND, PLANES, T, S>(&product_kernel<KIND, PLANES, T, S>, g, g.tiles * batch, s);
+    const uint32_t groups = g.tiles * batch;
+    if constexpr (KIND == APPLY) {
+        switch ((g.x ? FIRST : 0) | (g.out ? LAST : 0)) {
+            case FIRST:
+                return launch_tiles<S>(&product_kernel<KIND, FIRST, PLANES, T, S>, g, groups, s);
+            case LAST:
+                return launch_tiles<S>(&product_kernel<KIND, LAST, PLANES, T, S>, g, groups, s);
+            case FIRST | LAST:
+                return launch_tiles<S>(&product_kernel<KIND, FIRST | LAST, PLANES, T, S>, g, groups, s);
+        }
+    }
+    return launch_tiles<S>(&product_kernel<KIND, MIDDLE, PLANES, T, S>, g, groups, s);
 }
 
 template <Kind KIND, int PLANES, typename T>

@@ -204,8 +204,11 @@ struct Product {
     // results: rows x cols (padded), as operands, and transposed
     _Float16 *d, *dt;
     uint32_t rows, cols;
-    // APPLY: X in fp32; in the first step x itself is read, times the inverse norm
-    float* master;
+    // APPLY: X between the steps: fp32 (two planes), or its operand `prev` and the
+    // fp16 rest `master` in the same unit (one); in the first step x itself is
+    // read, times the inverse norm
+    void* master;
+    const _Float16* prev;
     const void* x;
     const float* inverse;
     uint64_t m, n, x_ld, x_stride;
@@ -481,8 +484,9 @@ template <Kind KIND, int STEP, int PLANES, typename T, typename S> struct Result
           turn(KIND == APPLY ? !last : t.ti != t.tj),
           addend_factor(first ? g_.inverse[t.batch] * g_.factor2 : g_.factor2) {}
 
-    // What is added to the sums of (i, j .. j + 3).  Read for a whole block before
-    // its first store: the loads do not wait for each other.
+    // What is added to the sums of (i, j .. j + 3): A, or X, or x in the first
+    // step.  Read for a whole block before its first store, so that the loads do
+    // not wait for each other.
     __device__ __forceinline__ f4 addend(uint32_t i, uint32_t j) const {
         f4 w = {};
         if constexpr (KIND == SQUARE) {
@@ -496,63 +500,84 @@ template <Kind KIND, int STEP, int PLANES, typename T, typename S> struct Result
                 for (int e = 0; e < 4; e++) w[e] += (float)lo[e];
             }
         }
-        if constexpr (KIND == APPLY) {
-            if constexpr (first) {
-                typedef T T4 __attribute__((ext_vector_type(4), aligned(sizeof(T))));
-                const T* xr = static_cast<const T*>(g.x) + batch * g.x_stride + i * g.x_ld + j;
-                if (i < g.m && j + 3 < g.n) {
-                    const T4 v = *reinterpret_cast<const T4*>(xr);
+        if constexpr (first) {
+            typedef T T4 __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+            const T* xr = static_cast<const T*>(g.x) + batch * g.x_stride + i * g.x_ld + j;
+            if (i < g.m && j + 3 < g.n) {
+                const T4 v = *reinterpret_cast<const T4*>(xr);
 #pragma unroll
-                    for (int e = 0; e < 4; e++) w[e] = (float)v[e];
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; e++)
-                        if (i < g.m && j + e < g.n) w[e] = (float)xr[e];
-                }
+                for (int e = 0; e < 4; e++) w[e] = (float)v[e];
             } else {
-                w = *reinterpret_cast<const f4*>(g.master + base + (size_t)i * g.cols + j);
+#pragma unroll
+                for (int e = 0; e < 4; e++)
+                    if (i < g.m && j + e < g.n) w[e] = (float)xr[e];
+            }
+        } else if constexpr (KIND == APPLY) {
+            const size_t at = base + (size_t)i * g.cols + j;
+            if constexpr (PLANES == 2) {
+                w = *reinterpret_cast<const f4*>(static_cast<const float*>(g.master) + at);
+            } else {
+                const h4 hi = *reinterpret_cast<const h4*>(g.prev + at);
+                const h4 lo = *reinterpret_cast<const h4*>(static_cast<const _Float16*>(g.master) + at);
+#pragma unroll
+                for (int e = 0; e < 4; e++) w[e] = (float)hi[e] + (float)lo[e];
             }
         }
         return w;
     }
 
-    // Results (i, j .. j + 3) are stored, and returned for the transpose.
-    __device__ __forceinline__ f4 straight(uint32_t i, uint32_t j, f4 sum, f4 add) const {
+    __device__ __forceinline__ f4 result(f4 sum, f4 add) const {
         f4 w = sum * g.factor;
         if constexpr (KIND != GRAM) w += add * addend_factor;
-        if constexpr (KIND == APPLY) {
-            typedef T T4 __attribute__((ext_vector_type(4), aligned(sizeof(T))));
-            if constexpr (last) {
-                w *= g.out_scale;
-                T* o = static_cast<T*>(g.out) + batch * g.out_stride + i * g.out_ld + j;
-                if (i < g.m && j + 3 < g.n) {
-                    T4 v;
+        return w;
+    }
+
+    // A block's results in LDS, 8 consecutive j of one i a lane, so that rows of
+    // 128 bytes are stored.  Lanes `at`, at + step, ... of the EM EN / 8.
+    __device__ __forceinline__ void straight(const float* stage, uint32_t ib, uint32_t jb, uint32_t at,
+                                             uint32_t step) const {
+        constexpr int kPer = S::EN / 8;  // lanes for one i
+        for (uint32_t q = at; q < S::EM * kPer; q += step) {
+            const uint32_t ii = q / kPer, jj = q % kPer * 8, i = ib + ii, j = jb + jj;
+            f4 w[2];
 #pragma unroll
-                    for (int e = 0; e < 4; e++) v[e] = (T)w[e];
-                    *reinterpret_cast<T4*>(o) = v;
+            for (int h = 0; h < 2; h++) w[h] = *reinterpret_cast<const f4*>(stage + staged<S::EN>(ii, jj + 4 * h));
+            if constexpr (last) {
+                typedef T T8 __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+                T* o = static_cast<T*>(g.out) + batch * g.out_stride + i * g.out_ld + j;
+                if (i < g.m && j + 7 < g.n) {
+                    T8 v;
+#pragma unroll
+                    for (int e = 0; e < 8; e++) v[e] = (T)(w[e >> 2][e & 3] * g.out_scale);
+                    *reinterpret_cast<T8*>(o) = v;
                 } else {
 #pragma unroll
-                    for (int e = 0; e < 4; e++)
-                        if (i < g.m && j + e < g.n) o[e] = (T)w[e];
+                    for (int e = 0; e < 8; e++)
+                        if (i < g.m && j + e < g.n) o[e] = (T)(w[e >> 2][e & 3] * g.out_scale);
                 }
-                return w;
             } else {
-            *reinterpret_cast<f4*>(g.master + base + (size_t)i * g.cols + j) = w;
-            w *= g.next;
+                const size_t mat = base + (size_t)i * g.cols + j;
+                if constexpr (KIND == APPLY && PLANES == 2) {
+                    f4* mm = reinterpret_cast<f4*>(static_cast<float*>(g.master) + mat);
+                    mm[0] = w[0];
+                    mm[1] = w[1];
+                }
+                h8 hi, lo;
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    _Float16 x, y;
+                    split<2>(w[e >> 2][e & 3] * (KIND == APPLY ? g.next : 1.0f), x, y);
+                    hi[e] = x;
+                    lo[e] = y;
+                }
+                _Float16* D = g.d + base * PLANES + operand_at<PLANES>(i, g.cols, j);
+                *reinterpret_cast<h8*>(D) = hi;
+                if constexpr (PLANES == 2)
+                    *reinterpret_cast<h8*>(D + 32) = lo;
+                else if constexpr (KIND == APPLY)
+                    *reinterpret_cast<h8*>(static_cast<_Float16*>(g.master) + mat) = lo;
             }
         }
-        h4 hi, lo;
-#pragma unroll
-        for (int e = 0; e < 4; e++) {
-            _Float16 x, y = 0;
-            split<PLANES>(w[e], x, y);
-            hi[e] = x;
-            lo[e] = y;
-        }
-        _Float16* D = g.d + base * PLANES + operand_at<PLANES>(i, g.cols, j);
-        *reinterpret_cast<h4*>(D) = hi;
-        if constexpr (PLANES == 2) *reinterpret_cast<h4*>(D + 32) = lo;
-        return w;
     }
 
     // The transpose of a block in LDS: 8 consecutive i of one j a lane.  Lanes
@@ -566,7 +591,7 @@ template <Kind KIND, int STEP, int PLANES, typename T, typename S> struct Result
 #pragma unroll
             for (int e = 0; e < 8; e++) {
                 _Float16 x, y = 0;
-                split<PLANES>(stage[staged<S::EN>(ii + e, jj)], x, y);
+                split<PLANES>(stage[staged<S::EN>(ii + e, jj)] * (KIND == APPLY ? g.next : 1.0f), x, y);
                 hi[e] = x;
                 lo[e] = y;
             }
@@ -603,15 +628,14 @@ __device__ __forceinline__ void finish(const Product& g, const Tile& tile, char*
             for (int u = 0; u < EM / 16; u++)
 #pragma unroll
                 for (int v = 0; v < EN / 16; v++) {
-                    const f4 w = out.straight(ib + 16 * u + fi, jb + 16 * v + fj,
-                                              acc[eu * (EM / 16) + u][ev * (EN / 16) + v], add[u][v]);
+                    const f4 w = out.result(acc[eu * (EM / 16) + u][ev * (EN / 16) + v], add[u][v]);
                     *reinterpret_cast<f4*>(stage + staged<EN>(16 * u + fi, 16 * v + fj)) = w;
                 }
-            if (!out.turn) continue;
             // only this wave's results are read
             __builtin_amdgcn_s_waitcnt(0xc07f);
             __builtin_amdgcn_wave_barrier();
-            out.turned(stage, ib, jb, lane, 64);
+            out.straight(stage, ib, jb, lane, 64);
+            if (out.turn) out.turned(stage, ib, jb, lane, 64);
             __builtin_amdgcn_wave_barrier();
         }
 }
@@ -698,11 +722,10 @@ __global__ __launch_bounds__(S::EM * 4) void join_kernel(Product g) {
     for (int v = 0; v < EN / 16; v++) add[v] = out.addend(ib + fi, jb + 16 * v + fj);
 #pragma unroll
     for (int v = 0; v < EN / 16; v++)
-        *reinterpret_cast<f4*>(s_stage + staged<EN>(fi, 16 * v + fj)) =
-            out.straight(ib + fi, jb + 16 * v + fj, acc[v], add[v]);
-    if (!out.turn) return;
+        *reinterpret_cast<f4*>(s_stage + staged<EN>(fi, 16 * v + fj)) = out.result(acc[v], add[v]);
     lds_barrier();
-    out.turned(s_stage, ib, jb, threadIdx.x, EM * 4);
+    out.straight(s_stage, ib, jb, threadIdx.x, EM * 4);
+    if (out.turn) out.turned(s_stage, ib, jb, threadIdx.x, EM * 4);
 }
 
 // ---- thin matrices ---------------------------------------------------------------
@@ -1131,7 +1154,7 @@ OrthoLayout ortho_layout(const hc_orthogonalise_params& p) {
     }
     const size_t xs = any ? p.batch * L.rows * L.cols : 0, as = any ? p.batch * L.r * L.r : 0;
     L.inverse = take(p.batch * 4);
-    L.master = take(xs * 4);
+    L.master = take(xs * 2 * L.planes);
     L.x = take(xs * 2 * L.planes);
     L.xt[0] = take(xs * 2 * L.planes);
     L.xt[1] = take(xs * 2 * L.planes);
@@ -1326,13 +1349,15 @@ hipError_t orthogonalise_typed(const hc_orthogonalise_params& p, const OrthoStep
         g.p_stride = L.tall ? x_size : a_size;
         g.q_stride = L.tall ? a_size : x_size;
         g.factor = ldexpf(1.0f, -st.eb - st.ex);
-        g.factor2 = st.a;
+        // a X, from its unit
+        g.factor2 = t > 0 && PLANES == 1 ? ldexpf(st.a, -st.ex) : st.a;
         g.next = ldexpf(1.0f, st.ex_next);
         g.rows = L.rows;
         g.cols = L.cols;
         g.d = L.tall ? XT[(t + 1) & 1] : X;
         g.dt = L.tall ? X : XT[(t + 1) & 1];
-        g.master = reinterpret_cast<float*>(ws + L.master);
+        g.master = ws + L.master;
+        g.prev = L.tall ? XT[t & 1] : X;
         g.m = p.m;
         g.n = p.n;
         if (t == 0) {

@@ -484,64 +484,73 @@ template <Kind KIND, int STEP, int PLANES, typename T, typename S> struct Result
           turn(KIND == APPLY ? !last : t.ti != t.tj),
           addend_factor(first ? g_.inverse[t.batch] * g_.factor2 : g_.factor2) {}
 
-    // What is added to the sums of (i, j .. j + 3): A, or X, or x in the first
-    // step.  Read for a whole block before its first store, so that the loads do
-    // not wait for each other.
-    __device__ __forceinline__ f4 addend(uint32_t i, uint32_t j) const {
-        f4 w = {};
+    // What is added to the sums of (i, j .. j + 7): A, or X, or x in the first step.
+    __device__ __forceinline__ void addend(uint32_t i, uint32_t j, f4 (&w)[2]) const {
         if constexpr (KIND == SQUARE) {
             const _Float16* A = g.p + batch * g.p_stride + operand_at<PLANES>(i, g.inner, j);
-            const h4 hi = *reinterpret_cast<const h4*>(A);
+            const h8 hi = *reinterpret_cast<const h8*>(A);
 #pragma unroll
-            for (int e = 0; e < 4; e++) w[e] = (float)hi[e];
+            for (int e = 0; e < 8; e++) w[e >> 2][e & 3] = (float)hi[e];
             if constexpr (PLANES == 2) {
-                const h4 lo = *reinterpret_cast<const h4*>(A + 32);
+                const h8 lo = *reinterpret_cast<const h8*>(A + 32);
 #pragma unroll
-                for (int e = 0; e < 4; e++) w[e] += (float)lo[e];
+                for (int e = 0; e < 8; e++) w[e >> 2][e & 3] += (float)lo[e];
             }
         }
         if constexpr (first) {
-            typedef T T4 __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+            typedef T T8 __attribute__((ext_vector_type(8), aligned(sizeof(T))));
             const T* xr = static_cast<const T*>(g.x) + batch * g.x_stride + i * g.x_ld + j;
-            if (i < g.m && j + 3 < g.n) {
-                const T4 v = *reinterpret_cast<const T4*>(xr);
+            if (i < g.m && j + 7 < g.n) {
+                const T8 v = *reinterpret_cast<const T8*>(xr);
 #pragma unroll
-                for (int e = 0; e < 4; e++) w[e] = (float)v[e];
+                for (int e = 0; e < 8; e++) w[e >> 2][e & 3] = (float)v[e];
             } else {
 #pragma unroll
-                for (int e = 0; e < 4; e++)
-                    if (i < g.m && j + e < g.n) w[e] = (float)xr[e];
+                for (int e = 0; e < 8; e++)
+                    w[e >> 2][e & 3] = i < g.m && j + e < g.n ? (float)xr[e] : 0.0f;
             }
         } else if constexpr (KIND == APPLY) {
             const size_t at = base + (size_t)i * g.cols + j;
             if constexpr (PLANES == 2) {
-                w = *reinterpret_cast<const f4*>(static_cast<const float*>(g.master) + at);
+                const f4* mm = reinterpret_cast<const f4*>(static_cast<const float*>(g.master) + at);
+                w[0] = mm[0];
+                w[1] = mm[1];
             } else {
-                const h4 hi = *reinterpret_cast<const h4*>(g.prev + at);
-                const h4 lo = *reinterpret_cast<const h4*>(static_cast<const _Float16*>(g.master) + at);
+                const h8 hi = *reinterpret_cast<const h8*>(g.prev + at);
+                const h8 lo = *reinterpret_cast<const h8*>(static_cast<const _Float16*>(g.master) + at);
 #pragma unroll
-                for (int e = 0; e < 4; e++) w[e] = (float)hi[e] + (float)lo[e];
+                for (int e = 0; e < 8; e++) w[e >> 2][e & 3] = (float)hi[e] + (float)lo[e];
             }
         }
-        return w;
     }
 
-    __device__ __forceinline__ f4 result(f4 sum, f4 add) const {
-        f4 w = sum * g.factor;
-        if constexpr (KIND != GRAM) w += add * addend_factor;
-        return w;
-    }
-
-    // A block's results in LDS, 8 consecutive j of one i a lane, so that rows of
-    // 128 bytes are stored.  Lanes `at`, at + step, ... of the EM EN / 8.
-    __device__ __forceinline__ void straight(const float* stage, uint32_t ib, uint32_t jb, uint32_t at,
+    // A block's sums in LDS become its results, 8 consecutive j of one i a lane, so
+    // that rows of 128 bytes are read and stored; what the transpose needs goes
+    // back to LDS.  N rounds of lanes `at`, at + step, ...: all addends are asked
+    // for before the first store, so that the loads do not wait for each other.
+    template <int N>
+    __device__ __forceinline__ void straight(float* stage, uint32_t ib, uint32_t jb, uint32_t at,
                                              uint32_t step) const {
         constexpr int kPer = S::EN / 8;  // lanes for one i
-        for (uint32_t q = at; q < S::EM * kPer; q += step) {
+        f4 add[N][2];
+        if constexpr (KIND != GRAM)
+#pragma unroll
+            for (int k = 0; k < N; k++) {
+                const uint32_t q = at + k * step;
+                addend(ib + q / kPer, jb + q % kPer * 8, add[k]);
+            }
+#pragma unroll
+        for (int k = 0; k < N; k++) {
+            const uint32_t q = at + k * step;
             const uint32_t ii = q / kPer, jj = q % kPer * 8, i = ib + ii, j = jb + jj;
             f4 w[2];
 #pragma unroll
-            for (int h = 0; h < 2; h++) w[h] = *reinterpret_cast<const f4*>(stage + staged<S::EN>(ii, jj + 4 * h));
+            for (int h = 0; h < 2; h++) {
+                f4* at_stage = reinterpret_cast<f4*>(stage + staged<S::EN>(ii, jj + 4 * h));
+                w[h] = *at_stage * g.factor;
+                if constexpr (KIND != GRAM) w[h] += add[k][h] * addend_factor;
+                if (turn) *at_stage = w[h];
+            }
             if constexpr (last) {
                 typedef T T8 __attribute__((ext_vector_type(8), aligned(sizeof(T))));
                 T* o = static_cast<T*>(g.out) + batch * g.out_stride + i * g.out_ld + j;
@@ -619,22 +628,18 @@ __device__ __forceinline__ void finish(const Product& g, const Tile& tile, char*
 #pragma unroll
         for (int ev = 0; ev < S::WN / EN; ev++) {
             const uint32_t ib = i0 + eu * EM, jb = j0 + ev * EN;
-            f4 add[EM / 16][EN / 16];
 #pragma unroll
             for (int u = 0; u < EM / 16; u++)
 #pragma unroll
-                for (int v = 0; v < EN / 16; v++) add[u][v] = out.addend(ib + 16 * u + fi, jb + 16 * v + fj);
-#pragma unroll
-            for (int u = 0; u < EM / 16; u++)
-#pragma unroll
-                for (int v = 0; v < EN / 16; v++) {
-                    const f4 w = out.result(acc[eu * (EM / 16) + u][ev * (EN / 16) + v], add[u][v]);
-                    *reinterpret_cast<f4*>(stage + staged<EN>(16 * u + fi, 16 * v + fj)) = w;
-                }
+                for (int v = 0; v < EN / 16; v++)
+                    *reinterpret_cast<f4*>(stage + staged<EN>(16 * u + fi, 16 * v + fj)) =
+                        acc[eu * (EM / 16) + u][ev * (EN / 16) + v];
             // only this wave's results are read
             __builtin_amdgcn_s_waitcnt(0xc07f);
             __builtin_amdgcn_wave_barrier();
-            out.straight(stage, ib, jb, lane, 64);
+            out.template straight<EM * EN / 512>(stage, ib, jb, lane, 64);
+            __builtin_amdgcn_s_waitcnt(0xc07f);
+            __builtin_amdgcn_wave_barrier();
             if (out.turn) out.turned(stage, ib, jb, lane, 64);
             __builtin_amdgcn_wave_barrier();
         }
@@ -717,14 +722,12 @@ __global__ __launch_bounds__(S::EM * 4) void join_kernel(Product g) {
     const uint32_t ib = tile.ti * S::BM + wave / (S::BN / S::WN) * S::WM + eu * EM;
     const uint32_t jb = tile.tj * S::BN + wave % (S::BN / S::WN) * S::WN + ev * EN;
     const uint32_t fi = 16 * u + (lane & 15), fj = (lane >> 4) * 4;
-    f4 add[EN / 16];
-#pragma unroll
-    for (int v = 0; v < EN / 16; v++) add[v] = out.addend(ib + fi, jb + 16 * v + fj);
 #pragma unroll
     for (int v = 0; v < EN / 16; v++)
-        *reinterpret_cast<f4*>(s_stage + staged<EN>(fi, 16 * v + fj)) = out.result(acc[v], add[v]);
+        *reinterpret_cast<f4*>(s_stage + staged<EN>(fi, 16 * v + fj)) = acc[v];
     lds_barrier();
-    out.straight(s_stage, ib, jb, threadIdx.x, EM * 4);
+    out.template straight<EN / 32>(s_stage, ib, jb, threadIdx.x, EM * 4);
+    lds_barrier();
     if (out.turn) out.turned(s_stage, ib, jb, threadIdx.x, EM * 4);
 }
 

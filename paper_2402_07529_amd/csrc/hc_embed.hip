@@ -56,6 +56,13 @@ template <typename T> __device__ __forceinline__ v4u load_raw(const T* p, int nv
     return __builtin_bit_cast(v4u, t);
 }
 
+// The same for what is read once.
+template <typename T> __device__ __forceinline__ v4u load_once(const T* p, int nv) {
+    if (nv == kVec<T>)
+        return __builtin_nontemporal_load(reinterpret_cast<const typename Wide<T>::V*>(p));
+    return load_raw<T>(p, nv);
+}
+
 // ---- lookup ----------------------------------------------------------------------
 
 template <typename ID>
@@ -115,7 +122,13 @@ __global__ __launch_bounds__(kBlock) void embed_kernel(const T* __restrict__ tab
                 t[j] = (T)y;
             }
             if (nv == VEC) {
-                *reinterpret_cast<typename Wide<T>::V*>(q) = __builtin_bit_cast(v4u, t);
+                // from 64 MB on past the caches, which then keep the table's rows:
+                // 2^20 rows of 64 fp32 91 -> 74 us
+                typedef typename Wide<T>::V V;
+                if constexpr (U > 1)
+                    __builtin_nontemporal_store((V)__builtin_bit_cast(v4u, t), reinterpret_cast<V*>(q));
+                else
+                    *reinterpret_cast<V*>(q) = __builtin_bit_cast(v4u, t);
             } else {
 #pragma unroll
                 for (int j = 0; j < VEC; j++)
@@ -151,7 +164,7 @@ hipError_t embed_typed(const hc_embed_params& p, const void* table, const void* 
                            (uint32_t)slabs, p.scale);
         return hipGetLastError();
     };
-    // four units a group once that still leaves every CU 16 workgroups
+    // four units a group once that still leaves every CU 16 workgroups (64 MB)
     if (units >= groups * 4 * 4096) return launch(&embed_kernel<T, ID, 4>, groups * 4);
     return launch(&embed_kernel<T, ID, 1>, groups);
 }
@@ -546,29 +559,38 @@ struct SumArgs {
     void* partial;
 };
 
+// The pairs that a workgroup's chunks look at lie in LDS: positions from p0.  (A
+// pair read from memory would wait for the stores of the sums before it, as all
+// vector memory of a wave completes in order.)
+constexpr uint32_t kGroupPairs = 2048;  // of the chunks themselves, see chunk_for
+struct NearPairs {
+    const Pair* s;
+    uint32_t p0;
+    __device__ __forceinline__ Pair operator[](uint32_t i) const { return s[i - p0]; }
+};
+
 // One chunk's columns of one slab (a group of lanes).  A run of pairs covers
 // boundary c if it holds the pairs on both sides of chunk c's start.  A run that
 // covers two boundaries is shared by the chunks that it reaches; any other is
 // summed whole by the chunk it begins in.
 template <typename TI, typename TO, bool ROWS>
-__device__ __forceinline__ void sum_chunk(const SumArgs& a, const TI* __restrict__ x,
-                                          TO* __restrict__ dst, uint32_t c, uint32_t slab,
-                                          uint32_t heads) {
+__device__ __forceinline__ void sum_chunk(const SumArgs& a, const NearPairs& pairs,
+                                          const TI* __restrict__ x, TO* __restrict__ dst, uint32_t c,
+                                          uint32_t slab, uint32_t heads) {
     typedef typename Sum<TO>::A A;
     constexpr int VEC = kVec<TI>;
-    constexpr int U = 8;
+    constexpr int U = 4;  // two batches in flight; 8: 175 us by rows of 2^20 ids (169), 72 BERT (68)
     const uint32_t col = ((slab << a.log2g) + (threadIdx.x & ((1u << a.log2g) - 1u))) * VEC;
     if (col >= a.dim) return;
     const int nv = (int)min((uint32_t)VEC, a.dim - col);
     const uint32_t C = a.chunk, n = a.count;
     uint32_t start = c * C;
     const uint32_t end = min(start + C, n);
-    // the keys around the chunk, all asked for at once
-    const uint32_t k_first = a.pairs[start].key, k_last = a.pairs[end - 1].key;
-    const uint32_t k_before = c > 0 ? a.pairs[start - 1].key : a.vocab;
-    const uint32_t k_earlier = c > 1 ? a.pairs[start - C - 1].key : a.vocab;
-    const uint32_t k_next = end < n ? a.pairs[end].key : a.vocab;
-    const uint32_t k_later = (uint64_t)end + C < n ? a.pairs[end + C].key : a.vocab;
+    const uint32_t k_first = pairs[start].key, k_last = pairs[end - 1].key;
+    const uint32_t k_before = c > 0 ? pairs[start - 1].key : a.vocab;
+    const uint32_t k_earlier = c > 1 ? pairs[start - C - 1].key : a.vocab;
+    const uint32_t k_next = end < n ? pairs[end].key : a.vocab;
+    const uint32_t k_later = (uint64_t)end + C < n ? pairs[end + C].key : a.vocab;
     if (k_first == a.vocab) return;
     uint32_t rank = heads;
     bool begins = k_before != k_first;
@@ -578,7 +600,7 @@ __device__ __forceinline__ void sum_chunk(const SumArgs& a, const TI* __restrict
             uint32_t lo = start, hi = end;  // first position with another key
             while (lo < hi) {
                 const uint32_t mid = (lo + hi) / 2;
-                if (a.pairs[mid].key == k_first) lo = mid + 1; else hi = mid;
+                if (pairs[mid].key == k_first) lo = mid + 1; else hi = mid;
             }
             if (lo == end) return;
             start = lo;
@@ -587,7 +609,7 @@ __device__ __forceinline__ void sum_chunk(const SumArgs& a, const TI* __restrict
             rank--;
         }
     }
-    uint32_t cur = begins && start != c * C ? a.pairs[start].key : k_first;
+    uint32_t cur = pairs[start].key;
     if (cur == a.vocab) return;
     // the last run goes on: shared if it covers the boundary after the next too,
     // else followed to its end
@@ -615,27 +637,35 @@ __device__ __forceinline__ void sum_chunk(const SumArgs& a, const TI* __restrict
             if (begins && col == 0) a.crossing[atomicAdd(a.crossing_count, 1u)] = make_uint2(c, rank);
         }
     };
-    bool done = false;
-    for (uint32_t i = start; i < limit && !done; i += U) {
-        Pair p[U];
-        v4u w[U];
+    // keys (vocab: nothing) and rows of U positions
+    auto ask = [&](uint32_t i, uint32_t (&key)[U], v4u (&w)[U]) {
 #pragma unroll
         for (int u = 0; u < U; u++) {
-            p[u] = i + u < limit ? a.pairs[i + u] : Pair{a.vocab, 0};
-            if (i + u >= end && p[u].key != k_last) p[u].key = a.vocab;
+            const Pair p = i + u < limit ? pairs[i + u] : Pair{a.vocab, 0};
+            key[u] = i + u >= end && p.key != k_last ? a.vocab : p.key;
+            if (key[u] != a.vocab) w[u] = load_once<TI>(x + (uint64_t)p.pos * a.x_ld + col, nv);
         }
-#pragma unroll
-        for (int u = 0; u < U; u++)
-            if (p[u].key != a.vocab) w[u] = load_raw<TI>(x + (uint64_t)p[u].pos * a.x_ld + col, nv);
+    };
+    uint32_t key[U], next_key[U];
+    v4u w[U], next_w[U];
+    ask(start, next_key, next_w);
+    for (uint32_t i = start; i < limit; i += U) {
 #pragma unroll
         for (int u = 0; u < U; u++) {
-            if (p[u].key == a.vocab) {
+            key[u] = next_key[u];
+            w[u] = next_w[u];
+        }
+        ask(i + U, next_key, next_w);  // before this batch's stores
+        bool done = false;
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            if (key[u] == a.vocab) {
                 done = true;
                 break;
             }
-            if (p[u].key != cur) {
+            if (key[u] != cur) {
                 flush(true);
-                cur = p[u].key;
+                cur = key[u];
                 begins = true;
                 if constexpr (ROWS) rank++;
 #pragma unroll
@@ -646,6 +676,7 @@ __device__ __forceinline__ void sum_chunk(const SumArgs& a, const TI* __restrict
 #pragma unroll
             for (int j = 0; j < VEC; j++) acc[j] += Sum<TO>::term(v[j], a.scale, a.fixed);
         }
+        if (done) break;
     }
     flush(!covers);
 }
@@ -681,37 +712,54 @@ template <typename TI, typename TO, bool ROWS>
 __global__ __launch_bounds__(kBlock) void segment_sum_kernel(SumArgs a, const TI* __restrict__ x,
                                                              TO* __restrict__ dst) {
     const uint64_t units = (uint64_t)a.chunks * a.slabs;
-    const uint64_t step = ((uint64_t)gridDim.x * kBlock) >> a.log2g;
-    const uint64_t first = ((uint64_t)blockIdx.x * kBlock) >> a.log2g;
+    const uint32_t groups = kBlock >> a.log2g;
+    __shared__ Pair s_pairs[kGroupPairs + 2 * 64 + 2];
     __shared__ uint32_t s_heads[kBlock + 1];  // before the workgroup's chunks, then in each
-    const bool count_heads = ROWS && a.heads == nullptr;  // then step covers all units
-    const uint32_t c0 = (uint32_t)(first / a.slabs);
-    if (count_heads) {
-        for (uint32_t i = threadIdx.x; i <= kBlock; i += kBlock) s_heads[i] = 0;
-        lds_barrier();
-        const uint32_t c1 = (uint32_t)(min(first + (kBlock >> a.log2g), units) - 1) / a.slabs;
+    const bool count_heads = ROWS && a.heads == nullptr;
+    for (uint64_t first = (uint64_t)blockIdx.x * groups; first < units;
+         first += (uint64_t)gridDim.x * groups) {
+        const uint32_t c0 = (uint32_t)(first / a.slabs);
+        const uint32_t c1 = (uint32_t)((min(first + groups, units) - 1) / a.slabs);
         const uint32_t lo = c0 * a.chunk, hi = min((c1 + 1) * a.chunk, a.count);
-        count_begins(a, lo, &s_heads[0]);
-        for (uint32_t i = lo + threadIdx.x; i < hi; i += kBlock) {
-            const uint32_t key = a.pairs[i].key;
-            if (key != a.vocab && (i == 0 || a.pairs[i - 1].key != key))
-                atomicAdd(&s_heads[1 + i / a.chunk - c0], 1u);
+        NearPairs pairs = {s_pairs, lo > a.chunk ? lo - a.chunk - 1 : 0u};
+        const uint32_t near = min(hi + a.chunk + 1, a.count) - pairs.p0;
+        lds_barrier();
+        {
+            constexpr int N = (kGroupPairs + 2 * 64 + 2 + kBlock - 1) / kBlock;
+            Pair p[N];
+#pragma unroll
+            for (int k = 0; k < N; k++)
+                if (k * kBlock + threadIdx.x < near) p[k] = a.pairs[pairs.p0 + k * kBlock + threadIdx.x];
+#pragma unroll
+            for (int k = 0; k < N; k++)
+                if (k * kBlock + threadIdx.x < near) s_pairs[k * kBlock + threadIdx.x] = p[k];
+        }
+        if (count_heads) {
+            for (uint32_t i = threadIdx.x; i <= kBlock; i += kBlock) s_heads[i] = 0;
+            lds_barrier();
+            count_begins(a, lo, &s_heads[0]);
+            for (uint32_t i = lo + threadIdx.x; i < hi; i += kBlock) {
+                const uint32_t key = pairs[i].key;
+                if (key != a.vocab && (i == 0 || pairs[i - 1].key != key))
+                    atomicAdd(&s_heads[1 + i / a.chunk - c0], 1u);
+            }
         }
         lds_barrier();
-        if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) {
+        if (count_heads && c1 + 1 == a.chunks && threadIdx.x == 0) {
             uint32_t all = 0;
             for (uint32_t k = 0; k <= c1 - c0 + 1; k++) all += s_heads[k];
             *a.touched = all;
         }
-    }
-    for (uint64_t unit = first + (threadIdx.x >> a.log2g); unit < units; unit += step) {
-        const uint32_t c = (uint32_t)(unit / a.slabs);
-        uint32_t heads = 0;
-        if (count_heads)
-            for (uint32_t k = 0; k <= c - c0; k++) heads += s_heads[k];
-        else if (ROWS)
-            heads = a.heads[c];
-        sum_chunk<TI, TO, ROWS>(a, x, dst, c, (uint32_t)(unit - (uint64_t)c * a.slabs), heads);
+        const uint64_t unit = first + (threadIdx.x >> a.log2g);
+        if (unit < units) {
+            const uint32_t c = (uint32_t)(unit / a.slabs);
+            uint32_t heads = 0;
+            if (count_heads)
+                for (uint32_t k = 0; k <= c - c0; k++) heads += s_heads[k];
+            else if (ROWS)
+                heads = a.heads[c];
+            sum_chunk<TI, TO, ROWS>(a, pairs, x, dst, c, (uint32_t)(unit - (uint64_t)c * a.slabs), heads);
+        }
     }
 }
 
@@ -807,7 +855,10 @@ uint32_t chunk_for(const hc_embed_params& p) {
     const uint64_t vectors = (p.dim + 3) / 4;
     const uint32_t log2g = group_log2(vectors);
     const uint64_t slabs = (vectors + (1ull << log2g) - 1) >> log2g;
+    // a workgroup's chunks (256 lanes' worth, 8 columns a lane at least) hold at
+    // most kGroupPairs pairs
     uint32_t chunk = 64;
+    while (chunk > 8 && (chunk * kBlock) >> group_log2((p.dim + 7) / 8) > kGroupPairs) chunk /= 2;
     while (chunk > 8 && ((p.count / chunk * slabs) << log2g) / 64 < 4096) chunk /= 2;
     return chunk;
 }

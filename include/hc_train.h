@@ -57,7 +57,8 @@ typedef struct {
 hc_status hc_embed(const hc_embed_params *p, hc_type type, const void *table, const void *ids,
                    void *out, hipStream_t stream);
 
-/* Workspace bytes (HOST pointer) of the two gradient calls, for any types. */
+/* Workspace bytes (HOST pointer) of the two gradient calls, for any types; they
+ * do for fewer ids of the same vocab and dim too. */
 hc_status hc_embed_grad_bytes(const hc_embed_params *p, size_t *bytes);
 
 /* dtable[v] = scale * sum of dout[i] over the i with ids[i] = v, for all v <

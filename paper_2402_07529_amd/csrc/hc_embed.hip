@@ -847,20 +847,42 @@ __global__ void clear_word_kernel(uint32_t* a) { *a = 0; }
 
 // ---- layout and launches ---------------------------------------------------------
 
-// Pairs per chunk: 64, or fewer (down to 8) while that leaves under 4096 waves
-// of sums (a lane takes four columns, a wave up to 64 lanes of one row).  Half
-// and twice as many waves: 30,522 x 768 bf16 with 32,768 ids 72 and 77 us (68),
-// 2^24 x 64 with 2^20 ids by rows 192 and 206 us (193).
-uint32_t chunk_for(const hc_embed_params& p) {
-    const uint64_t vectors = (p.dim + 3) / 4;
-    const uint32_t log2g = group_log2(vectors);
-    const uint64_t slabs = (vectors + (1ull << log2g) - 1) >> log2g;
-    // a workgroup's chunks (256 lanes' worth, 8 columns a lane at least) hold at
-    // most kGroupPairs pairs
+// Pairs per chunk: 64, or fewer (down to 8) while that leaves under kFewWaves
+// waves of sums (a lane takes four columns, a wave up to 64 lanes of one row).
+// Half and twice as many waves: 30,522 x 768 bf16 with 32,768 ids 72 and 77 us
+// (68), 2^24 x 64 with 2^20 ids by rows 192 and 206 us (193).
+constexpr uint64_t kFewWaves = 4096;
+
+// A workgroup's chunks (256 lanes' worth, 8 columns a lane at least) hold at most
+// kGroupPairs pairs.
+uint32_t most_chunk(uint64_t dim) {
     uint32_t chunk = 64;
-    while (chunk > 8 && (chunk * kBlock) >> group_log2((p.dim + 7) / 8) > kGroupPairs) chunk /= 2;
-    while (chunk > 8 && ((p.count / chunk * slabs) << log2g) / 64 < 4096) chunk /= 2;
+    while (chunk > 8 && (chunk * kBlock) >> group_log2((dim + 7) / 8) > kGroupPairs) chunk /= 2;
     return chunk;
+}
+
+// Lanes that a row's sums take, 64 a slab.
+uint64_t lanes_of_row(uint64_t dim) {
+    const uint64_t vectors = (dim + 3) / 4;
+    const uint32_t log2g = group_log2(vectors);
+    return ((vectors + (1ull << log2g) - 1) >> log2g) << log2g;
+}
+
+uint32_t chunk_for(const hc_embed_params& p) {
+    const uint64_t lanes = lanes_of_row(p.dim);
+    uint32_t chunk = most_chunk(p.dim);
+    while (chunk > 8 && p.count / chunk * lanes / 64 < kFewWaves) chunk /= 2;
+    return chunk;
+}
+
+// Chunks and sorting workgroups of up to `count` ids: more ids can make fewer of
+// either, and a workspace for more ids has to do for fewer.
+uint64_t most_chunks(uint64_t dim, uint64_t count) {
+    // a chunk is halved while it leaves fewer than kFewWaves waves, so the halves
+    // make fewer than twice as many
+    const uint64_t few = 2 * kFewWaves * 64 / lanes_of_row(dim) + 2, c = most_chunk(dim);
+    const uint64_t small = (count + 7) / 8 < few ? (count + 7) / 8 : few, large = (count + c - 1) / c;
+    return small > large ? small : large;
 }
 
 // Digits of the keys 0 .. vocab.
@@ -873,7 +895,15 @@ void digits_for(uint64_t vocab, uint32_t* passes, uint32_t* log2bins) {
 
 // Lanes of a sorting workgroup (8 pairs each): few enough pairs a workgroup to
 // spread them over the CUs, many enough that the counts stay few.
-uint32_t sort_threads(uint64_t count) { return count >= (1u << 19) ? 512 : 256; }
+constexpr uint64_t kManyIds = 1u << 19;
+uint32_t sort_threads(uint64_t count) { return count >= kManyIds ? 512 : 256; }
+
+uint64_t most_groups(uint64_t count) {
+    const uint64_t few = count < kManyIds ? count : kManyIds;
+    const uint64_t small = (few + 256 * kItems - 1) / (256 * kItems);
+    const uint64_t large = (count + 512 * kItems - 1) / (512 * kItems);
+    return small > large ? small : large;
+}
 
 struct GradLayout {
     uint32_t chunk, chunks, groups;
@@ -896,12 +926,13 @@ GradLayout grad_layout(const hc_embed_params& p) {
     };
     L.pairs[0] = take(p.count * sizeof(Pair));
     L.pairs[1] = take(L.small ? 0 : p.count * sizeof(Pair));
-    L.hist = take(L.small ? 0 : (size_t)L.groups * kMaxBins * 4);
+    const size_t chunks = most_chunks(p.dim, p.count);
+    L.hist = take(L.small ? 0 : most_groups(p.count) * kMaxBins * 4);
     L.total = take(kMaxBins * 4);
-    L.heads = take((size_t)L.chunks * 4);
+    L.heads = take(chunks * 4);
     L.crossing_count = take(4);
-    L.crossing = take((size_t)L.chunks * 8);
-    L.partial = take((size_t)L.chunks * 2 * ((p.dim + 7) / 8 * 8) * 8);
+    L.crossing = take(chunks * 8);
+    L.partial = take(chunks * 2 * ((p.dim + 7) / 8 * 8) * 8);
     L.bytes = at;
     return L;
 }

@@ -43,10 +43,16 @@ template <int PLANES> __device__ __forceinline__ void split(float v, _Float16& h
     if constexpr (PLANES == 2) lo = (_Float16)(v - (float)hi);
 }
 
+// Value (i, j) of a block in LDS, [i][EN]: its 4-value group is turned by i so
+// that rows written and columns read are spread over the banks.
+template <int EN> __device__ __forceinline__ uint32_t staged(uint32_t i, uint32_t j) {
+    return i * EN + ((((j >> 2) ^ i ^ (i >> 3)) & (EN / 4 - 1)) << 2) + (j & 3u);
+}
+
 // ---- norm and operands of X_0 ----------------------------------------------------
 
-constexpr int kPrepBlock = 256;
-constexpr uint32_t kNormParts = 1024;
+constexpr int kPrepBlock = 256, kNormBlock = 1024;
+constexpr uint32_t kNormParts = 256;  // every wave of the next launch sums them
 
 // 16 bytes at the alignment of their elements
 template <typename T> struct Wide16 {
@@ -56,13 +62,13 @@ template <typename T> struct Wide16 {
 // Sum of squares in 64 bits, a workgroup a part: 16-byte loads, four in flight a
 // lane.  rows == 1: the matrix lies in one piece.
 template <typename T>
-__global__ __launch_bounds__(kPrepBlock) void norm_kernel(const T* __restrict__ x, uint64_t rows,
+__global__ __launch_bounds__(kNormBlock) void norm_kernel(const T* __restrict__ x, uint64_t rows,
                                                           uint64_t cols, uint64_t ld,
                                                           uint64_t stride,
                                                           double* __restrict__ partial) {
     typedef typename Wide16<T>::V V;
     constexpr int VEC = 16 / sizeof(T);
-    __shared__ double s_sum[kPrepBlock / 64];
+    __shared__ double s_sum[kNormBlock / 64];
     const T* m = x + (uint64_t)blockIdx.y * stride;
     double acc = 0.0;
     auto span = [&](const T* p, uint64_t count, uint64_t first, uint64_t step) {
@@ -86,11 +92,11 @@ __global__ __launch_bounds__(kPrepBlock) void norm_kernel(const T* __restrict__ 
         }
     };
     if (rows == 1) {
-        span(m, cols, (uint64_t)blockIdx.x * kPrepBlock + threadIdx.x, (uint64_t)gridDim.x * kPrepBlock);
+        span(m, cols, (uint64_t)blockIdx.x * kNormBlock + threadIdx.x, (uint64_t)gridDim.x * kNormBlock);
     } else {
         // a wave a row
-        const uint32_t wave = blockIdx.x * (kPrepBlock / 64) + (threadIdx.x >> 6);
-        for (uint64_t r = wave; r < rows; r += (uint64_t)gridDim.x * (kPrepBlock / 64))
+        const uint32_t wave = blockIdx.x * (kNormBlock / 64) + (threadIdx.x >> 6);
+        for (uint64_t r = wave; r < rows; r += (uint64_t)gridDim.x * (kNormBlock / 64))
             span(m + r * ld, cols, threadIdx.x & 63, 64);
     }
     for (int d = 32; d > 0; d >>= 1) acc += __shfl_xor(acc, d);
@@ -98,7 +104,7 @@ __global__ __launch_bounds__(kPrepBlock) void norm_kernel(const T* __restrict__ 
     lds_barrier();
     if (threadIdx.x == 0) {
         double t = 0.0;
-        for (int w = 0; w < kPrepBlock / 64; w++) t += s_sum[w];
+        for (int w = 0; w < kNormBlock / 64; w++) t += s_sum[w];
         partial[(uint64_t)blockIdx.y * kNormParts + blockIdx.x] = t;
     }
 }
@@ -127,33 +133,64 @@ struct PrepArgs {
 // orientations.  Tiles cover the padded sides; the padding is zero.
 template <typename T, int PLANES>
 __global__ __launch_bounds__(kPrepBlock) void prepare_kernel(PrepArgs a, const T* __restrict__ x) {
-    __shared__ float s_tile[64][65];
+    __shared__ __align__(16) float s_tile[64 * 64];
     const uint32_t b = blockIdx.z;
     const float f = inverse_norm(a.partial + (uint64_t)b * kNormParts, a.parts, a.eps);
     if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) a.inverse[b] = f;
     const float scale = __builtin_ldexpf(1.0f, a.shift);
     const T* m = x + (uint64_t)b * a.stride;
     const uint32_t row0 = blockIdx.y * 64, col0 = blockIdx.x * 64;
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const size_t base = (size_t)b * a.rows * a.cols * PLANES;
-    for (uint32_t j = wave; j < 64; j += 4) {
-        const uint32_t r = row0 + j, c = col0 + lane;
-        const float v = r < a.m && c < a.n ? (float)m[(uint64_t)r * a.ld + c] * f * scale : 0.0f;
-        s_tile[j][lane] = v;
-        _Float16* d = a.straight + base + operand_at<PLANES>(r, a.cols, c);
-        _Float16 hi, lo = 0;
-        split<PLANES>(v, hi, lo);
-        d[0] = hi;
-        if (PLANES == 2) d[32] = lo;
+    // 8 values of a row a lane, then 8 of a column: 16-byte stores
+    typedef T T8 __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+    float v[2][8];
+#pragma unroll
+    for (int k = 0; k < 2; k++) {
+        const uint32_t q = threadIdx.x + kPrepBlock * k;
+        const uint32_t r = row0 + q / 8, c = col0 + q % 8 * 8;
+        const T* p = m + (uint64_t)r * a.ld + c;
+        if (r < a.m && c + 7 < a.n) {
+            const T8 t = *reinterpret_cast<const T8*>(p);
+#pragma unroll
+            for (int e = 0; e < 8; e++) v[k][e] = (float)t[e];
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; e++) v[k][e] = r < a.m && c + e < a.n ? (float)p[e] : 0.0f;
+        }
+    }
+    auto store = [](_Float16* d, const float (&w)[8]) {
+        h8 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            _Float16 x, y = 0;
+            split<PLANES>(w[e], x, y);
+            hi[e] = x;
+            lo[e] = y;
+        }
+        *reinterpret_cast<h8*>(d) = hi;
+        if constexpr (PLANES == 2) *reinterpret_cast<h8*>(d + 32) = lo;
+    };
+#pragma unroll
+    for (int k = 0; k < 2; k++) {
+        const uint32_t q = threadIdx.x + kPrepBlock * k, ii = q / 8, jj = q % 8 * 8;
+        const bool in = row0 + ii < a.m;
+#pragma unroll
+        for (int e = 0; e < 8; e++)  // the padding stays zero whatever f is
+            v[k][e] = in && col0 + jj + e < a.n ? v[k][e] * f * scale : 0.0f;
+#pragma unroll
+        for (int h = 0; h < 2; h++)
+            *reinterpret_cast<f4*>(s_tile + staged<64>(ii, jj + 4 * h)) =
+                f4{v[k][4 * h], v[k][4 * h + 1], v[k][4 * h + 2], v[k][4 * h + 3]};
+        store(a.straight + base + operand_at<PLANES>(row0 + ii, a.cols, col0 + jj), v[k]);
     }
     lds_barrier();
-    for (uint32_t j = wave; j < 64; j += 4) {
-        const uint32_t r = col0 + j, c = row0 + lane;
-        _Float16* d = a.turned + base + operand_at<PLANES>(r, a.rows, c);
-        _Float16 hi, lo = 0;
-        split<PLANES>(s_tile[lane][j], hi, lo);
-        d[0] = hi;
-        if (PLANES == 2) d[32] = lo;
+#pragma unroll
+    for (int k = 0; k < 2; k++) {
+        const uint32_t q = threadIdx.x + kPrepBlock * k, jj = q / 8, ii = q % 8 * 8;
+        float w[8];
+#pragma unroll
+        for (int e = 0; e < 8; e++) w[e] = s_tile[staged<64>(ii + e, jj)];
+        store(a.turned + base + operand_at<PLANES>(col0 + jj, a.rows, row0 + ii), w);
     }
 }
 
@@ -231,12 +268,6 @@ template <int BM_, int BN_, int WM_, int WN_, int STAGES_> struct Shape {
     static constexpr int kLdsBytes =
         kStages * kStageBytes > kWaves * EM * EN * 4 ? kStages * kStageBytes : kWaves * EM * EN * 4;
 };
-
-// Result (i, j) of a block in LDS, [i][EN]: its 4-value group is turned by i so
-// that rows written and columns read are spread over the banks.
-template <int EN> __device__ __forceinline__ uint32_t staged(uint32_t i, uint32_t j) {
-    return i * EN + ((((j >> 2) ^ i ^ (i >> 3)) & (EN / 4 - 1)) << 2) + (j & 3u);
-}
 
 // 16-byte chunk c of row `row` of an operand tile in LDS lies at c ^ (row mod
 // 8): the reads of one chunk of 16 rows then touch all banks evenly.
@@ -707,15 +738,28 @@ __global__ __launch_bounds__(S::EM * 4) void join_kernel(Product g) {
     while (stream_begin(g, lines, w + 1) <= first) w++;
     if (stream_begin(g, lines, w + 1) >= last) return;  // one stream did it all
     const uint32_t lane = threadIdx.x & 63, u = threadIdx.x >> 6;
+    uint32_t end = w + 1;  // streams w .. end - 1 have a part of it
+    while (end < g.streams && stream_begin(g, lines, end) < last) end++;
+    // the first may begin inside the tile before; the others begin in this one
+    const uint32_t head = stream_begin(g, lines, w) > first ? 0 : 1;
+    const f4* part = reinterpret_cast<const f4*>(g.part) +
+                     ((eu * (EM / 16) + u) * FN + ev * (EN / 16)) * S::kThreads + wave * 64 + lane;
+    constexpr int kAhead = 4;  // parts asked for at once: one at a time 16 us for 18, 4 us more a part
     f4 acc[EN / 16] = {};
-    for (; w < g.streams; w++) {
-        const uint64_t begin = stream_begin(g, lines, w);
-        if (begin >= last) break;
-        const f4* part = reinterpret_cast<const f4*>(g.part) +
-                         ((size_t)w * 2 + (begin > first ? 0 : 1)) * (S::BM * S::BN / 4) +
-                         ((eu * (EM / 16) + u) * FN + ev * (EN / 16)) * S::kThreads + wave * 64 + lane;
+    for (uint32_t w0 = w; w0 < end; w0 += kAhead) {
+        f4 v[kAhead][EN / 16];
 #pragma unroll
-        for (int v = 0; v < EN / 16; v++) acc[v] += part[v * S::kThreads];
+        for (int q = 0; q < kAhead; q++)
+#pragma unroll
+            for (int k = 0; k < EN / 16; k++)
+                if (w0 + q < end)
+                    v[q][k] = part[((size_t)(w0 + q) * 2 + (w0 + q == w ? head : 0)) * (S::BM * S::BN / 4) +
+                                   k * S::kThreads];
+#pragma unroll
+        for (int q = 0; q < kAhead; q++)
+#pragma unroll
+            for (int k = 0; k < EN / 16; k++)
+                if (w0 + q < end) acc[k] += v[q][k];
     }
     const Tile tile = tile_at<KIND>(g, t);
     const Results<KIND, MIDDLE, PLANES, T, S> out(g, tile);
@@ -1291,9 +1335,9 @@ hipError_t orthogonalise_typed(const hc_orthogonalise_params& p, const OrthoStep
     double* partial = reinterpret_cast<double*>(ws + L.partial);
     const bool flat = p.x_ld == p.n;
     const uint64_t rows = flat ? 1 : p.m, cols = flat ? p.m * p.n : p.n;
-    uint64_t parts = flat ? (cols + kPrepBlock * 16 - 1) / (kPrepBlock * 16) : (p.m + 3) / 4;
+    uint64_t parts = flat ? (cols + kNormBlock * 16 - 1) / (kNormBlock * 16) : (p.m + 15) / 16;
     if (parts > kNormParts) parts = kNormParts;
-    hipLaunchKernelGGL(norm_kernel<T>, dim3((uint32_t)parts, batch), dim3(kPrepBlock), 0, s,
+    hipLaunchKernelGGL(norm_kernel<T>, dim3((uint32_t)parts, batch), dim3(kNormBlock), 0, s,
                        static_cast<const T*>(x), rows, cols, p.x_ld, p.x_stride, partial);
     if (p.steps == 0) {
         hipLaunchKernelGGL(normalise_kernel<T>, dim3((uint32_t)(p.m < 1024 ? p.m : 1024), batch),

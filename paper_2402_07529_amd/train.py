@@ -14,8 +14,6 @@ from __future__ import annotations
 
 import ctypes
 
-import torch
-
 from . import _check, _lib, _ptr, _stream, _u32
 
 HC_T_I32, HC_T_F32, HC_T_BF16, HC_T_F16 = range(4)
@@ -55,16 +53,25 @@ _lib.hc_orthogonalise.argtypes = [_OP, _P, _P, _P, _Z, _P]
 for _f in TRAIN_EXPORTS:
     getattr(_lib, _f).restype = ctypes.c_int
 
-_TYPES = {torch.int32: HC_T_I32, torch.float32: HC_T_F32, torch.bfloat16: HC_T_BF16,
-          torch.float16: HC_T_F16}
-_ID_BITS = {torch.int32: 32, torch.int64: 64}
+_TYPES = {}     # torch's types, filled by the first call (importing the package needs no torch)
+_ID_BITS = {}
+
+
+def _code(table, dtype, message):
+    if not _TYPES:
+        import torch
+        _ID_BITS.update({torch.int32: 32, torch.int64: 64})
+        _TYPES.update({torch.int32: HC_T_I32, torch.float32: HC_T_F32, torch.bfloat16: HC_T_BF16,
+                       torch.float16: HC_T_F16})
+    code = table.get(dtype)
+    if code is None:
+        raise ValueError(f"{message} has dtype {dtype}, expected one of {tuple(table)}")
+    return code
 
 
 def _type(t, name):
     code = _TYPES.get(t.dtype)
-    if code is None:
-        raise ValueError(f"{name} has dtype {t.dtype}, expected one of {tuple(_TYPES)}")
-    return code
+    return _code(_TYPES, t.dtype, name) if code is None else code
 
 
 def _rows(t, name):
@@ -92,12 +99,17 @@ def _rows(t, name):
 def _ids(ids):
     bits = _ID_BITS.get(ids.dtype)
     if bits is None:
-        raise ValueError(f"ids has dtype {ids.dtype}, expected torch.int32 or torch.int64")
+        bits = _code(_ID_BITS, ids.dtype, "ids")
     if not ids.is_cuda:
         raise ValueError("ids must be a device tensor")
     if not ids.is_contiguous():
         raise ValueError("ids must be contiguous")
     return ids.data_ptr(), ids.numel(), bits
+
+
+def _bytes(ws):
+    import torch
+    return _ptr(ws, "ws", (torch.uint8,))
 
 
 def hc_embed(table, ids, out, scale: float = 1.0, stream=None):
@@ -125,6 +137,7 @@ def hc_embed_grad_bytes(vocab: int, dim: int, count: int) -> int:
 
 def alloc_embed_workspace(vocab: int, dim: int, count: int, device="cuda"):
     """Workspace of hc_embed_grad and hc_embed_grad_rows for up to `count` ids."""
+    import torch
     return torch.empty(max(hc_embed_grad_bytes(vocab, dim, count), 256), dtype=torch.uint8,
                        device=device)
 
@@ -149,7 +162,7 @@ def hc_embed_grad(dout, ids, dtable, ws, scale: float = 1.0, fixed: float = FIXE
     p, xt, x, i, gt, d, _ = _grad_args(dout, ids, dtable.shape[0], dtable, "dtable", scale, fixed,
                                        padding)
     _check(_lib.hc_embed_grad(ctypes.byref(p), xt, x, i, gt, d, 1 if accumulate else 0,
-                              _ptr(ws, "ws", (torch.uint8,)), ws.numel(), _stream(stream)),
+                              _bytes(ws), ws.numel(), _stream(stream)),
            "hc_embed_grad")
 
 
@@ -161,7 +174,7 @@ def hc_embed_grad_rows(dout, ids, vocab: int, rows, values, touched, ws, scale: 
     p, xt, x, i, gt, d, cap = _grad_args(dout, ids, vocab, values, "values", scale, fixed, padding)
     _check(_lib.hc_embed_grad_rows(ctypes.byref(p), xt, x, i, gt, _ptr(rows, "rows", _u32(), cap), d,
                                    cap, _ptr(touched, "touched", _u32(), 1),
-                                   _ptr(ws, "ws", (torch.uint8,)), ws.numel(), _stream(stream)),
+                                   _bytes(ws), ws.numel(), _stream(stream)),
            "hc_embed_grad_rows")
 
 
@@ -212,6 +225,7 @@ def hc_orthogonalise_bytes(x, steps: int = 5) -> int:
 
 def alloc_orthogonalise_workspace(x):
     """Workspace of hc_orthogonalise for matrices of x's shape and type."""
+    import torch
     return torch.empty(max(hc_orthogonalise_bytes(x), 256), dtype=torch.uint8, device=x.device)
 
 
@@ -221,5 +235,5 @@ def hc_orthogonalise(x, out, ws, steps: int = 5, coeffs=MUON, eps: float = 1e-7,
     x, out: [m, n] or [batch, m, n] float32 or bfloat16, rows contiguous; coeffs (a, b, c), or a
     triple for each step."""
     p, px, po = _ortho_params(x, out, steps, coeffs, eps, scale)
-    _check(_lib.hc_orthogonalise(ctypes.byref(p), px, po, _ptr(ws, "ws", (torch.uint8,)), ws.numel(),
+    _check(_lib.hc_orthogonalise(ctypes.byref(p), px, po, _bytes(ws), ws.numel(),
                                  _stream(stream)), "hc_orthogonalise")

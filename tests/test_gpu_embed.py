@@ -211,6 +211,21 @@ def test_gradient_repeats_bit_for_bit():
     assert torch.equal(got[0], got[1]) and torch.equal(got[0], got[2])
 
 
+def test_workspace_for_more_ids():
+    """One workspace, laid out for 2^19 + 5 ids, for any smaller number of them."""
+    torch, hc = _hc()
+    vocab, dim = 900, 55
+    ws = hc.alloc_embed_workspace(vocab, dim, 2**19 + 5)
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    for count in (2**19 + 5, 2**19 - 1, 171155, 85000, 20000, 8192, 700, 1):
+        ids = (torch.rand(count, device="cuda", generator=gen) ** 3 * vocab).int()
+        x = torch.randint(-8, 8, (count, dim), device="cuda", generator=gen).float()
+        out = torch.empty(vocab, dim, device="cuda")
+        hc.hc_embed_grad(x, ids, out, ws)
+        want = torch.zeros(vocab, dim, device="cuda", dtype=torch.float64)
+        assert torch.equal(out.double(), want.index_add(0, ids.long(), x.double())), count
+
+
 def test_gradient_nan_and_infinity_stay_in_their_rows():
     torch, hc = _hc()
     x = torch.ones(6, 40, device="cuda")

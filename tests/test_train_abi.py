@@ -142,3 +142,28 @@ def test_binding_refuses_host_tensors_and_shapes():
         hc.hc_embed_grad(t, torch.zeros(4, dtype=torch.int32), t, torch.zeros(256, dtype=torch.uint8))
     with pytest.raises(ValueError):
         hc.hc_orthogonalise(t, t.clone(), torch.zeros(256, dtype=torch.uint8))
+
+
+@pytest.mark.parametrize("dim", [1, 4, 5, 16, 64, 100, 768, 1500, 5000])
+def test_gradient_workspace_grows_with_the_count(dim):
+    """A workspace for up to `count` ids does for any smaller number of them."""
+    import paper_2402_07529_amd as hc
+    last, count = 0, 0
+    while count < 2**22:
+        need = hc.hc_embed_grad_bytes(70000, dim, count)
+        assert need >= last, (dim, count)
+        last = need
+        count += max(1, count // 37)
+    for edge in (8192, 2**19, 2**20):
+        sizes = [hc.hc_embed_grad_bytes(70000, dim, edge + k) for k in range(-3, 4)]
+        assert sizes == sorted(sizes)
+
+
+def test_chunks_fit_their_bound():
+    """What a call lays out never needs more than what the bytes call reported for it: counts at
+    and around where the split changes."""
+    import paper_2402_07529_amd as hc
+    for dim in (1, 3, 17, 64, 65, 513, 1500):
+        for count in [2**k + d for k in range(3, 21) for d in (-1, 0, 1)]:
+            # two partial sums of dim elements a chunk of at most 64 pairs, and the sorted pairs
+            assert hc.hc_embed_grad_bytes(1000, dim, count) >= count * 8 + -(-count // 64) * 16 * dim

@@ -804,10 +804,11 @@ struct Thin {
     uint64_t m, n, x_ld, x_stride, out_ld, out_stride;
     bool tall;
     uint32_t slabs, per, parts;    // 64-column slabs, of a workgroup, workgroups
+    uint32_t parts_in;             // parts of A to sum (1: summed by a launch between)
     const void* x;
     void* out;                     // last step
     float* master;                 // X in fp32, in the lanes' order
-    const float* part_in;          // parts of A, [batch][parts][R][R]
+    const float* part_in;          // parts of A, [batch][parts_in][R][R]
     float* part_out;
     const double* norm;            // first launch
     uint32_t norm_parts;
@@ -857,11 +858,11 @@ __global__ __launch_bounds__(256) void thin_kernel(Thin g) {
         f = inverse_norm(g.norm + (uint64_t)batch * kNormParts, g.norm_parts, g.eps);
     } else {
         // A: the parts' sum
-        const f4* in = reinterpret_cast<const f4*>(g.part_in) + (size_t)batch * g.parts * (R * R / 4);
+        const f4* in = reinterpret_cast<const f4*>(g.part_in) + (size_t)batch * g.parts_in * (R * R / 4);
         constexpr int N = R * R / 4 / 256;
         f4 sum[N] = {};
 #pragma unroll 2
-        for (uint32_t w = 0; w < g.parts; w++)
+        for (uint32_t w = 0; w < g.parts_in; w++)
 #pragma unroll
             for (int k = 0; k < N; k++) sum[k] += in[(size_t)w * (R * R / 4) + k * 256 + threadIdx.x];
 #pragma unroll
@@ -1020,6 +1021,34 @@ __global__ __launch_bounds__(256) void thin_kernel(Thin g) {
             out[((16 * (GT * wave + u) + li) * R + 16 * v + 4 * lg) / 4] = gram[u][v] * g.gram;
 }
 
+// Many parts of A, summed by a launch of its own: a wave takes 64 groups of 4
+// values and a quarter of the parts, in order, and the quarters are added in order.
+template <int R>
+__global__ __launch_bounds__(256) void thin_sum_kernel(const float* __restrict__ part_in, uint32_t parts,
+                                                       float* __restrict__ a) {
+    constexpr uint32_t N = R * R / 4;
+    __shared__ f4 s_sum[4][64];
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t at = blockIdx.x * 64 + lane;
+    const f4* in = reinterpret_cast<const f4*>(part_in) + (size_t)blockIdx.y * parts * N + at;
+    const uint32_t per = (parts + 3) / 4, end = min((wave + 1) * per, parts);
+    f4 sum = {};
+    for (uint32_t w = wave * per; w < end; w += 8) {
+        f4 v[8];
+#pragma unroll
+        for (int q = 0; q < 8; q++)
+            if (w + q < end) v[q] = in[(size_t)(w + q) * N];
+#pragma unroll
+        for (int q = 0; q < 8; q++)
+            if (w + q < end) sum += v[q];
+    }
+    s_sum[wave][lane] = sum;
+    lds_barrier();
+    if (wave == 0)
+        reinterpret_cast<f4*>(a)[(size_t)blockIdx.y * N + at] =
+            ((s_sum[0][lane] + s_sum[1][lane]) + s_sum[2][lane]) + s_sum[3][lane];
+}
+
 // ---- layout and launches ---------------------------------------------------------
 
 typedef Shape<256, 256, 128, 64, 2> Large;
@@ -1058,12 +1087,19 @@ constexpr TileCost kTileCosts[3] = {
     {128, 2, 0.50, 0.86, 8.0, 0.70, 0.98},
     {64, 4, 0.35, 0.70, 6.0, 0.45, 0.92},
 };
-// Streams (256-tiles only): a share's steps run at no common phase, so less of
-// what they read is shared, and partial sums go to memory and back in a launch
-// of its own.  Where the tiles fill most CUs this is slower than whole tiles:
-// 528 tiles of 128 on 512 places 911 us, 676 as whole tiles.
-constexpr double kStreamStep = 1.95, kStreamStep2 = 2.50, kStreamEnds = 36.0;
-constexpr uint32_t kLeastSteps = 8;
+// Streams: a share's steps run at no common phase, so less of what they read is
+// shared, and partial sums go to memory and back in a launch of its own.  Where
+// the tiles fill most CUs this is slower than whole tiles (528 tiles of 128 on
+// 512 places 911 us, 676 as whole tiles), so only up to 3 tiles for 5 CUs.
+struct StreamCost {
+    double step, step2;  // one plane, two
+    uint32_t least;      // steps of a share
+    double ends;         // first loads, and a tile of sums written by one workgroup
+};
+constexpr StreamCost kStreamCosts[3] = {{1.95, 2.50, 8, 15.0}, {0.86, 0.98, 4, 8.0}, {0.50, 0.60, 4, 6.0}};
+constexpr double kJoin = 7.0, kJoinPart = 0.2;  // and for each of a tile's parts
+
+constexpr double kLaunch = 4.0, kBytesPerUs = 5e6;
 
 double plain_cost(const TileCost& c, uint64_t tiles, uint32_t lines, int planes, int cus) {
     const double alone = planes == 1 ? c.alone : c.alone2, shared = planes == 1 ? c.shared : c.shared2;
@@ -1090,16 +1126,18 @@ double best_way(uint64_t tiles256, uint64_t tiles128, uint64_t tiles64, uint32_t
             *way = Way{kTileCosts[k].tile, 0, 0, 0};
         }
     }
-    if (tiles256 != 0 && tiles256 * 5 <= (uint64_t)cus * 3) {
-        const uint64_t most = tiles256 * lines / kLeastSteps;
-        const uint64_t streams = most < (uint64_t)cus ? most : (uint64_t)cus;
-        if (streams > tiles256) {
-            const double t = (double)(tiles256 * lines) / streams *
-                                 (planes == 1 ? kStreamStep : kStreamStep2) + kStreamEnds;
-            if (t < best) {
-                best = t;
-                *way = Way{256, (uint32_t)streams, 0, 0};
-            }
+    for (int k = 0; k < 3; k++) {
+        const StreamCost& c = kStreamCosts[k];
+        if (tiles[k] == 0 || tiles[k] * 5 > (uint64_t)cus * 3) continue;
+        const uint64_t shares = tiles[k] * lines / c.least;
+        const uint64_t streams = shares < (uint64_t)cus ? shares : (uint64_t)cus;
+        if (streams <= tiles[k]) continue;
+        const double size = 4.0 * kTileCosts[k].tile * kTileCosts[k].tile;
+        const double t = (double)(tiles[k] * lines) / streams * (planes == 1 ? c.step : c.step2) + c.ends +
+                         kJoin + kJoinPart * streams / tiles[k] + (streams + tiles[k]) * size / kBytesPerUs;
+        if (t < best) {
+            best = t;
+            *way = Way{kTileCosts[k].tile, (uint32_t)streams, 0, 0};
         }
     }
     return best;
@@ -1107,7 +1145,6 @@ double best_way(uint64_t tiles256, uint64_t tiles128, uint64_t tiles64, uint32_t
 
 // CUs of the gfx950; a product is split over no more.
 constexpr int kMaxCus = 256;
-constexpr double kLaunch = 4.0;
 
 // APPLY, whose results are r x k: tiles of one size, or as many as fill whole
 // rounds of the CUs and smaller ones for the rest of the longer side.
@@ -1142,6 +1179,7 @@ double best_apply(uint64_t batch, uint64_t r, uint64_t k, uint64_t pad, uint32_t
 }
 
 constexpr uint64_t kThinSide = 128;
+constexpr uint32_t kFewParts64 = 16, kFewParts128 = 4;
 
 struct OrthoLayout {
     uint32_t rows, cols, r;  // padded m, n and their smaller
@@ -1149,6 +1187,7 @@ struct OrthoLayout {
     bool tall, thin;
     Way way[3];  // by Kind
     uint32_t slabs, per, parts;  // thin
+    bool sum_parts;
     size_t partial, inverse, master, x, xt[2], a, b, part, bytes;
 };
 
@@ -1169,7 +1208,10 @@ void plan_products(const hc_orthogonalise_params& p, int cus, OrthoLayout* L) {
         const double t =
             best_way(half[0], half[1], half[2], (uint32_t)(k * L->planes / kLine), L->planes, cus, &way[GRAM]) +
             best_way(half[0], half[1], half[2], (uint32_t)(r * L->planes / kLine), L->planes, cus, &way[SQUARE]) +
-            best_apply(p.batch, r, k, pad, (uint32_t)(r * L->planes / kLine), L->planes, cus, &way[APPLY]);
+            best_apply(p.batch, r, k, pad, (uint32_t)(r * L->planes / kLine), L->planes, cus, &way[APPLY]) +
+            // what an apply reads and writes, 10 or 16 bytes a value with its
+            // padding, is hardly overlapped with its products
+            (double)(p.batch * rows * cols * (L->planes == 1 ? 10 : 16)) / kBytesPerUs;
         if (t < best) {
             best = t;
             L->rows = (uint32_t)rows;
@@ -1186,13 +1228,16 @@ OrthoLayout ortho_layout(const hc_orthogonalise_params& p) {
     L.thin = r <= kThinSide;
     L.planes = p.type == HC_T_F32 || r <= kTwoPlaneSide ? 2 : 1;
     if (L.thin) {
-        // a workgroup reads all parts of A (16 KiB each with 64 rows, 64 KiB
-        // with 128), so they are kept few
-        const uint32_t most = r <= 64 ? 32 : 16;
+        // a workgroup a slab, up to two workgroups a CU; few parts of A (16 KiB
+        // each with 64 rows, 64 KiB with 128) are read by every workgroup, more are
+        // summed between the steps (120 x 4000: 16 parts read by all 195 us)
         L.r = r <= 64 ? 64 : 128;
         L.slabs = (uint32_t)(((L.tall ? p.m : p.n) + 63) / 64);
-        L.per = (L.slabs + most - 1) / most;
+        const uint64_t most = 2 * kMaxCus, groups = (uint64_t)L.slabs * p.batch;
+        const uint32_t few = r <= 64 ? kFewParts64 : kFewParts128;
+        L.per = (uint32_t)(groups > most ? (groups + most - 1) / most : 1);
         L.parts = (L.slabs + L.per - 1) / L.per;
+        L.sum_parts = L.parts > few;
     } else {
         plan_products(p, kMaxCus, &L);
         L.r = L.tall ? L.cols : L.rows;
@@ -1210,6 +1255,7 @@ OrthoLayout ortho_layout(const hc_orthogonalise_params& p) {
         L.master = take(any ? p.batch * L.slabs * 64 * L.r * 4 : 0);
         L.xt[0] = take(part);  // the parts of A, of this step and the next
         L.xt[1] = take(part);
+        L.a = take(any && L.sum_parts ? p.batch * L.r * L.r * 4 : 0);
         L.bytes = at;
         return L;
     }
@@ -1221,9 +1267,12 @@ OrthoLayout ortho_layout(const hc_orthogonalise_params& p) {
     L.xt[1] = take(xs * 2 * L.planes);
     L.a = take(as * 2 * L.planes);
     L.b = take(as * 2 * L.planes);
-    uint32_t streams = 0;
-    for (const Way& w : L.way) streams = w.streams > streams ? w.streams : streams;
-    L.part = take(any ? (size_t)streams * 2 * 256 * 256 * 4 : 0);
+    size_t part = 0;
+    for (const Way& w : L.way) {
+        const size_t bytes = (size_t)w.streams * 2 * w.tile * w.tile * 4;
+        part = bytes > part ? bytes : part;
+    }
+    L.part = take(any ? part : 0);
     L.bytes = at;
     return L;
 }
@@ -1250,7 +1299,7 @@ hipError_t product_shape(Product g, uint32_t batch, uint32_t streams, uint32_t k
     }
     g.batch = batch;
     g.streams = streams;
-    if constexpr (S::BM == 256 && KIND != APPLY) {
+    if constexpr (KIND != APPLY) {
         if (streams) {
             const hipError_t e =
                 launch_tiles<S>(&stream_kernel<KIND, PLANES, T, S>, g, streams, s);
@@ -1279,8 +1328,8 @@ template <Kind KIND, int PLANES, typename T>
 hipError_t product_tiles(const Product& g, int tile, uint32_t batch, uint32_t streams, uint32_t k0,
                          uint32_t k1, hipStream_t s) {
     if (tile == 256) return product_shape<KIND, PLANES, T, Large>(g, batch, streams, k0, k1, s);
-    if (tile == 128) return product_shape<KIND, PLANES, T, Medium>(g, batch, 0, k0, k1, s);
-    return product_shape<KIND, PLANES, T, Small>(g, batch, 0, k0, k1, s);
+    if (tile == 128) return product_shape<KIND, PLANES, T, Medium>(g, batch, streams, k0, k1, s);
+    return product_shape<KIND, PLANES, T, Small>(g, batch, streams, k0, k1, s);
 }
 
 template <Kind KIND, int PLANES, typename T>
@@ -1323,9 +1372,17 @@ hipError_t thin_typed(const hc_orthogonalise_params& p, const OrthoLayout& L, co
     g.part_out = parts[0];
     next(steps[0]);
     hipLaunchKernelGGL((thin_kernel<T, R, true>), grid, dim3(256), kFirstLds, s, g);
+    float* a = reinterpret_cast<float*>(ws + L.a);
     for (uint32_t t = 0; t < p.steps; t++) {
         const OrthoStep& st = steps[t];
         g.part_in = parts[t & 1];
+        g.parts_in = L.parts;
+        if (L.sum_parts) {
+            hipLaunchKernelGGL(thin_sum_kernel<R>, dim3(R * R / 256, (uint32_t)p.batch), dim3(256), 0, s,
+                               g.part_in, L.parts, a);
+            g.part_in = a;
+            g.parts_in = 1;
+        }
         g.part_out = parts[(t + 1) & 1];
         g.a = st.a;
         g.sb = ldexpf(st.b, st.eb - st.ea);

@@ -146,7 +146,7 @@ def _stream(stream):
     Stream object around it where torch offers that: 0.3 us a call instead of 2.7)."""
     global _current_stream
     if stream is not None:
-        return ctypes.c_void_p(stream.cuda_stream)
+        return stream.cuda_stream
     if _current_stream is None:
         import torch
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
@@ -156,7 +156,7 @@ def _stream(stream):
             _current_stream = lambda: raw(device())  # noqa: E731
         else:
             _current_stream = lambda: torch.cuda.current_stream().cuda_stream  # noqa: E731
-    return ctypes.c_void_p(_current_stream())
+    return _current_stream()
 
 
 def _ptr(t, name, dtype=None, numel=None):

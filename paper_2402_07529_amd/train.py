@@ -79,18 +79,20 @@ def _rows(t, name):
     contiguous and whose others are one stride apart (a matrix, or contiguous)."""
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
-    shape = t.shape
-    if len(shape) < 2:
+    dims = t.dim()
+    if dims == 2:
+        rows, cols = t.shape
+        if t.is_contiguous():
+            return t.data_ptr(), rows, cols, cols
+    elif dims > 2:
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be a matrix or contiguous")
+        cols = t.shape[-1]
+        return t.data_ptr(), t.numel() // cols if cols else 0, cols, cols
+    else:
         raise ValueError(f"{name} needs two dimensions or more")
-    cols = shape[-1]
-    if t.is_contiguous():
-        rows = shape[0] if len(shape) == 2 else (t.numel() // cols if cols else 0)
-        return t.data_ptr(), rows, cols, cols
-    if len(shape) > 2:
-        raise ValueError(f"{name} must be a matrix or contiguous")
     if cols > 1 and t.stride(1) != 1:
         raise ValueError(f"{name}'s rows must be contiguous")
-    rows = shape[0]
     if rows > 1 and t.stride(0) < cols:
         raise ValueError(f"{name}'s rows overlap")
     return t.data_ptr(), rows, cols, t.stride(0) if rows > 1 else cols

@@ -80,9 +80,10 @@ hc_status hc_embed_grad(const hc_embed_params *p, hc_type x_type, const void *do
 
 /* The touched rows alone: rows[u] (uint32, ascending) are the distinct valid
  * ids and values[u * table_ld ..] their sums as above, for u < cap; entries
- * past cap are not written (cap = 0: rows and values may be NULL).  *touched (uint32, DEVICE) is how many there are,
- * at most min(count, vocab).  Row r's elements are parameters r * dim .. of a
- * flat gradient: with its index expanded this is hc_encode_coo's input. */
+ * past cap are not written (cap = 0: rows and values may be NULL).  *touched
+ * (uint32, DEVICE) is how many there are, at most min(count, vocab).  Row r's
+ * elements are parameters r * dim .. of a flat gradient: with its index expanded
+ * this is hc_encode_coo's input. */
 hc_status hc_embed_grad_rows(const hc_embed_params *p, hc_type x_type, const void *dout,
                              const void *ids, hc_type g_type, uint32_t *rows, void *values,
                              uint64_t cap, uint32_t *touched, void *ws, size_t ws_bytes,
@@ -108,8 +109,10 @@ typedef struct {
  * (or from the right with X_t^T X_t where m > n: the same matrix).  Singular
  * values s of X_t become a s + b s^3 + c s^5; the default coefficients (Muon's,
  * Jordan et al. 2024) bring those above a few thousandths to about 1 in five
- * steps.  Works on the matrix cores with operands of 11 bits (HC_T_BF16) or two
- * times 11 bits (HC_T_F32), sums and X in 32 bits.  The coefficients must keep
+ * steps.  Works on the matrix cores with sums in 32 bits.  HC_T_F32, and
+ * HC_T_BF16 whose shorter side is at most 256: operands of two times 11 bits, X
+ * in fp32 between the steps.  HC_T_BF16 otherwise: operands of 11 bits, X as an
+ * operand and an 11-bit rest (22 bits).  The coefficients must keep
  * the bound on the singular values (1, mapped through every step) within
  * 2^-10 .. 2^10 and b A + c A^2 within 2^10 (HC_EUNSUPPORTED).  NaN or infinity
  * in a matrix makes that matrix's output NaN; other matrices are unaffected. */

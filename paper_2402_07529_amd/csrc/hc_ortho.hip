@@ -233,6 +233,15 @@ enum Kind { GRAM, SQUARE, APPLY };
 // APPLY's step: the first reads x itself, the last writes the output.
 enum Step { MIDDLE = 0, FIRST = 1, LAST = 2 };
 
+// Few tiles: each is cut along l into pieces, one or two a workgroup, whose sums
+// a launch of its own adds up.  The first `tiles` of them in `first` pieces, the
+// others in `second`.
+struct Cuts {
+    uint32_t tiles, first, others, second;
+    __host__ __device__ uint32_t groups() const { return max(tiles * first, others * second); }
+    __host__ __device__ uint32_t pieces() const { return tiles * first + others * second; }
+};
+
 struct Product {
     const _Float16 *p, *q;
     uint32_t inner;                  // length of l, a multiple of 64
@@ -240,11 +249,8 @@ struct Product {
     uint32_t tiles;                  // of one matrix that this launch makes
     uint32_t first;                  // APPLY: first of them along the longer side
     uint32_t batch;
-    // Streams: workgroups that share the steps of all tiles evenly, tile after
-    // tile, and leave the sums of tiles that they do only part of in `part` (two
-    // tiles a workgroup: of the one it begins inside, of the one it ends inside).
-    uint32_t streams;
-    float* part;
+    Cuts cuts;
+    float* part;                     // sums of the tiles' pieces
     size_t p_stride, q_stride;       // between matrices of the batch (stored values)
     float factor;                    // takes the sum to the result's unit
     float factor2;                   // SQUARE: takes the operand A to it; APPLY: a
@@ -699,11 +705,6 @@ __device__ __forceinline__ void finish(const Product& g, const Tile& tile, char*
         }
 }
 
-// First step of stream w, counted over all tiles.
-__device__ __forceinline__ uint64_t stream_begin(const Product& g, uint32_t lines, uint32_t w) {
-    return (uint64_t)w * g.tiles * g.batch * lines / g.streams;
-}
-
 // One tile a workgroup.
 template <Kind KIND, int STEP, int PLANES, typename T, typename S>
 __global__ __launch_bounds__(S::kThreads) void product_kernel(Product g) {
@@ -714,75 +715,65 @@ __global__ __launch_bounds__(S::kThreads) void product_kernel(Product g) {
     finish<KIND, STEP, PLANES, T, S>(g, tile, s_mem, acc);
 }
 
-// An equal share of all tiles' steps a workgroup.
-template <Kind KIND, int PLANES, typename T, typename S>
-__global__ __launch_bounds__(S::kThreads) void stream_kernel(Product g) {
+// Pieces of the tiles.  Neighbouring workgroups of an XCD take the same piece of
+// neighbouring tiles, and begin together, so that its L2 serves most of what they
+// read: 4096 x 25088 (bf16, 136 tiles on 256 CUs) 368 us, 412 with equal shares of
+// all steps in a row, which run at no common phase; 1500 x 6000 (fp32) 52, 64.
+template <Kind KIND, int PLANES, typename S>
+__global__ __launch_bounds__(S::kThreads) void pieces_kernel(Product g) {
     constexpr int FM = S::WM / 16, FN = S::WN / 16;
     extern __shared__ __align__(16) char s_mem[];
-    const uint32_t lines = g.inner * PLANES / kLine;
-    const uint32_t stream = blockIdx.x;
-    uint64_t at = stream_begin(g, lines, stream);
-    const uint64_t end = stream_begin(g, lines, stream + 1);
-    while (at < end) {
-        const uint32_t t = (uint32_t)(at / lines), l0 = (uint32_t)(at - (uint64_t)t * lines);
-        const uint32_t l1 = (uint32_t)min((uint64_t)lines, l0 + (end - at));
-        const Tile tile = tile_at<KIND>(g, t);
+    const uint32_t lines = g.inner * PLANES / kLine, w = by_xcd(blockIdx.x, gridDim.x);
+    for (uint32_t k = 0; k < 2; k++) {
+        const uint32_t tiles = k == 0 ? g.cuts.tiles : g.cuts.others;
+        const uint32_t cuts = k == 0 ? g.cuts.first : g.cuts.second;
+        if (w >= tiles * cuts) continue;
+        const uint32_t piece = w / tiles, t = (k == 0 ? 0 : g.cuts.tiles) + w - piece * tiles;
         f4 acc[FM][FN] = {};
-        accumulate<PLANES, S>(g, tile, l0, l1, s_mem, acc);
-        if (l1 - l0 == lines) {
-            finish<KIND, MIDDLE, PLANES, T, S>(g, tile, s_mem, acc);
-        } else {
-            f4* part = reinterpret_cast<f4*>(g.part) +
-                       ((size_t)stream * 2 + (l0 > 0 ? 0 : 1)) * (S::BM * S::BN / 4);
+        accumulate<PLANES, S>(g, tile_at<KIND>(g, t), piece * lines / cuts,
+                              (piece + 1) * lines / cuts, s_mem, acc);
+        f4* part = reinterpret_cast<f4*>(g.part) +
+                   (size_t)((k == 0 ? 0 : g.cuts.tiles * g.cuts.first) + w) * (S::BM * S::BN / 4);
 #pragma unroll
-            for (int u = 0; u < FM; u++)
+        for (int u = 0; u < FM; u++)
 #pragma unroll
-                for (int v = 0; v < FN; v++) part[(u * FN + v) * S::kThreads + threadIdx.x] = acc[u][v];
-        }
-        at += l1 - l0;
-        __syncthreads();
+            for (int v = 0; v < FN; v++) part[(u * FN + v) * S::kThreads + threadIdx.x] = acc[u][v];
     }
 }
 
-// Tiles that several streams shared: their sums, in the streams' order.  A
-// workgroup takes an EM x EN block of a wave's part, a wave of it 16 rows.
+// The sums of the tiles' pieces, in order.  A workgroup takes an EM x EN block of
+// a wave's part, a wave of it 16 rows.
 template <Kind KIND, int PLANES, typename T, typename S>
 __global__ __launch_bounds__(S::EM * 4) void join_kernel(Product g) {
     constexpr int FN = S::WN / 16, EM = S::EM, EN = S::EN;
     constexpr uint32_t kBlocks = S::kWaves * (S::WM / EM) * (S::WN / EN);  // of a tile
     __shared__ __align__(16) float s_stage[EM * EN];
-    const uint32_t lines = g.inner * PLANES / kLine;
     const uint32_t t = blockIdx.x / kBlocks, block = blockIdx.x - t * kBlocks;
     const uint32_t wave = block % S::kWaves, sub = block / S::kWaves;
     const uint32_t eu = sub / (S::WN / EN), ev = sub % (S::WN / EN);
-    const uint64_t first = (uint64_t)t * lines, last = first + lines;
-    uint32_t w = (uint32_t)(first * g.streams / ((uint64_t)g.tiles * g.batch * lines));
-    while (w > 0 && stream_begin(g, lines, w) > first) w--;
-    while (stream_begin(g, lines, w + 1) <= first) w++;
-    if (stream_begin(g, lines, w + 1) >= last) return;  // one stream did it all
+    const bool second = t >= g.cuts.tiles;
+    const uint32_t cuts = second ? g.cuts.second : g.cuts.first;
+    const uint32_t step = second ? g.cuts.others : g.cuts.tiles;  // from piece to piece
+    const size_t piece0 = second ? g.cuts.tiles * (size_t)g.cuts.first + (t - g.cuts.tiles) : t;
     const uint32_t lane = threadIdx.x & 63, u = threadIdx.x >> 6;
-    uint32_t end = w + 1;  // streams w .. end - 1 have a part of it
-    while (end < g.streams && stream_begin(g, lines, end) < last) end++;
-    // the first may begin inside the tile before; the others begin in this one
-    const uint32_t head = stream_begin(g, lines, w) > first ? 0 : 1;
     const f4* part = reinterpret_cast<const f4*>(g.part) +
                      ((eu * (EM / 16) + u) * FN + ev * (EN / 16)) * S::kThreads + wave * 64 + lane;
-    constexpr int kAhead = 4;  // parts asked for at once: one at a time 16 us for 18, 4 us more a part
+    constexpr int kAhead = 4;  // pieces asked for at once: one at a time 16 us for 18, 4 us more a piece
     f4 acc[EN / 16] = {};
-    for (uint32_t w0 = w; w0 < end; w0 += kAhead) {
+    for (uint32_t c = 0; c < cuts; c += kAhead) {
         f4 v[kAhead][EN / 16];
 #pragma unroll
         for (int q = 0; q < kAhead; q++)
 #pragma unroll
             for (int k = 0; k < EN / 16; k++)
-                if (w0 + q < end)
-                    v[q][k] = part[((size_t)(w0 + q) * 2 + (w0 + q == w ? head : 0)) * (S::BM * S::BN / 4) +
+                if (c + q < cuts)
+                    v[q][k] = part[(piece0 + (size_t)(c + q) * step) * (S::BM * S::BN / 4) +
                                    k * S::kThreads];
 #pragma unroll
         for (int q = 0; q < kAhead; q++)
 #pragma unroll
             for (int k = 0; k < EN / 16; k++)
-                if (w0 + q < end) acc[k] += v[q][k];
+                if (c + q < cuts) acc[k] += v[q][k];
     }
     const Tile tile = tile_at<KIND>(g, t);
     const Results<KIND, MIDDLE, PLANES, T, S> out(g, tile);
@@ -1073,12 +1064,11 @@ typedef Shape<64, 64, 32, 32, 3> Small;
 // sides are bound by launches, not by products.
 constexpr uint64_t kTwoPlaneSide = 256;
 
-// How a product runs: the tile, and the streams that share its steps (0: a
-// workgroup a tile).  APPLY: `cut` values of the longer side in tiles of `tile`,
+// How a product runs: the tile, and how it is cut (cuts.tiles = 0: not).  APPLY: `cut` values of the longer side in tiles of `tile`,
 // the rest in tiles of `rest`.
 struct Way {
     int tile;
-    uint32_t streams;
+    Cuts cuts;
     uint32_t cut;
     int rest;
 };
@@ -1099,16 +1089,13 @@ constexpr TileCost kTileCosts[3] = {
     {128, 2, 0.50, 0.86, 8.0, 0.70, 0.98},
     {64, 4, 0.35, 0.70, 6.0, 0.45, 0.92},
 };
-// Streams: a share's steps run at no common phase, so less of what they read is
-// shared, and partial sums go to memory and back in a launch of its own.  Where
-// the tiles fill most CUs this is slower than whole tiles (528 tiles of 128 on
-// 512 places 911 us, 676 as whole tiles), so only up to 3 tiles for 5 CUs.
-struct StreamCost {
-    double step, step2;  // one plane, two
-    uint32_t least;      // steps of a share
-    double ends;         // first loads, and a tile of sums written by one workgroup
+// Pieces of tiles: a piece's first loads and the tile of sums that it writes take
+// `ends`; the sums go to memory and back in a launch of its own.
+struct PieceCost {
+    uint32_t least;  // steps of a piece
+    double ends;
 };
-constexpr StreamCost kStreamCosts[3] = {{1.95, 2.50, 8, 15.0}, {0.86, 0.98, 4, 8.0}, {0.50, 0.60, 4, 6.0}};
+constexpr PieceCost kPieceCosts[3] = {{4, 8.0}, {4, 5.0}, {4, 4.0}};
 constexpr double kJoin = 7.0, kJoinPart = 0.2;  // and for each of a tile's parts
 
 constexpr double kLaunch = 4.0, kBytesPerUs = 5e6;
@@ -1126,6 +1113,34 @@ double plain_cost(const TileCost& c, uint64_t tiles, uint32_t lines, int planes,
     return t;
 }
 
+// A workgroup on every CU (full = 0), or as many as fit: every tile in as many
+// pieces as there is room for, or one more of as many tiles as that leaves room
+// for and the others in the pieces that fill it.
+void try_pieces(int k, int full, uint64_t n, uint32_t lines, int planes, int cus, double* best,
+                Way* way) {
+    const TileCost& T = kTileCosts[k];
+    const PieceCost& c = kPieceCosts[k];
+    if (full && T.resident == 1) return;
+    const uint64_t slots = (uint64_t)cus * (full ? T.resident : 1), most = lines / c.least;
+    if (n == 0 || n >= slots) return;
+    const double step = planes == 1 ? (full ? T.shared : T.alone) : (full ? T.shared2 : T.alone2);
+    const double size = 4.0 * T.tile * T.tile;
+    for (int more = 0; more < 2; more++) {
+        const uint64_t first = slots / n + more < most ? slots / n + more : most;
+        if (first < 2) continue;
+        const uint64_t take = slots / first < n ? slots / first : n, others = n - take;
+        const uint64_t second = others == 0 ? 0 : slots / others < most ? slots / others : most;
+        double t = (lines + first - 1) / first * step + c.ends;
+        if (others) t += (lines + second - 1) / second * step + c.ends;
+        t += kJoin + kJoinPart * (first > second ? first : second) +
+             (take * first + others * second + n) * size / kBytesPerUs;
+        if (t < *best) {
+            *best = t;
+            *way = Way{T.tile, {(uint32_t)take, (uint32_t)first, (uint32_t)others, (uint32_t)second}, 0, 0};
+        }
+    }
+}
+
 double best_way(uint64_t tiles256, uint64_t tiles128, uint64_t tiles64, uint32_t lines, int planes,
                 int cus, Way* way) {
     const uint64_t tiles[3] = {tiles256, tiles128, tiles64};
@@ -1135,22 +1150,11 @@ double best_way(uint64_t tiles256, uint64_t tiles128, uint64_t tiles64, uint32_t
         const double t = plain_cost(kTileCosts[k], tiles[k], lines, planes, cus);
         if (t < best) {
             best = t;
-            *way = Way{kTileCosts[k].tile, 0, 0, 0};
+            *way = Way{kTileCosts[k].tile, {}, 0, 0};
         }
     }
     for (int k = 0; k < 3; k++) {
-        const StreamCost& c = kStreamCosts[k];
-        if (tiles[k] == 0 || tiles[k] * 5 > (uint64_t)cus * 3) continue;
-        const uint64_t shares = tiles[k] * lines / c.least;
-        const uint64_t streams = shares < (uint64_t)cus ? shares : (uint64_t)cus;
-        if (streams <= tiles[k]) continue;
-        const double size = 4.0 * kTileCosts[k].tile * kTileCosts[k].tile;
-        const double t = (double)(tiles[k] * lines) / streams * (planes == 1 ? c.step : c.step2) + c.ends +
-                         kJoin + kJoinPart * streams / tiles[k] + (streams + tiles[k]) * size / kBytesPerUs;
-        if (t < best) {
-            best = t;
-            *way = Way{kTileCosts[k].tile, (uint32_t)streams, 0, 0};
-        }
+        for (int full = 0; full < 2; full++) try_pieces(k, full, tiles[k], lines, planes, cus, &best, way);
     }
     return best;
 }
@@ -1171,7 +1175,7 @@ double best_apply(uint64_t batch, uint64_t r, uint64_t k, uint64_t pad, uint32_t
         const double whole = plain_cost(T, across * along, lines, planes, cus);
         if (whole < best) {
             best = whole;
-            *way = Way{T.tile, 0, (uint32_t)k, 0};
+            *way = Way{T.tile, {}, (uint32_t)k, 0};
         }
         const uint64_t slots = (uint64_t)cus * T.resident;
         const uint64_t part = across * along / slots * slots / across;  // whole rounds
@@ -1183,7 +1187,7 @@ double best_apply(uint64_t batch, uint64_t r, uint64_t k, uint64_t pad, uint32_t
                                         lines, planes, cus);
             if (t < best) {
                 best = t;
-                *way = Way{T.tile, 0, (uint32_t)(part * tile), kTileCosts[d].tile};
+                *way = Way{T.tile, {}, (uint32_t)(part * tile), kTileCosts[d].tile};
             }
         }
     }
@@ -1281,7 +1285,7 @@ OrthoLayout ortho_layout(const hc_orthogonalise_params& p) {
     L.b = take(as * 2 * L.planes);
     size_t part = 0;
     for (const Way& w : L.way) {
-        const size_t bytes = (size_t)w.streams * 2 * w.tile * w.tile * 4;
+        const size_t bytes = (size_t)w.cuts.pieces() * w.tile * w.tile * 4;
         part = bytes > part ? bytes : part;
     }
     L.part = take(any ? part : 0);
@@ -1299,7 +1303,7 @@ hipError_t launch_tiles(K kernel, const Product& g, uint32_t groups, hipStream_t
 
 // [k0, k1) of the longer side (APPLY), or all of it.
 template <Kind KIND, int PLANES, typename T, typename S>
-hipError_t product_shape(Product g, uint32_t batch, uint32_t streams, uint32_t k0, uint32_t k1,
+hipError_t product_shape(Product g, uint32_t batch, const Cuts& cuts, uint32_t k0, uint32_t k1,
                          hipStream_t s) {
     g.tiles_i = g.rows / S::BM;
     g.tiles_j = g.cols / S::BN;
@@ -1310,11 +1314,10 @@ hipError_t product_shape(Product g, uint32_t batch, uint32_t streams, uint32_t k
         g.tiles = g.tiles_i * (g.tiles_i + 1) / 2;
     }
     g.batch = batch;
-    g.streams = streams;
+    g.cuts = cuts;
     if constexpr (KIND != APPLY) {
-        if (streams) {
-            const hipError_t e =
-                launch_tiles<S>(&stream_kernel<KIND, PLANES, T, S>, g, streams, s);
+        if (cuts.tiles) {
+            const hipError_t e = launch_tiles<S>(&pieces_kernel<KIND, PLANES, S>, g, cuts.groups(), s);
             if (e != hipSuccess) return e;
             hipLaunchKernelGGL((join_kernel<KIND, PLANES, T, S>),
                                dim3(g.tiles * batch * (S::BM / S::EM) * (S::BN / S::EN)),
@@ -1337,19 +1340,19 @@ hipError_t product_shape(Product g, uint32_t batch, uint32_t streams, uint32_t k
 }
 
 template <Kind KIND, int PLANES, typename T>
-hipError_t product_tiles(const Product& g, int tile, uint32_t batch, uint32_t streams, uint32_t k0,
+hipError_t product_tiles(const Product& g, int tile, uint32_t batch, const Cuts& cuts, uint32_t k0,
                          uint32_t k1, hipStream_t s) {
-    if (tile == 256) return product_shape<KIND, PLANES, T, Large>(g, batch, streams, k0, k1, s);
-    if (tile == 128) return product_shape<KIND, PLANES, T, Medium>(g, batch, streams, k0, k1, s);
-    return product_shape<KIND, PLANES, T, Small>(g, batch, streams, k0, k1, s);
+    if (tile == 256) return product_shape<KIND, PLANES, T, Large>(g, batch, cuts, k0, k1, s);
+    if (tile == 128) return product_shape<KIND, PLANES, T, Medium>(g, batch, cuts, k0, k1, s);
+    return product_shape<KIND, PLANES, T, Small>(g, batch, cuts, k0, k1, s);
 }
 
 template <Kind KIND, int PLANES, typename T>
 hipError_t product(const Product& g, const OrthoLayout& L, uint32_t batch, hipStream_t s) {
     const Way w = L.way[KIND];
-    const hipError_t e = product_tiles<KIND, PLANES, T>(g, w.tile, batch, w.streams, 0, w.cut, s);
+    const hipError_t e = product_tiles<KIND, PLANES, T>(g, w.tile, batch, w.cuts, 0, w.cut, s);
     if (e != hipSuccess || w.rest == 0) return e;
-    return product_tiles<KIND, PLANES, T>(g, w.rest, batch, 0, w.cut, g.rows > g.cols ? g.rows : g.cols, s);
+    return product_tiles<KIND, PLANES, T>(g, w.rest, batch, {}, w.cut, g.rows > g.cols ? g.rows : g.cols, s);
 }
 
 template <typename T, int R>

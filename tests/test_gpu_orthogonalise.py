@@ -138,6 +138,24 @@ def test_larger(m, n, dtype):
     assert _rel(out, _formula(torch, x, 5)) <= TOL[dtype]
 
 
+@pytest.mark.parametrize("dtype,m,n", [("float32", 4096, 4096), ("bfloat16", 4000, 9000), ("float32", 6000, 1650)])
+def test_tiles_in_pieces(dtype, m, n):
+    """Products of fewer tiles than compute units, in one and in two groups of pieces; the formula on the GPU."""
+    torch, hc = _hc()
+    d = _matrix(torch, m, n, "random", dtype).cuda()
+    out = torch.empty_like(d)
+    ws = hc.alloc_orthogonalise_workspace(d)
+    ws.fill_(255)
+    hc.hc_orthogonalise(d, out, ws, steps=2)
+    y = d.double() if m <= n else d.double().T.contiguous()
+    y = y / torch.linalg.vector_norm(y)
+    a, b, c = MUON
+    for _ in range(2):
+        g = y @ y.T.contiguous()
+        y = a * y + (b * g + c * (g @ g)) @ y
+    assert _rel(out, y if m <= n else y.T) <= TOL[dtype]
+
+
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
 @pytest.mark.parametrize("m,n", [(40, 70), (300, 200)])
 def test_zero_nan_and_infinity(dtype, m, n):

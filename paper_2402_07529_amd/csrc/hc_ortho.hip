@@ -235,11 +235,14 @@ enum Step { MIDDLE = 0, FIRST = 1, LAST = 2 };
 
 // Few tiles: each is cut along l into pieces, one or two a workgroup, whose sums
 // a launch of its own adds up.  The first `tiles` of them in `first` pieces, the
-// others in `second`.
+// others in `second`.  first == 1: those fill the CUs whole, in a launch before
+// (528 tiles of 4096 x 4096 on 512 places, bf16: 104 us as whole tiles, 97).
 struct Cuts {
     uint32_t tiles, first, others, second;
-    __host__ __device__ uint32_t groups() const { return max(tiles * first, others * second); }
-    __host__ __device__ uint32_t pieces() const { return tiles * first + others * second; }
+    __host__ __device__ uint32_t whole() const { return first == 1 ? tiles : 0; }
+    __host__ __device__ uint32_t first_pieces() const { return first == 1 ? 0 : tiles * first; }
+    __host__ __device__ uint32_t pieces() const { return first_pieces() + others * second; }
+    __host__ __device__ uint32_t groups() const { return max(first_pieces(), others * second); }
 };
 
 struct Product {
@@ -727,13 +730,13 @@ __global__ __launch_bounds__(S::kThreads) void pieces_kernel(Product g) {
     for (uint32_t k = 0; k < 2; k++) {
         const uint32_t tiles = k == 0 ? g.cuts.tiles : g.cuts.others;
         const uint32_t cuts = k == 0 ? g.cuts.first : g.cuts.second;
-        if (w >= tiles * cuts) continue;
+        if (w >= (k == 0 ? g.cuts.first_pieces() : tiles * cuts)) continue;
         const uint32_t piece = w / tiles, t = (k == 0 ? 0 : g.cuts.tiles) + w - piece * tiles;
         f4 acc[FM][FN] = {};
         accumulate<PLANES, S>(g, tile_at<KIND>(g, t), piece * lines / cuts,
                               (piece + 1) * lines / cuts, s_mem, acc);
         f4* part = reinterpret_cast<f4*>(g.part) +
-                   (size_t)((k == 0 ? 0 : g.cuts.tiles * g.cuts.first) + w) * (S::BM * S::BN / 4);
+                   (size_t)((k == 0 ? 0 : g.cuts.first_pieces()) + w) * (S::BM * S::BN / 4);
 #pragma unroll
         for (int u = 0; u < FM; u++)
 #pragma unroll
@@ -748,13 +751,14 @@ __global__ __launch_bounds__(S::EM * 4) void join_kernel(Product g) {
     constexpr int FN = S::WN / 16, EM = S::EM, EN = S::EN;
     constexpr uint32_t kBlocks = S::kWaves * (S::WM / EM) * (S::WN / EN);  // of a tile
     __shared__ __align__(16) float s_stage[EM * EN];
-    const uint32_t t = blockIdx.x / kBlocks, block = blockIdx.x - t * kBlocks;
+    const uint32_t tile_block = blockIdx.x / kBlocks, block = blockIdx.x - tile_block * kBlocks;
+    const uint32_t t = g.cuts.whole() + tile_block;
     const uint32_t wave = block % S::kWaves, sub = block / S::kWaves;
     const uint32_t eu = sub / (S::WN / EN), ev = sub % (S::WN / EN);
     const bool second = t >= g.cuts.tiles;
     const uint32_t cuts = second ? g.cuts.second : g.cuts.first;
     const uint32_t step = second ? g.cuts.others : g.cuts.tiles;  // from piece to piece
-    const size_t piece0 = second ? g.cuts.tiles * (size_t)g.cuts.first + (t - g.cuts.tiles) : t;
+    const size_t piece0 = second ? g.cuts.first_pieces() + (t - g.cuts.tiles) : t;
     const uint32_t lane = threadIdx.x & 63, u = threadIdx.x >> 6;
     const f4* part = reinterpret_cast<const f4*>(g.part) +
                      ((eu * (EM / 16) + u) * FN + ev * (EN / 16)) * S::kThreads + wave * 64 + lane;
@@ -1113,31 +1117,44 @@ double plain_cost(const TileCost& c, uint64_t tiles, uint32_t lines, int planes,
     return t;
 }
 
-// A workgroup on every CU (full = 0), or as many as fit: every tile in as many
-// pieces as there is room for, or one more of as many tiles as that leaves room
-// for and the others in the pieces that fill it.
+// With a workgroup on every CU (full = 0) or as many as fit: every tile in as
+// many pieces as there is room for; one more of as many tiles as that leaves room
+// for, the others in the pieces that fill it; or whole rounds of whole tiles, the
+// others in pieces.
 void try_pieces(int k, int full, uint64_t n, uint32_t lines, int planes, int cus, double* best,
                 Way* way) {
     const TileCost& T = kTileCosts[k];
     const PieceCost& c = kPieceCosts[k];
     if (full && T.resident == 1) return;
     const uint64_t slots = (uint64_t)cus * (full ? T.resident : 1), most = lines / c.least;
-    if (n == 0 || n >= slots) return;
+    const uint64_t round = (uint64_t)cus * T.resident;
+    if (n == 0 || most < 2) return;
     const double step = planes == 1 ? (full ? T.shared : T.alone) : (full ? T.shared2 : T.alone2);
     const double size = 4.0 * T.tile * T.tile;
-    for (int more = 0; more < 2; more++) {
-        const uint64_t first = slots / n + more < most ? slots / n + more : most;
-        if (first < 2) continue;
-        const uint64_t take = slots / first < n ? slots / first : n, others = n - take;
-        const uint64_t second = others == 0 ? 0 : slots / others < most ? slots / others : most;
-        double t = (lines + first - 1) / first * step + c.ends;
-        if (others) t += (lines + second - 1) / second * step + c.ends;
-        t += kJoin + kJoinPart * (first > second ? first : second) +
-             (take * first + others * second + n) * size / kBytesPerUs;
-        if (t < *best) {
-            *best = t;
-            *way = Way{T.tile, {(uint32_t)take, (uint32_t)first, (uint32_t)others, (uint32_t)second}, 0, 0};
+    auto pieces = [&](uint64_t tiles, uint64_t cuts) {
+        return tiles == 0 ? 0.0
+                          : (lines + cuts - 1) / cuts * step + c.ends +
+                                ((cuts + 1) * tiles) * size / kBytesPerUs + kJoinPart * cuts;
+    };
+    auto consider = [&](double t, uint64_t tiles, uint64_t first, uint64_t second) {
+        if (t >= *best) return;
+        *best = t;
+        *way = Way{T.tile, {(uint32_t)tiles, (uint32_t)first, (uint32_t)(n - tiles), (uint32_t)second}, 0, 0};
+    };
+    if (n < slots) {
+        for (int more = 0; more < 2; more++) {
+            const uint64_t first = slots / n + more < most ? slots / n + more : most;
+            if (first < 2) continue;
+            const uint64_t take = slots / first < n ? slots / first : n, others = n - take;
+            const uint64_t second = others == 0 ? 0 : slots / others < most ? slots / others : most;
+            consider(pieces(take, first) + pieces(others, second) + kJoin, take, first, second);
         }
+    }
+    const uint64_t whole = n / round * round, others = n - whole;
+    if (whole && others && slots / others >= 2) {
+        const uint64_t second = slots / others < most ? slots / others : most;
+        consider(plain_cost(T, whole, lines, planes, cus) + kLaunch + pieces(others, second) + kJoin,
+                 whole, 1, second);
     }
 }
 
@@ -1317,10 +1334,14 @@ hipError_t product_shape(Product g, uint32_t batch, const Cuts& cuts, uint32_t k
     g.cuts = cuts;
     if constexpr (KIND != APPLY) {
         if (cuts.tiles) {
-            const hipError_t e = launch_tiles<S>(&pieces_kernel<KIND, PLANES, S>, g, cuts.groups(), s);
+            hipError_t e = hipSuccess;
+            if (cuts.whole())
+                e = launch_tiles<S>(&product_kernel<KIND, MIDDLE, PLANES, T, S>, g, cuts.whole(), s);
+            if (e == hipSuccess)
+                e = launch_tiles<S>(&pieces_kernel<KIND, PLANES, S>, g, cuts.groups(), s);
             if (e != hipSuccess) return e;
             hipLaunchKernelGGL((join_kernel<KIND, PLANES, T, S>),
-                               dim3(g.tiles * batch * (S::BM / S::EM) * (S::BN / S::EN)),
+                               dim3((g.tiles * batch - cuts.whole()) * (S::BM / S::EM) * (S::BN / S::EN)),
                                dim3(S::EM * 4), 0, s, g);
             return hipGetLastError();
         }

@@ -858,10 +858,11 @@ __global__ void clear_word_kernel(uint32_t* a) { *a = 0; }
 
 // ---- layout and launches ---------------------------------------------------------
 
-// Pairs per chunk: 64, or fewer (down to 8) while that leaves under kFewWaves
+// Pairs per chunk: 64, or fewer (down to 4) while that leaves under kFewWaves
 // waves of sums (a lane takes four columns, a wave up to 64 lanes of one row).
 // Half and twice as many waves: 30,522 x 768 bf16 with 32,768 ids 72 and 77 us
-// (68), 2^24 x 64 with 2^20 ids by rows 192 and 206 us (193).
+// (68), 2^24 x 64 with 2^20 ids by rows 192 and 206 us (193).  Down to 4: 4099
+// ids by rows of 64 24.7 us, 26.6 with 8 at least.
 constexpr uint64_t kFewWaves = 4096;
 
 // A workgroup's chunks (256 lanes' worth, 8 columns a lane at least) hold at most
@@ -882,7 +883,7 @@ uint64_t lanes_of_row(uint64_t dim) {
 uint32_t chunk_for(const hc_embed_params& p) {
     const uint64_t lanes = lanes_of_row(p.dim);
     uint32_t chunk = most_chunk(p.dim);
-    while (chunk > 8 && p.count / chunk * lanes / 64 < kFewWaves) chunk /= 2;
+    while (chunk > 4 && p.count / chunk * lanes / 64 < kFewWaves) chunk /= 2;
     return chunk;
 }
 
@@ -892,7 +893,7 @@ uint64_t most_chunks(uint64_t dim, uint64_t count) {
     // a chunk is halved while it leaves fewer than kFewWaves waves, so the halves
     // make fewer than twice as many
     const uint64_t few = 2 * kFewWaves * 64 / lanes_of_row(dim) + 2, c = most_chunk(dim);
-    const uint64_t small = (count + 7) / 8 < few ? (count + 7) / 8 : few, large = (count + c - 1) / c;
+    const uint64_t small = (count + 3) / 4 < few ? (count + 3) / 4 : few, large = (count + c - 1) / c;
     return small > large ? small : large;
 }
 

@@ -255,14 +255,14 @@ __device__ __forceinline__ uint32_t wave_rank(volatile uint32_t* cnt, uint32_t d
 }
 
 // Up to kSmallCount ids: one launch.  A pair's place is the number of pairs
-// before it in the order, and every workgroup counts that for `own` pairs (a
-// power of two) against all keys, held in LDS: its lanes are `own` pairs times
-// 1024 / own interleaved slices of the keys.  4099 ids, 25-bit keys: 5 us, where
+// before it in the order, and every workgroup counts that for kSmallOwn pairs
+// against all keys, held in LDS: its lanes are kSmallOwn pairs times 64
+// interleaved slices of the keys.  4099 ids, 25-bit keys: 5.8 us, where
 // a radix sort by one workgroup took 23.  The other workgroups write zeros.
-constexpr uint32_t kSmallThreads = 1024, kSmallCount = 8192;
+constexpr uint32_t kSmallThreads = 1024, kSmallCount = 8192, kSmallOwn = 16;
 
 struct SmallSort {
-    uint32_t count, groups, log2own;
+    uint32_t count, groups;
     Pair* out;
     uint32_t* crossing_count;
     Zeros zeros;
@@ -271,7 +271,7 @@ struct SmallSort {
 template <typename ID>
 __global__ __launch_bounds__(kSmallThreads) void small_sort_kernel(FromIds<ID> src, SmallSort a) {
     extern __shared__ __align__(16) uint32_t s_key[];  // padded to a multiple of 4 keys
-    __shared__ uint32_t s_rank[64];
+    __shared__ uint32_t s_rank[kSmallOwn];
     if (blockIdx.x >= a.groups) {
         zero_piece(a.zeros, a.zeros.first + blockIdx.x - a.groups);
         return;
@@ -288,23 +288,26 @@ __global__ __launch_bounds__(kSmallThreads) void small_sort_kernel(FromIds<ID> s
         const uint32_t k = u * kSmallThreads + threadIdx.x;
         if (k < quads * 4) s_key[k] = keys[u];
     }
-    const uint32_t own = 1u << a.log2own;
-    if (threadIdx.x < own) s_rank[threadIdx.x] = 0;
+    if (threadIdx.x < kSmallOwn) s_rank[threadIdx.x] = 0;
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.crossing_count = 0;
     lds_barrier();
-    const uint32_t i = (blockIdx.x << a.log2own) + (threadIdx.x & (own - 1u));
+    const uint32_t first = blockIdx.x * kSmallOwn, i = first + threadIdx.x % kSmallOwn;
     const uint32_t key = i < a.count ? s_key[i] : 0u;
-    uint32_t before = 0;
-    for (uint32_t q = threadIdx.x >> a.log2own; q < quads; q += kSmallThreads >> a.log2own) {
+    // smaller keys, and equal ones of earlier pairs: of workgroups before this one,
+    // then (a slice each) of this one's own
+    const uint32_t slice = threadIdx.x / kSmallOwn;
+    uint32_t before = i < a.count && slice < i - first && s_key[first + slice] == key ? 1u : 0u;
+#pragma unroll 4
+    for (uint32_t q = slice; q < quads; q += kSmallThreads / kSmallOwn) {
         const v4u k = *reinterpret_cast<const v4u*>(s_key + 4 * q);
+        const uint32_t bound = 4 * q < first ? key + 1 : key;
 #pragma unroll
-        for (uint32_t j = 0; j < 4; j++)  // keys are below 2^31
-            before += k[j] < key + (4 * q + j < i ? 1u : 0u) ? 1u : 0u;
+        for (uint32_t j = 0; j < 4; j++) before += k[j] < bound ? 1u : 0u;
     }
-    for (uint32_t d = own; d < 64; d <<= 1) before += __shfl_xor(before, d);
-    if (lane_id() < own) atomicAdd(&s_rank[lane_id()], before);
+    for (uint32_t d = kSmallOwn; d < 64; d <<= 1) before += __shfl_xor(before, d);
+    if (lane_id() < kSmallOwn) atomicAdd(&s_rank[lane_id()], before);
     lds_barrier();
-    if (threadIdx.x < own && i < a.count) a.out[s_rank[threadIdx.x]] = Pair{key, i};
+    if (threadIdx.x < kSmallOwn && i < a.count) a.out[s_rank[threadIdx.x]] = Pair{key, i};
 }
 
 // More ids (2^20 of 25 bits: three passes of 7 + 4 + 12 us): per pass every
@@ -1035,8 +1038,7 @@ hipError_t sort_ids(const hc_embed_params& p, const void* ids, const GradLayout&
     }
     SmallSort a = {};
     a.count = (uint32_t)p.count;
-    a.log2own = a.count > 4096 ? 5 : 4;  // up to 256 workgroups
-    a.groups = (a.count + (1u << a.log2own) - 1) >> a.log2own;
+    a.groups = (a.count + kSmallOwn - 1) / kSmallOwn;
     a.out = reinterpret_cast<Pair*>(ws + L.pairs[0]);
     a.crossing_count = reinterpret_cast<uint32_t*>(ws + L.crossing_count);
     a.zeros = z;

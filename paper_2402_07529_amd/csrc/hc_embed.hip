@@ -259,7 +259,8 @@ __device__ __forceinline__ uint32_t wave_rank(volatile uint32_t* cnt, uint32_t d
 // against all keys, held in LDS: its lanes are kSmallOwn pairs times 64
 // interleaved slices of the keys.  4099 ids, 25-bit keys: 5.8 us, where
 // a radix sort by one workgroup took 23.  The other workgroups write zeros.
-constexpr uint32_t kSmallThreads = 1024, kSmallCount = 8192, kSmallOwn = 16;
+constexpr uint32_t kSmallThreads = 1024, kSmallCount = 12288, kSmallOwn = 16;
+constexpr uint32_t kSmallCount1 = 8192;  // where one radix pass would do
 
 struct SmallSort {
     uint32_t count, groups;
@@ -544,6 +545,8 @@ __device__ __forceinline__ void store_sum(TO* p, int nv, const typename Sum<TO>:
     }
 }
 
+constexpr uint32_t kCountedHeads = 8192;  // 4096 pairs a round of loads
+
 struct SumArgs {
     const Pair* pairs;
     uint32_t count, chunk, chunks, vocab, dim, dim8;
@@ -552,7 +555,7 @@ struct SumArgs {
     float scale, fixed;
     bool accumulate;
     // by rows; heads: runs that begin before each chunk (NULL, for up to
-    // kSmallCount pairs: counted by the sums, which then set *touched)
+    // kCountedHeads pairs: counted by the sums, which then set *touched)
     uint32_t* rows;
     const uint32_t* heads;
     uint32_t* touched;
@@ -691,7 +694,7 @@ __device__ __forceinline__ void sum_chunk(const SumArgs& a, const NearPairs& pai
 }
 
 // This wave's share of the runs that begin at positions below `hi` (all lanes of
-// a workgroup call it, at most kSmallCount positions): two pairs a lane and load,
+// a workgroup call it, at most kCountedHeads positions): two pairs a lane and load,
 // 8 loads in flight.
 __device__ __forceinline__ uint32_t count_begins(const SumArgs& a, uint32_t hi) {
     uint32_t found = 0;
@@ -932,7 +935,11 @@ GradLayout grad_layout(const hc_embed_params& p) {
     L.chunks = (uint32_t)((p.count + L.chunk - 1) / L.chunk);
     const uint64_t tile = sort_threads(p.count) * kItems;
     L.groups = (uint32_t)((p.count + tile - 1) / tile);
-    L.small = p.count <= kSmallCount;
+    // one launch or radix passes: 10,000 ids into 30,522 rows of 768 48 us (63),
+    // 12,288 54 (63), 15,000 63 (66); in one pass (300 rows of 64) 12,288 39 (35)
+    uint32_t passes, log2bins;
+    digits_for(p.vocab, &passes, &log2bins);
+    L.small = p.count <= (passes > 1 ? kSmallCount : kSmallCount1);
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t o = at;
@@ -1146,7 +1153,7 @@ hipError_t launch_embed_grad(const hc_embed_params& p, hc_type x_type, const voi
     a.partial = ws + L.partial;
     if (!rows) return sum_from<false>(a, x_type, out.type, dout, out.dst, di.cus, s);
     a.touched = out.touched;
-    if (!L.small) {
+    if (p.count > kCountedHeads) {
         uint32_t* heads = reinterpret_cast<uint32_t*>(ws + L.heads);
         a.heads = heads;
         hipLaunchKernelGGL(head_count_kernel, dim3((uint32_t)((p.count + kBlock - 1) / kBlock)),

@@ -158,6 +158,14 @@ def test_gradient(vocab, dim, count, kind, x_type, g_type):
         _check(torch, got, *_reference(torch, dout, ids, vocab, scale, padding), g_type)
 
 
+@pytest.mark.parametrize("vocab,dim,count", [(5000, 64, 12288), (5000, 64, 12289), (300, 64, 8191), (300, 64, 8193),
+                                             (2**24, 4, 12287), (900, 3, 4093), (900, 5, 5)])
+@pytest.mark.parametrize("kind", ["uniform", "hot", "invalid"])
+@pytest.mark.parametrize("g_type", ["float32", "int32"])
+def test_gradient_either_side_of_a_sort(vocab, dim, count, kind, g_type):
+    test_gradient(vocab, dim, count, kind, "float32", g_type)
+
+
 @pytest.mark.parametrize("vocab,dim,count,gap,offset", [(100, 7, 200, 3, 1), (64, 64, 500, 8, 4),
                                                         (33, 130, 3000, 1, 3)])
 @pytest.mark.parametrize("x_type,g_type", [("float32", "float32"), ("bfloat16", "bfloat16"),

@@ -259,8 +259,7 @@ __device__ __forceinline__ uint32_t wave_rank(volatile uint32_t* cnt, uint32_t d
 // against all keys, held in LDS: its lanes are kSmallOwn pairs times 64
 // interleaved slices of the keys.  4099 ids, 25-bit keys: 5.8 us, where
 // a radix sort by one workgroup took 23.  The other workgroups write zeros.
-constexpr uint32_t kSmallThreads = 1024, kSmallCount = 12288, kSmallOwn = 16;
-constexpr uint32_t kSmallCount1 = 8192;  // where one radix pass would do
+constexpr uint32_t kSmallThreads = 1024, kSmallCount = 6144, kSmallOwn = 16;
 
 struct SmallSort {
     uint32_t count, groups;
@@ -309,6 +308,114 @@ __global__ __launch_bounds__(kSmallThreads) void small_sort_kernel(FromIds<ID> s
     if (lane_id() < kSmallOwn) atomicAdd(&s_rank[lane_id()], before);
     lds_barrier();
     if (threadIdx.x < kSmallOwn && i < a.count) a.out[s_rank[threadIdx.x]] = Pair{key, i};
+}
+
+// Up to kMergeCount ids: two launches.  The first sorts blocks of kMergeBlock pairs
+// as above, kBlockOwn of them a workgroup, a slice of the keys a wave.  In the
+// second every workgroup holds all sorted keys in LDS, and eight lanes a pair
+// search the other blocks for its place.  Both bounds as measured, the whole call
+// by rows of 64: 4099 ids 20 us in one launch, 22 in two; 6000 24 and 24; 8192 27
+// and 25.5; 16,384 33 in two, 67 in radix passes, and 32,768 of 768 bf16 70 and 82.
+constexpr uint32_t kMergeCount = 32768, kMergeBlock = 1024, kBlockOwn = 64, kMergeOwn = 128;
+
+struct MergeSort {
+    uint32_t count, groups, blocks;
+    uint32_t *keys, *pos;  // of the sorted blocks
+    Pair* out;
+    uint32_t* crossing_count;
+    Zeros zeros;
+};
+
+template <typename ID>
+__global__ __launch_bounds__(kMergeBlock) void block_sort_kernel(FromIds<ID> src, MergeSort a) {
+    __shared__ __align__(16) uint32_t s_key[kMergeBlock];
+    __shared__ uint32_t s_rank[kBlockOwn];
+    if (blockIdx.x >= a.groups) {
+        zero_piece(a.zeros, a.zeros.first + blockIdx.x - a.groups);
+        return;
+    }
+    constexpr uint32_t kParts = kMergeBlock / kBlockOwn, kSlices = kMergeBlock / 64;
+    static_assert(kBlockOwn == 64 && kParts == kSlices, "a lane a pair; see `own` below");
+    const uint32_t base = blockIdx.x / kParts * kMergeBlock, part = blockIdx.x % kParts;
+    s_key[threadIdx.x] = base + threadIdx.x < a.count ? src.get(base + threadIdx.x).key : ~0u;
+    if (threadIdx.x < kBlockOwn) s_rank[threadIdx.x] = 0;
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.crossing_count = 0;
+    lds_barrier();
+    const uint32_t i = part * kBlockOwn + lane_id(), key = s_key[i];
+    uint32_t before = 0;
+#pragma unroll
+    for (uint32_t k = 0; k < kSlices; k++) {
+        const uint32_t q = k * kSlices + (threadIdx.x >> 6);
+        const v4u w = *reinterpret_cast<const v4u*>(s_key + 4 * q);
+        if (k == part) {  // these four may be on either side of i
+#pragma unroll
+            for (uint32_t j = 0; j < 4; j++) before += w[j] < key + (4 * q + j < i ? 1u : 0u) ? 1u : 0u;
+        } else {
+            const uint32_t bound = k < part ? key + 1 : key;
+#pragma unroll
+            for (uint32_t j = 0; j < 4; j++) before += w[j] < bound ? 1u : 0u;
+        }
+    }
+    atomicAdd(&s_rank[lane_id()], before);
+    lds_barrier();
+    if (threadIdx.x < kBlockOwn && base + i < a.count) {
+        a.keys[base + s_rank[threadIdx.x]] = key;
+        a.pos[base + s_rank[threadIdx.x]] = base + i;
+    }
+}
+
+__global__ __launch_bounds__(1024) void merge_kernel(MergeSort a) {
+    extern __shared__ __align__(16) uint32_t s_key[];  // whole blocks
+    if (blockIdx.x >= a.groups) {
+        zero_piece(a.zeros, a.zeros.first + blockIdx.x - a.groups);
+        return;
+    }
+    constexpr uint32_t kLanes = 1024 / kMergeOwn;                     // of a pair
+    constexpr uint32_t kEach = kMergeCount / kMergeBlock / kLanes;    // blocks a lane searches
+    constexpr uint32_t kLoads = kMergeCount / 4 / 1024;
+    v4u w[kLoads];
+#pragma unroll
+    for (uint32_t u = 0; u < kLoads; u++) {
+        const uint32_t k = (u * 1024 + threadIdx.x) * 4;
+        if (k < a.count) w[u] = *reinterpret_cast<const v4u*>(a.keys + k);  // the list is padded
+    }
+#pragma unroll
+    for (uint32_t u = 0; u < kLoads; u++) {
+        const uint32_t k = (u * 1024 + threadIdx.x) * 4;
+#pragma unroll
+        for (uint32_t j = 0; j < 4; j++)
+            if (k + j >= a.count) w[u][j] = ~0u;
+        if (k < a.blocks * kMergeBlock) *reinterpret_cast<v4u*>(s_key + k) = w[u];
+    }
+    const uint32_t i = blockIdx.x * kMergeOwn + threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
+    const uint32_t own = i / kMergeBlock;
+    const uint32_t at = i < a.count && lane == 0 ? a.pos[i] : 0;
+    lds_barrier();
+    const uint32_t key = i < a.count ? s_key[i] : 0;
+    // pairs before this one in each block: of smaller keys, and of equal ones if the
+    // block is an earlier one
+    uint32_t first[kEach], found[kEach], bound[kEach];
+#pragma unroll
+    for (uint32_t e = 0; e < kEach; e++) {
+        const uint32_t b = e * kLanes + lane;
+        first[e] = b < a.blocks ? b * kMergeBlock : 0;
+        bound[e] = b < own ? key + 1 : key;
+        found[e] = 0;
+    }
+#pragma unroll
+    for (uint32_t step = kMergeBlock / 2; step > 0; step /= 2)
+#pragma unroll
+        for (uint32_t e = 0; e < kEach; e++)
+            found[e] += s_key[first[e] + found[e] + step - 1] < bound[e] ? step : 0;
+    uint32_t rank = 0;
+#pragma unroll
+    for (uint32_t e = 0; e < kEach; e++) {
+        const uint32_t b = e * kLanes + lane;
+        found[e] += s_key[first[e] + found[e]] < bound[e] ? 1 : 0;
+        rank += b >= a.blocks ? 0 : b == own ? i % kMergeBlock : found[e];
+    }
+    for (uint32_t d = 1; d < kLanes; d <<= 1) rank += __shfl_xor(rank, d);
+    if (lane == 0 && i < a.count) a.out[rank] = Pair{key, at};
 }
 
 // More ids (2^20 of 25 bits: three passes of 7 + 4 + 12 us): per pass every
@@ -925,7 +1032,7 @@ uint64_t most_groups(uint64_t count) {
 
 struct GradLayout {
     uint32_t chunk, chunks, groups;
-    bool small;
+    bool small, merge;  // how ids are sorted; neither: radix passes
     size_t pairs[2], hist, total, heads, crossing_count, crossing, partial, bytes;
 };
 
@@ -935,11 +1042,8 @@ GradLayout grad_layout(const hc_embed_params& p) {
     L.chunks = (uint32_t)((p.count + L.chunk - 1) / L.chunk);
     const uint64_t tile = sort_threads(p.count) * kItems;
     L.groups = (uint32_t)((p.count + tile - 1) / tile);
-    // one launch or radix passes: 10,000 ids into 30,522 rows of 768 48 us (63),
-    // 12,288 54 (63), 15,000 63 (66); in one pass (300 rows of 64) 12,288 39 (35)
-    uint32_t passes, log2bins;
-    digits_for(p.vocab, &passes, &log2bins);
-    L.small = p.count <= (passes > 1 ? kSmallCount : kSmallCount1);
+    L.small = p.count <= kSmallCount;
+    L.merge = !L.small && p.count <= kMergeCount;
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t o = at;
@@ -947,9 +1051,9 @@ GradLayout grad_layout(const hc_embed_params& p) {
         return o;
     };
     L.pairs[0] = take(p.count * sizeof(Pair));
-    L.pairs[1] = take(L.small ? 0 : p.count * sizeof(Pair));
+    L.pairs[1] = take(L.small ? 0 : L.merge ? 2 * align256(p.count * 4) : p.count * sizeof(Pair));
     const size_t chunks = most_chunks(p.dim, p.count);
-    L.hist = take(L.small ? 0 : most_groups(p.count) * kMaxBins * 4);
+    L.hist = take(L.small || L.merge ? 0 : most_groups(p.count) * kMaxBins * 4);
     L.total = take(kMaxBins * 4);
     L.heads = take(chunks * 4);
     L.crossing_count = take(4);
@@ -1039,6 +1143,30 @@ template <typename ID>
 hipError_t sort_ids(const hc_embed_params& p, const void* ids, const GradLayout& L, char* ws,
                     const Pair** sorted, Zeros z, hipStream_t s) {
     const FromIds<ID> src = {static_cast<const ID*>(ids), (uint32_t)p.vocab, p.padding};
+    if (L.merge) {
+        MergeSort a = {};
+        a.count = (uint32_t)p.count;
+        a.blocks = (a.count + kMergeBlock - 1) / kMergeBlock;
+        a.keys = reinterpret_cast<uint32_t*>(ws + L.pairs[1]);
+        a.pos = reinterpret_cast<uint32_t*>(ws + L.pairs[1] + align256(p.count * 4));
+        a.out = reinterpret_cast<Pair*>(ws + L.pairs[0]);
+        a.crossing_count = reinterpret_cast<uint32_t*>(ws + L.crossing_count);
+        a.zeros = z;
+        *sorted = a.out;
+        const int lds = (int)(a.blocks * kMergeBlock * 4);
+        const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(&merge_kernel), lds);
+        if (e != hipSuccess) return e;
+        uint32_t n = share(&z, 2);
+        a.groups = a.blocks * (kMergeBlock / kBlockOwn);
+        hipLaunchKernelGGL(block_sort_kernel<ID>, dim3(a.groups + n), dim3(kMergeBlock), 0, s, src, a);
+        z.first += n;
+        a.zeros = z;
+        n = share(&z, 1);
+        a.groups = (a.count + kMergeOwn - 1) / kMergeOwn;
+        hipLaunchKernelGGL(merge_kernel, dim3(a.groups + n), dim3(1024), lds, s, a);
+        z.first += n;
+        return zero_rest(z, s);
+    }
     if (!L.small) {
         if (sort_threads(p.count) == 512) return sort_large<512>(p, src, L, ws, sorted, z, s);
         return sort_large<256>(p, src, L, ws, sorted, z, s);

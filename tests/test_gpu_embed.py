@@ -159,7 +159,9 @@ def test_gradient(vocab, dim, count, kind, x_type, g_type):
 
 
 @pytest.mark.parametrize("vocab,dim,count", [(5000, 64, 12288), (5000, 64, 12289), (300, 64, 8191), (300, 64, 8193),
-                                             (2**24, 4, 12287), (900, 3, 4093), (900, 5, 5)])
+                                             (2**24, 4, 12287), (900, 3, 4093), (900, 5, 5),
+                                             (2**20, 8, 6144), (77, 8, 6145), (2**24, 3, 7169), (2**24, 2, 32768),
+                                             (9000, 2, 32767), (9000, 2, 32769), (2**21, 4, 31745)])
 @pytest.mark.parametrize("kind", ["uniform", "hot", "invalid"])
 @pytest.mark.parametrize("g_type", ["float32", "int32"])
 def test_gradient_either_side_of_a_sort(vocab, dim, count, kind, g_type):

@@ -976,8 +976,8 @@ __global__ void clear_word_kernel(uint32_t* a) { *a = 0; }
 
 // Pairs per chunk: 64, or fewer (down to 4) while that leaves under kFewWaves
 // waves of sums (a lane takes four columns, a wave up to 64 lanes of one row).
-// Half and twice as many waves: 30,522 x 768 bf16 with 32,768 ids 72 and 77 us
-// (68), 2^24 x 64 with 2^20 ids by rows 192 and 206 us (193).  Down to 4: 4099
+// Half and twice as many waves: 30,522 x 768 bf16 with 32,768 ids 57 and 58 us
+// (49), 2^24 x 64 with 2^20 ids by rows 179 and 188 us (179).  Down to 4: 4099
 // ids by rows of 64 24.7 us, 26.6 with 8 at least.
 constexpr uint64_t kFewWaves = 4096;
 

@@ -236,7 +236,7 @@ enum Step { MIDDLE = 0, FIRST = 1, LAST = 2 };
 // Few tiles: each is cut along l into pieces, one or two a workgroup, whose sums
 // a launch of its own adds up.  The first `tiles` of them in `first` pieces, the
 // others in `second`.  first == 1: those fill the CUs whole, in a launch before
-// (528 tiles of 4096 x 4096 on 512 places, bf16: 104 us as whole tiles, 97).
+// (528 tiles of 4096 x 4096 on 512 places, bf16: 104 us as whole tiles, 88).
 struct Cuts {
     uint32_t tiles, first, others, second;
     __host__ __device__ uint32_t whole() const { return first == 1 ? tiles : 0; }
@@ -536,8 +536,8 @@ template <Kind KIND, int STEP, int PLANES, typename T, typename S> struct Result
           addend_factor(first ? g_.inverse[t.batch] * g_.factor2 : g_.factor2) {}
 
     // X between two steps passes the caches by in the tiles of large matrices,
-    // which they cannot hold: 4096 x 25088 7.12 -> 6.95 ms (twelve 768 x 768, in
-    // smaller tiles, would go from 289 to 295 us).
+    // which they cannot hold: 2 % of 4096 x 25088 (of twelve 768 x 768, in smaller
+    // tiles, it would cost 2 %).
     template <typename V> __device__ __forceinline__ static V load_x(const V* p) {
         if constexpr (S::BM == 256) return __builtin_nontemporal_load(p);
         return *p;

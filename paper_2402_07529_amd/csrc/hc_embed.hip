@@ -352,7 +352,8 @@ __global__ __launch_bounds__(kMergeBlock) void block_sort_kernel(FromIds<ID> src
         const v4u w = *reinterpret_cast<const v4u*>(s_key + 4 * q);
         if (k == part) {  // these four may be on either side of i
 #pragma unroll
-            for (uint32_t j = 0; j < 4; j++) before += w[j] < key + (4 * q + j < i ? 1u : 0u) ? 1u : 0u;
+            for (uint32_t j = 0; j < 4; j++)
+                before += w[j] < key + (4 * q + j < i ? 1u : 0u) ? 1u : 0u;
         } else {
             const uint32_t bound = k < part ? key + 1 : key;
 #pragma unroll
@@ -421,10 +422,9 @@ __global__ __launch_bounds__(1024) void merge_kernel(MergeSort a) {
     if (lane == 0 && i < a.count) a.out[rank] = Pair{key, at};
 }
 
-// More ids (2^20 of 25 bits: three passes of 7 + 4 + 12 us): per pass every
-// workgroup counts its tile's digits, the counts are
-// scanned per digit over the workgroups, and every workgroup moves its tile's
-// pairs to their places.  Each launch's workgroups past its own write zeros.
+// More ids (2^20 of 25 bits: three passes of 7 + 5 + 12 us): per pass every
+// workgroup counts its tile's digits, the counts are scanned per digit over the
+// workgroups, and every workgroup moves its tile's pairs to their places.  Each launch's workgroups past its own write zeros.
 template <uint32_t THREADS, typename SRC>
 __global__ __launch_bounds__(THREADS) void digit_count_kernel(SRC src, uint32_t count,
                                                               uint32_t groups, uint32_t shift,
@@ -701,7 +701,7 @@ __device__ __forceinline__ void sum_chunk(const SumArgs& a, const NearPairs& pai
                                           uint32_t slab, uint32_t heads) {
     typedef typename Sum<TO>::A A;
     constexpr int VEC = kVec<TI>;
-    constexpr int U = 4;  // two batches in flight; 8: 175 us by rows of 2^20 ids (169), 72 BERT (68)
+    constexpr int U = 4;  // two batches in flight; 8 is 4 % slower by rows of 2^20 ids and for BERT's
     const uint32_t col = ((slab << a.log2g) + (threadIdx.x & ((1u << a.log2g) - 1u))) * VEC;
     if (col >= a.dim) return;
     const int nv = (int)min((uint32_t)VEC, a.dim - col);
@@ -1196,7 +1196,8 @@ hipError_t sum_typed(SumArgs a, const void* x, void* dst, int cus, hipStream_t s
     const uint64_t units = (uint64_t)a.chunks * a.slabs, per_block = kBlock >> a.log2g;
     const uint64_t blocks = (units + per_block - 1) / per_block;
     hipLaunchKernelGGL((segment_sum_kernel<TI, TO, ROWS>),
-                       dim3((uint32_t)(blocks < kMaxGroups ? blocks : kMaxGroups)), dim3(kBlock), 0, s, a, static_cast<const TI*>(x), static_cast<TO*>(dst));
+                       dim3((uint32_t)(blocks < kMaxGroups ? blocks : kMaxGroups)), dim3(kBlock), 0, s, a,
+                       static_cast<const TI*>(x), static_cast<TO*>(dst));
     const uint32_t grid = a.chunks < (uint32_t)cus ? a.chunks : (uint32_t)cus;
     hipLaunchKernelGGL((segment_join_kernel<TI, TO, ROWS>), dim3(grid, a.slabs), dim3(kJoinBlock),
                        0, s, a, static_cast<TO*>(dst));

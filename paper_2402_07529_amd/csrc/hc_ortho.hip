@@ -306,6 +306,10 @@ __device__ __forceinline__ void phase_barrier() {
     __builtin_amdgcn_sched_barrier(0);
 }
 
+__device__ __forceinline__ f4 product16(h8 a, h8 b, f4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
+}
+
 // Fragments and products of one 128-byte step l.  A lane holds row lane % 16 of a
 // fragment, 8 values from chunk 4 h + lane / 16.  The first operand of the
 // instruction gives a lane's 4 consecutive results: Q, so that they lie along j.
@@ -324,7 +328,8 @@ __device__ __forceinline__ void main_loop(f4 (&acc)[S::WM / 16][S::WN / 16], con
         // this wave's loads of step l have landed (those of later steps may be on
         // their way), then everybody's; and everybody is done with step l - 1
         if (l + N - 2 < lines)
-            __builtin_amdgcn_s_waitcnt(0x0f70 | ((N - 2) * kLoads & 15) | ((N - 2) * kLoads >> 4) << 14);
+            __builtin_amdgcn_s_waitcnt(0x0f70 | ((N - 2) * kLoads & 15) |
+                                       ((N - 2) * kLoads >> 4) << 14);
         else
             __builtin_amdgcn_s_waitcnt(0x0f70);
         phase_barrier();
@@ -347,7 +352,7 @@ __device__ __forceinline__ void main_loop(f4 (&acc)[S::WM / 16][S::WN / 16], con
                 for (int u = 0; u < FM; u++)
 #pragma unroll
                     for (int v = 0; v < FN; v++)
-                        acc[u][v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fq[h][v], fp[h][u], acc[u][v], 0, 0, 0);
+                        acc[u][v] = product16(fq[h][v], fp[h][u], acc[u][v]);
             }
         }
         if constexpr (PLANES == 2) {  // high x high, low x high, high x low
@@ -357,7 +362,7 @@ __device__ __forceinline__ void main_loop(f4 (&acc)[S::WM / 16][S::WN / 16], con
                 for (int u = 0; u < FM; u++)
 #pragma unroll
                     for (int v = 0; v < FN; v++)
-                        acc[u][v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fq[t == 1][v], fp[t == 2][u], acc[u][v], 0, 0, 0);
+                        acc[u][v] = product16(fq[t == 1][v], fp[t == 2][u], acc[u][v]);
         }
     }
 }
@@ -409,7 +414,7 @@ __device__ __forceinline__ void main_loop_paired(f4 (&acc)[S::WM / 16][S::WN / 1
                 for (int u = 0; u < FM; u++)
 #pragma unroll
                     for (int v = 0; v < FN; v++)
-                        acc[u][v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fq[h][v], fp[h][u], acc[u][v], 0, 0, 0);
+                        acc[u][v] = product16(fq[h][v], fp[h][u], acc[u][v]);
             } else {
 #pragma unroll
                 for (int t = 0; t < 3; t++)
@@ -417,7 +422,7 @@ __device__ __forceinline__ void main_loop_paired(f4 (&acc)[S::WM / 16][S::WN / 1
                     for (int u = h * FM / 2; u < (h + 1) * FM / 2; u++)
 #pragma unroll
                         for (int v = 0; v < FN; v++)
-                            acc[u][v] = __builtin_amdgcn_mfma_f32_16x16x32_f16(fq[t == 1][v], fp[t == 2][u], acc[u][v], 0, 0, 0);
+                            acc[u][v] = product16(fq[t == 1][v], fp[t == 2][u], acc[u][v]);
             }
             __builtin_amdgcn_s_setprio(0);
             if (!second && h == 1) __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
@@ -844,10 +849,10 @@ __device__ __forceinline__ void split4(f4 w, h4& hi, h4& lo) {
 // (high + low) x (high + low).  The low x low product, which the other kernels
 // leave out, costs nothing here and takes 50 x 3000 from 1.8e-6 to 1.5e-6.
 __device__ __forceinline__ f4 mfma4(h8 ah, h8 al, h8 bh, h8 bl, f4 c) {
-    c = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, bh, c, 0, 0, 0);
-    c = __builtin_amdgcn_mfma_f32_16x16x32_f16(al, bh, c, 0, 0, 0);
-    c = __builtin_amdgcn_mfma_f32_16x16x32_f16(ah, bl, c, 0, 0, 0);
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(al, bl, c, 0, 0, 0);
+    c = product16(ah, bh, c);
+    c = product16(al, bh, c);
+    c = product16(ah, bl, c);
+    return product16(al, bl, c);
 }
 
 template <typename T, int R, bool FIRST>
@@ -1068,8 +1073,8 @@ typedef Shape<64, 64, 32, 32, 3> Small;
 // sides are bound by launches, not by products.
 constexpr uint64_t kTwoPlaneSide = 256;
 
-// How a product runs: the tile, and how it is cut (cuts.tiles = 0: not).  APPLY: `cut` values of the longer side in tiles of `tile`,
-// the rest in tiles of `rest`.
+// How a product runs: the tile, and how it is cut (cuts.tiles = 0: not).  APPLY:
+// `cut` values of the longer side in tiles of `tile`, the rest in tiles of `rest`.
 struct Way {
     int tile;
     Cuts cuts;

@@ -176,10 +176,12 @@ hipError_t embed_typed(const hc_embed_params& p, const void* table, const void* 
 
 // ---- gradient: zeros -------------------------------------------------------------
 
-// A dense gradient's zeros, cut into pieces of about 16 KiB, a workgroup each
-// (plain stores, short-lived workgroups: 7.9 TB/s on 200 MB, 6.0 on 4.3 GB; a
-// grid of 4096 striding workgroups 6.6 and 4.4, nontemporal stores 5.8 and 5.9).
-constexpr uint64_t kPieceBytes = 16384;
+// A dense gradient's zeros, cut into pieces of about 4 KiB: a 16-byte store for
+// each of 256 lanes, a workgroup one piece or as many as it has lanes for.  Each
+// XCD's workgroups take neighbouring pieces.  4.3 GB 7.1 TB/s, 477 MB 6.6 (16 KiB
+// a workgroup in the grid's order 5.9 and 5.7, with nontemporal stores 5.9 and
+// 5.6), 200 MB 7.2 in any of these forms but the last.
+constexpr uint64_t kPieceBytes = 4096, kPieceLanes = 256;
 
 struct Zeros {
     char* dst;            // NULL: none
@@ -187,7 +189,7 @@ struct Zeros {
     uint64_t row_bytes, ld_bytes;
     uint64_t per;         // rows a piece (rows > 1)
     uint64_t pieces;
-    uint64_t first;       // this launch's: [first, first + its extra workgroups)
+    uint64_t first;       // this launch's: from `first`, as many as its extra workgroups take
 };
 
 __device__ __forceinline__ void zero_bytes(char* p, uint64_t bytes, uint32_t at, uint32_t step) {
@@ -197,18 +199,22 @@ __device__ __forceinline__ void zero_bytes(char* p, uint64_t bytes, uint32_t at,
     if (at < (bytes & 15) / 2) reinterpret_cast<uint16_t*>(p + (bytes & ~15ull))[at] = 0;
 }
 
-__device__ __forceinline__ void zero_piece(const Zeros& z, uint64_t piece) {
+// Extra workgroup k of n.
+__device__ __forceinline__ void zero_pieces(const Zeros& z, uint32_t k, uint32_t n) {
+    const uint32_t per = n >> 3, each = max(blockDim.x / (uint32_t)kPieceLanes, 1u);
+    const uint64_t piece = z.first + (uint64_t)(k < 8 * per ? (k & 7u) * per + (k >> 3) : k) * each;
     if (z.rows == 1) {
         const uint64_t b = piece * kPieceBytes;
-        zero_bytes(z.dst + b, min(kPieceBytes, z.row_bytes - b), threadIdx.x, blockDim.x);
+        if (b < z.row_bytes)
+            zero_bytes(z.dst + b, min(each * kPieceBytes, z.row_bytes - b), threadIdx.x, blockDim.x);
         return;
     }
-    const uint64_t r0 = piece * z.per, r1 = min(r0 + z.per, z.rows);
+    const uint64_t r0 = piece * z.per, r1 = min(r0 + each * z.per, z.rows);
     for (uint64_t r = r0 + (threadIdx.x >> 6); r < r1; r += blockDim.x >> 6)
         zero_bytes(z.dst + r * z.ld_bytes, z.row_bytes, threadIdx.x & 63, 64);
 }
 
-__global__ __launch_bounds__(kBlock) void zero_kernel(Zeros z) { zero_piece(z, z.first + blockIdx.x); }
+__global__ __launch_bounds__(kBlock) void zero_kernel(Zeros z) { zero_pieces(z, blockIdx.x, gridDim.x); }
 
 // ---- gradient: sort --------------------------------------------------------------
 
@@ -276,7 +282,7 @@ __global__ __launch_bounds__(kSmallThreads) void small_sort_kernel(FromIds<ID> s
     extern __shared__ __align__(16) uint32_t s_key[];  // padded to a multiple of 4 keys
     __shared__ uint32_t s_rank[kSmallOwn];
     if (blockIdx.x >= a.groups) {
-        zero_piece(a.zeros, a.zeros.first + blockIdx.x - a.groups);
+        zero_pieces(a.zeros, blockIdx.x - a.groups, gridDim.x - a.groups);
         return;
     }
     const uint32_t quads = (a.count + 3) / 4;
@@ -334,7 +340,7 @@ __global__ __launch_bounds__(kMergeBlock) void block_sort_kernel(FromIds<ID> src
     __shared__ __align__(16) uint32_t s_key[kMergeBlock];
     __shared__ uint32_t s_rank[kBlockOwn];
     if (blockIdx.x >= a.groups) {
-        zero_piece(a.zeros, a.zeros.first + blockIdx.x - a.groups);
+        zero_pieces(a.zeros, blockIdx.x - a.groups, gridDim.x - a.groups);
         return;
     }
     constexpr uint32_t kParts = kMergeBlock / kBlockOwn, kSlices = kMergeBlock / 64;
@@ -371,7 +377,7 @@ __global__ __launch_bounds__(kMergeBlock) void block_sort_kernel(FromIds<ID> src
 __global__ __launch_bounds__(1024) void merge_kernel(MergeSort a) {
     extern __shared__ __align__(16) uint32_t s_key[];  // whole blocks
     if (blockIdx.x >= a.groups) {
-        zero_piece(a.zeros, a.zeros.first + blockIdx.x - a.groups);
+        zero_pieces(a.zeros, blockIdx.x - a.groups, gridDim.x - a.groups);
         return;
     }
     constexpr uint32_t kLanes = 1024 / kMergeOwn;                     // of a pair
@@ -434,7 +440,7 @@ __global__ __launch_bounds__(THREADS) void digit_count_kernel(SRC src, uint32_t 
                                                               Zeros zeros) {
     __shared__ uint32_t s_cnt[kMaxBins];
     if (blockIdx.x >= groups) {
-        zero_piece(zeros, zeros.first + blockIdx.x - groups);
+        zero_pieces(zeros, blockIdx.x - groups, gridDim.x - groups);
         return;
     }
     if (blockIdx.x == 0 && threadIdx.x == 0) *crossing_count = 0;
@@ -461,7 +467,7 @@ __global__ __launch_bounds__(kBlock) void digit_scan_kernel(uint32_t* __restrict
                                                             Zeros zeros) {
     const uint32_t own = (bins + kBlock / 64 - 1) / (kBlock / 64);
     if (blockIdx.x >= own) {
-        zero_piece(zeros, zeros.first + blockIdx.x - own);
+        zero_pieces(zeros, blockIdx.x - own, gridDim.x - own);
         return;
     }
     const uint32_t bin = blockIdx.x * (kBlock / 64) + (threadIdx.x >> 6);
@@ -505,7 +511,7 @@ __global__ __launch_bounds__(THREADS) void digit_move_kernel(SRC src, uint32_t c
     __shared__ uint32_t s_cnt[kWaves][kMaxBins];
     __shared__ uint32_t s_tmp[kWaves];
     if (blockIdx.x >= groups) {
-        zero_piece(zeros, zeros.first + blockIdx.x - groups);
+        zero_pieces(zeros, blockIdx.x - groups, gridDim.x - groups);
         return;
     }
     const uint32_t bins = 1u << log2bins;
@@ -1083,20 +1089,27 @@ Zeros zeros_for(void* dst, uint64_t rows, uint64_t row_bytes, uint64_t ld_bytes)
     return z;
 }
 
-// A launch's share of the pieces: workgroups beyond its own.  The grid's lanes
-// stay below 2^32, so what does not fit is written by launches of its own.
-constexpr uint64_t kMaxPieces = 1ull << 20;
+// Workgroups of `threads` for the launch's share of the pieces, beyond its own;
+// `next` is where the launches after it go on.  The grid's lanes stay below 2^32,
+// so what does not fit is written by launches of its own.
+constexpr uint64_t kMaxZeroGroups = 1ull << 20;
 
-uint32_t share(Zeros* z, uint64_t launches_left) {
-    uint64_t n = z->pieces == 0 ? 0 : (z->pieces - z->first + launches_left - 1) / launches_left;
-    return (uint32_t)(n < kMaxPieces ? n : kMaxPieces);
+uint32_t share(const Zeros& z, uint64_t launches_left, uint32_t threads, Zeros* next) {
+    const uint64_t each = threads / kPieceLanes;
+    const uint64_t left = z.first < z.pieces ? z.pieces - z.first : 0;
+    uint64_t n = ((left + launches_left - 1) / launches_left + each - 1) / each;
+    if (n > kMaxZeroGroups) n = kMaxZeroGroups;
+    *next = z;
+    next->first += n * each;
+    return (uint32_t)n;
 }
 
 hipError_t zero_rest(Zeros z, hipStream_t s) {
     while (z.first < z.pieces) {
-        const uint32_t n = share(&z, 1);
+        Zeros next;
+        const uint32_t n = share(z, 1, kBlock, &next);
         hipLaunchKernelGGL(zero_kernel, dim3(n), dim3(kBlock), 0, s, z);
-        z.first += n;
+        z = next;
     }
     return hipGetLastError();
 }
@@ -1108,19 +1121,20 @@ void radix_pass(const SRC& src, uint32_t count, uint32_t shift, uint32_t log2bin
     const uint32_t bins = 1u << log2bins;
     uint32_t* hist = reinterpret_cast<uint32_t*>(ws + L.hist);
     uint32_t* total = reinterpret_cast<uint32_t*>(ws + L.total);
-    uint32_t n = share(z, launches_left);
+    Zeros next;
+    uint32_t n = share(*z, launches_left, THREADS, &next);
     hipLaunchKernelGGL((digit_count_kernel<THREADS, SRC>), dim3(L.groups + n), dim3(THREADS), 0, s,
                        src, count, L.groups, shift, bins, hist,
                        reinterpret_cast<uint32_t*>(ws + L.crossing_count), *z);
-    z->first += n;
-    n = share(z, launches_left - 1);
+    *z = next;
+    n = share(*z, launches_left - 1, kBlock, &next);
     hipLaunchKernelGGL(digit_scan_kernel, dim3((bins + kBlock / 64 - 1) / (kBlock / 64) + n),
                        dim3(kBlock), 0, s, hist, total, bins, L.groups, *z);
-    z->first += n;
-    n = share(z, launches_left - 2);
+    *z = next;
+    n = share(*z, launches_left - 2, THREADS, &next);
     hipLaunchKernelGGL((digit_move_kernel<THREADS, SRC>), dim3(L.groups + n), dim3(THREADS), 0, s,
                        src, count, L.groups, shift, log2bins, hist, total, out, *z);
-    z->first += n;
+    *z = next;
 }
 
 template <uint32_t THREADS, typename ID>
@@ -1154,21 +1168,21 @@ hipError_t sort_ids(const hc_embed_params& p, const void* ids, const GradLayout&
         a.pos = reinterpret_cast<uint32_t*>(ws + L.pairs[1] + align256(p.count * 4));
         a.out = reinterpret_cast<Pair*>(ws + L.pairs[0]);
         a.crossing_count = reinterpret_cast<uint32_t*>(ws + L.crossing_count);
-        a.zeros = z;
         *sorted = a.out;
         const int lds = (int)(a.blocks * kMergeBlock * 4);
         const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(&merge_kernel), lds);
         if (e != hipSuccess) return e;
-        uint32_t n = share(&z, 2);
+        Zeros next;
+        uint32_t n = share(z, 2, kMergeBlock, &next);
+        a.zeros = z;
         a.groups = a.blocks * (kMergeBlock / kBlockOwn);
         hipLaunchKernelGGL(block_sort_kernel<ID>, dim3(a.groups + n), dim3(kMergeBlock), 0, s, src, a);
-        z.first += n;
+        z = next;
+        n = share(z, 1, 1024, &next);
         a.zeros = z;
-        n = share(&z, 1);
         a.groups = (a.count + kMergeOwn - 1) / kMergeOwn;
         hipLaunchKernelGGL(merge_kernel, dim3(a.groups + n), dim3(1024), lds, s, a);
-        z.first += n;
-        return zero_rest(z, s);
+        return zero_rest(next, s);
     }
     if (!L.small) {
         if (sort_threads(p.count) == 512) return sort_large<512>(p, src, L, ws, sorted, z, s);
@@ -1180,12 +1194,12 @@ hipError_t sort_ids(const hc_embed_params& p, const void* ids, const GradLayout&
     a.out = reinterpret_cast<Pair*>(ws + L.pairs[0]);
     a.crossing_count = reinterpret_cast<uint32_t*>(ws + L.crossing_count);
     a.zeros = z;
-    const uint32_t n = share(&z, 1);
+    Zeros next;
+    const uint32_t n = share(z, 1, kSmallThreads, &next);
     hipLaunchKernelGGL(small_sort_kernel<ID>, dim3(a.groups + n), dim3(kSmallThreads),
                        (a.count + 3) / 4 * 16, s, src, a);
     *sorted = a.out;
-    z.first += n;
-    return zero_rest(z, s);
+    return zero_rest(next, s);
 }
 
 template <typename TI, typename TO, bool ROWS>

@@ -1242,7 +1242,7 @@ void plan_products(const hc_orthogonalise_params& p, int cus, OrthoLayout* L) {
             if (t > pad) continue;
             half[s] = p.batch * (r / t) * (r / t + 1) / 2;
         }
-        Way way[3];
+        Way way[3] = {};
         const double t =
             best_way(half[0], half[1], half[2], (uint32_t)(k * L->planes / kLine), L->planes, cus, &way[GRAM]) +
             best_way(half[0], half[1], half[2], (uint32_t)(r * L->planes / kLine), L->planes, cus, &way[SQUARE]) +
@@ -1260,7 +1260,8 @@ void plan_products(const hc_orthogonalise_params& p, int cus, OrthoLayout* L) {
 }
 
 OrthoLayout ortho_layout(const hc_orthogonalise_params& p) {
-    OrthoLayout L;
+    OrthoLayout L = {};
+    if (p.batch == 0) return L;  // no matrices: nothing to plan, no workspace
     const uint64_t r = p.m < p.n ? p.m : p.n;
     L.tall = p.m > p.n;
     L.thin = r <= kThinSide;

@@ -3,6 +3,8 @@ invalid arguments are refused, with a message, before anything is enqueued."""
 import ctypes
 import os
 import re
+import subprocess
+import sys
 
 import pytest
 
@@ -167,3 +169,17 @@ def test_chunks_fit_their_bound():
         for count in [2**k + d for k in range(3, 21) for d in (-1, 0, 1)]:
             # two partial sums of dim elements a chunk of at most 64 pairs, and the sorted pairs
             assert hc.hc_embed_grad_bytes(1000, dim, count) >= count * 8 + -(-count // 64) * 16 * dim
+
+
+@pytest.mark.parametrize("m,n", [(64, 96), (200, 300), (768, 768), (5000, 257)])
+def test_an_empty_batch_needs_no_workspace(m, n):
+    """0 bytes for no matrices, at sides of every plan.  In a process of its own: the size was a
+    division by zero for shorter sides above 128."""
+    code = ("import ctypes, paper_2402_07529_amd as hc\n"
+            "for t in (hc.HC_T_F32, hc.HC_T_BF16):\n"
+            f"    p = hc.hc_orthogonalise_params({m}, {n}, 0, {n}, 0, {n}, 0, t, 5, None, 1e-7, 1.0)\n"
+            "    size = ctypes.c_size_t(7)\n"
+            "    assert hc.lib().hc_orthogonalise_bytes(ctypes.byref(p), ctypes.byref(size)) == hc.HC_OK\n"
+            "    assert size.value == 0\n")
+    got = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=120)
+    assert got.returncode == 0, (got.returncode, got.stderr)

@@ -119,13 +119,22 @@ __global__ __launch_bounds__(kNormBlock) void norm_kernel(const T* __restrict__ 
     }
 }
 
-// 1 / (norm + eps), or NaN where the norm is not finite.  Every lane calls it.
-__device__ __forceinline__ float inverse_norm(const double* partial, uint32_t parts, float eps) {
+// 1 / (norm + eps), or NaN where the norm is not finite, as two factors: the norm
+// of finite fp32 values reaches 2^144, whose inverse no fp32 holds.  From 2^64 on
+// `pre` is 2^-64 (what it takes below the normal range is nothing beside the norm).
+struct Inverse {
+    float pre, rest;
+    __device__ __forceinline__ float of(float v) const { return v * pre * rest; }
+};
+
+// Every lane calls it.
+__device__ __forceinline__ Inverse inverse_norm(const double* partial, uint32_t parts, float eps) {
     double t = 0.0;
     for (uint32_t i = lane_id(); i < parts; i += 64) t += partial[i];
     for (int d = 32; d > 0; d >>= 1) t += __shfl_xor(t, d);
     const double n = sqrt(t);
-    return n < __builtin_inf() ? (float)(1.0 / (n + (double)eps)) : __builtin_nanf("");
+    const float pre = n >= 0x1p64 ? 0x1p-64f : 1.0f;
+    return {pre, n < __builtin_inf() ? (float)(1.0 / ((n + (double)eps) * pre)) : __builtin_nanf("")};
 }
 
 struct PrepArgs {
@@ -135,7 +144,7 @@ struct PrepArgs {
     float eps;
     int shift;
     const double* partial;
-    float* inverse;                // 1 / (norm + eps) of each matrix
+    Inverse* inverse;              // 1 / (norm + eps) of each matrix
     _Float16 *straight, *turned;   // operands in x's orientation and transposed
 };
 
@@ -146,7 +155,7 @@ template <typename T, int PLANES>
 __global__ __launch_bounds__(kPrepBlock) void prepare_kernel(PrepArgs a, const T* __restrict__ x) {
     __shared__ __align__(16) float s_tile[64 * 64];
     const uint32_t b = blockIdx.z;
-    const float f = inverse_norm(a.partial + (uint64_t)b * kNormParts, a.parts, a.eps);
+    const Inverse f = inverse_norm(a.partial + (uint64_t)b * kNormParts, a.parts, a.eps);
     if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) a.inverse[b] = f;
     const float scale = __builtin_ldexpf(1.0f, a.shift);
     const T* m = x + (uint64_t)b * a.stride;
@@ -187,7 +196,7 @@ __global__ __launch_bounds__(kPrepBlock) void prepare_kernel(PrepArgs a, const T
         const bool in = row0 + ii < a.m;
 #pragma unroll
         for (int e = 0; e < 8; e++)  // the padding stays zero whatever f is
-            v[k][e] = in && col0 + jj + e < a.n ? v[k][e] * f * scale : 0.0f;
+            v[k][e] = in && col0 + jj + e < a.n ? f.of(v[k][e]) * scale : 0.0f;
 #pragma unroll
         for (int h = 0; h < 2; h++)
             *reinterpret_cast<f4*>(s_tile + staged<64>(ii, jj + 4 * h)) =
@@ -212,12 +221,12 @@ __global__ __launch_bounds__(kPrepBlock) void normalise_kernel(hc_orthogonalise_
                                                                T* __restrict__ out,
                                                                const double* __restrict__ partial,
                                                                uint32_t parts) {
-    const float f = inverse_norm(partial + (uint64_t)blockIdx.y * kNormParts, parts, p.eps);
+    const Inverse f = inverse_norm(partial + (uint64_t)blockIdx.y * kNormParts, parts, p.eps);
     const T* m = x + (uint64_t)blockIdx.y * p.x_stride;
     T* o = out + (uint64_t)blockIdx.y * p.out_stride;
     for (uint64_t r = blockIdx.x; r < p.m; r += gridDim.x)
         for (uint64_t i = threadIdx.x; i < p.n; i += kPrepBlock)
-            o[r * p.out_ld + i] = (T)((float)m[r * p.x_ld + i] * f * p.scale);
+            o[r * p.out_ld + i] = (T)(f.of((float)m[r * p.x_ld + i]) * p.scale);
 }
 
 // ---- products --------------------------------------------------------------------
@@ -267,7 +276,7 @@ struct Product {
     void* master;
     const _Float16* prev;
     const void* x;
-    const float* inverse;
+    const Inverse* inverse;
     uint64_t m, n, x_ld, x_stride;
     // APPLY, last step: the output instead of the operands
     void* out;
@@ -532,13 +541,14 @@ template <Kind KIND, int STEP, int PLANES, typename T, typename S> struct Result
     size_t base;      // of the matrix
     uint32_t batch;
     bool turn;        // the transpose is stored too
-    float addend_factor;
+    float addend_pre, addend_factor;
     static constexpr bool first = KIND == APPLY && (STEP & FIRST), last = KIND == APPLY && (STEP & LAST);
 
     __device__ __forceinline__ Results(const Product& g_, const Tile& t)
         : g(g_), base((size_t)t.batch * g_.rows * g_.cols), batch(t.batch),
           turn(KIND == APPLY ? !last : t.ti != t.tj),
-          addend_factor(first ? g_.inverse[t.batch] * g_.factor2 : g_.factor2) {}
+          addend_pre(first ? g_.inverse[t.batch].pre : 1.0f),
+          addend_factor(first ? g_.inverse[t.batch].rest * g_.factor2 : g_.factor2) {}
 
     // X between two steps passes the caches by in the tiles of large matrices,
     // which they cannot hold: 2 % of 4096 x 25088 (of twelve 768 x 768, in smaller
@@ -616,6 +626,7 @@ template <Kind KIND, int STEP, int PLANES, typename T, typename S> struct Result
             for (int h = 0; h < 2; h++) {
                 f4* at_stage = reinterpret_cast<f4*>(stage + staged<S::EN>(ii, jj + 4 * h));
                 w[h] = *at_stage * g.factor;
+                if constexpr (first) add[k][h] *= addend_pre;
                 if constexpr (KIND != GRAM) w[h] += add[k][h] * addend_factor;
                 if (turn) *at_stage = w[h];
             }
@@ -865,7 +876,7 @@ __global__ __launch_bounds__(256) void thin_kernel(Thin g) {
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint32_t li = lane & 15, lg = lane >> 4;
     const uint32_t batch = blockIdx.y;
-    float f = 0.0f;
+    Inverse f = {};
     if constexpr (FIRST) {
         f = inverse_norm(g.norm + (uint64_t)batch * kNormParts, g.norm_parts, g.eps);
     } else {
@@ -946,7 +957,7 @@ __global__ __launch_bounds__(256) void thin_kernel(Thin g) {
                 for (int e = 0; e < 4; e++) {
                     const uint32_t row = 16 * u + 4 * lg + e;
                     const uint64_t i = g.tall ? col : row, j = g.tall ? row : col;
-                    mine[u][e] = i < g.m && j < g.n ? (float)x[i * g.x_ld + j] * f : 0.0f;
+                    mine[u][e] = i < g.m && j < g.n ? f.of((float)x[i * g.x_ld + j]) : 0.0f;
                 }
         } else {
 #pragma unroll
@@ -1299,7 +1310,7 @@ OrthoLayout ortho_layout(const hc_orthogonalise_params& p) {
         return L;
     }
     const size_t xs = any ? p.batch * L.rows * L.cols : 0, as = any ? p.batch * L.r * L.r : 0;
-    L.inverse = take(p.batch * 4);
+    L.inverse = take(p.batch * sizeof(Inverse));
     L.master = take(xs * 2 * L.planes);
     L.x = take(xs * 2 * L.planes);
     L.xt[0] = take(xs * 2 * L.planes);
@@ -1465,7 +1476,7 @@ hipError_t orthogonalise_typed(const hc_orthogonalise_params& p, const OrthoStep
                        reinterpret_cast<_Float16*>(ws + L.xt[1])};
     _Float16* A = reinterpret_cast<_Float16*>(ws + L.a);
     _Float16* B = reinterpret_cast<_Float16*>(ws + L.b);
-    float* inverse = reinterpret_cast<float*>(ws + L.inverse);
+    Inverse* inverse = reinterpret_cast<Inverse*>(ws + L.inverse);
     PrepArgs q = {};
     q.m = p.m;
     q.n = p.n;

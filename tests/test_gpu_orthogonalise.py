@@ -218,3 +218,19 @@ def test_empty_batch_and_refusals():
     with pytest.raises(hc.HCError) as e:
         hc.hc_orthogonalise(x, x.clone(), ws[:256])
     assert e.value.status == hc.HC_EWORKSPACE
+
+
+@pytest.mark.parametrize("m,n", [(40, 70), (100, 20000), (300, 200), (520, 1300)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("steps", [0, 1, 5])
+def test_norms_past_what_the_inverse_holds(m, n, dtype, steps):
+    """Finite matrices of entries near 1e38: norms of 5e39 to 1.4e41, whose inverses are below fp32's
+    normal range (2^-126).  No steps: two fp32 products after the inverse's own rounding and the result's,
+    2^-24 each."""
+    torch, hc = _hc()
+    x = (_matrix(torch, m, n, "random", "float32").clamp(-3, 3) * 1e38).to(getattr(torch, dtype))
+    d = x.cuda()
+    out = torch.empty_like(d)
+    hc.hc_orthogonalise(d, out, hc.alloc_orthogonalise_workspace(d), steps=steps)
+    tol = TOL[dtype] if steps else {"float32": 4 * 2.0**-24, "bfloat16": 2.0**-9 + 4 * 2.0**-24}[dtype]
+    assert _rel(out, _formula(torch, x, steps)) <= tol

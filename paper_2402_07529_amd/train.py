@@ -145,6 +145,7 @@ def alloc_embed_workspace(vocab: int, dim: int, count: int, device="cuda"):
 
 
 def _grad_args(dout, ids, vocab, dst, name, scale, fixed, padding):
+    """Arguments of the gradient calls; vocab None: as many rows as dst has."""
     x, rows, dim, x_ld = _rows(dout, "dout")
     d, dst_rows, cols, dst_ld = _rows(dst, name)
     i, count, bits = _ids(ids)
@@ -152,6 +153,8 @@ def _grad_args(dout, ids, vocab, dst, name, scale, fixed, padding):
         raise ValueError(f"dout has {rows} rows, ids {count} elements")
     if cols != dim:
         raise ValueError(f"{name} has {cols} columns, dout {dim}")
+    if vocab is None:
+        vocab = dst_rows
     p = hc_embed_params(vocab, count, dim, dst_ld, x_ld, padding, bits, 0, scale, fixed)
     return p, _type(dout, "dout"), x, i, _type(dst, name), d, dst_rows
 
@@ -161,8 +164,7 @@ def hc_embed_grad(dout, ids, dtable, ws, scale: float = 1.0, fixed: float = FIXE
     """dtable[v] = scale * sum of dout[i] over ids[i] == v (or added to dtable).  dout [.., dim]
     float32, bfloat16 or float16; dtable [vocab, dim] one of them, or int32: fixed point with
     `fixed` units per 1.0.  Ids outside the table and `padding` add nothing."""
-    p, xt, x, i, gt, d, _ = _grad_args(dout, ids, dtable.shape[0], dtable, "dtable", scale, fixed,
-                                       padding)
+    p, xt, x, i, gt, d, _ = _grad_args(dout, ids, None, dtable, "dtable", scale, fixed, padding)
     _check(_lib.hc_embed_grad(ctypes.byref(p), xt, x, i, gt, d, 1 if accumulate else 0,
                               _bytes(ws), ws.numel(), _stream(stream)),
            "hc_embed_grad")

@@ -356,3 +356,19 @@ def test_binding_refusals():
     r, v, n = i.clone(), ok.clone(), i[:1].clone()
     with pytest.raises(ValueError):
         hc.hc_embed_grad_rows(ok, i, 10, r[:3], v, n, ws)
+
+
+def test_table_of_more_dimensions():
+    """A contiguous table of three dimensions is its rows: lookup and gradient take the same ones."""
+    torch, hc = _hc()
+    table = torch.randn(3, 5, 8, device="cuda")
+    ids = torch.tensor([14, 0, 7, 14, 15, -1], device="cuda")
+    rows = torch.empty(6, 8, device="cuda")
+    hc.hc_embed(table, ids, rows)
+    assert torch.equal(rows[:4], table.view(15, 8)[ids[:4]]) and not bool(rows[4:].any())
+    want, got = torch.empty(15, 8, device="cuda"), torch.full((3, 5, 8), 7.0, device="cuda")
+    ws = hc.alloc_embed_workspace(15, 8, 6)
+    hc.hc_embed_grad(rows, ids, want, ws)
+    assert torch.equal(want[14], rows[0] + rows[3]) and torch.equal(want[7], rows[2])
+    hc.hc_embed_grad(rows, ids, got, ws)
+    assert torch.equal(got.view(15, 8), want)

@@ -95,7 +95,9 @@ typedef struct {
     uint64_t m, n;        /* 1 .. 65536 each                                      */
     uint64_t batch;       /* 0 .. 65535                                           */
     uint64_t x_ld, x_stride;      /* elements; x_ld >= n                          */
-    uint64_t out_ld, out_stride;  /* the same of the output                       */
+    uint64_t out_ld, out_stride;  /* the same of the output, whose matrices lie one
+                                     after the other, or all their rows i before
+                                     any row i + 1                                */
     uint32_t type;        /* hc_type of x and out: HC_T_F32 or HC_T_BF16          */
     uint32_t steps;       /* Newton-Schulz steps, 0 .. 32                         */
     const float *coeffs;  /* HOST: a, b, c of each step (3 * steps values), or

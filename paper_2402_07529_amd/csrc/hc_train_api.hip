@@ -120,7 +120,9 @@ hc_status check_ortho(const hc_orthogonalise_params* p, OrthoStep* steps) {
     if (p->x_ld > (1ull << 40) || p->out_ld > (1ull << 40) || p->x_stride > (1ull << 46) ||
         p->out_stride > (1ull << 46))
         return fail(HC_EINVAL, "row strides must be at most 2^40 elements, matrix strides 2^46");
-    if (p->batch > 1 && p->out_stride < (p->m - 1) * p->out_ld + p->n)
+    // one matrix after the other, or all matrices' row i before any row i + 1
+    if (p->batch > 1 && p->out_stride < (p->m - 1) * p->out_ld + p->n &&
+        (p->out_stride < p->n || (p->m > 1 && p->out_ld < (p->batch - 1) * p->out_stride + p->n)))
         return fail(HC_EINVAL, "the output's matrices overlap");
     if (p->type != HC_T_F32 && p->type != HC_T_BF16)
         return fail(HC_EINVAL, "type must be HC_T_F32 or HC_T_BF16");

@@ -234,3 +234,17 @@ def test_norms_past_what_the_inverse_holds(m, n, dtype, steps):
     hc.hc_orthogonalise(d, out, hc.alloc_orthogonalise_workspace(d), steps=steps)
     tol = TOL[dtype] if steps else {"float32": 4 * 2.0**-24, "bfloat16": 2.0**-9 + 4 * 2.0**-24}[dtype]
     assert _rel(out, _formula(torch, x, steps)) <= tol
+
+
+@pytest.mark.parametrize("m,n", [(70, 40), (300, 400)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_matrices_interleaved_by_rows(m, n, dtype):
+    """[m, batch, n] tensors, seen as batch matrices: input and output."""
+    torch, hc = _hc()
+    xs = [_matrix(torch, m, n, "lowrank", dtype, seed=b) for b in range(3)]
+    x = torch.stack(xs, 1).cuda().transpose(0, 1)
+    out = torch.full_like(x.transpose(0, 1), 7).transpose(0, 1)
+    assert out.stride() == (n, 3 * n, 1)
+    hc.hc_orthogonalise(x, out, hc.alloc_orthogonalise_workspace(x))
+    for b in range(3):
+        assert _rel(out[b], _formula(torch, xs[b], 5)) <= TOL[dtype], b

@@ -183,3 +183,16 @@ def test_an_empty_batch_needs_no_workspace(m, n):
             "    assert size.value == 0\n")
     got = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=120)
     assert got.returncode == 0, (got.returncode, got.stderr)
+
+
+def test_output_matrices_may_interleave_by_rows():
+    """Row i of all matrices before any row i + 1, as a [m, batch, n] tensor holds them, does not overlap."""
+    import paper_2402_07529_amd as hc
+    size = ctypes.c_size_t()
+    for m, n, batch, ld, stride, ok in ((64, 96, 3, 288, 96, True), (64, 96, 3, 287, 96, False),
+                                        (64, 96, 3, 288, 95, False), (64, 96, 3, 300, 102, True),
+                                        (64, 96, 3, 300, 103, False), (1, 96, 3, 96, 96, True),
+                                        (1, 96, 3, 96, 95, False), (64, 96, 65535, 2**40, 2**24, True)):
+        p = _ortho(hc, m=m, n=n, batch=batch, x_ld=n, out_ld=ld, out_stride=stride)
+        want = hc.HC_OK if ok else hc.HC_EINVAL
+        assert hc.lib().hc_orthogonalise_bytes(ctypes.byref(p), ctypes.byref(size)) == want, (ld, stride)

@@ -1133,6 +1133,13 @@ double plain_cost(const TileCost& c, uint64_t tiles, uint32_t lines, int planes,
     return t;
 }
 
+// Products that are cut into pieces.  Those of 256-tiles in two planes, and of
+// 64-tiles in a square in one, are never the least estimate (not once in 900,000
+// random sides and batches) and not built.
+constexpr bool has_pieces(Kind kind, int planes, int tile) {
+    return kind == APPLY ? false : planes == 2 ? tile < 256 : kind == GRAM || tile > 64;
+}
+
 // With a workgroup on every CU (full = 0) or as many as fit: every tile in as
 // many pieces as there is room for; one more of as many tiles as that leaves room
 // for, the others in the pieces that fill it; or whole rounds of whole tiles, the
@@ -1174,8 +1181,8 @@ void try_pieces(int k, int full, uint64_t n, uint32_t lines, int planes, int cus
     }
 }
 
-double best_way(uint64_t tiles256, uint64_t tiles128, uint64_t tiles64, uint32_t lines, int planes,
-                int cus, Way* way) {
+double best_way(Kind kind, uint64_t tiles256, uint64_t tiles128, uint64_t tiles64, uint32_t lines,
+                int planes, int cus, Way* way) {
     const uint64_t tiles[3] = {tiles256, tiles128, tiles64};
     double best = 1e30;
     for (int k = 0; k < 3; k++) {
@@ -1187,6 +1194,7 @@ double best_way(uint64_t tiles256, uint64_t tiles128, uint64_t tiles64, uint32_t
         }
     }
     for (int k = 0; k < 3; k++) {
+        if (!has_pieces(kind, planes, kTileCosts[k].tile)) continue;
         for (int full = 0; full < 2; full++) try_pieces(k, full, tiles[k], lines, planes, cus, &best, way);
     }
     return best;
@@ -1255,8 +1263,10 @@ void plan_products(const hc_orthogonalise_params& p, int cus, OrthoLayout* L) {
         }
         Way way[3] = {};
         const double t =
-            best_way(half[0], half[1], half[2], (uint32_t)(k * L->planes / kLine), L->planes, cus, &way[GRAM]) +
-            best_way(half[0], half[1], half[2], (uint32_t)(r * L->planes / kLine), L->planes, cus, &way[SQUARE]) +
+            best_way(GRAM, half[0], half[1], half[2], (uint32_t)(k * L->planes / kLine), L->planes, cus,
+                     &way[GRAM]) +
+            best_way(SQUARE, half[0], half[1], half[2], (uint32_t)(r * L->planes / kLine), L->planes, cus,
+                     &way[SQUARE]) +
             best_apply(p.batch, r, k, pad, (uint32_t)(r * L->planes / kLine), L->planes, cus, &way[APPLY]) +
             // what an apply reads and writes, 10 or 16 bytes a value with its
             // padding, is hardly overlapped with its products
@@ -1349,7 +1359,7 @@ hipError_t product_shape(Product g, uint32_t batch, const Cuts& cuts, uint32_t k
     }
     g.batch = batch;
     g.cuts = cuts;
-    if constexpr (KIND != APPLY) {
+    if constexpr (has_pieces(KIND, PLANES, S::BM)) {
         if (cuts.tiles) {
             hipError_t e = hipSuccess;
             if (cuts.whole())

@@ -113,6 +113,7 @@ PLANS = [  # what the products of each run as, by their sizes
     ("float32", 35, 223, 950, 0, 0),        # apply: 256-tiles
     ("float32", 24, 384, 900, 13, 1),       # apply: 128-tiles, the rest in 64
     ("float32", 12, 768, 768, 0, 0),        # all in 128-tiles
+    ("float32", 157, 403, 510, 0, 0),       # Gram, square: 256-tiles
     ("float32", 5, 900, 4600, 0, 0),        # Gram: 128-tiles in two groups
     ("float32", 16, 900, 900, 0, 0),        # Gram, square: whole rounds of 128-tiles and pieces
     ("float32", 2, 1500, 1500, 0, 0),       # Gram, square: 128-tiles in pieces

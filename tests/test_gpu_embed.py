@@ -372,3 +372,57 @@ def test_table_of_more_dimensions():
     assert torch.equal(want[14], rows[0] + rows[3]) and torch.equal(want[7], rows[2])
     hc.hc_embed_grad(rows, ids, got, ws)
     assert torch.equal(got.view(15, 8), want)
+
+
+@pytest.mark.parametrize("vocab,dim,count,dtype", [(3000, 64, 262144 + 5, "float32"), (500, 770, 32768 + 3, "bfloat16"),
+                                                   (500, 770, 32768 + 3, "float16"), (700, 768, 43691 + 9, "bfloat16"),
+                                                   (50000, 3, 2**22 + 77, "float16")])
+@pytest.mark.parametrize("gap,offset", [(0, 0), (3, 1)])
+def test_large_lookup(vocab, dim, count, dtype, gap, offset):
+    """Lookups that give every group of lanes four rows (or parts of rows), with a remainder."""
+    torch, hc = _hc()
+    gen = torch.Generator(device="cuda").manual_seed(dim + count)
+    dt, scale = getattr(torch, dtype), 3.7
+    ids = torch.randint(-vocab // 8, vocab + vocab // 8, (count,), device="cuda", generator=gen)
+    ids[-1] = vocab - 1
+    _, table = _strided(torch, vocab, dim, gap, offset, dt)
+    table.copy_(torch.randn(vocab, dim, device="cuda", generator=gen))
+    flat, out = _strided(torch, count, dim, gap, offset, dt)
+    hc.hc_embed(table, ids.int(), out, scale=scale)
+    valid = (ids >= 0) & (ids < vocab)
+    want = (table[torch.where(valid, ids, 0)].float() * scale).to(dt)
+    want[~valid] = 0
+    assert torch.equal(out, want)
+    out.fill_(7)
+    assert bool((flat == 7).all()), "wrote outside its rows"
+
+
+@pytest.mark.parametrize("vocab,dim,count", [(900, 40, 1500), (900, 40, 20000), (300, 700, 5000), (5000, 3, 70001)])
+@pytest.mark.parametrize("hot", [0, 450, 899])
+@pytest.mark.parametrize("x_type,g_type", [("float32", "float32"), ("float32", "int32"), ("bfloat16", "bfloat16")])
+def test_rows_past_the_cap_are_not_written(vocab, dim, count, hot, x_type, g_type):
+    """Fewer places than touched rows, with a frequent id (its run shared by many chunks) among the
+    first, the middle and the last: the first `cap` rows are written, the count is of all."""
+    torch, hc = _hc()
+    hot = hot * (vocab - 1) // 899
+    gen = torch.Generator().manual_seed(count + hot)
+    ids = torch.randint(-3, vocab, (count,), generator=gen)
+    ids[torch.rand(count, generator=gen) < 0.6] = hot
+    distinct = torch.unique(ids[ids >= 0])
+    n = distinct.numel()
+    gt = getattr(torch, g_type)
+    x, d = torch.randn(count, dim, generator=gen).to(getattr(torch, x_type)).cuda(), ids.cuda()
+    ws = hc.alloc_embed_workspace(vocab, dim, count)
+    dense = torch.empty((vocab, dim), device="cuda", dtype=gt)
+    hc.hc_embed_grad(x, d, dense, ws)
+    at = int((distinct == hot).nonzero())
+    for cap in sorted({0, 1, at, at + 1, n - 1, n, n + 5}):
+        rows = torch.full((n + 9,), -5, device="cuda", dtype=torch.int32)
+        values = torch.full((n + 9, dim), 3, device="cuda", dtype=gt)
+        touched = torch.full((1,), -1, device="cuda", dtype=torch.int32)
+        hc.hc_embed_grad_rows(x, d, vocab, rows[:cap], values[:cap], touched, ws)
+        k = min(cap, n)
+        assert int(touched) == n
+        assert torch.equal(rows[:k].cpu().long(), distinct[:k])
+        assert torch.equal(values[:k], dense[distinct[:k].cuda()])
+        assert bool((rows[k:] == -5).all()) and bool((values[k:] == 3).all()), cap

@@ -196,3 +196,52 @@ def test_output_matrices_may_interleave_by_rows():
         p = _ortho(hc, m=m, n=n, batch=batch, x_ld=n, out_ld=ld, out_stride=stride)
         want = hc.HC_OK if ok else hc.HC_EINVAL
         assert hc.lib().hc_orthogonalise_bytes(ctypes.byref(p), ctypes.byref(size)) == want, (ld, stride)
+
+
+def _gradient_needs(dim, count):
+    """Bytes that a gradient of `count` ids touches, by how it splits them: sorted pairs, the sort's
+    own list (and, past 32,768 ids, 512 counts a workgroup), and for each chunk of pairs a head count, a
+    shared run and two partial sums of 64-bit elements."""
+    def group(vectors):
+        if vectors > 64 and 16 < vectors % 64 <= 32:
+            return 32
+        return 1 << min(6, (vectors - 1).bit_length())
+
+    def up(v, a):
+        return -(-v // a) * a
+
+    chunk, row = 64, -(-dim // 8)
+    while chunk > 8 and chunk * 256 // group(row) > 2048:
+        chunk //= 2
+    lanes = up(-(-dim // 4), group(-(-dim // 4)))
+    while chunk > 4 and count // chunk * lanes // 64 < 4096:
+        chunk //= 2
+    chunks = -(-count // chunk)
+    need = up(count * 8, 256) + up(512 * 4, 256) + 256
+    if 6144 < count <= 32768:
+        need += 2 * up(count * 4, 256)
+    elif count > 32768:
+        threads = 512 if count >= 2**19 else 256
+        need += up(count * 8, 256) + up(-(-count // (threads * 8)) * 512 * 4, 256)
+    return need + up(chunks * 4, 256) + up(chunks * 8, 256) + up(chunks * 2 * up(dim, 8) * 8, 256)
+
+
+@pytest.mark.parametrize("dim", [1, 3, 17, 64, 65, 513, 640, 768, 1500, 2100, 5000])
+def test_workspace_holds_what_a_gradient_touches(dim):
+    """What is reported for a number of ids is enough for it and for every smaller number, around
+    every place where chunks, sorting workgroups or the sort itself change."""
+    import paper_2402_07529_amd as hc
+    edges = {1, 2, 3, 5, 6144, 8192, 32768, 2**19, 2**20}
+    edges |= {2**k for k in range(3, 22)} | {3 * 2**k for k in range(2, 20)}
+    lanes = -(-dim // 4)
+    for chunk in (4, 8, 16, 32, 64):        # a chunk is halved until it leaves 4096 waves
+        for per_row in (lanes, lanes + 31, lanes + 63):
+            edges.add(chunk * 64 * 4096 // per_row)
+    counts = sorted({e + d for e in edges for d in (-65, -1, 0, 1, 64) if 0 < e + d <= 2**22})
+    most = 0
+    for count in counts:
+        most = max(most, _gradient_needs(dim, count))
+        assert hc.hc_embed_grad_bytes(70000, dim, count) >= most, count
+    for edge in (6144, 32768):
+        sizes = [hc.hc_embed_grad_bytes(70000, dim, edge + k) for k in range(-3, 4)]
+        assert sizes == sorted(sizes)

@@ -22,7 +22,7 @@ and the training-side operators around them (include/hc_train.h, see train.py):
     hc_embed, hc_embed_grad, hc_embed_grad_rows   embedding lookup and its gradient
     hc_orthogonalise      Newton-Schulz orthogonalisation of a weight's update
 
-The library must be built (``python -m paper_2402_07529_amd.build``); there is
+The library must be built (``python paper_2402_07529_amd/build.py``); there is
 no fallback: importing this package without libhc.so raises.
 """
 from __future__ import annotations
@@ -91,7 +91,7 @@ class hc_params(ctypes.Structure):
 
 
 if not os.path.exists(LIB_PATH):
-    raise ImportError(f"libhc.so not built at {LIB_PATH}; run python -m paper_2402_07529_amd.build")
+    raise ImportError(f"libhc.so not built at {LIB_PATH}; run python paper_2402_07529_amd/build.py")
 
 _lib = ctypes.CDLL(LIB_PATH)
 _P = ctypes.c_void_p

@@ -144,8 +144,11 @@ __global__ __launch_bounds__(kBlock) void embed_kernel(const T* __restrict__ tab
 constexpr uint64_t kMaxGroups = 1ull << 22;
 
 // Lanes of a group: enough 16-byte vectors for a row, at most a wave; half a wave
-// where that leaves fewer lanes idle in the last of a row's groups (30,522 x 768
-// bf16: gradient of 32,768 ids 59 -> 49 us, lookup of 262,144 95 -> 85).
+// where the last of a row's groups would hold 17 to 32 vectors (30,522 x 768 bf16:
+// gradient of 32,768 ids 59 -> 49 us, lookup of 262,144 95 -> 85).  With 1 to 16 of
+// them half waves are faster for one thing and slower for another, and a whole
+// wave stays: 640 bf16 columns 53 us (46 in half waves) and 84 (76), 320 fp32
+// columns 42 (46) and 80 (77), 576 fp32 columns 60 (57) and 140 (144).
 uint32_t group_log2(uint64_t vectors) {
     if (vectors > 64 && vectors % 64 > 16 && vectors % 64 <= 32) return 5;
     uint32_t g = 0;
@@ -428,9 +431,10 @@ __global__ __launch_bounds__(1024) void merge_kernel(MergeSort a) {
     if (lane == 0 && i < a.count) a.out[rank] = Pair{key, at};
 }
 
-// More ids (2^20 of 25 bits: three passes of 7 + 5 + 12 us): per pass every
+// More ids (2^20 of 25 bits: three passes of 8 + 5 + 12 us): per pass every
 // workgroup counts its tile's digits, the counts are scanned per digit over the
-// workgroups, and every workgroup moves its tile's pairs to their places.  Each launch's workgroups past its own write zeros.
+// workgroups, and every workgroup moves its tile's pairs to their places.  Each
+// launch's workgroups past its own write zeros.
 template <uint32_t THREADS, typename SRC>
 __global__ __launch_bounds__(THREADS) void digit_count_kernel(SRC src, uint32_t count,
                                                               uint32_t groups, uint32_t shift,
@@ -685,7 +689,7 @@ struct SumArgs {
 };
 
 // Sums of the sorted pairs.  Bound by the random rows that they read: 2^20 rows
-// of 64 fp32 in 78 us, 268 MB read and 57 MB written.
+// of 64 fp32 in 84 us, 279 MB read and 61 MB written.
 //
 // The pairs that a workgroup's chunks look at lie in LDS: positions from p0.  (A
 // pair read from memory would wait for the stores of the sums before it, as all
@@ -896,7 +900,7 @@ __global__ __launch_bounds__(kBlock) void segment_sum_kernel(SumArgs a, const TI
 }
 
 // Joins the partial sums of the shared runs (a chain of a few loads: 4 us with
-// none, 12 to 16 with the 1 % most frequent of Zipf(1.1) ids): a workgroup takes one
+// none, 9 to 16 with the 1 % most frequent of Zipf(1.1) ids): a workgroup takes one
 // run's columns, its groups of lanes a contiguous share of the run's chunks
 // each, in order, and the groups' sums are added in order.
 constexpr int kJoinBlock = 512;

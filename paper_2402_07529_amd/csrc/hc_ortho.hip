@@ -9,19 +9,22 @@
 // matters stays normal), sums are fp32, and X itself is kept with 22 bits or
 // more beside its operands: a X is added in fp32, so that rounding an operand
 // only reaches X through B, which is small where X's singular values are.  For
-// bf16 matrices one fp16 plane, X being its operand plus an fp16 rest: on random
-// and on low-rank matrices with sides of 256 or more the result is 3e-4 to
-// 2.0e-3 from the exact one, about the 1.7e-3 of rounding it to bf16 (bf16
-// operands: 2e-3 to 1.4e-2; fp16 operands alone: up to 2e-2).  For fp32 matrices
-// an operand is the sum of two fp16 planes and a product three matrix products
-// (high x high, high x low, low x high), X is fp32: 1e-6 to 3e-6 from the exact
-// result, 0.7 to 1.4 times what fp32 products of the matrix library leave.
+// bf16 matrices one fp16 plane, X being its operand plus an fp16 rest: five steps
+// leave the result 1.8e-3 (low rank over noise) to 2.7e-3 (400 x 5000, random)
+// from the exact one, of which rounding it to bf16 is 1.7e-3, what fp32 products
+// leave; nine steps up to 4.9e-3, twelve 6.9e-3 (library products in bf16, five
+// steps: 1.7e-2 and more; fp16 operands without the rest: up to 2e-2).  That
+// form holds X to 2^-38, so where all of x is below about 1e-10 eps the result
+// loses bits, and below 1e-12 eps it is zero.  For fp32 matrices an operand is
+// the sum of two fp16 planes and a product three matrix products (high x high,
+// high x low, low x high), X is fp32: five steps 1e-6 to 9e-6 from the exact
+// result, 0.35 to 1.15 times what fp32 products of the matrix library leave.
 //
 // What bounds it.  Large matrices: the matrix cores, of which the main loop of a
 // 256-tile gets 1.31 PFLOP/s (4096 x 25088, the apply without its results; a
 // library product of 8192^3 1.37), and then X's way to memory and back in the
 // apply (10 or 16 bytes a value), hardly overlapped as all CUs end their tiles
-// together: 791 us where the products alone take 629.  Half of the Gram product
+// together: 780 us where the products alone take 629.  Half of the Gram product
 // and of the square are computed and mirrored.  Small ones: the chain of
 // launches, three a step (thin ones one or two) of 6 to 8 us each.
 #include "hc_device.h"
@@ -69,7 +72,7 @@ template <typename T> struct Wide16 {
 };
 
 // Sum of squares in 64 bits, a workgroup a part: 16-byte loads, four in flight a
-// lane.  rows == 1: the matrix lies in one piece.  4096 x 25088 bf16: 45 us, 4.5
+// lane.  rows == 1: the matrix lies in one piece.  4096 x 25088 bf16: 52 us, 4.0
 // TB/s.
 template <typename T>
 __global__ __launch_bounds__(kNormBlock) void norm_kernel(const T* __restrict__ x, uint64_t rows,

@@ -12,6 +12,13 @@
  *   hc_orthogonalise         Newton-Schulz orthogonalisation of matrices, as
  *                            the Muon optimiser does with an update
  *   hc_orthogonalise_bytes   its workspace
+ *   hc_dropout               dropout, or its gradient, with a residual; the mask
+ *                            is made from a seed and a place, and not stored
+ *   hc_linear                matrix product with bias, activation, dropout and
+ *                            residual
+ *   hc_linear_bytes          its workspace
+ *   hc_linear_grad           its gradient: of the input, the weight and the bias
+ *   hc_linear_grad_bytes     its workspace
  *
  * The conventions are those of hc.h: device pointers unless marked "host",
  * memory owned by the caller, calls asynchronous on `stream`, errors returned
@@ -125,6 +132,89 @@ typedef struct {
 hc_status hc_orthogonalise_bytes(const hc_orthogonalise_params *p, size_t *bytes);
 hc_status hc_orthogonalise(const hc_orthogonalise_params *p, const void *x, void *out, void *ws,
                            size_t ws_bytes, hipStream_t stream);
+
+/* Dropout's masks.  Element (r, c) of a call is dropped where 16 bits, uniform
+ * and independent, are below T = round(65536 p); what is kept is scaled by
+ * 65536 / (65536 - T).  So p is rounded to a multiple of 2^-16, and below 2^-17
+ * nothing is dropped.  The bits depend on seed, draw, r and c alone, not on the
+ * shape, the type or the operator: a backward pass gives the same seed and draw
+ * and gets the forward pass's mask.  They are those of Philox4x32-10 (Salmon et
+ * al. 2011) with key = seed (low word first) and counter = (c div 8, r, draw mod
+ * 2^32, draw div 2^32): element c takes half c mod 2 (0: the low one) of word
+ * (c mod 8) div 2.  `counter` (DEVICE, or NULL) is a number that is added to
+ * draw when the kernels run: a captured graph whose counter goes on between the
+ * replays draws a new mask in each. */
+typedef struct {
+    uint64_t rows;         /* 0 .. 2^31 - 1                                       */
+    uint64_t cols;         /* 1 .. 2^31 - 1; at most 2^38 elements in all         */
+    uint64_t x_ld, residual_ld, out_ld; /* elements between rows, >= cols          */
+    uint64_t seed, draw;   /* a program's seed, and which of its draws this is    */
+    float p;               /* probability of a drop, 0 .. 1                       */
+    uint32_t reserved;     /* must be 0                                           */
+} hc_dropout_params;
+
+/* out = residual + mask * x (residual NULL: mask * x), in 32 bits and rounded
+ * once to `type` (HC_T_F32, HC_T_BF16, HC_T_F16: all three buffers').  A dropped
+ * element adds nothing, whatever x holds there.  On an output gradient this is
+ * the gradient: the residual's is the output's itself.  out may be x or residual
+ * (at the same address and stride). */
+hc_status hc_dropout(const hc_dropout_params *p, hc_type type, const void *x, const void *residual,
+                     void *out, const uint64_t *counter, hipStream_t stream);
+
+/* Activations: max(z, 0), z Phi(z), z s(z), tanh z, s(z) with s the logistic
+ * function and Phi the normal distribution's. */
+typedef enum {
+    HC_ACT_NONE = 0, HC_ACT_RELU = 1, HC_ACT_GELU = 2, HC_ACT_SILU = 3, HC_ACT_TANH = 4,
+    HC_ACT_SIGMOID = 5
+} hc_act;
+
+/* A layer of n outputs and k inputs on m rows: x [m, k], w [n, k], all else
+ * [m, n], rows contiguous.  m n, m k and n k are at most 2^38. */
+typedef struct {
+    uint64_t m;            /* 0 .. 2^31 - 1                                       */
+    uint64_t n, k;         /* 1 .. 2^24                                           */
+    uint64_t x_ld, w_ld;   /* elements between rows, here and below: at least the
+                              columns, at most 2^31                               */
+    uint64_t y_ld;         /* of y; of dy in the gradient                         */
+    uint64_t z_ld, residual_ld;
+    uint64_t dx_ld, dw_ld; /* gradient                                            */
+    uint64_t seed, draw;   /* as in hc_dropout; the place is y's                  */
+    float p;
+    uint32_t act;          /* hc_act                                              */
+    float fixed;           /* gradient, int32: units per 1.0 of the fixed point,
+                              finite and > 0 (not read otherwise)                 */
+    uint32_t reserved;     /* must be 0                                           */
+} hc_linear_params;
+
+/* z = x w^T + bias (NULL: none), y = residual (NULL: none) + mask * act(z), with
+ * products and sums in fp32 (z is not rounded before act).  All of `type`
+ * (HC_T_F32, HC_T_BF16, HC_T_F16).  z (NULL: not wanted) is what the gradient of
+ * an activation asks for.  Sums are taken in an order that depends on the shape
+ * and strides alone: two calls agree bit for bit.  Infinities in x or w may give
+ * NaN where fp32 matrices are wide.  y may be residual (same address and stride).
+ * The workspace does for fewer rows of the same n, k and strides too. */
+hc_status hc_linear_bytes(const hc_linear_params *p, hc_type type, size_t *bytes);
+hc_status hc_linear(const hc_linear_params *p, hc_type type, const void *x, const void *w,
+                    const void *bias, const void *residual, void *y, void *z,
+                    const uint64_t *counter, void *ws, size_t ws_bytes, hipStream_t stream);
+
+/* dz = act'(z) * mask * dy, then dx = dz w, dw = dz^T x and db = the sum of dz's
+ * rows; each may be NULL (not wanted), and x, w, z where nothing wanted reads
+ * them (w: dx; x: dw; z: an activation).  The residual's gradient is dy itself.
+ * dy, x, w, z and dx: `type`.  z holds what hc_linear wrote there (for HC_ACT_RELU
+ * y itself does where there is neither dropout nor residual).
+ *   dw and db: g_type, fp32 sums rounded once, or HC_T_I32: a sum times `fixed`,
+ * rounded to the nearest whole number, ties to even, saturating at +-(2^31 - 1)
+ * (NaN: 0).  accumulate != 0 adds them to what dw and db hold (int32 saturating).
+ *   16-bit types: the products take dz rounded to `type`, and where g_type is
+ * HC_T_F32 or HC_T_I32 dw takes the rest too (twice 8 or 11 bits).  Without
+ * activation and dropout dz is dy.  db takes dz unrounded.
+ *   m = 0 gives zeros.  Order and infinities as in hc_linear. */
+hc_status hc_linear_grad_bytes(const hc_linear_params *p, hc_type type, size_t *bytes);
+hc_status hc_linear_grad(const hc_linear_params *p, hc_type type, const void *dy, const void *x,
+                         const void *w, const void *z, void *dx, hc_type g_type, void *dw,
+                         void *db, int accumulate, const uint64_t *counter, void *ws,
+                         size_t ws_bytes, hipStream_t stream);
 
 #ifdef __cplusplus
 }

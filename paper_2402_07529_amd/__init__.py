@@ -21,6 +21,9 @@ and the training-side operators around them (include/hc_train.h, see train.py):
 
     hc_embed, hc_embed_grad, hc_embed_grad_rows   embedding lookup and its gradient
     hc_orthogonalise      Newton-Schulz orthogonalisation of a weight's update
+    hc_dropout            dropout or its gradient, with a residual
+    hc_linear, hc_linear_grad   matrix product with bias, activation, dropout and
+                          residual, and its gradient
 
 The library must be built (``python paper_2402_07529_amd/build.py``); there is
 no fallback: importing this package without libhc.so raises.
@@ -378,7 +381,9 @@ def alloc_workspace(p: hc_params, max_support: int = 0, device="cuda"):
 
 
 from .train import (  # noqa: E402  (it takes this module's helpers)
-    FIXED_POINT, HC_T_BF16, HC_T_F16, HC_T_F32, HC_T_I32, MUON, TRAIN_EXPORTS,
-    alloc_embed_workspace, alloc_orthogonalise_workspace, hc_embed, hc_embed_grad,
-    hc_embed_grad_bytes, hc_embed_grad_rows, hc_embed_params, hc_orthogonalise,
+    ACTIVATIONS, FIXED_POINT, HC_T_BF16, HC_T_F16, HC_T_F32, HC_T_I32, MUON, TRAIN_EXPORTS,
+    alloc_embed_workspace, alloc_linear_grad_workspace, alloc_linear_workspace,
+    alloc_orthogonalise_workspace, hc_dropout, hc_dropout_params, hc_embed, hc_embed_grad,
+    hc_embed_grad_bytes, hc_embed_grad_rows, hc_embed_params, hc_linear, hc_linear_bytes,
+    hc_linear_grad, hc_linear_grad_bytes, hc_linear_params, hc_orthogonalise,
     hc_orthogonalise_bytes, hc_orthogonalise_params)

@@ -133,6 +133,49 @@ hc_status check_ortho(const hc_orthogonalise_params* p, OrthoStep* steps) {
     return ortho_steps(p, steps);
 }
 
+// ---- layers ----------------------------------------------------------------------
+
+constexpr uint64_t kMostElements = 1ull << 38, kMostStride = 1ull << 31;
+
+hc_status check_drop(float p) {
+    return p >= 0.0f && p <= 1.0f ? HC_OK : fail(HC_EINVAL, "p must be in [0, 1]");
+}
+
+Dropout dropout_of(float p, uint64_t seed, uint64_t draw, const uint64_t* counter) {
+    Dropout d = {seed, draw, counter, (uint32_t)floor((double)p * 65536.0 + 0.5), 0.0f};
+    d.scale = d.limit < 65536 ? (float)(65536.0 / (65536.0 - d.limit)) : 0.0f;
+    return d;
+}
+
+hc_status check_dropout(const hc_dropout_params* p) {
+    if (p == nullptr) return fail(HC_EINVAL, "params is NULL");
+    if (p->rows > 0x7fffffffull) return fail(HC_EINVAL, "rows must be at most 2^31 - 1");
+    if (p->cols < 1 || p->cols > 0x7fffffffull) return fail(HC_EINVAL, "cols must be in [1, 2^31 - 1]");
+    if (p->rows * p->cols > kMostElements) return fail(HC_EINVAL, "at most 2^38 elements");
+    if (p->reserved != 0) return fail(HC_EINVAL, "reserved must be 0");
+    return check_drop(p->p);
+}
+
+// A row stride of an operand of `cols` columns that is there.
+bool bad_stride(uint64_t ld, uint64_t cols) { return ld < cols || ld > kMostStride; }
+
+hc_status check_linear(const hc_linear_params* p, uint32_t type) {
+    if (p == nullptr) return fail(HC_EINVAL, "params is NULL");
+    if (!float_type(type)) return fail(HC_EINVAL, "unknown type");
+    if (p->m > 0x7fffffffull) return fail(HC_EINVAL, "m must be at most 2^31 - 1");
+    if (p->n < 1 || p->k < 1 || p->n > (1ull << 24) || p->k > (1ull << 24))
+        return fail(HC_EINVAL, "n and k must be in [1, 2^24]");
+    if (p->m * p->n > kMostElements || p->m * p->k > kMostElements || p->n * p->k > kMostElements)
+        return fail(HC_EINVAL, "matrices have at most 2^38 elements");
+    if (bad_stride(p->x_ld, p->k) || bad_stride(p->w_ld, p->k) || bad_stride(p->y_ld, p->n))
+        return fail(HC_EINVAL, "row strides must be at least the columns and at most 2^31");
+    if (p->act > HC_ACT_SIGMOID) return fail(HC_EINVAL, "unknown act");
+    if (p->reserved != 0) return fail(HC_EINVAL, "reserved must be 0");
+    return check_drop(p->p);
+}
+
+bool misaligned(const void* q, uint32_t type) { return q && !aligned(q, type_bytes(type)); }
+
 }  // namespace
 
 }  // namespace hc
@@ -226,6 +269,100 @@ hc_status hc_orthogonalise(const hc_orthogonalise_params* p, const void* x, void
         return fail(HC_EWORKSPACE, "workspace smaller than hc_orthogonalise_bytes reports");
     const hipError_t e = launch_orthogonalise(*p, steps, x, out, ws, stream);
     return e == hipSuccess ? HC_OK : fail_hip(e, "hc_orthogonalise");
+}
+
+hc_status hc_dropout(const hc_dropout_params* p, hc_type type, const void* x, const void* residual,
+                     void* out, const uint64_t* counter, hipStream_t stream) {
+    clear_error();
+    const hc_status s = check_dropout(p);
+    if (s != HC_OK) return s;
+    if (!float_type(type)) return fail(HC_EINVAL, "unknown type");
+    if (bad_stride(p->x_ld, p->cols) || bad_stride(p->out_ld, p->cols) ||
+        (residual && bad_stride(p->residual_ld, p->cols)))
+        return fail(HC_EINVAL, "row strides must be at least cols and at most 2^31");
+    if (p->rows == 0) return HC_OK;
+    if (!x || !out) return fail(HC_EINVAL, "buffers must be non-NULL");
+    if (misaligned(x, type) || misaligned(residual, type) || misaligned(out, type) ||
+        !aligned(counter, 8))
+        return fail(HC_EINVAL, "buffers must be aligned to their elements");
+    if ((out == x && p->out_ld != p->x_ld) || (out == residual && p->out_ld != p->residual_ld))
+        return fail(HC_EINVAL, "in place the strides must be the same");
+    const hipError_t e =
+        launch_dropout(*p, dropout_of(p->p, p->seed, p->draw, counter), type, x, residual, out, stream);
+    return e == hipSuccess ? HC_OK : fail_hip(e, "hc_dropout");
+}
+
+hc_status hc_linear_bytes(const hc_linear_params* p, hc_type type, size_t* bytes) {
+    clear_error();
+    const hc_status s = check_linear(p, type);
+    if (s != HC_OK) return s;
+    if (!bytes) return fail(HC_EINVAL, "bytes is NULL");
+    *bytes = linear_bytes(*p, type);
+    return HC_OK;
+}
+
+hc_status hc_linear(const hc_linear_params* p, hc_type type, const void* x, const void* w,
+                    const void* bias, const void* residual, void* y, void* z,
+                    const uint64_t* counter, void* ws, size_t ws_bytes, hipStream_t stream) {
+    clear_error();
+    const hc_status s = check_linear(p, type);
+    if (s != HC_OK) return s;
+    if ((z && bad_stride(p->z_ld, p->n)) || (residual && bad_stride(p->residual_ld, p->n)))
+        return fail(HC_EINVAL, "row strides must be at least the columns and at most 2^31");
+    if (p->m == 0) return HC_OK;
+    if (!x || !w || !y || !ws) return fail(HC_EINVAL, "buffers must be non-NULL");
+    if (misaligned(x, type) || misaligned(w, type) || misaligned(bias, type) ||
+        misaligned(residual, type) || misaligned(y, type) || misaligned(z, type) || !aligned(counter, 8))
+        return fail(HC_EINVAL, "buffers must be aligned to their elements");
+    if (y == residual && p->y_ld != p->residual_ld)
+        return fail(HC_EINVAL, "in place the strides must be the same");
+    if (y == x || y == w || z == y || (z && (z == x || z == w || z == residual)))
+        return fail(HC_EINVAL, "outputs overlap inputs or each other");
+    if (!aligned(ws, 256)) return fail(HC_EINVAL, "ws must be 256-byte aligned");
+    if (ws_bytes < linear_bytes(*p, type))
+        return fail(HC_EWORKSPACE, "workspace smaller than hc_linear_bytes reports");
+    const hipError_t e = launch_linear(*p, dropout_of(p->p, p->seed, p->draw, counter), type, x, w,
+                                       bias, residual, y, z, ws, stream);
+    return e == hipSuccess ? HC_OK : fail_hip(e, "hc_linear");
+}
+
+hc_status hc_linear_grad_bytes(const hc_linear_params* p, hc_type type, size_t* bytes) {
+    clear_error();
+    const hc_status s = check_linear(p, type);
+    if (s != HC_OK) return s;
+    if (!bytes) return fail(HC_EINVAL, "bytes is NULL");
+    *bytes = linear_grad_bytes(*p, type);
+    return HC_OK;
+}
+
+hc_status hc_linear_grad(const hc_linear_params* p, hc_type type, const void* dy, const void* x,
+                         const void* w, const void* z, void* dx, hc_type g_type, void* dw,
+                         void* db, int accumulate, const uint64_t* counter, void* ws,
+                         size_t ws_bytes, hipStream_t stream) {
+    clear_error();
+    const hc_status s = check_linear(p, type);
+    if (s != HC_OK) return s;
+    if ((p->act != HC_ACT_NONE && bad_stride(p->z_ld, p->n)) || (dx && bad_stride(p->dx_ld, p->k)) ||
+        (dw && bad_stride(p->dw_ld, p->k)))
+        return fail(HC_EINVAL, "row strides must be at least the columns and at most 2^31");
+    if (!float_type(g_type) && g_type != HC_T_I32) return fail(HC_EINVAL, "unknown g_type");
+    if (g_type == HC_T_I32 && (dw || db) && (!isfinite(p->fixed) || !(p->fixed > 0.0f)))
+        return fail(HC_EINVAL, "fixed must be finite and > 0");
+    if (!ws) return fail(HC_EINVAL, "buffers must be non-NULL");
+    if (p->m != 0 && (!dy || (dx && !w) || (dw && !x) || (p->act != HC_ACT_NONE && !z)))
+        return fail(HC_EINVAL, "buffers must be non-NULL");
+    if (misaligned(dy, type) || misaligned(x, type) || misaligned(w, type) || misaligned(z, type) ||
+        misaligned(dx, type) || misaligned(dw, g_type) || misaligned(db, g_type) || !aligned(counter, 8))
+        return fail(HC_EINVAL, "buffers must be aligned to their elements");
+    for (const void* out : {(const void*)dx, (const void*)dw, (const void*)db})
+        if (out && (out == dy || out == x || out == w || (out == z && p->act != HC_ACT_NONE)))
+            return fail(HC_EINVAL, "outputs overlap inputs");
+    if (!aligned(ws, 256)) return fail(HC_EINVAL, "ws must be 256-byte aligned");
+    if (ws_bytes < linear_grad_bytes(*p, type))
+        return fail(HC_EWORKSPACE, "workspace smaller than hc_linear_grad_bytes reports");
+    LinearGrad g = {dy, x, w, z, dx, dw, db, g_type, accumulate != 0};
+    const hipError_t e = launch_linear_grad(*p, dropout_of(p->p, p->seed, p->draw, counter), type, g, ws, stream);
+    return e == hipSuccess ? HC_OK : fail_hip(e, "hc_linear_grad");
 }
 
 }  // extern "C"

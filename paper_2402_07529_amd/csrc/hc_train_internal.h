@@ -47,4 +47,33 @@ size_t orthogonalise_bytes(const hc_orthogonalise_params& p);
 hipError_t launch_orthogonalise(const hc_orthogonalise_params& p, const OrthoStep* steps,
                                 const void* x, void* out, void* ws, hipStream_t s);
 
+// ---- layers ----------------------------------------------------------------------
+
+// Dropout as the kernels take it: an element is dropped where its 16 bits are
+// below `limit` (0: none is), and the others are scaled.
+struct Dropout {
+    uint64_t seed, draw;
+    const uint64_t* counter;  // device, added to draw; may be null
+    uint32_t limit;
+    float scale;
+};
+
+hipError_t launch_dropout(const hc_dropout_params& p, const Dropout& d, hc_type type, const void* x,
+                          const void* residual, void* out, hipStream_t s);
+
+size_t linear_bytes(const hc_linear_params& p, hc_type type);
+hipError_t launch_linear(const hc_linear_params& p, const Dropout& d, hc_type type, const void* x,
+                         const void* w, const void* bias, const void* residual, void* y, void* z,
+                         void* ws, hipStream_t s);
+
+size_t linear_grad_bytes(const hc_linear_params& p, hc_type type);
+struct LinearGrad {
+    const void *dy, *x, *w, *z;
+    void *dx, *dw, *db;
+    hc_type g_type;
+    bool accumulate;
+};
+hipError_t launch_linear_grad(const hc_linear_params& p, const Dropout& d, hc_type type,
+                              const LinearGrad& g, void* ws, hipStream_t s);
+
 }  // namespace hc

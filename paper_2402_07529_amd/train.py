@@ -1,6 +1,6 @@
 """Python binding of the training-side operators (include/hc_train.h): embedding
-lookup with scaling, its gradient by sorted token ids, and Newton-Schulz
-orthogonalisation.  Argument marshalling only, like the package's other calls;
+lookup with scaling, its gradient by sorted token ids, Newton-Schulz
+orthogonalisation, dropout, and the linear layer with its gradient.  Argument marshalling only, like the package's other calls;
 the names mirror the C ABI:
 
     hc_embed              out[i] = scale * table[ids[i]]
@@ -9,6 +9,9 @@ the names mirror the C ABI:
     hc_embed_grad_rows    the touched rows alone: ids, sums and their number
     hc_orthogonalise      the Newton-Schulz polynomial of a matrix, as the Muon
                           optimiser orthogonalises an update
+    hc_dropout            dropout or its gradient, with a residual
+    hc_linear             matrix product with bias, activation, dropout, residual
+    hc_linear_grad        its gradient: of the input, the weight and the bias
 """
 from __future__ import annotations
 
@@ -21,7 +24,9 @@ FIXED_POINT = 2.0**20          # fixed point of the int32 gradients
 MUON = (3.4445, -4.7750, 2.0315)
 
 TRAIN_EXPORTS = ("hc_embed", "hc_embed_grad_bytes", "hc_embed_grad", "hc_embed_grad_rows",
-                 "hc_orthogonalise_bytes", "hc_orthogonalise")
+                 "hc_orthogonalise_bytes", "hc_orthogonalise", "hc_dropout", "hc_linear_bytes",
+                 "hc_linear", "hc_linear_grad_bytes", "hc_linear_grad")
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3, "tanh": 4, "sigmoid": 5}
 
 
 class hc_embed_params(ctypes.Structure):
@@ -41,6 +46,22 @@ class hc_orthogonalise_params(ctypes.Structure):
                 ("eps", ctypes.c_float), ("scale", ctypes.c_float)]
 
 
+class hc_dropout_params(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_uint64), ("cols", ctypes.c_uint64), ("x_ld", ctypes.c_uint64),
+                ("residual_ld", ctypes.c_uint64), ("out_ld", ctypes.c_uint64),
+                ("seed", ctypes.c_uint64), ("draw", ctypes.c_uint64), ("p", ctypes.c_float),
+                ("reserved", ctypes.c_uint32)]
+
+
+class hc_linear_params(ctypes.Structure):
+    _fields_ = [("m", ctypes.c_uint64), ("n", ctypes.c_uint64), ("k", ctypes.c_uint64),
+                ("x_ld", ctypes.c_uint64), ("w_ld", ctypes.c_uint64), ("y_ld", ctypes.c_uint64),
+                ("z_ld", ctypes.c_uint64), ("residual_ld", ctypes.c_uint64),
+                ("dx_ld", ctypes.c_uint64), ("dw_ld", ctypes.c_uint64),
+                ("seed", ctypes.c_uint64), ("draw", ctypes.c_uint64), ("p", ctypes.c_float),
+                ("act", ctypes.c_uint32), ("fixed", ctypes.c_float), ("reserved", ctypes.c_uint32)]
+
+
 _P, _Z = ctypes.c_void_p, ctypes.c_size_t
 _EP, _OP = ctypes.POINTER(hc_embed_params), ctypes.POINTER(hc_orthogonalise_params)
 _lib.hc_embed.argtypes = [_EP, ctypes.c_int, _P, _P, _P, _P]
@@ -50,6 +71,13 @@ _lib.hc_embed_grad_rows.argtypes = [_EP, ctypes.c_int, _P, _P, ctypes.c_int, _P,
                                     ctypes.c_uint64, _P, _P, _Z, _P]
 _lib.hc_orthogonalise_bytes.argtypes = [_OP, ctypes.POINTER(_Z)]
 _lib.hc_orthogonalise.argtypes = [_OP, _P, _P, _P, _Z, _P]
+_DP, _LP = ctypes.POINTER(hc_dropout_params), ctypes.POINTER(hc_linear_params)
+_lib.hc_dropout.argtypes = [_DP, ctypes.c_int, _P, _P, _P, _P, _P]
+_lib.hc_linear_bytes.argtypes = [_LP, ctypes.c_int, ctypes.POINTER(_Z)]
+_lib.hc_linear.argtypes = [_LP, ctypes.c_int, _P, _P, _P, _P, _P, _P, _P, _P, _Z, _P]
+_lib.hc_linear_grad_bytes.argtypes = [_LP, ctypes.c_int, ctypes.POINTER(_Z)]
+_lib.hc_linear_grad.argtypes = [_LP, ctypes.c_int, _P, _P, _P, _P, _P, ctypes.c_int, _P, _P,
+                                ctypes.c_int, _P, _P, _Z, _P]
 for _f in TRAIN_EXPORTS:
     getattr(_lib, _f).restype = ctypes.c_int
 
@@ -241,3 +269,158 @@ def hc_orthogonalise(x, out, ws, steps: int = 5, coeffs=MUON, eps: float = 1e-7,
     p, px, po = _ortho_params(x, out, steps, coeffs, eps, scale)
     _check(_lib.hc_orthogonalise(ctypes.byref(p), px, po, _bytes(ws), ws.numel(),
                                  _stream(stream)), "hc_orthogonalise")
+
+
+_current_device = None
+
+
+def _on_device(*tensors):
+    """Refuses tensors of another device than the current one, whose stream is used."""
+    global _current_device
+    if _current_device is None:
+        import torch
+        _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    current = _current_device()
+    for t in tensors:
+        if t is not None and t.get_device() != current:
+            raise ValueError(f"a tensor is on device {t.device}, the current one is cuda:{current}")
+
+
+def _counter(t):
+    if t is None:
+        return None
+    import torch
+    types = (torch.int64, torch.uint64) if hasattr(torch, "uint64") else (torch.int64,)
+    return _ptr(t, "counter", types, 1)
+
+
+def _like(t, name, x, rows, cols):
+    """(pointer, row stride) of a [rows, cols] tensor of x's type; None: none."""
+    if t is None:
+        return None, 0
+    if t.dtype != x.dtype:
+        raise ValueError(f"{name} is {t.dtype}, expected {x.dtype}")
+    p, r, c, ld = _rows(t, name)
+    if r != rows or c != cols:
+        raise ValueError(f"{name} is {r} x {c}, expected {rows} x {cols}")
+    return p, ld
+
+
+def _uint64(v):
+    return v & (2**64 - 1)
+
+
+def hc_dropout(x, out, p: float, seed: int, draw: int = 0, residual=None, counter=None, stream=None):
+    """out = residual + mask * x, or mask * x: an element is dropped with probability p (a multiple
+    of 2^-16), the others are scaled by 1 / (1 - p).  x, out and residual [.., cols] float32,
+    bfloat16 or float16; out may be x or residual.  The mask depends on seed, draw and an
+    element's row and column alone: the same call on an output gradient is the backward pass.
+    counter (int64, one element, on the device) is added to draw when the kernel runs."""
+    px, rows, cols, x_ld = _rows(x, "x")
+    po, out_ld = _like(out, "out", x, rows, cols)
+    pr, r_ld = _like(residual, "residual", x, rows, cols)
+    _on_device(x, out, residual, counter)
+    q = hc_dropout_params(rows, cols, x_ld, r_ld, out_ld, _uint64(seed), _uint64(draw), p, 0)
+    _check(_lib.hc_dropout(ctypes.byref(q), _type(x, "x"), px, pr, po, _counter(counter),
+                           _stream(stream)), "hc_dropout")
+
+
+def _act(act):
+    code = ACTIVATIONS.get(act)
+    if code is None:
+        raise ValueError(f"act is {act!r}, expected one of {tuple(ACTIVATIONS)}")
+    return code
+
+
+def _layer(m, n, k, x_ld, w_ld, y_ld, z_ld=0, residual_ld=0, dx_ld=0, dw_ld=0, seed=0, draw=0, p=0.0,
+           act="none", fixed=1.0):
+    return hc_linear_params(m, n, k, x_ld, w_ld, y_ld, z_ld, residual_ld, dx_ld, dw_ld, _uint64(seed),
+                            _uint64(draw), p, _act(act), fixed, 0)
+
+
+def _layer_bytes(call, where, x, w):
+    px, m, k, x_ld = _rows(x, "x")
+    pw, n, kw, w_ld = _rows(w, "w")
+    if kw != k:
+        raise ValueError(f"w has {kw} columns, x {k}")
+    b = _Z()
+    _check(call(ctypes.byref(_layer(m, n, k, x_ld, w_ld, n)), _type(x, "x"), ctypes.byref(b)), where)
+    return b.value
+
+
+def hc_linear_bytes(x, w) -> int:
+    return _layer_bytes(_lib.hc_linear_bytes, "hc_linear_bytes", x, w)
+
+
+def alloc_linear_workspace(x, w):
+    """Workspace of hc_linear for x [.., k] and w [n, k] (and for fewer rows of x)."""
+    import torch
+    return torch.empty(max(hc_linear_bytes(x, w), 256), dtype=torch.uint8, device=x.device)
+
+
+def hc_linear(x, w, y, ws, bias=None, residual=None, z=None, act: str = "none", p: float = 0.0,
+              seed: int = 0, draw: int = 0, counter=None, stream=None):
+    """y = residual + mask * act(x w^T + bias), with hc_dropout's mask of y's rows and columns where
+    p > 0.  x [.., k], w [n, k], bias [n], residual, y and z [.., n], all float32, bfloat16 or
+    float16; act "none", "relu", "gelu" (by erf), "silu", "tanh" or "sigmoid".  z, where given,
+    gets x w^T + bias: hc_linear_grad reads it.  y may be residual."""
+    px, m, k, x_ld = _rows(x, "x")
+    pw, n, kw, w_ld = _rows(w, "w")
+    if kw != k or w.dtype != x.dtype:
+        raise ValueError(f"w is {w.dtype} with {kw} columns, x {x.dtype} with {k}")
+    py, y_ld = _like(y, "y", x, m, n)
+    pz, z_ld = _like(z, "z", x, m, n)
+    pr, r_ld = _like(residual, "residual", x, m, n)
+    _on_device(x, w, y, ws, bias, residual, z, counter)
+    q = _layer(m, n, k, x_ld, w_ld, y_ld, z_ld, r_ld, 0, 0, seed, draw, p, act)
+    _check(_lib.hc_linear(ctypes.byref(q), _type(x, "x"), px, pw, _ptr(bias, "bias", (x.dtype,), n),
+                          pr, py, pz, _counter(counter), _bytes(ws), ws.numel(), _stream(stream)),
+           "hc_linear")
+
+
+def hc_linear_grad_bytes(x, w) -> int:
+    return _layer_bytes(_lib.hc_linear_grad_bytes, "hc_linear_grad_bytes", x, w)
+
+
+def alloc_linear_grad_workspace(x, w):
+    """Workspace of hc_linear_grad for x [.., k] and w [n, k] (and for fewer rows of x)."""
+    import torch
+    return torch.empty(max(hc_linear_grad_bytes(x, w), 256), dtype=torch.uint8, device=x.device)
+
+
+def hc_linear_grad(dy, ws, x=None, w=None, z=None, dx=None, dw=None, db=None, act: str = "none",
+                   p: float = 0.0, seed: int = 0, draw: int = 0, fixed: float = FIXED_POINT,
+                   accumulate: bool = False, counter=None, stream=None):
+    """The gradient of hc_linear for the output gradient dy [.., n]: dz = act'(z) * mask * dy, then
+    dx = dz w, dw = dz^T x and db = dz's rows summed, those of them that are given.  dx needs w, dw
+    needs x, an activation needs z; dy, x, w, z and dx are of one type.  dw [n, k] and db [n] are
+    both float32, bfloat16, float16, or int32: fixed point with `fixed` units per 1.0; accumulate
+    adds to them.  The residual's gradient is dy itself."""
+    py, m, n, y_ld = _rows(dy, "dy")
+    for t, name, needs, what in ((dx, "dx", w, "w"), (dw, "dw", x, "x")):
+        if t is not None and needs is None:
+            raise ValueError(f"{name} needs {what}")
+    if act != "none" and z is None:
+        raise ValueError(f"the gradient of {act} needs z")
+    k = next((t.shape[-1] for t in (x, w, dx, dw) if t is not None), 1)
+    px, x_ld = _like(x, "x", dy, m, k)
+    pw, w_ld = _like(w, "w", dy, n, k)
+    pz, z_ld = _like(z, "z", dy, m, n)
+    pdx, dx_ld = _like(dx, "dx", dy, m, k)
+    pdw, dw_ld, g_type = None, 0, HC_T_F32
+    if dw is not None:
+        pdw, rows, cols, dw_ld = _rows(dw, "dw")
+        g_type = _type(dw, "dw")
+        if rows != n or cols != k:
+            raise ValueError(f"dw is {rows} x {cols}, expected {n} x {k}")
+    if db is not None:
+        if dw is not None and db.dtype != dw.dtype:
+            raise ValueError(f"db is {db.dtype}, dw {dw.dtype}")
+        g_type = _type(db, "db")
+    _on_device(dy, ws, x, w, z, dx, dw, db, counter)
+    q = _layer(m, n, k, x_ld if x is not None else k, w_ld if w is not None else k, y_ld, z_ld, 0, dx_ld,
+               dw_ld, seed, draw, p, act, fixed)
+    pdb = None if db is None else _ptr(db, "db", (db.dtype,), n)
+    _check(_lib.hc_linear_grad(ctypes.byref(q), _type(dy, "dy"), py, px, pw, pz, pdx, g_type, pdw,
+                               pdb, 1 if accumulate else 0, _counter(counter), _bytes(ws), ws.numel(),
+                               _stream(stream)), "hc_linear_grad")

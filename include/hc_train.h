@@ -206,9 +206,10 @@ hc_status hc_linear(const hc_linear_params *p, hc_type type, const void *x, cons
  *   dw and db: g_type, fp32 sums rounded once, or HC_T_I32: a sum times `fixed`,
  * rounded to the nearest whole number, ties to even, saturating at +-(2^31 - 1)
  * (NaN: 0).  accumulate != 0 adds them to what dw and db hold (int32 saturating).
- *   16-bit types: the products take dz rounded to `type`, and where g_type is
- * HC_T_F32 or HC_T_I32 dw takes the rest too (twice 8 or 11 bits).  Without
- * activation and dropout dz is dy.  db takes dz unrounded.
+ *   16-bit types: dx, and a 16-bit dw, take dz rounded to `type`; a dw of
+ * HC_T_F32 or HC_T_I32 takes it in three bf16 parts (24 bits) or two fp16 ones
+ * (22 bits), three or two times the products.  Without activation and dropout dz
+ * is dy.  db takes dz unrounded.
  *   m = 0 gives zeros.  Order and infinities as in hc_linear. */
 hc_status hc_linear_grad_bytes(const hc_linear_params *p, hc_type type, size_t *bytes);
 hc_status hc_linear_grad(const hc_linear_params *p, hc_type type, const void *dy, const void *x,

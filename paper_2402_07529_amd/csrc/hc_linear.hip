@@ -3,13 +3,14 @@
 //   forward   D = y,  D[i][j] = sum over l of x[i][l] w[j][l]
 //   dx        D = dx, D[i][j] = sum over l of dz[i][l] w[l][j]
 //   dw        D = dw, D[i][j] = sum over l of dz[l][i] x[l][j]
+#include "hc_internal.h"
 #include "hc_layer.h"
+#include "hc_tiles.h"
 
 namespace hc {
 
 namespace {
 
-typedef float f4 __attribute__((ext_vector_type(4)));
 typedef float f8 __attribute__((ext_vector_type(8)));
 
 enum Kind { FORWARD, DX, DW };
@@ -46,15 +47,35 @@ __device__ __forceinline__ void finish_forward(const Forward& f, const Masks& ma
     store8(static_cast<T*>(f.y) + row * f.y_ld + col, count, v);
 }
 
+// An operand may be a sum of planes, and a product the sum of some products of
+// planes: pass s takes plane p_planes >> 4 s of P and q_planes >> 4 s of Q.  The
+// small ones come first; the first pass's sums are multiplied by `factor`.
+struct Passes {
+    uint32_t count, p_planes, q_planes;
+    float factor;
+};
+constexpr Passes kOnePass = {1, 0, 0, 1.0f};
+// dz in three bf16 parts that follow each other; in an fp16 part and 2^11 times the
+// rest, which as it is would lose bits below fp16's normal range
+constexpr float kRestUnit = 0x1p11f;
+constexpr Passes kRestBf16 = {3, 0x012, 0x000, 1.0f};
+constexpr Passes kRestF16 = {2, 0x01, 0x00, 1.0f / kRestUnit};
+// Three bf16 planes each, of 8 bits that follow each other: products down to 2^-16
+// of the largest.  What is left out is below 2^-23 of a product of two fp32 values.
+constexpr Passes kThreePlanes = {6, 0x010120, 0x001102, 1.0f};
+
 struct Product {
     const void *p, *q;       // operands
-    const void* p_rest;      // DW: dz = p + p_rest, or null
     uint64_t p_ld, q_ld;
+    uint64_t p_cols, q_cols;    // stored elements of a row: its columns, or with zeros behind
+    uint64_t p_plane, q_plane;  // elements between planes
+    Passes passes;
     uint64_t rows, inner;    // of D; length of l
-    uint32_t cols, tiles_j;
-    uint64_t tiles;
-    uint32_t pieces;         // each tile's l is cut into
-    float* part;             // their sums, [piece][rows][part_ld]
+    uint32_t cols;
+    uint32_t tiles_i, tiles_j;
+    uint32_t whole, cut;     // tiles that a workgroup makes whole, and that are cut
+    uint32_t pieces;         // along l into this many pieces
+    float* part;             // the pieces' sums
     uint32_t part_ld;
     Forward forward;
     Gradient gradient;
@@ -71,15 +92,7 @@ __device__ __forceinline__ void finish8(const Product& g, const Masks& masks, ui
 
 // ---- products of any shape, stride and alignment -----------------------------------
 
-typedef _Float16 h8 __attribute__((ext_vector_type(8)));
-typedef __bf16 b8 __attribute__((ext_vector_type(8)));
-
-__device__ __forceinline__ f4 product16(h8 a, h8 b, f4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
-}
-__device__ __forceinline__ f4 product16(b8 a, b8 b, f4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-}
+using hc::product16;
 __device__ __forceinline__ f4 product16(f8 a, f8 b, f4 c) {
 #pragma unroll
     for (int e = 0; e < 8; e++) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
@@ -152,38 +165,46 @@ __global__ __launch_bounds__(256) void direct_kernel(Product g) {
     __shared__ __align__(16) float s_out[kDirect * (kDirect + 4)];
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const uint32_t wi = wave / 2 * 32, wj = wave % 2 * 32;
-    const uint64_t piece = blockIdx.x / g.tiles, tile = blockIdx.x - piece * g.tiles;
+    const uint32_t piece = blockIdx.x / g.cut, tile = blockIdx.x - piece * g.cut;
     const uint64_t ti = tile / g.tiles_j, row0 = ti * kDirect;
     const uint32_t col0 = (uint32_t)(tile - ti * g.tiles_j) * kDirect;
-    const uint64_t lines = (g.inner + kStep - 1) / kStep, all = g.p_rest ? 2 * lines : lines;
+    const uint64_t lines = (g.inner + kStep - 1) / kStep, all = g.passes.count * lines;
     const uint64_t first = piece * all / g.pieces, end = (piece + 1) * all / g.pieces;
     const T* q = static_cast<const T*>(g.q);
     f4 acc[2][2] = {};
     T rp[8], rq[8];
-    auto load = [&](uint64_t s) {
-        const bool rest = s >= lines;
-        const uint64_t l = (rest ? s - lines : s) * kStep;
-        direct_load<PS>(static_cast<const T*>(rest ? g.p_rest : g.p), g.p_ld, g.rows, row0, l, g.inner, rp);
-        direct_load<QS>(q, g.q_ld, (uint64_t)g.cols, col0, l, g.inner, rq);
-    };
-    if (first < end) load(first);
-    for (uint64_t s = first; s < end; s++) {
-        __syncthreads();
-        direct_store<PS>(s_p, rp);
-        direct_store<QS>(s_q, rq);
-        __syncthreads();
-        if (s + 1 < end) load(s + 1);
-        V fp[2], fq[2];
+    for (uint64_t s = first; s < end;) {
+        const uint32_t pass = (uint32_t)(s / lines);
+        const uint64_t stop = min(end, (pass + 1) * lines);
+        const T* p = static_cast<const T*>(g.p) + (g.passes.p_planes >> 4 * pass & 15u) * g.p_plane;  // Q has one
+        auto load = [&](uint64_t l) {
+            direct_load<PS>(p, g.p_ld, g.rows, row0, l, g.inner, rp);
+            direct_load<QS>(q, g.q_ld, (uint64_t)g.cols, col0, l, g.inner, rq);
+        };
+        load((s - pass * lines) * kStep);
+        for (; s < stop; s++) {
+            __syncthreads();
+            direct_store<PS>(s_p, rp);
+            direct_store<QS>(s_q, rq);
+            __syncthreads();
+            if (s + 1 < stop) load((s + 1 - pass * lines) * kStep);
+            V fp[2], fq[2];
 #pragma unroll
-        for (int u = 0; u < 2; u++) {
-            const uint32_t at = (16 * u + (lane & 15)) * kDirectLd<T> + (lane >> 4) * 8;
-            fp[u] = *reinterpret_cast<const V*>(s_p + wi * kDirectLd<T> + at);
-            fq[u] = *reinterpret_cast<const V*>(s_q + wj * kDirectLd<T> + at);
+            for (int u = 0; u < 2; u++) {
+                const uint32_t at = (16 * u + (lane & 15)) * kDirectLd<T> + (lane >> 4) * 8;
+                fp[u] = *reinterpret_cast<const V*>(s_p + wi * kDirectLd<T> + at);
+                fq[u] = *reinterpret_cast<const V*>(s_q + wj * kDirectLd<T> + at);
+            }
+#pragma unroll
+            for (int u = 0; u < 2; u++)
+#pragma unroll
+                for (int v = 0; v < 2; v++) acc[u][v] = product16(fq[v], fp[u], acc[u][v]);
         }
+        if (pass == 0 && g.passes.count > 1)
 #pragma unroll
-        for (int u = 0; u < 2; u++)
+            for (int u = 0; u < 2; u++)
 #pragma unroll
-            for (int v = 0; v < 2; v++) acc[u][v] = product16(fq[v], fp[u], acc[u][v]);
+                for (int v = 0; v < 2; v++) acc[u][v] *= g.passes.factor;
     }
     constexpr uint32_t LD = kDirect + 4;
 #pragma unroll
@@ -205,7 +226,7 @@ __global__ __launch_bounds__(256) void direct_kernel(Product g) {
 #pragma unroll
         for (int e = 0; e < 8; e++) v[e] = s_out[ii * LD + jj + e];
         if (g.pieces > 1)
-            store8(g.part + (piece * g.rows + row) * g.part_ld + col, 8, v);
+            store8(g.part + ((uint64_t)piece * g.rows + row) * g.part_ld + col, 8, v);
         else
             finish8<KIND, T>(g, masks, row, col, v);
     }
@@ -213,7 +234,7 @@ __global__ __launch_bounds__(256) void direct_kernel(Product g) {
 
 // The sums of the tiles' pieces, in order, a lane eight columns of a row.
 template <Kind KIND, typename T>
-__global__ __launch_bounds__(256) void join_kernel(Product g) {
+__global__ __launch_bounds__(256) void direct_join_kernel(Product g) {
     const uint32_t groups = g.part_ld / 8;
     const uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x, row = at / groups;
     if (row >= g.rows) return;
@@ -230,6 +251,310 @@ __global__ __launch_bounds__(256) void join_kernel(Product g) {
     finish8<KIND, T>(g, masks, row, col, v);
 }
 
+// ---- products in tiles fed from memory to LDS directly -------------------------------
+
+// Where a wave's loads of one operand's tile go.  ROWS: of the tile.  Along rows
+// a load is 8 rows of 128 bytes, across them 512 / ROWS lines of 2 ROWS bytes;
+// lane i writes 16 bytes at 16 i of 1024, so it reads the chunk that belongs
+// there.  Bounds are the buffer's: what lies behind the operand's last element
+// reads as zero, and so do chunks past the end of l in its rows, whose lanes get
+// an offset behind any buffer.  A stored row is a multiple of 8 elements, so that no
+// chunk ends in the middle of a buffer.
+constexpr uint32_t kNowhere = 0x80000000u;
+
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, char* to, uint32_t at) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)to, 16, at, 0, 0, 0);
+}
+
+template <bool ACROSS, int ROWS, int WAVES> struct Loads {
+    static constexpr int N = ROWS / 8 / WAVES;  // of a wave and step
+    static constexpr uint32_t kChunks = ACROSS ? ROWS / 8 : 8, kLines = 64 / kChunks;
+    uint32_t at[N];
+    uint32_t chunk;      // along rows: the first of the lane's 8 values of l
+    const char* base;    // of this step
+    uint64_t left;       // bytes from there to the end of the plane
+    uint64_t step;       // bytes
+    const char* first;   // of plane 0
+    uint64_t all, plane_bytes;
+
+    // lines: stored rows of the operand, of `cols` elements; row0: of the tile
+    __device__ __forceinline__ void init(const void* p, uint64_t ld, uint64_t cols, uint64_t plane,
+                                         uint64_t lines, uint64_t row0, uint32_t wave, uint32_t lane) {
+#pragma unroll
+        for (int u = 0; u < N; u++) {
+            const uint32_t line = (wave * N + u) * kLines + lane / kChunks;
+            const uint32_t c = (lane % kChunks) ^ (ACROSS ? turn<ROWS>(line) : line & 7u);
+            at[u] = line * (uint32_t)(2 * ld) + c * 16;
+            if (!ACROSS) chunk = c * 8;
+        }
+        const uint64_t before = 2 * row0 * (ACROSS ? 1 : ld);
+        first = static_cast<const char*>(p) + before;
+        all = 2 * ((lines - 1) * ld + cols) - before;
+        step = ACROSS ? 128 * ld : 128;
+        plane_bytes = 2 * plane;
+    }
+    __device__ __forceinline__ void seek(uint32_t plane, uint32_t l) {
+        base = first + plane * plane_bytes + l * step;
+        left = all - l * step;
+    }
+    // l_left: values of l from this step on
+    __device__ __forceinline__ void fetch(char* tile, uint32_t wave, uint64_t l_left) {
+        const __amdgpu_buffer_rsrc_t r = buffer_rsrc(base, (uint32_t)(left < kNowhere ? left : kNowhere));
+        const bool out = !ACROSS && l_left < 64 && chunk >= (uint32_t)l_left;
+#pragma unroll
+        for (int u = 0; u < N; u++)
+            load_to_lds(r, tile + (wave * N + u) * 1024, out ? kNowhere : at[u]);
+        base += step;
+        left -= step;
+    }
+};
+
+template <Kind KIND> constexpr bool kPAcross = KIND == DW;
+template <Kind KIND> constexpr bool kQAcross = KIND != FORWARD;
+
+// Steps [s0, s1) of all passes' steps of a tile, added to acc.
+template <Kind KIND, typename V, typename S>
+__device__ __forceinline__ void accumulate(const Product& g, uint32_t ti, uint32_t tj, uint32_t s0,
+                                           uint32_t s1, char* s_mem, f4 (&acc)[S::WM / 16][S::WN / 16]) {
+    constexpr bool PA = kPAcross<KIND>, QA = kQAcross<KIND>;
+    const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    const uint32_t wi = wave / (S::BN / S::WN) * S::WM, wj = wave % (S::BN / S::WN) * S::WN;
+    Loads<PA, S::BM, S::kWaves> lp;
+    Loads<QA, S::BN, S::kWaves> lq;
+    lp.init(g.p, g.p_ld, g.p_cols, g.p_plane, PA ? g.inner : g.rows, (uint64_t)ti * S::BM, wave, lane);
+    lq.init(g.q, g.q_ld, g.q_cols, g.q_plane, QA ? g.inner : g.cols, (uint64_t)tj * S::BN, wave, lane);
+    const uint32_t lines = (uint32_t)((g.inner + 63) / 64);
+    uint32_t pass = s0 / lines, l = s0 - pass * lines;
+    auto seek = [&]() {
+        lp.seek(g.passes.p_planes >> 4 * pass & 15u, l);
+        lq.seek(g.passes.q_planes >> 4 * pass & 15u, l);
+    };
+    // called for one step after the other
+    auto fetch = [&](uint32_t, uint32_t buf) {
+        char* base = s_mem + buf * S::kStageBytes;
+        const uint64_t l_left = g.inner - (uint64_t)l * 64;
+        lp.fetch(base, wave, l_left);
+        lq.fetch(base + S::BM * kLine * 2, wave, l_left);
+        if (++l == lines) {
+            l = 0;
+            pass++;
+            seek();
+        }
+    };
+    typedef AlongRows<V> Along;
+    typedef typename std::conditional<PA, AcrossRows<V, S::BM>, Along>::type RP;
+    typedef typename std::conditional<QA, AcrossRows<V, S::BN>, Along>::type RQ;
+    seek();
+    auto run = [&](uint32_t steps) {
+        fetch(0, 0);
+        if constexpr (S::kWaves == 8)
+            main_loop_paired<1, S, V, RP, RQ>(acc, fetch, s_mem, steps, wi, wj, lane, wave);
+        else
+            main_loop<1, S, V, RP, RQ>(acc, fetch, s_mem, steps, wi, wj, lane);
+        __syncthreads();
+    };
+    if (KIND == DW && g.passes.factor != 1.0f && s0 < lines) {
+        const uint32_t stop = min(s1, lines);
+        run(stop - s0);
+#pragma unroll
+        for (int u = 0; u < S::WM / 16; u++)
+#pragma unroll
+            for (int v = 0; v < S::WN / 16; v++) acc[u][v] *= g.passes.factor;
+        s0 = stop;
+    }
+    if (s0 < s1) run(s1 - s0);
+}
+
+// Tile t: blocks of 8 tiles along i by 4 along j, so that the tiles that an XCD
+// works on share rows of both operands in its L2.
+__device__ __forceinline__ void tile_at(const Product& g, uint32_t t, uint32_t& ti, uint32_t& tj) {
+    const uint32_t stripe = t / (4 * g.tiles_i);
+    t -= stripe * 4 * g.tiles_i;
+    const uint32_t w = min(4u, g.tiles_j - 4 * stripe), block = t / (8 * w);
+    t -= block * 8 * w;
+    const uint32_t h = min(8u, g.tiles_i - 8 * block);
+    ti = 8 * block + t % h;
+    tj = 4 * stripe + t / h;
+}
+
+// A block's sums in LDS become results, eight columns of a row a lane.
+template <Kind KIND, typename T, typename S, int LANES>
+__device__ __forceinline__ void finish_block(const Product& g, const Masks& masks, const float* stage,
+                                             uint64_t ib, uint32_t jb, uint32_t at) {
+    constexpr int kPer = S::EN / 8;  // lanes for a row
+#pragma unroll
+    for (int k = 0; k < S::EM * S::EN / 8 / LANES; k++) {
+        const uint32_t q = at + k * LANES, ii = q / kPer, jj = q % kPer * 8;
+        const uint64_t row = ib + ii;
+        const uint32_t col = jb + jj;
+        float v[8];
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const f4 w = *reinterpret_cast<const f4*>(stage + staged<S::EN>(ii, jj + 4 * h));
+#pragma unroll
+            for (int e = 0; e < 4; e++) v[4 * h + e] = w[e];
+        }
+        if (row < g.rows && col < g.cols) finish8<KIND, T>(g, masks, row, col, v);
+    }
+}
+
+template <Kind KIND> __device__ __forceinline__ Masks masks_for(const Product& g) {
+    Masks masks = {};
+    if constexpr (KIND == FORWARD) masks = masks_of(g.forward.drop);
+    return masks;
+}
+
+// A tile a workgroup, or a piece of one.  Neighbouring workgroups take the same
+// piece of neighbouring tiles.
+template <Kind KIND, typename T, typename V, typename S>
+__global__ __launch_bounds__(S::kThreads) void tiled_kernel(Product g) {
+    constexpr int FM = S::WM / 16, FN = S::WN / 16, EM = S::EM, EN = S::EN;
+    extern __shared__ __align__(16) char s_mem[];
+    const uint32_t steps = g.passes.count * (uint32_t)((g.inner + 63) / 64);
+    const bool piece = blockIdx.x >= g.whole;
+    uint32_t t, s0 = 0, s1 = steps, w = 0;
+    if (piece) {
+        w = by_xcd(blockIdx.x - g.whole, gridDim.x - g.whole);
+        const uint32_t k = w / g.cut;
+        t = g.whole + w - k * g.cut;
+        s0 = (uint32_t)((uint64_t)k * steps / g.pieces);
+        s1 = (uint32_t)((uint64_t)(k + 1) * steps / g.pieces);
+    } else {
+        t = by_xcd(blockIdx.x, g.whole);
+    }
+    uint32_t ti, tj;
+    tile_at(g, t, ti, tj);
+    f4 acc[FM][FN] = {};
+    accumulate<KIND, V, S>(g, ti, tj, s0, s1, s_mem, acc);
+    if (piece) {
+        f4* part = reinterpret_cast<f4*>(g.part) + (size_t)w * (S::BM * S::BN / 4);
+#pragma unroll
+        for (int u = 0; u < FM; u++)
+#pragma unroll
+            for (int v = 0; v < FN; v++) part[(u * FN + v) * S::kThreads + threadIdx.x] = acc[u][v];
+        return;
+    }
+    const Masks masks = masks_for<KIND>(g);
+    const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    const uint64_t i0 = (uint64_t)ti * S::BM + wave / (S::BN / S::WN) * S::WM;
+    const uint32_t j0 = tj * S::BN + wave % (S::BN / S::WN) * S::WN;
+    const uint32_t fi = lane & 15, fj = (lane >> 4) * 4;
+    float* stage = reinterpret_cast<float*>(s_mem) + wave * EM * EN;
+#pragma unroll
+    for (int eu = 0; eu < S::WM / EM; eu++)
+#pragma unroll
+        for (int ev = 0; ev < S::WN / EN; ev++) {
+#pragma unroll
+            for (int u = 0; u < EM / 16; u++)
+#pragma unroll
+                for (int v = 0; v < EN / 16; v++)
+                    *reinterpret_cast<f4*>(stage + staged<EN>(16 * u + fi, 16 * v + fj)) =
+                        acc[eu * (EM / 16) + u][ev * (EN / 16) + v];
+            // only this wave's results are read
+            __builtin_amdgcn_s_waitcnt(0xc07f);
+            __builtin_amdgcn_wave_barrier();
+            finish_block<KIND, T, S, 64>(g, masks, stage, i0 + eu * EM, j0 + ev * EN, lane);
+            __builtin_amdgcn_s_waitcnt(0xc07f);
+            __builtin_amdgcn_wave_barrier();
+        }
+}
+
+// The sums of the cut tiles' pieces, in order.  A workgroup takes an EM x EN block
+// of a wave's part, a wave of it 16 rows.
+template <Kind KIND, typename T, typename S>
+__global__ __launch_bounds__(S::EM * 4) void join_kernel(Product g) {
+    constexpr int FN = S::WN / 16, EM = S::EM, EN = S::EN;
+    constexpr uint32_t kBlocks = S::kWaves * (S::WM / EM) * (S::WN / EN);  // of a tile
+    __shared__ __align__(16) float s_stage[EM * EN];
+    const uint32_t c = blockIdx.x / kBlocks, block = blockIdx.x - c * kBlocks;
+    const uint32_t wave = block % S::kWaves, sub = block / S::kWaves;
+    const uint32_t eu = sub / (S::WN / EN), ev = sub % (S::WN / EN);
+    const uint32_t lane = threadIdx.x & 63, u = threadIdx.x >> 6;
+    const f4* part = reinterpret_cast<const f4*>(g.part) +
+                     ((eu * (EM / 16) + u) * FN + ev * (EN / 16)) * S::kThreads + wave * 64 + lane;
+    constexpr int kAhead = 4;  // pieces asked for at once
+    f4 acc[EN / 16] = {};
+    for (uint32_t q0 = 0; q0 < g.pieces; q0 += kAhead) {
+        f4 v[kAhead][EN / 16];
+#pragma unroll
+        for (int q = 0; q < kAhead; q++)
+#pragma unroll
+            for (int k = 0; k < EN / 16; k++)
+                if (q0 + q < g.pieces)
+                    v[q][k] = part[(c + (size_t)(q0 + q) * g.cut) * (S::BM * S::BN / 4) + k * S::kThreads];
+#pragma unroll
+        for (int q = 0; q < kAhead; q++)
+#pragma unroll
+            for (int k = 0; k < EN / 16; k++)
+                if (q0 + q < g.pieces) acc[k] += v[q][k];
+    }
+    uint32_t ti, tj;
+    tile_at(g, g.whole + c, ti, tj);
+    const uint64_t ib = (uint64_t)ti * S::BM + wave / (S::BN / S::WN) * S::WM + eu * EM;
+    const uint32_t jb = tj * S::BN + wave % (S::BN / S::WN) * S::WN + ev * EN;
+    const uint32_t fi = 16 * u + (lane & 15), fj = (lane >> 4) * 4;
+#pragma unroll
+    for (int v = 0; v < EN / 16; v++)
+        *reinterpret_cast<f4*>(s_stage + staged<EN>(fi, 16 * v + fj)) = acc[v];
+    lds_barrier();
+    finish_block<KIND, T, S, S::EM * 4>(g, masks_for<KIND>(g), s_stage, ib, jb, threadIdx.x);
+}
+
+// ---- operands as the tiles take them --------------------------------------------------
+
+// v = the sum of three bf16 values, exactly where v is normal and no smaller than
+// 2^-110.  The first is rounded, so that signs differ and what a product leaves out
+// does not add up, but not up to infinity; infinity and NaN leave nothing.
+__device__ __forceinline__ void split3(float v, __bf16 (&w)[3]) {
+    const uint32_t bits = __builtin_bit_cast(uint32_t, v);
+    w[0] = (__bf16)v;
+    if ((bits & 0x7fffffffu) >= 0x7f7f8000u) {  // rounds to infinity, or is not finite
+        if ((bits & 0x7fffffffu) < 0x7f800000u)
+            w[0] = (__bf16)__builtin_bit_cast(float, bits & 0xffff0000u);
+        else
+            v = 0.0f;
+    }
+    const float r = v == 0.0f ? 0.0f : v - (float)w[0];
+    w[1] = (__bf16)r;
+    w[2] = (__bf16)(r - (float)w[1]);
+}
+
+struct PackArgs {
+    const void* in;
+    void* out;
+    uint64_t rows, in_ld, out_ld, plane;
+    uint32_t cols;
+};
+
+template <typename T> __device__ __forceinline__ void store_planes(const PackArgs& a, uint64_t at, const float (&v)[8]) {
+    if constexpr (sizeof(T) == 4) {
+        b8 w[3];
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+            __bf16 s[3];
+            split3(v[e], s);
+#pragma unroll
+            for (int k = 0; k < 3; k++) w[k][e] = s[k];
+        }
+#pragma unroll
+        for (int k = 0; k < 3; k++) *reinterpret_cast<b8*>(static_cast<__bf16*>(a.out) + k * a.plane + at) = w[k];
+    } else {
+        store8(static_cast<T*>(a.out) + at, 8, v);
+    }
+}
+
+// A matrix of any stride and alignment as rows of a multiple of 64 values with
+// zeros behind them: 16-bit types as they are, fp32 in three planes.
+template <typename T> __global__ __launch_bounds__(256) void pack_kernel(PackArgs a) {
+    const uint32_t groups = (uint32_t)(a.out_ld / 8);
+    const uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x, row = at / groups;
+    if (row >= a.rows) return;
+    const uint32_t col = (uint32_t)(at - row * groups) * 8;
+    float v[8];
+    load8(static_cast<const T*>(a.in) + row * a.in_ld + (col < a.cols ? col : 0), col < a.cols ? a.cols - col : 0, v);
+    store_planes<T>(a, row * a.out_ld + col, v);
+}
+
 // ---- dz and the bias's gradient ----------------------------------------------------
 
 struct DzArgs {
@@ -240,8 +565,8 @@ struct DzArgs {
     uint32_t per;      // rows of a workgroup
     uint32_t width;    // lanes for a row, a power of two up to 64
     Dropout drop;
-    void *dz, *rest;   // [m][dz_ld], or null
-    uint64_t dz_ld;
+    PackArgs dz;       // where it goes (out: or null), zeros behind its columns
+    uint32_t planes;   // 1: in its own type; 2: and 2^11 times the rest; 3: bf16 parts
     float* part;       // the workgroups' sums, [blocks][n], or null
 };
 
@@ -254,7 +579,7 @@ template <typename T> __global__ __launch_bounds__(256) void dz_kernel(DzArgs a)
     const uint64_t end = min((uint64_t)(blockIdx.y + 1) * a.per, a.m);
     float sum[8] = {};
     if (group < a.groups) {
-        const uint32_t count = a.n - col;
+        const uint32_t count = col < a.n ? a.n - col : 0;
         for (uint64_t row = (uint64_t)blockIdx.y * a.per + sub; row < end; row += step) {
             float v[8];
             load8(static_cast<const T*>(a.dy) + row * a.dy_ld + col, count, v);
@@ -265,15 +590,27 @@ template <typename T> __global__ __launch_bounds__(256) void dz_kernel(DzArgs a)
 #pragma unroll
                 for (int e = 0; e < 8; e++) v[e] = backward<T>(a.act, z[e], v[e]);
             }
-            if (a.dz) store8(static_cast<T*>(a.dz) + row * a.dz_ld + col, count, v);
-            if (a.rest) {
-                float r[8];
 #pragma unroll
-                for (int e = 0; e < 8; e++) r[e] = v[e] - (float)(T)v[e];
-                store8(static_cast<T*>(a.rest) + row * a.dz_ld + col, count, r);
+            for (int e = 0; e < 8; e++) {
+                v[e] = (uint32_t)e < count ? v[e] : 0.0f;
+                sum[e] += v[e];
             }
+            if (!a.dz.out) continue;
+            const uint64_t at = row * a.dz.out_ld + col;
+            if (a.planes == 3) {
+                store_planes<float>(a.dz, at, v);
+            } else {
+                store8(static_cast<T*>(a.dz.out) + at, 8, v);
+                if (a.planes == 2) {
+                    // infinity and NaN leave nothing
 #pragma unroll
-            for (int e = 0; e < 8; e++) sum[e] += (uint32_t)e < count ? v[e] : 0.0f;
+                    for (int e = 0; e < 8; e++) {
+                        const float r = v[e] - (float)(T)v[e];
+                        v[e] = r - r == 0.0f ? r * kRestUnit : 0.0f;
+                    }
+                    store8(static_cast<T*>(a.dz.out) + a.dz.plane + at, 8, v);
+                }
+            }
         }
     }
     if (!a.part) return;
@@ -309,119 +646,295 @@ __global__ __launch_bounds__(1024) void bias_kernel(const float* __restrict__ pa
 
 // ---- layout and launches ------------------------------------------------------------
 
-constexpr uint64_t kSlots = 1024;        // workgroups that a product is cut for
-constexpr uint64_t kMostPieces = 64;
+constexpr int kCus = 256;                // of the gfx950
 constexpr uint64_t kBiasBlocks = 256;    // most workgroups along the rows of dz
 
 uint64_t up(uint64_t v, uint64_t to) { return (v + to - 1) / to; }
 
-struct DirectPlan {
-    uint64_t tiles;
-    uint32_t tiles_j, pieces;
-    size_t part_bytes;
-};
+// Direct products: cut along l until there are this many workgroups.
+constexpr uint64_t kSlots = 1024;
+constexpr uint64_t kMostPieces = 64;
 
-DirectPlan direct_plan(uint64_t rows, uint64_t cols, uint64_t lines) {
-    DirectPlan d = {};
-    d.tiles_j = (uint32_t)up(cols, kDirect);
-    d.tiles = up(rows, kDirect) * d.tiles_j;
-    uint64_t pieces = d.tiles ? kSlots / d.tiles : 1;
+template <Kind KIND, typename T> hipError_t direct(Product g, hipStream_t s) {
+    const uint64_t lines = up(g.inner, kStep) * g.passes.count;
+    g.tiles_j = (uint32_t)up(g.cols, kDirect);
+    const uint64_t tiles = up(g.rows, kDirect) * g.tiles_j;
+    uint64_t pieces = kSlots / tiles;
     pieces = pieces > lines / 4 ? lines / 4 : pieces;
     pieces = pieces > kMostPieces ? kMostPieces : pieces < 1 ? 1 : pieces;
-    d.pieces = (uint32_t)pieces;
-    d.part_bytes = pieces > 1 ? pieces * rows * up(cols, 8) * 32 : 0;
-    return d;
-}
-
-template <Kind KIND, typename T> hipError_t direct(Product g, float* part, hipStream_t s) {
-    const uint64_t lines = up(g.inner, kStep) * (g.p_rest ? 2 : 1);
-    const DirectPlan d = direct_plan(g.rows, g.cols, lines);
-    g.tiles = d.tiles;
-    g.tiles_j = d.tiles_j;
-    g.pieces = d.pieces;
-    g.part = part;
+    g.cut = (uint32_t)tiles;
+    g.pieces = (uint32_t)pieces;
     g.part_ld = (uint32_t)up(g.cols, 8) * 8;
-    hipLaunchKernelGGL((direct_kernel<KIND, T>), dim3((uint32_t)(d.tiles * d.pieces)), dim3(256), 0, s, g);
-    if (d.pieces > 1)
-        hipLaunchKernelGGL((join_kernel<KIND, T>), dim3((uint32_t)up(g.rows * (g.part_ld / 8), 256)),
+    hipLaunchKernelGGL((direct_kernel<KIND, T>), dim3((uint32_t)(tiles * pieces)), dim3(256), 0, s, g);
+    if (pieces > 1)
+        hipLaunchKernelGGL((direct_join_kernel<KIND, T>), dim3((uint32_t)up(g.rows * (g.part_ld / 8), 256)),
                            dim3(256), 0, s, g);
     return hipGetLastError();
 }
 
-template <Kind KIND> hipError_t product(const Product& g, hc_type type, float* part, hipStream_t s) {
-    if (type == HC_T_F32) return direct<KIND, float>(g, part, s);
-    if (type == HC_T_BF16) return direct<KIND, __bf16>(g, part, s);
-    return direct<KIND, _Float16>(g, part, s);
+typedef Shape<256, 256, 128, 64, 2> Large;
+typedef Shape<128, 128, 64, 64, 2> Medium;
+typedef Shape<64, 64, 32, 32, 3> Small;
+
+// Estimated times in us: a step takes a workgroup `alone` on its CU, or `shared` by
+// as many as fit; a tile's first loads and its results take `ends`, a piece's with
+// the tile of sums that it writes `piece_ends`.
+struct TileCost {
+    uint64_t tile, resident;
+    double alone, shared, ends, piece_ends;
+};
+constexpr TileCost kTileCosts[3] = {
+    {256, 1, 1.50, 1.50, 9.0, 8.0},
+    {128, 2, 0.50, 0.86, 6.0, 5.0},
+    {64, 3, 0.35, 0.70, 5.0, 4.0},
+};
+constexpr uint64_t kLeastSteps = 4;      // of a piece
+constexpr double kJoin = 5.0, kBytesPerUs = 5e6;
+
+struct TilePlan {
+    int shape;
+    uint32_t tiles_i, tiles_j, whole, cut, pieces;
+};
+
+double rounds(const TileCost& c, uint64_t groups, double steps, double ends) {
+    const uint64_t slots = kCus * c.resident, full = groups / slots, rest = groups % slots;
+    double t = (double)full * (steps * c.shared + ends);
+    if (rest) {
+        const double filled = c.resident == 1 || rest <= (uint64_t)kCus
+                                  ? 0.0 : (double)(rest - kCus) / (double)(slots - kCus);
+        t += steps * (c.alone + filled * (c.shared - c.alone)) + ends;
+    }
+    return t;
+}
+
+// The tile's size, and how many tiles are cut into how many pieces: none, all, or
+// those left after whole rounds of the CUs.
+TilePlan tile_plan(uint64_t rows, uint64_t cols, uint64_t steps) {
+    TilePlan best = {};
+    double least = 1e300;
+    for (int k = 0; k < 3; k++) {
+        const TileCost& c = kTileCosts[k];
+        const uint64_t ti = up(rows, c.tile), tj = up(cols, c.tile), n = ti * tj, slots = kCus * c.resident;
+        auto consider = [&](double t, uint64_t whole, uint64_t pieces) {
+            if (t >= least) return;
+            least = t;
+            best = {k, (uint32_t)ti, (uint32_t)tj, (uint32_t)whole, (uint32_t)(n - whole), (uint32_t)pieces};
+        };
+        consider(rounds(c, n, (double)steps, c.ends), n, 1);
+        const uint64_t rest = n % slots, most = steps / kLeastSteps < kMostPieces ? steps / kLeastSteps : kMostPieces;
+        if (rest == 0) continue;
+        const uint64_t whole = n - rest;
+        for (uint64_t room : {(uint64_t)kCus, slots}) {
+            const uint64_t pieces = room / rest < most ? room / rest : most;
+            if (pieces < 2) continue;
+            const double t = rounds(c, whole, (double)steps, c.ends) +
+                             rounds(c, rest * pieces, (double)up(steps, pieces), c.piece_ends) + kJoin +
+                             4.0 * (double)(c.tile * c.tile * rest * (pieces + 1)) / kBytesPerUs;
+            consider(t, whole, pieces);
+        }
+    }
+    return best;
+}
+
+template <Kind KIND, typename T, typename V, typename S>
+hipError_t tiled_shape(const Product& g, hipStream_t s) {
+    const auto kernel = &tiled_kernel<KIND, T, V, S>;
+    const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), S::kLdsBytes);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, dim3(g.whole + g.cut * g.pieces), dim3(S::kThreads), S::kLdsBytes, s, g);
+    if (g.cut) {
+        constexpr uint32_t kBlocks = S::kWaves * (S::WM / S::EM) * (S::WN / S::EN);
+        hipLaunchKernelGGL((join_kernel<KIND, T, S>), dim3(g.cut * kBlocks), dim3(S::EM * 4), 0, s, g);
+    }
+    return hipGetLastError();
+}
+
+template <Kind KIND, typename T, typename V> hipError_t tiled(Product g, hipStream_t s) {
+    const TilePlan p = tile_plan(g.rows, g.cols, up(g.inner, 64) * g.passes.count);
+    g.tiles_i = p.tiles_i;
+    g.tiles_j = p.tiles_j;
+    g.whole = p.whole;
+    g.cut = p.cut;
+    g.pieces = p.pieces;
+    if (p.shape == 0) return tiled_shape<KIND, T, V, Large>(g, s);
+    if (p.shape == 1) return tiled_shape<KIND, T, V, Medium>(g, s);
+    return tiled_shape<KIND, T, V, Small>(g, s);
+}
+
+// in_tiles: the operands are as the tiles take them (fp32 in three planes).
+template <Kind KIND> hipError_t product(const Product& g, hc_type type, bool in_tiles, hipStream_t s) {
+    if (in_tiles && g.inner) {
+        if (type == HC_T_F32) return tiled<KIND, float, b8>(g, s);
+        if (type == HC_T_BF16) return tiled<KIND, __bf16, b8>(g, s);
+        return tiled<KIND, _Float16, h8>(g, s);
+    }
+    if (type == HC_T_F32) return direct<KIND, float>(g, s);
+    if (type == HC_T_BF16) return direct<KIND, __bf16>(g, s);
+    return direct<KIND, _Float16>(g, s);
 }
 
 // Most bytes of partial sums for up to this many rows of D (fewer rows may be cut
-// into more pieces).
+// into more pieces): pieces fill the CUs once.
 size_t most_part_bytes(uint64_t rows, uint64_t cols) {
-    const uint64_t whole = up(rows, kDirect) * up(cols, kDirect);  // tiles
-    const uint64_t most = whole < 1 ? 0 : whole * kMostPieces < kSlots ? whole * kMostPieces : kSlots;
-    return most * kDirect * kDirect * 4 + 256;
+    size_t most = 0;
+    auto take = [&](uint64_t tile, uint64_t groups) {
+        const uint64_t tiles = up(rows, tile) * up(cols, tile);
+        const uint64_t n = tiles < groups / kMostPieces ? tiles * kMostPieces : groups;
+        const size_t bytes = n * tile * tile * 4;
+        most = bytes > most ? bytes : most;
+    };
+    for (const TileCost& c : kTileCosts) take(c.tile, kCus * c.resident);
+    take(kDirect, kSlots);
+    return most;
 }
 
-struct GradLayout {
-    size_t dz, rest, bias, part, bytes;
-    uint64_t dz_ld, per, blocks;
+// ---- which way a call goes --------------------------------------------------------------
+
+constexpr uint64_t kMostTileLd = 1ull << 22;  // a tile's rows within 2^31 bytes
+
+// A 16-bit operand whose rows the tiles can take where they are.
+bool tile_rows(const void* p, uint64_t cols, uint64_t ld) {
+    return aligned(p, 16) && cols % 8 == 0 && ld % 8 == 0 && ld <= kMostTileLd;
+}
+
+// Whether operands that the tiles cannot take as they are (fp32: all) are copied
+// for them, rather than multiplied directly: by estimated times that are linear in
+// m, so that what is copied for m rows is room for fewer.  Direct products reach 75
+// TFLOP/s in fp32 and 170 to 400 in 16 bits; tiles a sixth of 1000 and 1000.
+bool worth_packing(const hc_linear_params& p, hc_type type, double products) {
+    const double flops = 2.0 * (double)p.m * (double)p.n * (double)p.k * products;
+    const double bytes = (type == HC_T_F32 ? 16.0 : 4.0) *
+                         ((double)p.m * p.k + (double)p.n * p.k + (products > 1 ? (double)p.m * p.n : 0.0));
+    const double gain = type == HC_T_F32 ? 1.0 / 75e6 - 6.0 / 1000e6 : 1.0 / 280e6 - 1.0 / 1000e6;
+    return p.k <= kMostTileLd && p.n <= kMostTileLd && flops * gain > bytes / 4e6 + 15.0;
+}
+
+struct Layout {
+    size_t x, w, dz, bias, part, bytes;
+    uint64_t k_ld, n_ld;  // of packed rows
+    uint64_t per, blocks;
     uint32_t width;
+    bool pack;            // x and w
 };
 
-GradLayout grad_layout(const hc_linear_params& p, hc_type type) {
-    GradLayout L = {};
+size_t take(size_t& at, size_t bytes) {
+    const size_t o = at;
+    at += align256(bytes);
+    return o;
+}
+
+// Copies of x and w: where they are worth it, and they may be needed (a pointer's
+// alignment is not known here; one that is off by itself goes the direct way).
+void take_packed(const hc_linear_params& p, hc_type type, double products, size_t& at, Layout* L) {
+    const size_t size = type == HC_T_F32 ? 6 : 2;
+    L->k_ld = up(p.k, 64) * 64;
+    L->n_ld = up(p.n, 64) * 64;
+    L->pack = (type == HC_T_F32 || p.k % 8 || p.x_ld % 8 || p.w_ld % 8 || p.x_ld > kMostTileLd ||
+               p.w_ld > kMostTileLd) && worth_packing(p, type, products);
+    L->x = take(at, L->pack ? p.m * L->k_ld * size : 0);
+    L->w = take(at, L->pack ? p.n * L->k_ld * size : 0);
+}
+
+Layout linear_layout(const hc_linear_params& p, hc_type type) {
+    Layout L = {};
     size_t at = 0;
-    auto take = [&](size_t bytes) {
-        const size_t o = at;
-        at += align256(bytes);
-        return o;
-    };
-    const size_t size = type == HC_T_F32 ? 4 : 2;
-    L.dz_ld = up(p.n, 8) * 8;
-    const uint64_t groups = L.dz_ld / 8;
+    take_packed(p, type, 1.0, at, &L);
+    L.part = take(at, most_part_bytes(p.m, p.n));
+    L.bytes = at;
+    return L;
+}
+
+Layout grad_layout(const hc_linear_params& p, hc_type type) {
+    Layout L = {};
+    size_t at = 0;
+    take_packed(p, type, 2.0, at, &L);
+    const uint64_t groups = L.n_ld / 8;
     L.width = 1;
     while (L.width < 64 && L.width < groups) L.width *= 2;
     const uint64_t step = 256 / L.width;
     L.per = up(up(p.m, kBiasBlocks), step) * step;
     L.blocks = p.m ? up(p.m, L.per) : 0;
-    L.dz = take(p.m * L.dz_ld * size);
-    L.rest = take(type == HC_T_F32 ? 0 : p.m * L.dz_ld * size);
-    L.bias = take(kBiasBlocks * p.n * 4);
+    L.dz = take(at, p.m * L.n_ld * (type == HC_T_F32 ? (L.pack ? 6 : 4) : type == HC_T_BF16 ? 6 : 4));
+    L.bias = take(at, kBiasBlocks * p.n * 4);
     const size_t a = most_part_bytes(p.m, p.k), b = most_part_bytes(p.n, p.k);
-    L.part = take(a > b ? a : b);
+    L.part = take(at, a > b ? a : b);
     L.bytes = at;
     return L;
 }
 
+struct Operand {
+    const void* p;
+    uint64_t ld, cols, plane;
+};
+
+// rows x cols of an operand in tiles' form: where it is, or packed into `to`.
+hipError_t packed(hc_type type, bool pack, const void* p, uint64_t rows, uint64_t cols, uint64_t ld, void* to,
+                  uint64_t to_ld, Operand* out, hipStream_t s) {
+    *out = {p, ld, cols, 0};
+    if (!pack) return hipSuccess;
+    const PackArgs a = {p, to, rows, ld, to_ld, rows * to_ld, (uint32_t)cols};
+    *out = {to, to_ld, to_ld, a.plane};
+    const dim3 grid((uint32_t)up(rows * (to_ld / 8), 256));
+    if (type == HC_T_F32) hipLaunchKernelGGL(pack_kernel<float>, grid, dim3(256), 0, s, a);
+    else if (type == HC_T_BF16) hipLaunchKernelGGL(pack_kernel<__bf16>, grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL(pack_kernel<_Float16>, grid, dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+void set(Product* g, const Operand& p, const Operand& q) {
+    g->p = p.p;
+    g->p_ld = p.ld;
+    g->p_cols = p.cols;
+    g->p_plane = p.plane;
+    g->q = q.p;
+    g->q_ld = q.ld;
+    g->q_cols = q.cols;
+    g->q_plane = q.plane;
+}
+
 }  // namespace
 
-size_t linear_bytes(const hc_linear_params& p, hc_type) { return most_part_bytes(p.m, p.n); }
+size_t linear_bytes(const hc_linear_params& p, hc_type type) { return linear_layout(p, type).bytes; }
 
 hipError_t launch_linear(const hc_linear_params& p, const Dropout& d, hc_type type, const void* x,
                          const void* w, const void* bias, const void* residual, void* y, void* z,
-                         void* ws, hipStream_t s) {
+                         void* ws_, hipStream_t s) {
+    const Layout L = linear_layout(p, type);
+    char* ws = static_cast<char*>(ws_);
+    const bool fp32 = type == HC_T_F32;
+    const bool x_fits = !fp32 && tile_rows(x, p.k, p.x_ld), w_fits = !fp32 && tile_rows(w, p.k, p.w_ld);
+    const bool in_tiles = L.pack || (x_fits && w_fits);
+    Operand ox, ow;
+    hipError_t e = packed(type, L.pack && !x_fits, x, p.m, p.k, p.x_ld, ws + L.x, L.k_ld, &ox, s);
+    if (e != hipSuccess) return e;
+    e = packed(type, L.pack && !w_fits, w, p.n, p.k, p.w_ld, ws + L.w, L.k_ld, &ow, s);
+    if (e != hipSuccess) return e;
     Product g = {};
-    g.p = x;
-    g.q = w;
-    g.p_ld = p.x_ld;
-    g.q_ld = p.w_ld;
+    set(&g, ox, ow);
+    g.passes = fp32 && in_tiles ? kThreePlanes : kOnePass;
     g.rows = p.m;
     g.cols = (uint32_t)p.n;
     g.inner = p.k;
+    g.part = reinterpret_cast<float*>(ws + L.part);
     g.forward = {bias, residual, y, z, p.residual_ld, p.y_ld, p.z_ld, p.act, d};
-    return product<FORWARD>(g, type, static_cast<float*>(ws), s);
+    return product<FORWARD>(g, type, in_tiles, s);
 }
 
 size_t linear_grad_bytes(const hc_linear_params& p, hc_type type) { return grad_layout(p, type).bytes; }
 
 hipError_t launch_linear_grad(const hc_linear_params& p, const Dropout& d, hc_type type,
                               const LinearGrad& q, void* ws_, hipStream_t s) {
-    const GradLayout L = grad_layout(p, type);
+    const Layout L = grad_layout(p, type);
     char* ws = static_cast<char*>(ws_);
-    const bool plain = p.act == HC_ACT_NONE && d.limit == 0;
-    const bool rest = !plain && q.dw && type != HC_T_F32 && (q.g_type == HC_T_F32 || q.g_type == HC_T_I32);
-    const bool dz = !plain && (q.dx || q.dw);
-    const Gradient gradient = {nullptr, 0, (uint32_t)q.g_type, q.accumulate ? 1u : 0u, p.fixed};
+    const bool fp32 = type == HC_T_F32, plain = p.act == HC_ACT_NONE && d.limit == 0;
+    const bool x_fits = !fp32 && tile_rows(q.x, p.k, p.x_ld), w_fits = !fp32 && tile_rows(q.w, p.k, p.w_ld);
+    const bool in_tiles = L.pack || ((!q.dw || x_fits) && (!q.dx || w_fits));
+    // dz is dy itself where nothing changes it and the products can take it
+    const bool dy_fits = plain && (in_tiles ? !fp32 && tile_rows(q.dy, p.n, p.y_ld) : true);
+    const bool dz = !dy_fits && (q.dx || q.dw);
+    const bool rest = !plain && q.dw && !fp32 && (q.g_type == HC_T_F32 || q.g_type == HC_T_I32);
+    hipError_t e = hipSuccess;
+    Operand oz = {q.dy, p.y_ld, p.n, 0};
     if ((dz || q.db) && p.m) {
         DzArgs a = {};
         a.dy = q.dy;
@@ -430,58 +943,65 @@ hipError_t launch_linear_grad(const hc_linear_params& p, const Dropout& d, hc_ty
         a.z_ld = p.z_ld;
         a.m = p.m;
         a.n = (uint32_t)p.n;
-        a.groups = (uint32_t)(L.dz_ld / 8);
+        a.groups = (uint32_t)(L.n_ld / 8);
         a.act = p.act;
         a.per = (uint32_t)L.per;
         a.width = L.width;
         a.drop = d;
-        a.dz = dz ? ws + L.dz : nullptr;
-        a.rest = rest ? ws + L.rest : nullptr;
-        a.dz_ld = L.dz_ld;
+        if (dz) {
+            a.dz.out = ws + L.dz;
+            a.dz.out_ld = L.n_ld;
+            a.dz.plane = p.m * L.n_ld;
+            a.planes = fp32 ? (in_tiles ? 3 : 1) : !rest ? 1 : type == HC_T_BF16 ? 3 : 2;
+            oz = {a.dz.out, L.n_ld, L.n_ld, a.dz.plane};
+        }
         a.part = q.db ? reinterpret_cast<float*>(ws + L.bias) : nullptr;
         const dim3 grid((uint32_t)up(a.groups, L.width), (uint32_t)L.blocks);
-        if (type == HC_T_F32) hipLaunchKernelGGL(dz_kernel<float>, grid, dim3(256), 0, s, a);
+        if (fp32) hipLaunchKernelGGL(dz_kernel<float>, grid, dim3(256), 0, s, a);
         else if (type == HC_T_BF16) hipLaunchKernelGGL(dz_kernel<__bf16>, grid, dim3(256), 0, s, a);
         else hipLaunchKernelGGL(dz_kernel<_Float16>, grid, dim3(256), 0, s, a);
-        const hipError_t e = hipGetLastError();
+        e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
+    const Gradient gradient = {nullptr, 0, (uint32_t)q.g_type, q.accumulate ? 1u : 0u, p.fixed};
     if (q.db) {
         Gradient b = gradient;
         b.out = q.db;
         hipLaunchKernelGGL(bias_kernel, dim3((uint32_t)up(p.n, 64)), dim3(1024), 0, s,
                            reinterpret_cast<const float*>(ws + L.bias), (uint32_t)L.blocks, (uint32_t)p.n, b);
-        const hipError_t e = hipGetLastError();
+        e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
     Product g = {};
-    g.p = dz ? ws + L.dz : q.dy;
-    g.p_ld = dz ? L.dz_ld : p.y_ld;
-    float* part = reinterpret_cast<float*>(ws + L.part);
+    g.part = reinterpret_cast<float*>(ws + L.part);
+    g.cols = (uint32_t)p.k;
+    g.passes = fp32 && in_tiles ? kThreePlanes : kOnePass;
     if (q.dx && p.m) {
+        Operand ow;
+        e = packed(type, L.pack && !w_fits, q.w, p.n, p.k, p.w_ld, ws + L.w, L.k_ld, &ow, s);
+        if (e != hipSuccess) return e;
         Product h = g;
-        h.q = q.w;
-        h.q_ld = p.w_ld;
+        set(&h, oz, ow);
         h.rows = p.m;
-        h.cols = (uint32_t)p.k;
         h.inner = p.n;
         h.gradient.out = q.dx;
         h.gradient.ld = p.dx_ld;
-        const hipError_t e = product<DX>(h, type, part, s);
+        e = product<DX>(h, type, in_tiles, s);
         if (e != hipSuccess) return e;
     }
     if (q.dw) {
+        Operand ox;
+        e = packed(type, L.pack && !x_fits && p.m, q.x, p.m, p.k, p.x_ld, ws + L.x, L.k_ld, &ox, s);
+        if (e != hipSuccess) return e;
         Product h = g;
-        if (rest) h.p_rest = ws + L.rest;
-        h.q = q.x;
-        h.q_ld = p.x_ld;
+        set(&h, oz, ox);
+        if (rest) h.passes = type == HC_T_BF16 ? kRestBf16 : kRestF16;
         h.rows = p.n;
-        h.cols = (uint32_t)p.k;
         h.inner = p.m;
         h.gradient = gradient;
         h.gradient.out = q.dw;
         h.gradient.ld = p.dw_ld;
-        return product<DW>(h, type, part, s);
+        return product<DW>(h, type, in_tiles, s);
     }
     return hipSuccess;
 }

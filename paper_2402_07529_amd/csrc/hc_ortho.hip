@@ -27,17 +27,15 @@
 // together: 780 us where the products alone take 629.  Half of the Gram product
 // and of the square are computed and mirrored.  Small ones: the chain of
 // launches, three a step (thin ones one or two) of 6 to 8 us each.
-#include "hc_device.h"
 #include "hc_internal.h"
+#include "hc_tiles.h"
 #include "hc_train_internal.h"
 
 namespace hc {
 
 namespace {
 
-typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h4 __attribute__((ext_vector_type(4)));
-typedef float f4 __attribute__((ext_vector_type(4)));
 
 // ---- operand planes --------------------------------------------------------------
 
@@ -53,12 +51,6 @@ template <int PLANES> __device__ __forceinline__ size_t operand_at(size_t row, u
 template <int PLANES> __device__ __forceinline__ void split(float v, _Float16& hi, _Float16& lo) {
     hi = (_Float16)v;
     if constexpr (PLANES == 2) lo = (_Float16)(v - (float)hi);
-}
-
-// Value (i, j) of a block in LDS, [i][EN]: its 4-value group is turned by i so
-// that rows written and columns read are spread over the banks.
-template <int EN> __device__ __forceinline__ uint32_t staged(uint32_t i, uint32_t j) {
-    return i * EN + ((((j >> 2) ^ i ^ (i >> 3)) & (EN / 4 - 1)) << 2) + (j & 3u);
 }
 
 // ---- norm and operands of X_0 ----------------------------------------------------
@@ -287,163 +279,6 @@ struct Product {
     float out_scale;
 };
 
-constexpr int kLine = 64;  // stored values of a tile's row in LDS: 128 bytes
-
-// A workgroup's tile: BM x BN, a wave's part WM x WN.
-template <int BM_, int BN_, int WM_, int WN_, int STAGES_> struct Shape {
-    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, kStages = STAGES_;
-    static constexpr int kWaves = (BM / WM) * (BN / WN);
-    static constexpr int kThreads = kWaves * 64;
-    static constexpr int kStageBytes = (BM + BN) * kLine * 2;
-    // a wave's results pass through LDS in blocks of EM x EN
-    static constexpr int EM = WM < 64 ? WM : 64, EN = WN < 64 ? WN : 64;
-    static constexpr int kLdsBytes =
-        kStages * kStageBytes > kWaves * EM * EN * 4 ? kStages * kStageBytes : kWaves * EM * EN * 4;
-};
-
-// 16-byte chunk c of row `row` of an operand tile in LDS lies at c ^ (row mod
-// 8): the reads of one chunk of 16 rows then touch all banks evenly.
-__device__ __forceinline__ uint32_t swizzled(uint32_t row, uint32_t c) {
-    return row * kLine + ((c ^ (row & 7u)) << 3);
-}
-
-typedef __attribute__((address_space(3))) void lds_void;
-
-// A barrier that keeps every instruction on its side.
-__device__ __forceinline__ void phase_barrier() {
-    __builtin_amdgcn_sched_barrier(0);
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
-}
-
-__device__ __forceinline__ f4 product16(h8 a, h8 b, f4 c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
-}
-
-// Fragments and products of one 128-byte step l.  A lane holds row lane % 16 of a
-// fragment, 8 values from chunk 4 h + lane / 16.  The first operand of the
-// instruction gives a lane's 4 consecutive results: Q, so that they lie along j.
-template <int PLANES, typename S, typename F>
-__device__ __forceinline__ void main_loop(f4 (&acc)[S::WM / 16][S::WN / 16], const F& fetch,
-                                          const char* s_mem, uint32_t lines, uint32_t wi,
-                                          uint32_t wj, uint32_t lane) {
-    constexpr int FM = S::WM / 16, FN = S::WN / 16;
-    constexpr uint32_t N = S::kStages;
-    constexpr uint32_t kLoads = (S::BM + S::BN) / 8 / S::kWaves;  // of a wave and step
-#pragma unroll
-    for (uint32_t l = 1; l + 1 < N; l++)
-        if (l < lines) fetch(l, l);
-    uint32_t buf = 0;
-    for (uint32_t l = 0; l < lines; l++) {
-        // this wave's loads of step l have landed (those of later steps may be on
-        // their way), then everybody's; and everybody is done with step l - 1
-        if (l + N - 2 < lines)
-            __builtin_amdgcn_s_waitcnt(0x0f70 | ((N - 2) * kLoads & 15) |
-                                       ((N - 2) * kLoads >> 4) << 14);
-        else
-            __builtin_amdgcn_s_waitcnt(0x0f70);
-        phase_barrier();
-        if (l + N - 1 < lines) fetch(l + N - 1, buf == 0 ? N - 1 : buf - 1);
-        const _Float16* sp = reinterpret_cast<const _Float16*>(s_mem + buf * S::kStageBytes);
-        buf = buf + 1 == N ? 0 : buf + 1;
-        const _Float16* sq = sp + S::BM * kLine;
-        h8 fp[2][FM], fq[2][FN];
-#pragma unroll
-        for (int h = 0; h < 2; h++) {
-            const uint32_t c = 4 * h + (lane >> 4);
-#pragma unroll
-            for (int u = 0; u < FM; u++)
-                fp[h][u] = *reinterpret_cast<const h8*>(sp + swizzled(wi + 16 * u + (lane & 15), c));
-#pragma unroll
-            for (int v = 0; v < FN; v++)
-                fq[h][v] = *reinterpret_cast<const h8*>(sq + swizzled(wj + 16 * v + (lane & 15), c));
-            if constexpr (PLANES == 1) {
-#pragma unroll
-                for (int u = 0; u < FM; u++)
-#pragma unroll
-                    for (int v = 0; v < FN; v++)
-                        acc[u][v] = product16(fq[h][v], fp[h][u], acc[u][v]);
-            }
-        }
-        if constexpr (PLANES == 2) {  // high x high, low x high, high x low
-#pragma unroll
-            for (int t = 0; t < 3; t++)
-#pragma unroll
-                for (int u = 0; u < FM; u++)
-#pragma unroll
-                    for (int v = 0; v < FN; v++)
-                        acc[u][v] = product16(fq[t == 1][v], fp[t == 2][u], acc[u][v]);
-        }
-    }
-}
-
-// Eight waves, two on each SIMD: a step is two halves, a half one phase of LDS
-// reads and one phase of products, with a barrier after every phase.  The second
-// four waves run one phase behind, so that on every SIMD one wave multiplies
-// while the other reads.  Buffers: the first four waves read step l in phases 4 l
-// and 4 l + 2, the second in 4 l + 1 and 4 l + 3, so from phase 4 l + 4 on the
-// buffer is free and takes step l + 2, which each wave asks for in its first
-// phase of step l + 1 and waits for before the barrier that ends phase 4 l + 7.
-template <int PLANES, typename S, typename F>
-__device__ __forceinline__ void main_loop_paired(f4 (&acc)[S::WM / 16][S::WN / 16], const F& fetch,
-                                                 const char* s_mem, uint32_t lines, uint32_t wi,
-                                                 uint32_t wj, uint32_t lane, uint32_t wave) {
-    constexpr int FM = S::WM / 16, FN = S::WN / 16;
-    const bool second = wave >= 4;
-    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
-    phase_barrier();
-    if (second) phase_barrier();
-    for (uint32_t l = 0; l < lines; l++) {
-        const _Float16* sp = reinterpret_cast<const _Float16*>(s_mem + (l & 1) * S::kStageBytes);
-        const _Float16* sq = sp + S::BM * kLine;
-        h8 fp[2][FM], fq[2][FN];
-#pragma unroll
-        for (int h = 0; h < 2; h++) {
-            // one plane: a half is 32 of the 64 values of l.  Two planes: a half is
-            // half of the rows, with all of Q read in the first
-#pragma unroll
-            for (int c2 = 0; c2 < 2; c2++) {
-                if (PLANES == 1 && c2 != h) continue;
-                const uint32_t c = 4 * c2 + (lane >> 4);
-#pragma unroll
-                for (int v = 0; v < FN; v++)
-                    if (PLANES == 1 || h == 0)
-                        fq[c2][v] = *reinterpret_cast<const h8*>(sq + swizzled(wj + 16 * v + (lane & 15), c));
-#pragma unroll
-                for (int u = 0; u < FM; u++)
-                    if (PLANES == 1 || u / (FM / 2) == h)
-                        fp[c2][u] = *reinterpret_cast<const h8*>(sp + swizzled(wi + 16 * u + (lane & 15), c));
-            }
-            if (h == 0 && l + 1 < lines) fetch(l + 1, (l + 1) & 1);
-            if (second && h == 1) __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
-            __builtin_amdgcn_s_waitcnt(0xc07f);                        // lgkmcnt(0)
-            phase_barrier();
-            __builtin_amdgcn_s_setprio(1);
-            if constexpr (PLANES == 1) {
-#pragma unroll
-                for (int u = 0; u < FM; u++)
-#pragma unroll
-                    for (int v = 0; v < FN; v++)
-                        acc[u][v] = product16(fq[h][v], fp[h][u], acc[u][v]);
-            } else {
-#pragma unroll
-                for (int t = 0; t < 3; t++)
-#pragma unroll
-                    for (int u = h * FM / 2; u < (h + 1) * FM / 2; u++)
-#pragma unroll
-                        for (int v = 0; v < FN; v++)
-                            acc[u][v] = product16(fq[t == 1][v], fp[t == 2][u], acc[u][v]);
-            }
-            __builtin_amdgcn_s_setprio(0);
-            if (!second && h == 1) __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
-            phase_barrier();
-        }
-    }
-    if (!second) phase_barrier();
-}
-
 // A tile's matrix and place.
 struct Tile {
     uint32_t batch, ti, tj;
@@ -490,13 +325,6 @@ template <Kind KIND> __device__ __forceinline__ Tile tile_at(const Product& g, u
     return o;
 }
 
-// Workgroups go to the 8 XCDs in turn; each XCD takes a contiguous share of the
-// tiles, so that what neighbouring tiles read is shared in its L2.
-__device__ __forceinline__ uint32_t by_xcd(uint32_t block, uint32_t blocks) {
-    const uint32_t xcd = block & 7u, k = block >> 3, per = blocks >> 3, more = blocks & 7u;
-    return xcd * per + min(xcd, more) + k;
-}
-
 // Steps [l0, l1) of a tile, added to acc.
 template <int PLANES, typename S>
 __device__ __forceinline__ void accumulate(const Product& g, const Tile& tile, uint32_t l0,
@@ -532,9 +360,9 @@ __device__ __forceinline__ void accumulate(const Product& g, const Tile& tile, u
     };
     fetch(0, 0);
     if constexpr (S::kWaves == 8)
-        main_loop_paired<PLANES, S>(acc, fetch, s_mem, l1 - l0, wi, wj, lane, wave);
+        main_loop_paired<PLANES, S, h8, AlongRows<h8>, AlongRows<h8>>(acc, fetch, s_mem, l1 - l0, wi, wj, lane, wave);
     else
-        main_loop<PLANES, S>(acc, fetch, s_mem, l1 - l0, wi, wj, lane);
+        main_loop<PLANES, S, h8, AlongRows<h8>, AlongRows<h8>>(acc, fetch, s_mem, l1 - l0, wi, wj, lane);
     __syncthreads();
 }
 

@@ -5,8 +5,9 @@ Tolerances, from the arithmetic.  A sum of t products in fp32, in any grouping, 
 of an fp32 value leave 2^-23 of a product).  An activation's slope is at most 1.13, and its own
 error is layer_reference.FUNCTION relative to its factors.  Dropout's factor and a residual are 3
 roundings.  The result is rounded by half a unit.  In the gradient of 16-bit types dz is rounded by
-half a unit h before the products, by h^2 where the gradient is wider; what fp16 holds below its
-normal range is 2^-25 off."""
+half a unit h before the products; where the gradient is wider bf16 takes three parts (2^-24) and
+fp16 two (2^-22).  What fp16 holds below its normal range is 2^-25 off, as a rest in units of 2^-11
+2^-36."""
 import pytest
 
 import layer_reference as ref
@@ -120,8 +121,10 @@ def check_grad(torch, L, act, p, seed, draw, dx, dw, db, out, old=None, fixed=No
 
     if dw is not None:
         two = plain or d == "float32"
-        wide = one if two or out in ("bfloat16", "float16") else slope_off + h * h * dz.abs() + ref.FLOOR[d]
-        terms = m if two or out in ("bfloat16", "float16") else 2 * m
+        wide, terms = one, m
+        if not two and out not in ("bfloat16", "float16"):
+            wide = slope_off + h * h * dz.abs() * (1 if d == "float16" else h) + ref.FLOOR[d] * 2**-11
+            terms = (2 if d == "float16" else 3) * m
         want, size = dz.t() @ x, dz.abs().t() @ x.abs()
         widened(want, wide.t() @ x.abs() + size * ((terms + 2) * ref.UNIT + part) * (1 + h), "dw", dw)
     if db is not None:

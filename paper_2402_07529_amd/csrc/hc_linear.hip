@@ -269,6 +269,7 @@ __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, char* to, 
 template <bool ACROSS, int ROWS, int WAVES> struct Loads {
     static constexpr int N = ROWS / 8 / WAVES;  // of a wave and step
     static constexpr uint32_t kChunks = ACROSS ? ROWS / 8 : 8, kLines = 64 / kChunks;
+    static constexpr uint32_t kBlock = ACROSS ? Across<ROWS>::kBlock : 1024;
     uint32_t at[N];
     uint32_t chunk;      // along rows: the first of the lane's 8 values of l
     const char* base;    // of this step
@@ -283,7 +284,7 @@ template <bool ACROSS, int ROWS, int WAVES> struct Loads {
 #pragma unroll
         for (int u = 0; u < N; u++) {
             const uint32_t line = (wave * N + u) * kLines + lane / kChunks;
-            const uint32_t c = (lane % kChunks) ^ (ACROSS ? turn<ROWS>(line) : line & 7u);
+            const uint32_t c = (lane % kChunks) ^ (ACROSS ? Across<ROWS>::turn(line) : line & 7u);
             at[u] = line * (uint32_t)(2 * ld) + c * 16;
             if (!ACROSS) chunk = c * 8;
         }
@@ -303,7 +304,7 @@ template <bool ACROSS, int ROWS, int WAVES> struct Loads {
         const bool out = !ACROSS && l_left < 64 && chunk >= (uint32_t)l_left;
 #pragma unroll
         for (int u = 0; u < N; u++)
-            load_to_lds(r, tile + (wave * N + u) * 1024, out ? kNowhere : at[u]);
+            load_to_lds(r, tile + (wave * N + u) * kBlock, out ? kNowhere : at[u]);
         base += step;
         left -= step;
     }
@@ -311,12 +312,22 @@ template <bool ACROSS, int ROWS, int WAVES> struct Loads {
 
 template <Kind KIND> constexpr bool kPAcross = KIND == DW;
 template <Kind KIND> constexpr bool kQAcross = KIND != FORWARD;
+template <Kind KIND, typename V, typename S> struct Reads {
+    typedef AlongRows<V> Along;
+    typedef typename std::conditional<kPAcross<KIND>, AcrossRows<V, S::BM>, Along>::type P;
+    typedef typename std::conditional<kQAcross<KIND>, AcrossRows<V, S::BN>, Along>::type Q;
+    typedef Stage<S, P, Q> InLds;
+    // the tiles of all stages, or the results
+    static constexpr uint32_t kTiles = S::kStages * InLds::kBytes, kResults = S::kWaves * S::EM * S::EN * 4;
+    static constexpr uint32_t kLdsBytes = kTiles > kResults ? kTiles : kResults;
+};
 
 // Steps [s0, s1) of all passes' steps of a tile, added to acc.
 template <Kind KIND, typename V, typename S>
 __device__ __forceinline__ void accumulate(const Product& g, uint32_t ti, uint32_t tj, uint32_t s0,
                                            uint32_t s1, char* s_mem, f4 (&acc)[S::WM / 16][S::WN / 16]) {
     constexpr bool PA = kPAcross<KIND>, QA = kQAcross<KIND>;
+    typedef Reads<KIND, V, S> R;
     const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const uint32_t wi = wave / (S::BN / S::WN) * S::WM, wj = wave % (S::BN / S::WN) * S::WN;
     Loads<PA, S::BM, S::kWaves> lp;
@@ -331,26 +342,23 @@ __device__ __forceinline__ void accumulate(const Product& g, uint32_t ti, uint32
     };
     // called for one step after the other
     auto fetch = [&](uint32_t, uint32_t buf) {
-        char* base = s_mem + buf * S::kStageBytes;
+        char* base = s_mem + buf * R::InLds::kBytes;
         const uint64_t l_left = g.inner - (uint64_t)l * 64;
         lp.fetch(base, wave, l_left);
-        lq.fetch(base + S::BM * kLine * 2, wave, l_left);
+        lq.fetch(base + R::InLds::kQ, wave, l_left);
         if (++l == lines) {
             l = 0;
             pass++;
             seek();
         }
     };
-    typedef AlongRows<V> Along;
-    typedef typename std::conditional<PA, AcrossRows<V, S::BM>, Along>::type RP;
-    typedef typename std::conditional<QA, AcrossRows<V, S::BN>, Along>::type RQ;
     seek();
     auto run = [&](uint32_t steps) {
         fetch(0, 0);
         if constexpr (S::kWaves == 8)
-            main_loop_paired<1, S, V, RP, RQ>(acc, fetch, s_mem, steps, wi, wj, lane, wave);
+            main_loop_paired<1, S, V, typename R::P, typename R::Q>(acc, fetch, s_mem, steps, wi, wj, lane, wave);
         else
-            main_loop<1, S, V, RP, RQ>(acc, fetch, s_mem, steps, wi, wj, lane);
+            main_loop<1, S, V, typename R::P, typename R::Q>(acc, fetch, s_mem, steps, wi, wj, lane);
         __syncthreads();
     };
     if (KIND == DW && g.passes.factor != 1.0f && s0 < lines) {
@@ -739,9 +747,10 @@ TilePlan tile_plan(uint64_t rows, uint64_t cols, uint64_t steps) {
 template <Kind KIND, typename T, typename V, typename S>
 hipError_t tiled_shape(const Product& g, hipStream_t s) {
     const auto kernel = &tiled_kernel<KIND, T, V, S>;
-    const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), S::kLdsBytes);
+    constexpr int kLds = Reads<KIND, V, S>::kLdsBytes;
+    const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), kLds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, dim3(g.whole + g.cut * g.pieces), dim3(S::kThreads), S::kLdsBytes, s, g);
+    hipLaunchKernelGGL(kernel, dim3(g.whole + g.cut * g.pieces), dim3(S::kThreads), kLds, s, g);
     if (g.cut) {
         constexpr uint32_t kBlocks = S::kWaves * (S::WM / S::EM) * (S::WN / S::EN);
         hipLaunchKernelGGL((join_kernel<KIND, T, S>), dim3(g.cut * kBlocks), dim3(S::EM * 4), 0, s, g);

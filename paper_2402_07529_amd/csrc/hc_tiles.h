@@ -59,34 +59,139 @@ __device__ __forceinline__ f4 product16(b8 a, b8 b, f4 c) {
 }
 
 // Fragments: 16 rows of an operand by 32 values of l, half h of a step.  A lane
-// holds row lane % 16, values 8 (lane / 16) .. + 7 of the half.
+// holds row lane % 16, values 8 (lane / 16) .. + 7 of the half.  kBlock: bytes in
+// LDS from one load instruction's 1024 bytes to the next.
 
 // An operand stored by rows along l: a tile is [row][64], 128 bytes a row.
 template <typename V> struct AlongRows {
-    __device__ __forceinline__ static V read(const char* tile, uint32_t row0, uint32_t h, uint32_t lane) {
-        return *reinterpret_cast<const V*>(tile + 2 * swizzled(row0 + (lane & 15), 4 * h + (lane >> 4)));
+    static constexpr uint32_t kBlock = 1024;
+    static constexpr bool kWaits = false;
+    template <int N>
+    __device__ __forceinline__ static void read(V (&f)[N], int first, int count, const char* tile,
+                                                uint32_t row0, uint32_t h, uint32_t lane) {
+#pragma unroll
+        for (int u = 0; u < N; u++)
+            if (u >= first && u < first + count)
+                f[u] = *reinterpret_cast<const V*>(tile + 2 * swizzled(row0 + 16 * u + (lane & 15), 4 * h + (lane >> 4)));
     }
 };
 
 // An operand stored by l, its rows' index contiguous: a tile is [64 of l][ROWS].
-// The transposing load gives lane t of 16 the column t of the four rows that lanes
-// 4 r .. 4 r + 3 point to.  The 16-byte chunk c of line l lies at c ^ turn(l): the
-// four lines of a load are then in different banks, and so are the groups of 16
-// lanes, 8 lines apart.
-template <int ROWS> __device__ __forceinline__ uint32_t turn(uint32_t l) {
-    return ((l & 3u) << 1 | (l >> 3 & 3u) << 3) & (ROWS / 8 - 1);
-}
+// The transposing load gives lane t of 16 column t of the four lines that lanes
+// 4 r .. 4 r + 3 point to, 32 bytes of each; two loads make a fragment.  Chunk c (16
+// bytes) of line l lies at c ^ turn(l) and blocks are padded, so that the 32 bytes
+// of the four lines, and those of the lanes 16 on (8 lines further), are in
+// different banks: with a pitch of 512 bytes two lines are in a block and the pad
+// moves the next two by 32 bytes, with 256 four and with 128 eight are.
+//
+// The loads are written in assembly, with their wait: before a builtin one the
+// compiler waits for all loads from memory to LDS that are on their way, also those
+// of the next step.
+template <int ROWS> struct Across {
+    static constexpr uint32_t kLines = 512 / ROWS;  // of a block
+    static constexpr uint32_t kBlock = 1024 + (ROWS == 256 ? 32 : 64);
+    __device__ __forceinline__ static uint32_t turn(uint32_t l) {
+        return ROWS == 256 ? (l & 1u) << 2 : ROWS == 128 ? (l & 3u) << 1 : (l & 2u);
+    }
+    // of line l, chunk c
+    __device__ __forceinline__ static uint32_t place(uint32_t l, uint32_t c) {
+        return l / kLines * kBlock + l % kLines * (2 * ROWS) + ((c ^ turn(l)) << 4);
+    }
+};
+
 template <typename V, int ROWS> struct AcrossRows {
-    __device__ __forceinline__ static V read(const char* tile, uint32_t row0, uint32_t h, uint32_t lane) {
-        typedef short s4 __attribute__((ext_vector_type(4)));
-        typedef __attribute__((address_space(3))) s4 lds_s4;
-        const uint32_t t = lane & 15, l = 32 * h + 8 * (lane >> 4) + (t >> 2);
-        const uint32_t c = row0 / 8 + (t >> 1 & 1u);
-        const char* at = tile + l * (ROWS * 2) + ((c ^ turn<ROWS>(l)) << 4) + ((t & 1u) << 3);
-        const s4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)at);
-        const s4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4*)(at + 4 * ROWS * 2));
+    static constexpr uint32_t kBlock = Across<ROWS>::kBlock;
+    static constexpr bool kWaits = true;
+    // from a load to the one of the next four lines
+    static constexpr uint32_t kFour = ROWS == 256 ? 2 * kBlock : ROWS == 128 ? kBlock : 4 * 2 * ROWS;
+    typedef short s4 __attribute__((ext_vector_type(4)));
+
+    __device__ __forceinline__ static V joined(s4 lo, s4 hi) {
         return __builtin_bit_cast(V, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
+    // all N of them; every load that was asked for before has landed too
+    template <int N>
+    __device__ __forceinline__ static void read(V (&f)[N], int, int, const char* tile, uint32_t row0,
+                                                uint32_t h, uint32_t lane) {
+        static_assert((ROWS == 256 && (N == 8 || N == 4)) || (ROWS == 128 && N == 4) || (ROWS == 64 && N == 2), "");
+        const uint32_t t = lane & 15, l = 32 * h + 8 * (lane >> 4) + (t >> 2), c = row0 / 8 + (t >> 1 & 1u);
+        const uint32_t base = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)tile + ((t & 1u) << 3);
+        // fragment u is 2 u chunks on, which turn() mixes with bits of u
+        auto at = [&](uint32_t u) { return base + Across<ROWS>::place(l, c + 2 * u); };
+        s4 a[N], b[N];
+        if constexpr (N == 8) {
+            asm volatile(
+                "ds_read_b64_tr_b16 %0, %16\n\t"
+                "ds_read_b64_tr_b16 %8, %16 offset:%18\n\t"
+                "ds_read_b64_tr_b16 %1, %16 offset:32\n\t"
+                "ds_read_b64_tr_b16 %9, %16 offset:%18+32\n\t"
+                "ds_read_b64_tr_b16 %2, %17\n\t"
+                "ds_read_b64_tr_b16 %10, %17 offset:%18\n\t"
+                "ds_read_b64_tr_b16 %3, %17 offset:32\n\t"
+                "ds_read_b64_tr_b16 %11, %17 offset:%18+32\n\t"
+                "ds_read_b64_tr_b16 %4, %16 offset:128\n\t"
+                "ds_read_b64_tr_b16 %12, %16 offset:%18+128\n\t"
+                "ds_read_b64_tr_b16 %5, %16 offset:160\n\t"
+                "ds_read_b64_tr_b16 %13, %16 offset:%18+160\n\t"
+                "ds_read_b64_tr_b16 %6, %17 offset:128\n\t"
+                "ds_read_b64_tr_b16 %14, %17 offset:%18+128\n\t"
+                "ds_read_b64_tr_b16 %7, %17 offset:160\n\t"
+                "ds_read_b64_tr_b16 %15, %17 offset:%18+160\n\t"
+                "s_waitcnt lgkmcnt(0)"
+                : "=&v"(a[0]), "=&v"(a[1]), "=&v"(a[2]), "=&v"(a[3]), "=&v"(a[4]), "=&v"(a[5]), "=&v"(a[6]),
+                  "=&v"(a[7]), "=&v"(b[0]), "=&v"(b[1]), "=&v"(b[2]), "=&v"(b[3]), "=&v"(b[4]), "=&v"(b[5]),
+                  "=&v"(b[6]), "=&v"(b[7])
+                : "v"(at(0)), "v"(at(2)), "n"(kFour)
+                : "memory");
+        } else if constexpr (N == 4 && ROWS == 256) {
+            asm volatile(
+                "ds_read_b64_tr_b16 %0, %8\n\t"
+                "ds_read_b64_tr_b16 %4, %8 offset:%10\n\t"
+                "ds_read_b64_tr_b16 %1, %8 offset:32\n\t"
+                "ds_read_b64_tr_b16 %5, %8 offset:%10+32\n\t"
+                "ds_read_b64_tr_b16 %2, %9\n\t"
+                "ds_read_b64_tr_b16 %6, %9 offset:%10\n\t"
+                "ds_read_b64_tr_b16 %3, %9 offset:32\n\t"
+                "ds_read_b64_tr_b16 %7, %9 offset:%10+32\n\t"
+                "s_waitcnt lgkmcnt(0)"
+                : "=&v"(a[0]), "=&v"(a[1]), "=&v"(a[2]), "=&v"(a[3]), "=&v"(b[0]), "=&v"(b[1]), "=&v"(b[2]),
+                  "=&v"(b[3])
+                : "v"(at(0)), "v"(at(2)), "n"(kFour)
+                : "memory");
+        } else if constexpr (N == 4) {
+            asm volatile(
+                "ds_read_b64_tr_b16 %0, %8\n\t"
+                "ds_read_b64_tr_b16 %4, %8 offset:%12\n\t"
+                "ds_read_b64_tr_b16 %1, %9\n\t"
+                "ds_read_b64_tr_b16 %5, %9 offset:%12\n\t"
+                "ds_read_b64_tr_b16 %2, %10\n\t"
+                "ds_read_b64_tr_b16 %6, %10 offset:%12\n\t"
+                "ds_read_b64_tr_b16 %3, %11\n\t"
+                "ds_read_b64_tr_b16 %7, %11 offset:%12\n\t"
+                "s_waitcnt lgkmcnt(0)"
+                : "=&v"(a[0]), "=&v"(a[1]), "=&v"(a[2]), "=&v"(a[3]), "=&v"(b[0]), "=&v"(b[1]), "=&v"(b[2]),
+                  "=&v"(b[3])
+                : "v"(at(0)), "v"(at(1)), "v"(at(2)), "v"(at(3)), "n"(kFour)
+                : "memory");
+        } else {
+            asm volatile(
+                "ds_read_b64_tr_b16 %0, %4\n\t"
+                "ds_read_b64_tr_b16 %2, %4 offset:%6\n\t"
+                "ds_read_b64_tr_b16 %1, %5\n\t"
+                "ds_read_b64_tr_b16 %3, %5 offset:%6\n\t"
+                "s_waitcnt lgkmcnt(0)"
+                : "=&v"(a[0]), "=&v"(a[1]), "=&v"(b[0]), "=&v"(b[1])
+                : "v"(at(0)), "v"(at(1)), "n"(kFour)
+                : "memory");
+        }
+#pragma unroll
+        for (int u = 0; u < N; u++) f[u] = joined(a[u], b[u]);
+    }
+};
+
+// Bytes of a step's tiles in LDS.
+template <typename S, typename RP, typename RQ> struct Stage {
+    static constexpr uint32_t kQ = S::BM / 8 * RP::kBlock, kBytes = kQ + S::BN / 8 * RQ::kBlock;
 };
 
 // Fragments and products of the steps.  The first operand of the instruction gives
@@ -113,16 +218,14 @@ __device__ __forceinline__ void main_loop(f4 (&acc)[S::WM / 16][S::WN / 16], con
             __builtin_amdgcn_s_waitcnt(0x0f70);
         phase_barrier();
         if (l + N - 1 < lines) fetch(l + N - 1, buf == 0 ? N - 1 : buf - 1);
-        const char* sp = s_mem + buf * S::kStageBytes;
+        const char* sp = s_mem + buf * Stage<S, RP, RQ>::kBytes;
         buf = buf + 1 == N ? 0 : buf + 1;
-        const char* sq = sp + S::BM * kLine * 2;
+        const char* sq = sp + Stage<S, RP, RQ>::kQ;
         V fp[2][FM], fq[2][FN];
 #pragma unroll
         for (int h = 0; h < 2; h++) {
-#pragma unroll
-            for (int u = 0; u < FM; u++) fp[h][u] = RP::read(sp, wi + 16 * u, h, lane);
-#pragma unroll
-            for (int v = 0; v < FN; v++) fq[h][v] = RQ::read(sq, wj + 16 * v, h, lane);
+            RP::read(fp[h], 0, FM, sp, wi, h, lane);
+            RQ::read(fq[h], 0, FN, sq, wj, h, lane);
             if constexpr (PLANES == 1) {
 #pragma unroll
                 for (int u = 0; u < FM; u++)
@@ -155,13 +258,15 @@ __device__ __forceinline__ void main_loop_paired(f4 (&acc)[S::WM / 16][S::WN / 1
                                                  const char* s_mem, uint32_t lines, uint32_t wi,
                                                  uint32_t wj, uint32_t lane, uint32_t wave) {
     constexpr int FM = S::WM / 16, FN = S::WN / 16;
+    // reads that wait for themselves come after the step's loads were asked for
+    constexpr bool kFetchFirst = RP::kWaits || RQ::kWaits;
     const bool second = wave >= 4;
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
     phase_barrier();
     if (second) phase_barrier();
     for (uint32_t l = 0; l < lines; l++) {
-        const char* sp = s_mem + (l & 1) * S::kStageBytes;
-        const char* sq = sp + S::BM * kLine * 2;
+        const char* sp = s_mem + (l & 1) * Stage<S, RP, RQ>::kBytes;
+        const char* sq = sp + Stage<S, RP, RQ>::kQ;
         V fp[2][FM], fq[2][FN];
 #pragma unroll
         for (int h = 0; h < 2; h++) {
@@ -170,14 +275,16 @@ __device__ __forceinline__ void main_loop_paired(f4 (&acc)[S::WM / 16][S::WN / 1
 #pragma unroll
             for (int c2 = 0; c2 < 2; c2++) {
                 if (PLANES == 1 && c2 != h) continue;
-#pragma unroll
-                for (int v = 0; v < FN; v++)
-                    if (PLANES == 1 || h == 0) fq[c2][v] = RQ::read(sq, wj + 16 * v, c2, lane);
-#pragma unroll
-                for (int u = 0; u < FM; u++)
-                    if (PLANES == 1 || u / (FM / 2) == h) fp[c2][u] = RP::read(sp, wi + 16 * u, c2, lane);
+                if (kFetchFirst && h == 0 && l + 1 < lines) fetch(l + 1, (l + 1) & 1);
+                if (RQ::kWaits) {
+                    RP::read(fp[c2], 0, FM, sp, wi, c2, lane);
+                    RQ::read(fq[c2], 0, FN, sq, wj, c2, lane);
+                } else {
+                    if (PLANES == 1 || h == 0) RQ::read(fq[c2], 0, FN, sq, wj, c2, lane);
+                    RP::read(fp[c2], PLANES == 1 ? 0 : h * FM / 2, PLANES == 1 ? FM : FM / 2, sp, wi, c2, lane);
+                }
             }
-            if (h == 0 && l + 1 < lines) fetch(l + 1, (l + 1) & 1);
+            if (!kFetchFirst && h == 0 && l + 1 < lines) fetch(l + 1, (l + 1) & 1);
             if (second && h == 1) __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
             __builtin_amdgcn_s_waitcnt(0xc07f);                        // lgkmcnt(0)
             phase_barrier();

@@ -489,3 +489,26 @@ def test_refusals():
     big = torch.randn(600, 64, device="cuda")
     with pytest.raises(hc.HCError):
         hc.hc_linear(big, big, torch.empty(600, 600, device="cuda"), ws[:256])
+
+
+# sizes that take each of the tiles: 256 (whole ones, cut ones, a ragged edge), 128 and 64
+TILED = [(2100, 1000, 520), (4096, 4096, 192), (1030, 2056, 72), (520, 264, 4104), (8200, 264, 136), (333, 520, 1000)]
+
+
+@pytest.mark.parametrize("m,n,k", TILED)
+@pytest.mark.parametrize("dtype", TYPES)
+def test_tiles(m, n, k, dtype):
+    torch, hc = _hc()
+    dt = getattr(torch, dtype)
+    L = Layer(torch, m, n, k, dtype, 8, 8)
+    y, z = torch.empty(m, n, device="cuda", dtype=dt), torch.empty(m, n, device="cuda", dtype=dt)
+    ws = hc.alloc_linear_workspace(L.x, L.w).fill_(0xFF)
+    hc.hc_linear(L.x, L.w, y, ws, bias=L.bias, residual=L.residual, z=z, act="gelu", p=0.1, seed=m, draw=n)
+    check_linear(torch, L, y, z, "gelu", 0.1, m, n, True, True)
+    for act, p, out in (("none", 0.0, "float32"), ("silu", 0.1, "float32"), ("gelu", 0.1, dtype)):
+        wide = getattr(torch, out)
+        dx, dw, db = torch.empty(m, k, device="cuda", dtype=dt), torch.empty(n, k, device="cuda", dtype=wide), \
+            torch.empty(n, device="cuda", dtype=wide)
+        ws = hc.alloc_linear_grad_workspace(L.x, L.w).fill_(0xFF)
+        hc.hc_linear_grad(L.dy, ws, x=L.x, w=L.w, z=L.z, dx=dx, dw=dw, db=db, act=act, p=p, seed=m, draw=n)
+        check_grad(torch, L, act, p, m, n, dx, dw, db, out)

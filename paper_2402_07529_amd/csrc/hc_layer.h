@@ -40,9 +40,9 @@ __device__ __forceinline__ MaskBits mask_bits(const Masks& m, uint32_t row, uint
 #pragma unroll
     for (int i = 0; i < 10; i++) {
         const uint64_t p = (uint64_t)a * 0xD2511F53u, q = (uint64_t)c * 0xCD9E8D57u;
-        a = (uint32_t)(q >> 32) ^ b ^ k0;
+        a = __builtin_amdgcn_bitop3_b32((uint32_t)(q >> 32), b, k0, 0x96);  // exclusive or
         b = (uint32_t)q;
-        c = (uint32_t)(p >> 32) ^ d ^ k1;
+        c = __builtin_amdgcn_bitop3_b32((uint32_t)(p >> 32), d, k1, 0x96);
         d = (uint32_t)p;
         k0 += 0x9E3779B9u;
         k1 += 0xBB67AE85u;
@@ -157,6 +157,31 @@ template <typename T> __device__ __forceinline__ float backward(uint32_t act, fl
         case HC_ACT_TANH: return g * (4.0f * logistic_slope<T>(2.0f * z));
         case HC_ACT_SIGMOID: return g * logistic_slope<T>(z);
         default: return g;
+    }
+}
+
+// Eight at once: one branch on the activation.
+template <typename T> __device__ __forceinline__ void activate8(uint32_t act, float (&v)[8]) {
+    switch (act) {
+#define HC_CASE(ACT)                                          \
+    case ACT:                                                 \
+        _Pragma("unroll") for (int e = 0; e < 8; e++) v[e] = activate<T>(ACT, v[e]); \
+        break;
+        HC_CASE(HC_ACT_RELU) HC_CASE(HC_ACT_GELU) HC_CASE(HC_ACT_SILU) HC_CASE(HC_ACT_TANH) HC_CASE(HC_ACT_SIGMOID)
+#undef HC_CASE
+        default: break;
+    }
+}
+
+template <typename T> __device__ __forceinline__ void backward8(uint32_t act, const float (&z)[8], float (&v)[8]) {
+    switch (act) {
+#define HC_CASE(ACT)                                          \
+    case ACT:                                                 \
+        _Pragma("unroll") for (int e = 0; e < 8; e++) v[e] = backward<T>(ACT, z[e], v[e]); \
+        break;
+        HC_CASE(HC_ACT_RELU) HC_CASE(HC_ACT_GELU) HC_CASE(HC_ACT_SILU) HC_CASE(HC_ACT_TANH) HC_CASE(HC_ACT_SIGMOID)
+#undef HC_CASE
+        default: break;
     }
 }
 

@@ -34,9 +34,7 @@ __device__ __forceinline__ void finish_forward(const Forward& f, const Masks& ma
         for (int e = 0; e < 8; e++) v[e] += b[e];
     }
     if (f.z) store8(static_cast<T*>(f.z) + row * f.z_ld + col, count, v);
-    if (f.act != HC_ACT_NONE)
-#pragma unroll
-        for (int e = 0; e < 8; e++) v[e] = activate<T>(f.act, v[e]);
+    activate8<T>(f.act, v);
     if (masks.limit) drop8(masks, (uint32_t)row, col / 8, v);
     if (f.residual) {
         float r[8];
@@ -510,19 +508,13 @@ __global__ __launch_bounds__(S::EM * 4) void join_kernel(Product g) {
 
 // ---- operands as the tiles take them --------------------------------------------------
 
-// v = the sum of three bf16 values, exactly where v is normal and no smaller than
-// 2^-110.  The first is rounded, so that signs differ and what a product leaves out
-// does not add up, but not up to infinity; infinity and NaN leave nothing.
+// v = the sum of three bf16 values, exactly where v is no smaller than 2^-110.  The
+// first is cut off, so that none becomes infinite, the others are rounded; infinity
+// leaves nothing, NaN is NaN in all.
 __device__ __forceinline__ void split3(float v, __bf16 (&w)[3]) {
-    const uint32_t bits = __builtin_bit_cast(uint32_t, v);
-    w[0] = (__bf16)v;
-    if ((bits & 0x7fffffffu) >= 0x7f7f8000u) {  // rounds to infinity, or is not finite
-        if ((bits & 0x7fffffffu) < 0x7f800000u)
-            w[0] = (__bf16)__builtin_bit_cast(float, bits & 0xffff0000u);
-        else
-            v = 0.0f;
-    }
-    const float r = v == 0.0f ? 0.0f : v - (float)w[0];
+    const uint32_t high = __builtin_bit_cast(uint32_t, v) & 0xffff0000u;
+    w[0] = __builtin_bit_cast(__bf16, (uint16_t)(high >> 16));
+    const float r = fabsf(v) == __builtin_inff() ? 0.0f : v - __builtin_bit_cast(float, high);
     w[1] = (__bf16)r;
     w[2] = (__bf16)(r - (float)w[1]);
 }
@@ -571,7 +563,7 @@ struct DzArgs {
     uint32_t n, groups;
     uint32_t act;
     uint32_t per;      // rows of a workgroup
-    uint32_t width;    // lanes for a row, a power of two up to 64
+    uint32_t width;    // lanes for a row, up to 64
     Dropout drop;
     PackArgs dz;       // where it goes (out: or null), zeros behind its columns
     uint32_t planes;   // 1: in its own type; 2: and 2^11 times the rest; 3: bf16 parts
@@ -582,11 +574,11 @@ struct DzArgs {
 template <typename T> __global__ __launch_bounds__(256) void dz_kernel(DzArgs a) {
     __shared__ float s_sum[256 * 8];
     const Masks masks = masks_of(a.drop);
-    const uint32_t group = blockIdx.x * a.width + threadIdx.x % a.width, sub = threadIdx.x / a.width;
-    const uint32_t step = 256 / a.width, col = group * 8;
+    const uint32_t lane = threadIdx.x % a.width, sub = threadIdx.x / a.width, step = 256 / a.width;
+    const uint32_t group = blockIdx.x * a.width + lane, col = group * 8;
     const uint64_t end = min((uint64_t)(blockIdx.y + 1) * a.per, a.m);
     float sum[8] = {};
-    if (group < a.groups) {
+    if (group < a.groups && sub < step) {
         const uint32_t count = col < a.n ? a.n - col : 0;
         for (uint64_t row = (uint64_t)blockIdx.y * a.per + sub; row < end; row += step) {
             float v[8];
@@ -595,14 +587,13 @@ template <typename T> __global__ __launch_bounds__(256) void dz_kernel(DzArgs a)
             if (a.act != HC_ACT_NONE) {
                 float z[8];
                 load8(static_cast<const T*>(a.z) + row * a.z_ld + col, count, z);
-#pragma unroll
-                for (int e = 0; e < 8; e++) v[e] = backward<T>(a.act, z[e], v[e]);
+                backward8<T>(a.act, z, v);
             }
+            if (count < 8)
 #pragma unroll
-            for (int e = 0; e < 8; e++) {
-                v[e] = (uint32_t)e < count ? v[e] : 0.0f;
-                sum[e] += v[e];
-            }
+                for (int e = 0; e < 8; e++) v[e] = (uint32_t)e < count ? v[e] : 0.0f;
+#pragma unroll
+            for (int e = 0; e < 8; e++) sum[e] += v[e];
             if (!a.dz.out) continue;
             const uint64_t at = row * a.dz.out_ld + col;
             if (a.planes == 3) {
@@ -633,20 +624,20 @@ template <typename T> __global__ __launch_bounds__(256) void dz_kernel(DzArgs a)
     }
 }
 
-// db: the workgroups' sums, 64 columns a workgroup, in 16 shares that are added
-// in order.
+// db: the workgroups' sums, 16 columns a workgroup, in 64 shares that are added in
+// order.
 __global__ __launch_bounds__(1024) void bias_kernel(const float* __restrict__ part, uint32_t blocks, uint32_t n,
                                                     Gradient g) {
-    __shared__ float s_sum[16][64];
-    const uint32_t lane = threadIdx.x & 63, share = threadIdx.x >> 6, col = blockIdx.x * 64 + lane;
+    __shared__ float s_sum[64][17];
+    const uint32_t lane = threadIdx.x & 15, share = threadIdx.x >> 4, col = blockIdx.x * 16 + lane;
     float t = 0.0f;
     if (col < n)
-        for (uint32_t b = blocks * share / 16; b < blocks * (share + 1) / 16; b++) t += part[(uint64_t)b * n + col];
+        for (uint32_t b = blocks * share / 64; b < blocks * (share + 1) / 64; b++) t += part[(uint64_t)b * n + col];
     s_sum[share][lane] = t;
     __syncthreads();
-    if (threadIdx.x < 64 && col < n) {
+    if (threadIdx.x < 16 && col < n) {
         t = 0.0f;
-        for (int k = 0; k < 16; k++) t += s_sum[k][lane];
+        for (int k = 0; k < 64; k++) t += s_sum[k][lane];
         float v[8] = {t};
         store_gradient(g, 0, col, 1, v);
     }
@@ -655,7 +646,7 @@ __global__ __launch_bounds__(1024) void bias_kernel(const float* __restrict__ pa
 // ---- layout and launches ------------------------------------------------------------
 
 constexpr int kCus = 256;                // of the gfx950
-constexpr uint64_t kBiasBlocks = 256;    // most workgroups along the rows of dz
+constexpr uint64_t kDzGroups = 2048;     // workgroups of dz
 
 uint64_t up(uint64_t v, uint64_t to) { return (v + to - 1) / to; }
 
@@ -858,13 +849,14 @@ Layout grad_layout(const hc_linear_params& p, hc_type type) {
     size_t at = 0;
     take_packed(p, type, 2.0, at, &L);
     const uint64_t groups = L.n_ld / 8;
-    L.width = 1;
-    while (L.width < 64 && L.width < groups) L.width *= 2;
-    const uint64_t step = 256 / L.width;
-    L.per = up(up(p.m, kBiasBlocks), step) * step;
+    // as few column blocks of up to 64 lanes as there can be, evenly wide
+    const uint64_t across = up(groups, 64);
+    L.width = (uint32_t)up(groups, across);
+    const uint64_t step = 256 / L.width, most = across < kDzGroups ? kDzGroups / across : 1;
+    L.per = up(up(p.m, most), step) * step;
     L.blocks = p.m ? up(p.m, L.per) : 0;
     L.dz = take(at, p.m * L.n_ld * (type == HC_T_F32 ? (L.pack ? 6 : 4) : type == HC_T_BF16 ? 6 : 4));
-    L.bias = take(at, kBiasBlocks * p.n * 4);
+    L.bias = take(at, (p.m < most ? p.m : most) * p.n * 4);
     const size_t a = most_part_bytes(p.m, p.k), b = most_part_bytes(p.n, p.k);
     L.part = take(at, a > b ? a : b);
     L.bytes = at;
@@ -976,7 +968,7 @@ hipError_t launch_linear_grad(const hc_linear_params& p, const Dropout& d, hc_ty
     if (q.db) {
         Gradient b = gradient;
         b.out = q.db;
-        hipLaunchKernelGGL(bias_kernel, dim3((uint32_t)up(p.n, 64)), dim3(1024), 0, s,
+        hipLaunchKernelGGL(bias_kernel, dim3((uint32_t)up(p.n, 16)), dim3(1024), 0, s,
                            reinterpret_cast<const float*>(ws + L.bias), (uint32_t)L.blocks, (uint32_t)p.n, b);
         e = hipGetLastError();
         if (e != hipSuccess) return e;

@@ -59,64 +59,65 @@ __device__ __forceinline__ void drop8(const Masks& m, uint32_t row, uint32_t gro
 
 // ---- activations -----------------------------------------------------------------
 
-// exp of the type's accuracy: the hardware's exponential is within 2 units of 24
-// bits plus |v| of them, far below half a unit of 11.
+// exp of the type's accuracy.  The hardware's 2^p is within a unit of 24 bits, but
+// p = v log2 e is rounded, which is |v| such units of the result: far below half a
+// unit of 11 bits, and for fp32 put right by the first term of what was lost.
 template <typename T> __device__ __forceinline__ float exp_of(float v) {
-    if constexpr (sizeof(T) == 4) return expf(v);
-    return __expf(v);
+    constexpr float kLog2e = 1.44269504088896341f, kLog2eRest = 1.92596299e-8f;
+    if constexpr (sizeof(T) != 4) return __builtin_amdgcn_exp2f(v * kLog2e);
+    v = v > 88.0f ? 88.0f : v < -104.0f ? -104.0f : v;  // infinity would meet its correction
+    const float p = v * kLog2e, rest = __builtin_fmaf(v, kLog2e, -p) + v * kLog2eRest;
+    const float e = __builtin_amdgcn_exp2f(p);
+    return __builtin_fmaf(e, 0.69314718055994531f * rest, e);
 }
 
 // v from below at a finite value, where the functions are 0 already in fp32: what
 // is left of minus infinity then is the limit, not infinity times zero.  NaN stays.
 __device__ __forceinline__ float above(float v, float least) { return v < least ? least : v; }
 
-// The normal distribution's Phi(z) and density phi(z).  16-bit types: Phi(-a) =
-// exp(-a^2 / 2) G(a), G by a polynomial of eighth degree in 1 / (1 + 0.24 a) fitted
-// to it in relative error (4.3e-7, 7.3e-7 with fp32 arithmetic: a gradient in 32
-// bits gets it too); 21 operations where erfcf and expf take some 60.
+// The normal distribution's Phi(z) and density phi(z): Phi(-a) = exp(-a^2 / 2) G(a),
+// G by a polynomial of eighth degree in 1 / (1 + 0.24 a) fitted to it in relative
+// error (4.3e-7, 7.3e-7 with fp32 arithmetic); 21 operations, where the device
+// library's erfc and exp take some 60 and make the tiles' results too long to unroll.
 template <typename T> __device__ __forceinline__ void normal(float z, float& cdf, float& density) {
-    if constexpr (sizeof(T) == 4) {
-        cdf = 0.5f * erfcf(-0.70710678118654752f * z);
-        density = 0.39894228040143268f * expf(-0.5f * z * z);
-    } else {
-        const float e = __expf(-0.5f * z * z), a = fabsf(z);
-        const float t = __builtin_amdgcn_rcpf(1.0f + 0.24f * a);
-        float g = -0.052992403507232666f;
-        g = g * t + 0.15279580652713776f;
-        g = g * t - 0.06570429354906082f;
-        g = g * t + 0.11838865280151367f;
-        g = g * t + 0.06339804083108902f;
-        g = g * t + 0.09283839911222458f;
-        g = g * t + 0.0955221951007843f;
-        g = g * t + 0.09575378894805908f;
-        g *= t * e;
-        cdf = z < 0.0f ? g : 1.0f - g;
-        density = 0.39894228040143268f * e;
-    }
+    const float a = fabsf(z), e = exp_of<T>(-0.5f * z * z);
+    const float t = __builtin_amdgcn_rcpf(1.0f + 0.24f * a);
+    float g = -0.052992403507232666f;
+    g = g * t + 0.15279580652713776f;
+    g = g * t - 0.06570429354906082f;
+    g = g * t + 0.11838865280151367f;
+    g = g * t + 0.06339804083108902f;
+    g = g * t + 0.09283839911222458f;
+    g = g * t + 0.0955221951007843f;
+    g = g * t + 0.09575378894805908f;
+    g *= t * e;
+    cdf = z < 0.0f ? g : 1.0f - g;
+    density = 0.39894228040143268f * e;
 }
 
-template <typename T> __device__ __forceinline__ float inverse_of(float v) {
-    if constexpr (sizeof(T) == 4) return 1.0f / v;
-    return __builtin_amdgcn_rcpf(v);  // within one unit of 24 bits
-}
+// 1 / v within a unit of 24 bits.
+__device__ __forceinline__ float inverse_of(float v) { return __builtin_amdgcn_rcpf(v); }
 
 template <typename T> __device__ __forceinline__ float logistic(float z) {
-    return inverse_of<T>(1.0f + exp_of<T>(-z));
+    return inverse_of(1.0f + exp_of<T>(-z));
 }
 
 // The logistic function's slope e / (1 + e)^2, e = exp(-|z|): nothing cancels.
 template <typename T> __device__ __forceinline__ float logistic_slope(float z) {
-    const float e = exp_of<T>(-fabsf(z)), r = inverse_of<T>(1.0f + e);
+    const float e = exp_of<T>(-fabsf(z)), r = inverse_of(1.0f + e);
     return e * r * r;
 }
 
+// Near 0, where the quotient would cancel, the series up to z^11, 4e-9 off.
 template <typename T> __device__ __forceinline__ float hyperbolic(float z) {
-    if constexpr (sizeof(T) == 4) return tanhf(z);
-    // near 0 the quotient would cancel: its series up to z^5, 17/315 z^6 off
-    const float s = z * z;
-    const float e = __expf(-2.0f * fabsf(z));
-    const float q = (1.0f - e) * __builtin_amdgcn_rcpf(1.0f + e);
-    return s < 0.01f ? z * (1.0f + s * (-0.33333333333f + s * 0.13333333333f)) : __builtin_copysignf(q, z);
+    const float s = z * z, e = exp_of<T>(-2.0f * fabsf(z));
+    const float q = (1.0f - e) * inverse_of(1.0f + e);
+    float c = -8.8632355299e-3f;
+    c = c * s + 2.1869488536e-2f;
+    c = c * s - 5.3968253968e-2f;
+    c = c * s + 1.3333333333e-1f;
+    c = c * s - 3.3333333333e-1f;
+    return s < 0.1f ? z + z * s * c : __builtin_copysignf(q, z);
 }
 
 template <typename T> __device__ __forceinline__ float activate(uint32_t act, float z) {
@@ -201,6 +202,18 @@ __device__ __forceinline__ void load8(const T* __restrict__ p, uint32_t count, f
     } else {
 #pragma unroll
         for (int e = 0; e < 8; e++) v[e] = (uint32_t)e < count ? (float)p[e] : 0.0f;
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ void load8_raw(const T* __restrict__ p, uint32_t count, T (&v)[8]) {
+    if (count >= 8) {
+        const typename Eight<T>::V t = *reinterpret_cast<const typename Eight<T>::V*>(p);
+#pragma unroll
+        for (int e = 0; e < 8; e++) v[e] = t[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; e++) v[e] = (uint32_t)e < count ? p[e] : (T)0.0f;
     }
 }
 

@@ -25,23 +25,18 @@ struct Forward {
 };
 
 template <typename T>
-__device__ __forceinline__ void finish_forward(const Forward& f, const Masks& masks, uint64_t row,
-                                               uint32_t col, uint32_t count, float (&v)[8]) {
-    if (f.bias) {
-        float b[8];
-        load8(static_cast<const T*>(f.bias) + col, count, b);
+__device__ __forceinline__ void finish_forward(const Forward& f, const Masks& masks, uint64_t row, uint64_t rows,
+                                               uint32_t col, uint32_t count, const float (&bias)[8],
+                                               const T (&residual)[8], float (&v)[8]) {
+    if (row >= rows || count == 0) return;
 #pragma unroll
-        for (int e = 0; e < 8; e++) v[e] += b[e];
-    }
+    for (int e = 0; e < 8; e++) v[e] += bias[e];
     if (f.z) store8(static_cast<T*>(f.z) + row * f.z_ld + col, count, v);
     activate8<T>(f.act, v);
     if (masks.limit) drop8(masks, (uint32_t)row, col / 8, v);
-    if (f.residual) {
-        float r[8];
-        load8(static_cast<const T*>(f.residual) + row * f.residual_ld + col, count, r);
+    if (f.residual)
 #pragma unroll
-        for (int e = 0; e < 8; e++) v[e] += r[e];
-    }
+        for (int e = 0; e < 8; e++) v[e] += (float)residual[e];
     store8(static_cast<T*>(f.y) + row * f.y_ld + col, count, v);
 }
 
@@ -83,9 +78,18 @@ template <Kind KIND, typename T>
 __device__ __forceinline__ void finish8(const Product& g, const Masks& masks, uint64_t row, uint32_t col,
                                         float (&v)[8]) {
     const uint32_t count = g.cols - col;
-    if constexpr (KIND == FORWARD) finish_forward<T>(g.forward, masks, row, col, count, v);
-    else if constexpr (KIND == DX) store8(static_cast<T*>(g.gradient.out) + row * g.gradient.ld + col, count, v);
-    else store_gradient(g.gradient, row, col, count, v);
+    if constexpr (KIND == FORWARD) {
+        const Forward& f = g.forward;
+        float bias[8] = {};
+        T residual[8];
+        if (f.bias) load8(static_cast<const T*>(f.bias) + col, count, bias);
+        if (f.residual) load8_raw(static_cast<const T*>(f.residual) + row * f.residual_ld + col, count, residual);
+        finish_forward<T>(f, masks, row, g.rows, col, count, bias, residual, v);
+    } else if constexpr (KIND == DX) {
+        store8(static_cast<T*>(g.gradient.out) + row * g.gradient.ld + col, count, v);
+    } else {
+        store_gradient(g.gradient, row, col, count, v);
+    }
 }
 
 // ---- products of any shape, stride and alignment -----------------------------------
@@ -254,9 +258,10 @@ __global__ __launch_bounds__(256) void direct_join_kernel(Product g) {
 // Where a wave's loads of one operand's tile go.  ROWS: of the tile.  Along rows
 // a load is 8 rows of 128 bytes, across them 512 / ROWS lines of 2 ROWS bytes;
 // lane i writes 16 bytes at 16 i of 1024, so it reads the chunk that belongs
-// there.  Bounds are the buffer's: what lies behind the operand's last element
-// reads as zero, and so do chunks past the end of l in its rows, whose lanes get
-// an offset behind any buffer.  A stored row is a multiple of 8 elements, so that no
+// there.  Bounds are the buffer's, which begins at each step anew: rows and lines
+// behind the last read as zero, and so do chunks past the end of l in its rows, whose
+// lanes get an offset behind any buffer.  Columns behind the last give what follows
+// them in memory, for results that are not stored; of the last line they read as zero.  A stored row is a multiple of 8 elements, so that no
 // chunk ends in the middle of a buffer.
 constexpr uint32_t kNowhere = 0x80000000u;
 
@@ -270,41 +275,52 @@ template <bool ACROSS, int ROWS, int WAVES> struct Loads {
     static constexpr uint32_t kBlock = ACROSS ? Across<ROWS>::kBlock : 1024;
     uint32_t at[N];
     uint32_t chunk;      // along rows: the first of the lane's 8 values of l
+    uint32_t ld2;        // bytes from line to line
+    uint32_t bytes;      // along rows: the tile's buffer; across: of its last line
+    const char* first;   // of the tile in plane 0
     const char* base;    // of this step
-    uint64_t left;       // bytes from there to the end of the plane
-    uint64_t step;       // bytes
-    const char* first;   // of plane 0
-    uint64_t all, plane_bytes;
+    uint64_t plane_bytes;
 
-    // lines: stored rows of the operand, of `cols` elements; row0: of the tile
-    __device__ __forceinline__ void init(const void* p, uint64_t ld, uint64_t cols, uint64_t plane,
-                                         uint64_t lines, uint64_t row0, uint32_t wave, uint32_t lane) {
+    __device__ __forceinline__ void init(uint64_t ld, uint64_t plane, uint32_t wave, uint32_t lane) {
+        ld2 = (uint32_t)(2 * ld);
 #pragma unroll
         for (int u = 0; u < N; u++) {
             const uint32_t line = (wave * N + u) * kLines + lane / kChunks;
             const uint32_t c = (lane % kChunks) ^ (ACROSS ? Across<ROWS>::turn(line) : line & 7u);
-            at[u] = line * (uint32_t)(2 * ld) + c * 16;
+            at[u] = line * ld2 + c * 16;
             if (!ACROSS) chunk = c * 8;
         }
-        const uint64_t before = 2 * row0 * (ACROSS ? 1 : ld);
-        first = static_cast<const char*>(p) + before;
-        all = 2 * ((lines - 1) * ld + cols) - before;
-        step = ACROSS ? 128 * ld : 128;
         plane_bytes = 2 * plane;
     }
-    __device__ __forceinline__ void seek(uint32_t plane, uint32_t l) {
-        base = first + plane * plane_bytes + l * step;
-        left = all - l * step;
+    // lines: stored rows of the operand, of `cols` elements; row0: of the tile
+    __device__ __forceinline__ void tile(const void* p, uint64_t cols, uint64_t lines, uint64_t row0) {
+        first = static_cast<const char*>(p) + row0 * (ACROSS ? 2 : ld2);
+        if (ACROSS) bytes = 2 * (uint32_t)min((uint64_t)ROWS, cols - row0);
+        else bytes = ((uint32_t)min((uint64_t)ROWS, lines - row0) - 1) * ld2 + 2 * (uint32_t)min((uint64_t)64, cols);
     }
-    // l_left: values of l from this step on
-    __device__ __forceinline__ void fetch(char* tile, uint32_t wave, uint64_t l_left) {
-        const __amdgpu_buffer_rsrc_t r = buffer_rsrc(base, (uint32_t)(left < kNowhere ? left : kNowhere));
-        const bool out = !ACROSS && l_left < 64 && chunk >= (uint32_t)l_left;
+    __device__ __forceinline__ void seek(uint32_t plane, uint32_t l) {
+        base = first + plane * plane_bytes + (uint64_t)l * (ACROSS ? ld2 : 2) * 64;
+    }
+    // left: values of l from this step on
+    __device__ __forceinline__ void fetch(char* tile, uint32_t wave, uint32_t left) {
+        char* to = tile + wave * (N * kBlock);
+        if constexpr (ACROSS) {
+            const __amdgpu_buffer_rsrc_t r = buffer_rsrc(base, (min(left, 64u) - 1) * ld2 + bytes);
 #pragma unroll
-        for (int u = 0; u < N; u++)
-            load_to_lds(r, tile + (wave * N + u) * kBlock, out ? kNowhere : at[u]);
-        base += step;
-        left -= step;
+            for (int u = 0; u < N; u++) load_to_lds(r, to + u * kBlock, at[u]);
+            base += (uint64_t)ld2 * 64;
+        } else {
+            const __amdgpu_buffer_rsrc_t r = buffer_rsrc(base, bytes);
+            if (left >= 64) {
+#pragma unroll
+                for (int u = 0; u < N; u++) load_to_lds(r, to + u * kBlock, at[u]);
+            } else {
+#pragma unroll
+                for (int u = 0; u < N; u++)
+                    load_to_lds(r, to + u * kBlock, chunk < left ? at[u] : kNowhere);
+            }
+            base += 128;
+        }
     }
 };
 
@@ -315,61 +331,8 @@ template <Kind KIND, typename V, typename S> struct Reads {
     typedef typename std::conditional<kPAcross<KIND>, AcrossRows<V, S::BM>, Along>::type P;
     typedef typename std::conditional<kQAcross<KIND>, AcrossRows<V, S::BN>, Along>::type Q;
     typedef Stage<S, P, Q> InLds;
-    // the tiles of all stages, or the results
-    static constexpr uint32_t kTiles = S::kStages * InLds::kBytes, kResults = S::kWaves * S::EM * S::EN * 4;
-    static constexpr uint32_t kLdsBytes = kTiles > kResults ? kTiles : kResults;
+    static constexpr uint32_t kLdsBytes = S::kStages * InLds::kBytes;
 };
-
-// Steps [s0, s1) of all passes' steps of a tile, added to acc.
-template <Kind KIND, typename V, typename S>
-__device__ __forceinline__ void accumulate(const Product& g, uint32_t ti, uint32_t tj, uint32_t s0,
-                                           uint32_t s1, char* s_mem, f4 (&acc)[S::WM / 16][S::WN / 16]) {
-    constexpr bool PA = kPAcross<KIND>, QA = kQAcross<KIND>;
-    typedef Reads<KIND, V, S> R;
-    const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
-    const uint32_t wi = wave / (S::BN / S::WN) * S::WM, wj = wave % (S::BN / S::WN) * S::WN;
-    Loads<PA, S::BM, S::kWaves> lp;
-    Loads<QA, S::BN, S::kWaves> lq;
-    lp.init(g.p, g.p_ld, g.p_cols, g.p_plane, PA ? g.inner : g.rows, (uint64_t)ti * S::BM, wave, lane);
-    lq.init(g.q, g.q_ld, g.q_cols, g.q_plane, QA ? g.inner : g.cols, (uint64_t)tj * S::BN, wave, lane);
-    const uint32_t lines = (uint32_t)((g.inner + 63) / 64);
-    uint32_t pass = s0 / lines, l = s0 - pass * lines;
-    auto seek = [&]() {
-        lp.seek(g.passes.p_planes >> 4 * pass & 15u, l);
-        lq.seek(g.passes.q_planes >> 4 * pass & 15u, l);
-    };
-    // called for one step after the other
-    auto fetch = [&](uint32_t, uint32_t buf) {
-        char* base = s_mem + buf * R::InLds::kBytes;
-        const uint64_t l_left = g.inner - (uint64_t)l * 64;
-        lp.fetch(base, wave, l_left);
-        lq.fetch(base + R::InLds::kQ, wave, l_left);
-        if (++l == lines) {
-            l = 0;
-            pass++;
-            seek();
-        }
-    };
-    seek();
-    auto run = [&](uint32_t steps) {
-        fetch(0, 0);
-        if constexpr (S::kWaves == 8)
-            main_loop_paired<1, S, V, typename R::P, typename R::Q>(acc, fetch, s_mem, steps, wi, wj, lane, wave);
-        else
-            main_loop<1, S, V, typename R::P, typename R::Q>(acc, fetch, s_mem, steps, wi, wj, lane);
-        __syncthreads();
-    };
-    if (KIND == DW && g.passes.factor != 1.0f && s0 < lines) {
-        const uint32_t stop = min(s1, lines);
-        run(stop - s0);
-#pragma unroll
-        for (int u = 0; u < S::WM / 16; u++)
-#pragma unroll
-            for (int v = 0; v < S::WN / 16; v++) acc[u][v] *= g.passes.factor;
-        s0 = stop;
-    }
-    if (s0 < s1) run(s1 - s0);
-}
 
 // Tile t: blocks of 8 tiles along i by 4 along j, so that the tiles that an XCD
 // works on share rows of both operands in its L2.
@@ -383,26 +346,73 @@ __device__ __forceinline__ void tile_at(const Product& g, uint32_t t, uint32_t& 
     tj = 4 * stripe + t / h;
 }
 
-// A block's sums in LDS become results, eight columns of a row a lane.
-template <Kind KIND, typename T, typename S, int LANES>
-__device__ __forceinline__ void finish_block(const Product& g, const Masks& masks, const float* stage,
-                                             uint64_t ib, uint32_t jb, uint32_t at) {
-    constexpr int kPer = S::EN / 8;  // lanes for a row
-#pragma unroll
-    for (int k = 0; k < S::EM * S::EN / 8 / LANES; k++) {
-        const uint32_t q = at + k * LANES, ii = q / kPer, jj = q % kPer * 8;
-        const uint64_t row = ib + ii;
-        const uint32_t col = jb + jj;
-        float v[8];
-#pragma unroll
-        for (int h = 0; h < 2; h++) {
-            const f4 w = *reinterpret_cast<const f4*>(stage + staged<S::EN>(ii, jj + 4 * h));
-#pragma unroll
-            for (int e = 0; e < 4; e++) v[4 * h + e] = w[e];
-        }
-        if (row < g.rows && col < g.cols) finish8<KIND, T>(g, masks, row, col, v);
+// A workgroup's next work: steps [s0, s1) of all passes' steps of a tile, the whole
+// of it or a piece.
+struct Work {
+    uint32_t ti, tj, s0, s1, piece;
+    bool whole;
+};
+
+// Work i of the launch; workgroup b takes b, b + gridDim.x, ...  Whole tiles come
+// first, the tiles of each round so that an XCD has neighbouring ones; then the
+// pieces, neighbouring workgroups the same piece of neighbouring tiles.
+__device__ __forceinline__ Work work_at(const Product& g, uint32_t i, uint32_t steps) {
+    Work w = {0, 0, 0, steps, 0, i < g.whole};
+    uint32_t t;
+    if (w.whole) {
+        const uint32_t round = i / gridDim.x * gridDim.x;
+        t = round + by_xcd(i - round, min(gridDim.x, g.whole - round));
+    } else {
+        w.piece = by_xcd(i - g.whole, g.cut * g.pieces);
+        const uint32_t k = w.piece / g.cut;
+        t = g.whole + w.piece - k * g.cut;
+        w.s0 = (uint32_t)((uint64_t)k * steps / g.pieces);
+        w.s1 = (uint32_t)((uint64_t)(k + 1) * steps / g.pieces);
     }
+    tile_at(g, t, w.ti, w.tj);
+    return w;
 }
+
+// Brings the steps of a tile to LDS, one after the other.
+template <Kind KIND, typename V, typename S> struct Feed {
+    static constexpr bool PA = kPAcross<KIND>, QA = kQAcross<KIND>;
+    typedef typename Reads<KIND, V, S>::InLds InLds;
+    Loads<PA, S::BM, S::kWaves> lp;
+    Loads<QA, S::BN, S::kWaves> lq;
+    char* s_mem;
+    uint32_t inner, wave, lines, pass, l, p_planes, q_planes;
+
+    __device__ __forceinline__ Feed(const Product& g, char* s_mem_, uint32_t wave_, uint32_t lane)
+        : s_mem(s_mem_), inner((uint32_t)g.inner), wave(wave_), lines((uint32_t)((g.inner + 63) / 64)),
+          p_planes(g.passes.p_planes), q_planes(g.passes.q_planes) {
+        lp.init(g.p_ld, g.p_plane, wave, lane);
+        lq.init(g.q_ld, g.q_plane, wave, lane);
+    }
+    __device__ __forceinline__ void seek() {
+        lp.seek(p_planes >> 4 * pass & 15u, l);
+        lq.seek(q_planes >> 4 * pass & 15u, l);
+    }
+    // the first step is on its way then
+    __device__ __forceinline__ void begin(const Product& g, const Work& w) {
+        lp.tile(g.p, g.p_cols, PA ? g.inner : g.rows, (uint64_t)w.ti * S::BM);
+        lq.tile(g.q, g.q_cols, QA ? g.inner : g.cols, (uint64_t)w.tj * S::BN);
+        pass = w.s0 / lines;
+        l = w.s0 - pass * lines;
+        seek();
+        fetch(0);
+    }
+    __device__ __forceinline__ void fetch(uint32_t buf) {
+        char* base = s_mem + buf * InLds::kBytes;
+        const uint32_t left = inner - l * 64;
+        lp.fetch(base, wave, left);
+        lq.fetch(base + InLds::kQ, wave, left);
+        if (++l == lines) {
+            l = 0;
+            pass++;
+            seek();
+        }
+    }
+};
 
 template <Kind KIND> __device__ __forceinline__ Masks masks_for(const Product& g) {
     Masks masks = {};
@@ -410,111 +420,199 @@ template <Kind KIND> __device__ __forceinline__ Masks masks_for(const Product& g
     return masks;
 }
 
-// A tile a workgroup, or a piece of one.  Neighbouring workgroups take the same
-// piece of neighbouring tiles.
+// Two neighbouring fragments of a lane, 4 columns of a row each, become 8
+// neighbouring columns: odd groups of 16 lanes of the first change places with even
+// ones of the second.  Lane group q then has columns 16 (q mod 2) + 8 (q div 2) .. + 7
+// of the 32, so that four lanes store 64 bytes of a 16-bit row.
+__device__ __forceinline__ uint32_t paired_col(uint32_t lane) { return (lane & 16u) + (lane >> 5) * 8; }
+__device__ __forceinline__ void pair_up(const f4& a, const f4& b, float (&v)[8]) {
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+        const float x = a[e], y = b[e];
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+        const uint32_t first = r[0], second = r[1];
+        v[e] = __uint_as_float(first);
+        v[4 + e] = __uint_as_float(second);
+    }
+}
+
+// f(0), f(STEP), ... below END, unrolled however long they are: an index into the sums
+// that is not a constant would put them all in memory.
+template <int END, int STEP, int I = 0, typename F> __device__ __forceinline__ void unrolled(const F& f) {
+    if constexpr (I < END) {
+        f(std::integral_constant<int, I>{});
+        unrolled<END, STEP, I + STEP>(f);
+    }
+}
+
+// Columns col .. col + 7 of FM rows 16 apart become results.  What is read for them
+// is asked for before the first is stored: a load behind a store would wait for it.
+template <Kind KIND, typename T, int FIRST, int FM, int FN>
+__device__ __forceinline__ void finish_rows(const Product& g, const Masks& masks, uint64_t row0, uint32_t col,
+                                            const f4 (&acc)[FM][FN]) {
+    constexpr int N = FM <= 4 ? FM : sizeof(T) == 4 ? 2 : 4;  // rows at a time
+    // every lane takes part in the exchange, also those behind the last column
+    const uint32_t count = col < g.cols ? g.cols - col : 0;
+    if constexpr (KIND == FORWARD) {
+        const Forward& f = g.forward;
+        float bias[8] = {};
+        if (f.bias) load8(static_cast<const T*>(f.bias) + col, count, bias);
+        unrolled<FM, N>([&](auto u0) __attribute__((always_inline)) {
+            T residual[N][8];
+            if (f.residual)
+#pragma unroll
+                for (int u = 0; u < N; u++)
+                    load8_raw(static_cast<const T*>(f.residual) + (row0 + 16 * (u0 + u)) * f.residual_ld + col,
+                              row0 + 16 * (u0 + u) < g.rows ? count : 0, residual[u]);
+            unrolled<N, 1>([&](auto u) __attribute__((always_inline)) {
+                float v[8];
+                pair_up(acc[u0 + u][FIRST], acc[u0 + u][FIRST + 1], v);
+                finish_forward<T>(f, masks, row0 + 16 * (u0 + u), g.rows, col, count, bias, residual[u], v);
+            });
+        });
+    } else {
+        unrolled<FM, 1>([&](auto u) __attribute__((always_inline)) {
+            float v[8];
+            pair_up(acc[u][FIRST], acc[u][FIRST + 1], v);
+            const uint64_t row = row0 + 16 * u;
+            if (row >= g.rows || count == 0) return;
+            if constexpr (KIND == DX) store8(static_cast<T*>(g.gradient.out) + row * g.gradient.ld + col, count, v);
+            else store_gradient(g.gradient, row, col, count, v);
+        });
+    }
+}
+
+// Workgroups of a CU by what LDS holds, as waves of a SIMD.
+template <typename S> constexpr int kWavesOfSimd = S::BM == 64 ? 3 : 2;
+
+// The kernel's arguments, to be loaded again: held over a main loop they would take
+// more scalar registers than there are.
+__device__ __forceinline__ const Product& again() {
+    typedef const __attribute__((address_space(4))) Product ConstantProduct;
+    ConstantProduct* p = (ConstantProduct*)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const Product*)p;
+}
+
+// A workgroup takes one tile, or piece of one, after the other.  The first step of
+// the next is on its way while results are stored.
 template <Kind KIND, typename T, typename V, typename S>
-__global__ __launch_bounds__(S::kThreads) void tiled_kernel(Product g) {
-    constexpr int FM = S::WM / 16, FN = S::WN / 16, EM = S::EM, EN = S::EN;
+__global__ __launch_bounds__(S::kThreads, kWavesOfSimd<S>) void tiled_kernel(Product g) {
+    constexpr int FM = S::WM / 16, FN = S::WN / 16;
+    typedef Reads<KIND, V, S> R;
     extern __shared__ __align__(16) char s_mem[];
     const uint32_t steps = g.passes.count * (uint32_t)((g.inner + 63) / 64);
-    const bool piece = blockIdx.x >= g.whole;
-    uint32_t t, s0 = 0, s1 = steps, w = 0;
-    if (piece) {
-        w = by_xcd(blockIdx.x - g.whole, gridDim.x - g.whole);
-        const uint32_t k = w / g.cut;
-        t = g.whole + w - k * g.cut;
-        s0 = (uint32_t)((uint64_t)k * steps / g.pieces);
-        s1 = (uint32_t)((uint64_t)(k + 1) * steps / g.pieces);
-    } else {
-        t = by_xcd(blockIdx.x, g.whole);
-    }
-    uint32_t ti, tj;
-    tile_at(g, t, ti, tj);
-    f4 acc[FM][FN] = {};
-    accumulate<KIND, V, S>(g, ti, tj, s0, s1, s_mem, acc);
-    if (piece) {
-        f4* part = reinterpret_cast<f4*>(g.part) + (size_t)w * (S::BM * S::BN / 4);
+    const uint32_t all = g.whole + g.cut * g.pieces;
+    const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    const uint32_t wi = wave / (S::BN / S::WN) * S::WM, wj = wave % (S::BN / S::WN) * S::WN;
+    const float factor = KIND == DW ? g.passes.factor : 1.0f;
+    Feed<KIND, V, S> feed(g, s_mem, wave, lane);
+    uint32_t i = blockIdx.x;
+    Work w = work_at(g, i, steps);
+    feed.begin(g, w);
+    for (;;) {
+        float zero = 0.0f;
+        asm volatile("" : "+v"(zero));  // or a register for each zero is held throughout
+        f4 acc[FM][FN];
 #pragma unroll
         for (int u = 0; u < FM; u++)
 #pragma unroll
-            for (int v = 0; v < FN; v++) part[(u * FN + v) * S::kThreads + threadIdx.x] = acc[u][v];
-        return;
-    }
-    const Masks masks = masks_for<KIND>(g);
-    const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
-    const uint64_t i0 = (uint64_t)ti * S::BM + wave / (S::BN / S::WN) * S::WM;
-    const uint32_t j0 = tj * S::BN + wave % (S::BN / S::WN) * S::WN;
-    const uint32_t fi = lane & 15, fj = (lane >> 4) * 4;
-    float* stage = reinterpret_cast<float*>(s_mem) + wave * EM * EN;
+            for (int v = 0; v < FN; v++) acc[u][v] = f4{zero, zero, zero, zero};
+        auto run = [&](uint32_t n) {
+            auto fetch = [&](uint32_t, uint32_t buf) { feed.fetch(buf); };
+            if constexpr (S::kWaves == 8)
+                main_loop_paired<1, S, V, typename R::P, typename R::Q>(acc, fetch, s_mem, n, wi, wj, lane, wave);
+            else
+                main_loop<1, S, V, typename R::P, typename R::Q>(acc, fetch, s_mem, n, wi, wj, lane);
+            __syncthreads();
+        };
+        uint32_t s0 = w.s0;
+        if (KIND == DW && factor != 1.0f && s0 < feed.lines) {
+            const uint32_t stop = min(w.s1, feed.lines);
+            run(stop - s0);
 #pragma unroll
-    for (int eu = 0; eu < S::WM / EM; eu++)
+            for (int u = 0; u < FM; u++)
 #pragma unroll
-        for (int ev = 0; ev < S::WN / EN; ev++) {
-#pragma unroll
-            for (int u = 0; u < EM / 16; u++)
-#pragma unroll
-                for (int v = 0; v < EN / 16; v++)
-                    *reinterpret_cast<f4*>(stage + staged<EN>(16 * u + fi, 16 * v + fj)) =
-                        acc[eu * (EM / 16) + u][ev * (EN / 16) + v];
-            // only this wave's results are read
-            __builtin_amdgcn_s_waitcnt(0xc07f);
-            __builtin_amdgcn_wave_barrier();
-            finish_block<KIND, T, S, 64>(g, masks, stage, i0 + eu * EM, j0 + ev * EN, lane);
-            __builtin_amdgcn_s_waitcnt(0xc07f);
-            __builtin_amdgcn_wave_barrier();
+                for (int v = 0; v < FN; v++) acc[u][v] *= factor;
+            s0 = stop;
+            if (s0 < w.s1) feed.fetch(0);
         }
+        if (s0 < w.s1) run(w.s1 - s0);
+        const Product& e = again();
+        i += gridDim.x;
+        Work next = {};
+        if (i < all) {
+            next = work_at(e, i, steps);
+            feed.begin(e, next);
+        }
+        if (w.whole) {
+            const Masks masks = masks_for<KIND>(e);
+            const uint64_t row0 = (uint64_t)w.ti * S::BM + wi + (lane & 15);
+            const uint32_t col0 = w.tj * S::BN + wj + paired_col(lane);
+            unrolled<FN, 2>([&](auto v) __attribute__((always_inline)) {
+                finish_rows<KIND, T, v>(e, masks, row0, col0 + 16 * v, acc);
+            });
+        } else {
+            f4* part = reinterpret_cast<f4*>(e.part) + (size_t)w.piece * (S::BM * S::BN / 4);
+#pragma unroll
+            for (int u = 0; u < FM; u++)
+#pragma unroll
+                for (int v = 0; v < FN; v++) part[(u * FN + v) * S::kThreads + threadIdx.x] = acc[u][v];
+        }
+        if (i >= all) return;
+        w = next;
+    }
 }
 
-// The sums of the cut tiles' pieces, in order.  A workgroup takes an EM x EN block
-// of a wave's part, a wave of it 16 rows.
-template <Kind KIND, typename T, typename S>
-__global__ __launch_bounds__(S::EM * 4) void join_kernel(Product g) {
-    constexpr int FN = S::WN / 16, EM = S::EM, EN = S::EN;
-    constexpr uint32_t kBlocks = S::kWaves * (S::WM / EM) * (S::WN / EN);  // of a tile
-    __shared__ __align__(16) float s_stage[EM * EN];
-    const uint32_t c = blockIdx.x / kBlocks, block = blockIdx.x - c * kBlocks;
-    const uint32_t wave = block % S::kWaves, sub = block / S::kWaves;
-    const uint32_t eu = sub / (S::WN / EN), ev = sub % (S::WN / EN);
-    const uint32_t lane = threadIdx.x & 63, u = threadIdx.x >> 6;
-    const f4* part = reinterpret_cast<const f4*>(g.part) +
-                     ((eu * (EM / 16) + u) * FN + ev * (EN / 16)) * S::kThreads + wave * 64 + lane;
-    constexpr int kAhead = 4;  // pieces asked for at once
-    f4 acc[EN / 16] = {};
+// The sums of the cut tiles' pieces, in order.  A wave takes two neighbouring
+// fragments of a wave's part of a tile.
+template <Kind KIND, typename T, typename S> __global__ __launch_bounds__(256) void join_kernel(Product g) {
+    constexpr uint32_t FM = S::WM / 16, FN = S::WN / 16, kPairs = S::kWaves * FM * FN / 2;  // of a tile
+    const uint32_t at = blockIdx.x * 4 + (threadIdx.x >> 6), c = at / kPairs, pair = at - c * kPairs;
+    const uint32_t wave = pair / (FM * FN / 2), u = pair / (FN / 2) % FM, v = pair % (FN / 2) * 2;
+    const uint32_t lane = threadIdx.x & 63;
+    const f4* part = reinterpret_cast<const f4*>(g.part) + (size_t)c * (S::BM * S::BN / 4) +
+                     (u * FN + v) * S::kThreads + wave * 64 + lane;
+    const size_t step = (size_t)g.cut * (S::BM * S::BN / 4);
+    constexpr uint32_t kAhead = 8;  // pieces asked for at once
+    f4 acc[1][2] = {};
     for (uint32_t q0 = 0; q0 < g.pieces; q0 += kAhead) {
-        f4 v[kAhead][EN / 16];
+        f4 a[kAhead], b[kAhead];
 #pragma unroll
-        for (int q = 0; q < kAhead; q++)
+        for (uint32_t q = 0; q < kAhead; q++)
+            if (q0 + q < g.pieces) {
+                a[q] = part[(q0 + q) * step];
+                b[q] = part[(q0 + q) * step + S::kThreads];
+            }
 #pragma unroll
-            for (int k = 0; k < EN / 16; k++)
-                if (q0 + q < g.pieces)
-                    v[q][k] = part[(c + (size_t)(q0 + q) * g.cut) * (S::BM * S::BN / 4) + k * S::kThreads];
-#pragma unroll
-        for (int q = 0; q < kAhead; q++)
-#pragma unroll
-            for (int k = 0; k < EN / 16; k++)
-                if (q0 + q < g.pieces) acc[k] += v[q][k];
+        for (uint32_t q = 0; q < kAhead; q++)
+            if (q0 + q < g.pieces) {
+                acc[0][0] += a[q];
+                acc[0][1] += b[q];
+            }
     }
     uint32_t ti, tj;
     tile_at(g, g.whole + c, ti, tj);
-    const uint64_t ib = (uint64_t)ti * S::BM + wave / (S::BN / S::WN) * S::WM + eu * EM;
-    const uint32_t jb = tj * S::BN + wave % (S::BN / S::WN) * S::WN + ev * EN;
-    const uint32_t fi = 16 * u + (lane & 15), fj = (lane >> 4) * 4;
-#pragma unroll
-    for (int v = 0; v < EN / 16; v++)
-        *reinterpret_cast<f4*>(s_stage + staged<EN>(fi, 16 * v + fj)) = acc[v];
-    lds_barrier();
-    finish_block<KIND, T, S, S::EM * 4>(g, masks_for<KIND>(g), s_stage, ib, jb, threadIdx.x);
+    const uint64_t row = (uint64_t)ti * S::BM + wave / (S::BN / S::WN) * S::WM + 16 * u + (lane & 15);
+    const uint32_t col = tj * S::BN + wave % (S::BN / S::WN) * S::WN + 16 * v + paired_col(lane);
+    finish_rows<KIND, T, 0>(g, masks_for<KIND>(g), row, col, acc);
 }
 
 // ---- operands as the tiles take them --------------------------------------------------
 
 // v = the sum of three bf16 values, exactly where v is no smaller than 2^-110.  The
-// first is cut off, so that none becomes infinite, the others are rounded; infinity
-// leaves nothing, NaN is NaN in all.
-__device__ __forceinline__ void split3(float v, __bf16 (&w)[3]) {
-    const uint32_t high = __builtin_bit_cast(uint32_t, v) & 0xffff0000u;
-    w[0] = __builtin_bit_cast(__bf16, (uint16_t)(high >> 16));
-    const float r = fabsf(v) == __builtin_inff() ? 0.0f : v - __builtin_bit_cast(float, high);
+// first is cut off, so that none becomes infinite, or rounded, where it is also used
+// alone; the others are rounded.  Infinity leaves nothing, NaN is NaN in all.
+template <bool ROUND> __device__ __forceinline__ void split3(float v, __bf16 (&w)[3]) {
+    float first;
+    if constexpr (ROUND) {
+        w[0] = (__bf16)v;
+        first = (float)w[0];
+    } else {
+        first = __uint_as_float(__float_as_uint(v) & 0xffff0000u);
+        w[0] = __builtin_bit_cast(__bf16, (uint16_t)(__float_as_uint(v) >> 16));
+    }
+    const float r = fabsf(first) == __builtin_inff() && v == v ? 0.0f : v - first;
     w[1] = (__bf16)r;
     w[2] = (__bf16)(r - (float)w[1]);
 }
@@ -526,13 +624,14 @@ struct PackArgs {
     uint32_t cols;
 };
 
-template <typename T> __device__ __forceinline__ void store_planes(const PackArgs& a, uint64_t at, const float (&v)[8]) {
+template <typename T, bool ROUND = false>
+__device__ __forceinline__ void store_planes(const PackArgs& a, uint64_t at, const float (&v)[8]) {
     if constexpr (sizeof(T) == 4) {
         b8 w[3];
 #pragma unroll
         for (int e = 0; e < 8; e++) {
             __bf16 s[3];
-            split3(v[e], s);
+            split3<ROUND>(v[e], s);
 #pragma unroll
             for (int k = 0; k < 3; k++) w[k][e] = s[k];
         }
@@ -597,7 +696,7 @@ template <typename T> __global__ __launch_bounds__(256) void dz_kernel(DzArgs a)
             if (!a.dz.out) continue;
             const uint64_t at = row * a.dz.out_ld + col;
             if (a.planes == 3) {
-                store_planes<float>(a.dz, at, v);
+                store_planes<float, sizeof(T) == 2>(a.dz, at, v);
             } else {
                 store8(static_cast<T*>(a.dz.out) + at, 8, v);
                 if (a.planes == 2) {
@@ -736,16 +835,16 @@ TilePlan tile_plan(uint64_t rows, uint64_t cols, uint64_t steps) {
 }
 
 template <Kind KIND, typename T, typename V, typename S>
-hipError_t tiled_shape(const Product& g, hipStream_t s) {
+hipError_t tiled_shape(const Product& g, uint64_t resident, hipStream_t s) {
     const auto kernel = &tiled_kernel<KIND, T, V, S>;
     constexpr int kLds = Reads<KIND, V, S>::kLdsBytes;
     const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(kernel), kLds);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kernel, dim3(g.whole + g.cut * g.pieces), dim3(S::kThreads), kLds, s, g);
-    if (g.cut) {
-        constexpr uint32_t kBlocks = S::kWaves * (S::WM / S::EM) * (S::WN / S::EN);
-        hipLaunchKernelGGL((join_kernel<KIND, T, S>), dim3(g.cut * kBlocks), dim3(S::EM * 4), 0, s, g);
-    }
+    const uint32_t all = g.whole + g.cut * g.pieces, slots = (uint32_t)(kCus * resident);
+    hipLaunchKernelGGL(kernel, dim3(all < slots ? all : slots), dim3(S::kThreads), kLds, s, g);
+    if (g.cut)
+        hipLaunchKernelGGL((join_kernel<KIND, T, S>),
+                           dim3(g.cut * (S::BM * S::BN / 512 / 4)), dim3(256), 0, s, g);
     return hipGetLastError();
 }
 
@@ -756,9 +855,10 @@ template <Kind KIND, typename T, typename V> hipError_t tiled(Product g, hipStre
     g.whole = p.whole;
     g.cut = p.cut;
     g.pieces = p.pieces;
-    if (p.shape == 0) return tiled_shape<KIND, T, V, Large>(g, s);
-    if (p.shape == 1) return tiled_shape<KIND, T, V, Medium>(g, s);
-    return tiled_shape<KIND, T, V, Small>(g, s);
+    const uint64_t resident = kTileCosts[p.shape].resident;
+    if (p.shape == 0) return tiled_shape<KIND, T, V, Large>(g, resident, s);
+    if (p.shape == 1) return tiled_shape<KIND, T, V, Medium>(g, resident, s);
+    return tiled_shape<KIND, T, V, Small>(g, resident, s);
 }
 
 // in_tiles: the operands are as the tiles take them (fp32 in three planes).

@@ -65,7 +65,7 @@ struct Product {
     Passes passes;
     uint64_t rows, inner;    // of D; length of l
     uint32_t cols;
-    uint32_t tiles_i, tiles_j;
+    uint32_t tiles_i, tiles_j, stripe;
     uint32_t whole, cut;     // tiles that a workgroup makes whole, and that are cut
     uint32_t pieces;         // along l into this many pieces
     float* part;             // the pieces' sums
@@ -334,16 +334,16 @@ template <Kind KIND, typename V, typename S> struct Reads {
     static constexpr uint32_t kLdsBytes = S::kStages * InLds::kBytes;
 };
 
-// Tile t: blocks of 8 tiles along i by 4 along j, so that the tiles that an XCD
-// works on share rows of both operands in its L2.
+// Tile t: blocks of 8 tiles along i by `stripe` along j, so that the tiles that an
+// XCD works on share rows of both operands in its L2.
 __device__ __forceinline__ void tile_at(const Product& g, uint32_t t, uint32_t& ti, uint32_t& tj) {
-    const uint32_t stripe = t / (4 * g.tiles_i);
-    t -= stripe * 4 * g.tiles_i;
-    const uint32_t w = min(4u, g.tiles_j - 4 * stripe), block = t / (8 * w);
+    const uint32_t stripe = t / (g.stripe * g.tiles_i);
+    t -= stripe * g.stripe * g.tiles_i;
+    const uint32_t w = min(g.stripe, g.tiles_j - g.stripe * stripe), block = t / (8 * w);
     t -= block * 8 * w;
     const uint32_t h = min(8u, g.tiles_i - 8 * block);
     ti = 8 * block + t % h;
-    tj = 4 * stripe + t / h;
+    tj = g.stripe * stripe + t / h;
 }
 
 // A workgroup's next work: steps [s0, s1) of all passes' steps of a tile, the whole
@@ -520,7 +520,7 @@ __global__ __launch_bounds__(S::kThreads, kWavesOfSimd<S>) void tiled_kernel(Pro
             for (int v = 0; v < FN; v++) acc[u][v] = f4{zero, zero, zero, zero};
         auto run = [&](uint32_t n) {
             auto fetch = [&](uint32_t, uint32_t buf) { feed.fetch(buf); };
-            if constexpr (S::kWaves == 8)
+            if constexpr (S::kStages == 2 && S::kWaves == 8)
                 main_loop_paired<1, S, V, typename R::P, typename R::Q>(acc, fetch, s_mem, n, wi, wj, lane, wave);
             else
                 main_loop<1, S, V, typename R::P, typename R::Q>(acc, fetch, s_mem, n, wi, wj, lane);
@@ -771,20 +771,23 @@ template <Kind KIND, typename T> hipError_t direct(Product g, hipStream_t s) {
 }
 
 typedef Shape<256, 256, 128, 64, 2> Large;
+typedef Shape<256, 128, 64, 64, 3> Tall;
 typedef Shape<128, 128, 64, 64, 2> Medium;
 typedef Shape<64, 64, 32, 32, 3> Small;
+constexpr int kShapes = 4;
 
 // Estimated times in us: a step takes a workgroup `alone` on its CU, or `shared` by
 // as many as fit; a tile's first loads and its results take `ends`, a piece's with
 // the tile of sums that it writes `piece_ends`.
 struct TileCost {
-    uint64_t tile, resident;
+    uint64_t bm, bn, resident;
     double alone, shared, ends, piece_ends;
 };
-constexpr TileCost kTileCosts[3] = {
-    {256, 1, 1.50, 1.50, 9.0, 8.0},
-    {128, 2, 0.50, 0.86, 6.0, 5.0},
-    {64, 3, 0.35, 0.70, 5.0, 4.0},
+constexpr TileCost kTileCosts[kShapes] = {
+    {256, 256, 1, 1.50, 1.50, 9.0, 8.0},
+    {256, 128, 1, 0.80, 0.80, 6.0, 5.0},
+    {128, 128, 2, 0.50, 0.86, 6.0, 5.0},
+    {64, 64, 3, 0.35, 0.70, 5.0, 4.0},
 };
 constexpr uint64_t kLeastSteps = 4;      // of a piece
 constexpr double kJoin = 5.0, kBytesPerUs = 5e6;
@@ -810,9 +813,9 @@ double rounds(const TileCost& c, uint64_t groups, double steps, double ends) {
 TilePlan tile_plan(uint64_t rows, uint64_t cols, uint64_t steps) {
     TilePlan best = {};
     double least = 1e300;
-    for (int k = 0; k < 3; k++) {
+    for (int k = 0; k < kShapes; k++) {
         const TileCost& c = kTileCosts[k];
-        const uint64_t ti = up(rows, c.tile), tj = up(cols, c.tile), n = ti * tj, slots = kCus * c.resident;
+        const uint64_t ti = up(rows, c.bm), tj = up(cols, c.bn), n = ti * tj, slots = kCus * c.resident;
         auto consider = [&](double t, uint64_t whole, uint64_t pieces) {
             if (t >= least) return;
             least = t;
@@ -827,7 +830,7 @@ TilePlan tile_plan(uint64_t rows, uint64_t cols, uint64_t steps) {
             if (pieces < 2) continue;
             const double t = rounds(c, whole, (double)steps, c.ends) +
                              rounds(c, rest * pieces, (double)up(steps, pieces), c.piece_ends) + kJoin +
-                             4.0 * (double)(c.tile * c.tile * rest * (pieces + 1)) / kBytesPerUs;
+                             4.0 * (double)(c.bm * c.bn * rest * (pieces + 1)) / kBytesPerUs;
             consider(t, whole, pieces);
         }
     }
@@ -855,9 +858,15 @@ template <Kind KIND, typename T, typename V> hipError_t tiled(Product g, hipStre
     g.whole = p.whole;
     g.cut = p.cut;
     g.pieces = p.pieces;
-    const uint64_t resident = kTileCosts[p.shape].resident;
+    const TileCost& c = kTileCosts[p.shape];
+    // as wide as Q's rows fit an XCD's L2 beside P's
+    const uint64_t panel = c.bn * g.inner * 2 * g.passes.count;
+    const uint64_t stripe = panel < (1u << 21) / 4 ? (1u << 21) / panel : 4;
+    g.stripe = (uint32_t)(stripe < p.tiles_j ? stripe : p.tiles_j);
+    const uint64_t resident = c.resident;
     if (p.shape == 0) return tiled_shape<KIND, T, V, Large>(g, resident, s);
-    if (p.shape == 1) return tiled_shape<KIND, T, V, Medium>(g, resident, s);
+    if (p.shape == 1) return tiled_shape<KIND, T, V, Tall>(g, resident, s);
+    if (p.shape == 2) return tiled_shape<KIND, T, V, Medium>(g, resident, s);
     return tiled_shape<KIND, T, V, Small>(g, resident, s);
 }
 
@@ -877,14 +886,14 @@ template <Kind KIND> hipError_t product(const Product& g, hc_type type, bool in_
 // into more pieces): pieces fill the CUs once.
 size_t most_part_bytes(uint64_t rows, uint64_t cols) {
     size_t most = 0;
-    auto take = [&](uint64_t tile, uint64_t groups) {
-        const uint64_t tiles = up(rows, tile) * up(cols, tile);
+    auto take = [&](uint64_t bm, uint64_t bn, uint64_t groups) {
+        const uint64_t tiles = up(rows, bm) * up(cols, bn);
         const uint64_t n = tiles < groups / kMostPieces ? tiles * kMostPieces : groups;
-        const size_t bytes = n * tile * tile * 4;
+        const size_t bytes = n * bm * bn * 4;
         most = bytes > most ? bytes : most;
     };
-    for (const TileCost& c : kTileCosts) take(c.tile, kCus * c.resident);
-    take(kDirect, kSlots);
+    for (const TileCost& c : kTileCosts) take(c.bm, c.bn, kCus * c.resident);
+    take(kDirect, kDirect, kSlots);
     return most;
 }
 

@@ -253,6 +253,116 @@ __global__ __launch_bounds__(256) void direct_join_kernel(Product g) {
     finish8<KIND, T>(g, masks, row, col, v);
 }
 
+// ---- small products --------------------------------------------------------------
+
+// A tile of 16 x 16 a workgroup, whose eight waves share l: what bounds a small
+// product is a chain of latencies, so a wave asks for the fragments of four steps at
+// once, from memory to registers, and the waves' sums are added up in LDS in order.
+// 16 tokens through 768 x 768 (bf16): one launch of 2.6 us, in 64-tiles 5.
+constexpr uint32_t kSplitTile = 16, kSplitWaves = 8, kSplitAhead = 4;
+
+// 8 values of l of an operand's row, zeros behind its ends.
+template <bool ACROSS, typename T>
+__device__ __forceinline__ void split_load(const T* p, uint64_t ld, uint64_t row, uint64_t rows, uint32_t l,
+                                           uint32_t inner, T (&v)[8]) {
+    const uint32_t left = row < rows && l < inner ? inner - l : 0;
+    if constexpr (ACROSS) {
+        const T* at = p + (uint64_t)l * ld + row;
+#pragma unroll
+        for (int e = 0; e < 8; e++) v[e] = (uint32_t)e < left ? at[e * ld] : (T)0.0f;
+    } else {
+        load8_raw(p + row * ld + l, left, v);
+    }
+}
+
+template <Kind KIND, typename T>
+__device__ __forceinline__ void split_tile(const Product& g, uint32_t tile, float (&s_sum)[kSplitWaves][16][20]) {
+    constexpr bool PA = KIND == DW, QA = KIND != FORWARD;
+    typedef T V __attribute__((ext_vector_type(8)));
+    const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    const uint32_t ti = tile / g.tiles_j, tj = tile - ti * g.tiles_j;
+    const uint64_t row0 = (uint64_t)ti * kSplitTile;
+    const uint32_t col0 = tj * kSplitTile, inner = (uint32_t)g.inner;
+    const uint32_t lines = (inner + kStep - 1) / kStep;
+    f4 acc = {};
+    for (uint32_t pass = 0; pass < g.passes.count; pass++) {
+        const T* p = static_cast<const T*>(g.p) + (g.passes.p_planes >> 4 * pass & 15u) * g.p_plane;
+        for (uint32_t s = wave; s < lines; s += kSplitWaves * kSplitAhead) {
+            T rp[kSplitAhead][8], rq[kSplitAhead][8];
+#pragma unroll
+            for (uint32_t k = 0; k < kSplitAhead; k++) {
+                const uint32_t l = (s + k * kSplitWaves) * kStep + (lane >> 4) * 8;
+                split_load<PA>(p, g.p_ld, row0 + (lane & 15), g.rows, l, inner, rp[k]);
+                split_load<QA>(static_cast<const T*>(g.q), g.q_ld, col0 + (lane & 15), g.cols, l, inner, rq[k]);
+            }
+#pragma unroll
+            for (uint32_t k = 0; k < kSplitAhead; k++) {
+                V a, b;
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    a[e] = rp[k][e];
+                    b[e] = rq[k][e];
+                }
+                acc = product16(b, a, acc);
+            }
+        }
+        if (pass == 0 && g.passes.count > 1) acc *= g.passes.factor;
+    }
+    *reinterpret_cast<f4*>(&s_sum[wave][lane & 15][(lane >> 4) * 4]) = acc;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        const uint32_t i = threadIdx.x / 2, j = threadIdx.x % 2 * 8;
+        float v[8] = {};
+        for (uint32_t w = 0; w < kSplitWaves; w++)
+#pragma unroll
+            for (int e = 0; e < 8; e++) v[e] += s_sum[w][i][j + e];
+        Masks masks = {};
+        if constexpr (KIND == FORWARD) masks = masks_of(g.forward.drop);
+        if (row0 + i < g.rows && col0 + j < g.cols) finish8<KIND, T>(g, masks, row0 + i, col0 + j, v);
+    }
+}
+
+template <typename T> __global__ __launch_bounds__(512) void split_forward_kernel(Product g) {
+    __shared__ __align__(16) float s_sum[kSplitWaves][16][20];
+    split_tile<FORWARD, T>(g, blockIdx.x, s_sum);
+}
+
+// The gradients of a small layer in one launch: tiles of dx, then of dw, then 64
+// columns of db a workgroup, whose waves take an eighth of the rows each.
+struct SplitGrad {
+    Product dx, dw;
+    uint32_t dx_tiles, dw_tiles;
+    const void* dy;   // db: or null
+    uint64_t dy_ld, m;
+    uint32_t n;
+    Gradient db;
+};
+
+template <typename T> __global__ __launch_bounds__(512) void split_grad_kernel(SplitGrad g) {
+    __shared__ __align__(16) float s_sum[kSplitWaves][16][20];
+    if (blockIdx.x < g.dx_tiles) {
+        split_tile<DX, T>(g.dx, blockIdx.x, s_sum);
+    } else if (blockIdx.x < g.dx_tiles + g.dw_tiles) {
+        split_tile<DW, T>(g.dw, blockIdx.x - g.dx_tiles, s_sum);
+    } else {
+        float* sums = &s_sum[0][0][0];
+        const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        const uint32_t col = (blockIdx.x - g.dx_tiles - g.dw_tiles) * 64 + lane;
+        const T* dy = static_cast<const T*>(g.dy);
+        float t = 0.0f;
+        if (col < g.n)
+            for (uint64_t row = g.m * wave / kSplitWaves; row < g.m * (wave + 1) / kSplitWaves; row++)
+                t += (float)dy[row * g.dy_ld + col];
+        sums[wave * 64 + lane] = t;
+        __syncthreads();
+        if (wave == 0 && col < g.n) {
+            float v[8] = {};
+            for (uint32_t w = 0; w < kSplitWaves; w++) v[0] += sums[w * 64 + lane];
+            store_gradient(g.db, 0, col, 1, v);
+        }
+    }
+}
+
 // ---- products in tiles fed from memory to LDS directly -------------------------------
 
 // Where a wave's loads of one operand's tile go.  ROWS: of the tile.  Along rows
@@ -667,6 +777,7 @@ struct DzArgs {
     PackArgs dz;       // where it goes (out: or null), zeros behind its columns
     uint32_t planes;   // 1: in its own type; 2: and 2^11 times the rest; 3: bf16 parts
     float* part;       // the workgroups' sums, [blocks][n], or null
+    Gradient db;       // one workgroup along the rows: the sums themselves
 };
 
 // dz = act'(z) mask dy, and each workgroup's sums of its rows.
@@ -719,7 +830,13 @@ template <typename T> __global__ __launch_bounds__(256) void dz_kernel(DzArgs a)
         float t = 0.0f;
         for (uint32_t r = 0; r < step; r++) t += s_sum[r * a.width * 8 + c];
         const uint32_t at = blockIdx.x * a.width * 8 + c;
-        if (at < a.n) a.part[(uint64_t)blockIdx.y * a.n + at] = t;
+        if (at >= a.n) continue;
+        if (gridDim.y > 1) {
+            a.part[(uint64_t)blockIdx.y * a.n + at] = t;
+        } else {
+            float v[8] = {t};
+            store_gradient(a.db, 0, at, 1, v);
+        }
     }
 }
 
@@ -746,6 +863,8 @@ __global__ __launch_bounds__(1024) void bias_kernel(const float* __restrict__ pa
 
 constexpr int kCus = 256;                // of the gfx950
 constexpr uint64_t kDzGroups = 2048;     // workgroups of dz
+constexpr uint64_t kSplitBias = 2048;    // rows whose db a small layer's launch sums too
+constexpr uint64_t kDzAlone = 32;        // rows that one workgroup takes, without a launch for db
 
 uint64_t up(uint64_t v, uint64_t to) { return (v + to - 1) / to; }
 
@@ -795,6 +914,7 @@ constexpr double kJoin = 5.0, kBytesPerUs = 5e6;
 struct TilePlan {
     int shape;
     uint32_t tiles_i, tiles_j, whole, cut, pieces;
+    double us;
 };
 
 double rounds(const TileCost& c, uint64_t groups, double steps, double ends) {
@@ -819,7 +939,7 @@ TilePlan tile_plan(uint64_t rows, uint64_t cols, uint64_t steps) {
         auto consider = [&](double t, uint64_t whole, uint64_t pieces) {
             if (t >= least) return;
             least = t;
-            best = {k, (uint32_t)ti, (uint32_t)tj, (uint32_t)whole, (uint32_t)(n - whole), (uint32_t)pieces};
+            best = {k, (uint32_t)ti, (uint32_t)tj, (uint32_t)whole, (uint32_t)(n - whole), (uint32_t)pieces, t};
         };
         consider(rounds(c, n, (double)steps, c.ends), n, 1);
         const uint64_t rest = n % slots, most = steps / kLeastSteps < kMostPieces ? steps / kLeastSteps : kMostPieces;
@@ -870,9 +990,48 @@ template <Kind KIND, typename T, typename V> hipError_t tiled(Product g, hipStre
     return tiled_shape<KIND, T, V, Small>(g, resident, s);
 }
 
-// in_tiles: the operands are as the tiles take them (fp32 in three planes).
-template <Kind KIND> hipError_t product(const Product& g, hc_type type, bool in_tiles, hipStream_t s) {
-    if (in_tiles && g.inner) {
+// Estimated time of a small product: its tiles' rows come from L2 again and again.
+double split_cost(uint64_t rows, uint64_t cols, uint64_t inner, uint32_t passes, hc_type type) {
+    const double tiles = (double)up(rows, kSplitTile) * (double)up(cols, kSplitTile);
+    return 2.5 + tiles * passes * (double)inner * (2 * kSplitTile) * (type == HC_T_F32 ? 4 : 2) / 6e6;
+}
+
+// How a product runs: operands as the tiles take them (fp32 in three planes) or as
+// they are, and then in small tiles or not.
+enum Way { SPLIT, DIRECT, TILED };
+
+Way way_of(const Product& g, hc_type type, bool in_tiles) {
+    if (g.inner == 0) return DIRECT;
+    if (in_tiles && type == HC_T_F32) return TILED;
+    const double split = split_cost(g.rows, g.cols, g.inner, g.passes.count, type);
+    // a direct product takes 0.8 us a step of 32, cut into up to 64 pieces
+    const double other = in_tiles ? tile_plan(g.rows, g.cols, up(g.inner, 64) * g.passes.count).us
+                                  : 3.0 + 0.8 * (double)up(up(g.inner, kStep), 4) +
+                                        (double)g.rows * g.cols * g.inner * 2 / (type == HC_T_F32 ? 75e6 : 280e6);
+    return split < other ? SPLIT : in_tiles ? TILED : DIRECT;
+}
+
+uint32_t split_tiles(Product* g) {
+    g->tiles_j = (uint32_t)up(g->cols, kSplitTile);
+    return (uint32_t)up(g->rows, kSplitTile) * g->tiles_j;
+}
+
+template <typename T> hipError_t split_forward(Product g, hipStream_t s) {
+    const uint32_t tiles = split_tiles(&g);
+    hipLaunchKernelGGL(split_forward_kernel<T>, dim3(tiles), dim3(512), 0, s, g);
+    return hipGetLastError();
+}
+
+template <typename T> hipError_t split_grad(SplitGrad g, hipStream_t s) {
+    g.dx_tiles = g.dx.gradient.out ? split_tiles(&g.dx) : 0;
+    g.dw_tiles = g.dw.gradient.out ? split_tiles(&g.dw) : 0;
+    const uint32_t all = g.dx_tiles + g.dw_tiles + (g.dy ? (uint32_t)up(g.n, 64) : 0);
+    if (all) hipLaunchKernelGGL(split_grad_kernel<T>, dim3(all), dim3(512), 0, s, g);
+    return hipGetLastError();
+}
+
+template <Kind KIND> hipError_t product(const Product& g, hc_type type, Way way, hipStream_t s) {
+    if (way == TILED) {
         if (type == HC_T_F32) return tiled<KIND, float, b8>(g, s);
         if (type == HC_T_BF16) return tiled<KIND, __bf16, b8>(g, s);
         return tiled<KIND, _Float16, h8>(g, s);
@@ -962,7 +1121,7 @@ Layout grad_layout(const hc_linear_params& p, hc_type type) {
     const uint64_t across = up(groups, 64);
     L.width = (uint32_t)up(groups, across);
     const uint64_t step = 256 / L.width, most = across < kDzGroups ? kDzGroups / across : 1;
-    L.per = up(up(p.m, most), step) * step;
+    L.per = p.m <= kDzAlone ? kDzAlone : up(up(p.m, most), step) * step;
     L.blocks = p.m ? up(p.m, L.per) : 0;
     L.dz = take(at, p.m * L.n_ld * (type == HC_T_F32 ? (L.pack ? 6 : 4) : type == HC_T_BF16 ? 6 : 4));
     L.bias = take(at, (p.m < most ? p.m : most) * p.n * 4);
@@ -1027,7 +1186,11 @@ hipError_t launch_linear(const hc_linear_params& p, const Dropout& d, hc_type ty
     g.inner = p.k;
     g.part = reinterpret_cast<float*>(ws + L.part);
     g.forward = {bias, residual, y, z, p.residual_ld, p.y_ld, p.z_ld, p.act, d};
-    return product<FORWARD>(g, type, in_tiles, s);
+    const Way way = way_of(g, type, in_tiles);
+    if (way != SPLIT) return product<FORWARD>(g, type, way, s);
+    if (type == HC_T_F32) return split_forward<float>(g, s);
+    if (type == HC_T_BF16) return split_forward<__bf16>(g, s);
+    return split_forward<_Float16>(g, s);
 }
 
 size_t linear_grad_bytes(const hc_linear_params& p, hc_type type) { return grad_layout(p, type).bytes; }
@@ -1039,13 +1202,33 @@ hipError_t launch_linear_grad(const hc_linear_params& p, const Dropout& d, hc_ty
     const bool fp32 = type == HC_T_F32, plain = p.act == HC_ACT_NONE && d.limit == 0;
     const bool x_fits = !fp32 && tile_rows(q.x, p.k, p.x_ld), w_fits = !fp32 && tile_rows(q.w, p.k, p.w_ld);
     const bool in_tiles = L.pack || ((!q.dw || x_fits) && (!q.dx || w_fits));
-    // dz is dy itself where nothing changes it and the products can take it
-    const bool dy_fits = plain && (in_tiles ? !fp32 && tile_rows(q.dy, p.n, p.y_ld) : true);
-    const bool dz = !dy_fits && (q.dx || q.dw);
     const bool rest = !plain && q.dw && !fp32 && (q.g_type == HC_T_F32 || q.g_type == HC_T_I32);
+    Product dx = {}, dw = {};
+    dx.part = dw.part = reinterpret_cast<float*>(ws + L.part);
+    dx.cols = dw.cols = (uint32_t)p.k;
+    dx.passes = dw.passes = fp32 && in_tiles ? kThreePlanes : kOnePass;
+    dx.rows = dw.inner = p.m;
+    dx.inner = dw.rows = p.n;
+    if (rest) dw.passes = type == HC_T_BF16 ? kRestBf16 : kRestF16;
+    const Gradient gradient = {nullptr, 0, (uint32_t)q.g_type, q.accumulate ? 1u : 0u, p.fixed};
+    dw.gradient = gradient;
+    if (p.m) {
+        dx.gradient.out = q.dx;
+        dx.gradient.ld = p.dx_ld;
+    }
+    dw.gradient.out = q.dw;
+    dw.gradient.ld = p.dw_ld;
+    Gradient db = gradient;
+    db.out = q.db;
+    const Way dx_way = way_of(dx, type, in_tiles), dw_way = way_of(dw, type, in_tiles);
+    // small layers go in one launch, where nothing is packed for it; db too if dz is dy
+    const bool together = !(fp32 && in_tiles) && (!dx.gradient.out || dx_way == SPLIT) && (!q.dw || dw_way == SPLIT);
+    // dz is dy itself where nothing changes it and the products can take it
+    const bool dy_fits = plain && (in_tiles && !together ? !fp32 && tile_rows(q.dy, p.n, p.y_ld) : true);
+    const bool dz = !dy_fits && (q.dx || q.dw), db_together = together && plain && p.m <= kSplitBias;
     hipError_t e = hipSuccess;
     Operand oz = {q.dy, p.y_ld, p.n, 0};
-    if ((dz || q.db) && p.m) {
+    if ((dz || (q.db && !db_together)) && p.m) {
         DzArgs a = {};
         a.dy = q.dy;
         a.z = q.z;
@@ -1065,7 +1248,8 @@ hipError_t launch_linear_grad(const hc_linear_params& p, const Dropout& d, hc_ty
             a.planes = fp32 ? (in_tiles ? 3 : 1) : !rest ? 1 : type == HC_T_BF16 ? 3 : 2;
             oz = {a.dz.out, L.n_ld, L.n_ld, a.dz.plane};
         }
-        a.part = q.db ? reinterpret_cast<float*>(ws + L.bias) : nullptr;
+        a.part = q.db && !db_together ? reinterpret_cast<float*>(ws + L.bias) : nullptr;
+        a.db = db;
         const dim3 grid((uint32_t)up(a.groups, L.width), (uint32_t)L.blocks);
         if (fp32) hipLaunchKernelGGL(dz_kernel<float>, grid, dim3(256), 0, s, a);
         else if (type == HC_T_BF16) hipLaunchKernelGGL(dz_kernel<__bf16>, grid, dim3(256), 0, s, a);
@@ -1073,45 +1257,43 @@ hipError_t launch_linear_grad(const hc_linear_params& p, const Dropout& d, hc_ty
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    const Gradient gradient = {nullptr, 0, (uint32_t)q.g_type, q.accumulate ? 1u : 0u, p.fixed};
-    if (q.db) {
-        Gradient b = gradient;
-        b.out = q.db;
+    if (q.db && !db_together && L.blocks != 1) {
         hipLaunchKernelGGL(bias_kernel, dim3((uint32_t)up(p.n, 16)), dim3(1024), 0, s,
-                           reinterpret_cast<const float*>(ws + L.bias), (uint32_t)L.blocks, (uint32_t)p.n, b);
+                           reinterpret_cast<const float*>(ws + L.bias), (uint32_t)L.blocks, (uint32_t)p.n, db);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    Product g = {};
-    g.part = reinterpret_cast<float*>(ws + L.part);
-    g.cols = (uint32_t)p.k;
-    g.passes = fp32 && in_tiles ? kThreePlanes : kOnePass;
-    if (q.dx && p.m) {
+    if (together) {
+        set(&dx, oz, {q.w, p.w_ld, p.k, 0});
+        set(&dw, oz, {q.x, p.x_ld, p.k, 0});
+        SplitGrad g = {};
+        g.dx = dx;
+        g.dw = dw;
+        if (db_together && q.db) {
+            g.dy = p.m ? q.dy : ws;  // not read without rows
+            g.dy_ld = p.y_ld;
+            g.m = p.m;
+            g.n = (uint32_t)p.n;
+            g.db = db;
+        }
+        if (fp32) return split_grad<float>(g, s);
+        if (type == HC_T_BF16) return split_grad<__bf16>(g, s);
+        return split_grad<_Float16>(g, s);
+    }
+    if (dx.gradient.out) {
         Operand ow;
         e = packed(type, L.pack && !w_fits, q.w, p.n, p.k, p.w_ld, ws + L.w, L.k_ld, &ow, s);
         if (e != hipSuccess) return e;
-        Product h = g;
-        set(&h, oz, ow);
-        h.rows = p.m;
-        h.inner = p.n;
-        h.gradient.out = q.dx;
-        h.gradient.ld = p.dx_ld;
-        e = product<DX>(h, type, in_tiles, s);
+        set(&dx, oz, ow);
+        e = product<DX>(dx, type, dx_way == SPLIT ? (in_tiles ? TILED : DIRECT) : dx_way, s);
         if (e != hipSuccess) return e;
     }
     if (q.dw) {
         Operand ox;
         e = packed(type, L.pack && !x_fits && p.m, q.x, p.m, p.k, p.x_ld, ws + L.x, L.k_ld, &ox, s);
         if (e != hipSuccess) return e;
-        Product h = g;
-        set(&h, oz, ox);
-        if (rest) h.passes = type == HC_T_BF16 ? kRestBf16 : kRestF16;
-        h.rows = p.n;
-        h.inner = p.m;
-        h.gradient = gradient;
-        h.gradient.out = q.dw;
-        h.gradient.ld = p.dw_ld;
-        return product<DW>(h, type, in_tiles, s);
+        set(&dw, oz, ox);
+        return product<DW>(dw, type, dw_way == SPLIT ? (in_tiles ? TILED : DIRECT) : dw_way, s);
     }
     return hipSuccess;
 }

@@ -146,7 +146,7 @@ hc_status hc_orthogonalise(const hc_orthogonalise_params *p, const void *x, void
  * replays draws a new mask in each. */
 typedef struct {
     uint64_t rows;         /* 0 .. 2^31 - 1                                       */
-    uint64_t cols;         /* 1 .. 2^31 - 1; at most 2^38 elements in all         */
+    uint64_t cols;         /* 1 .. 2^31 - 1; at most 2^35 elements in all         */
     uint64_t x_ld, residual_ld, out_ld; /* elements between rows, >= cols          */
     uint64_t seed, draw;   /* a program's seed, and which of its draws this is    */
     float p;               /* probability of a drop, 0 .. 1                       */
@@ -169,9 +169,9 @@ typedef enum {
 } hc_act;
 
 /* A layer of n outputs and k inputs on m rows: x [m, k], w [n, k], all else
- * [m, n], rows contiguous.  m n, m k and n k are at most 2^38. */
+ * [m, n], rows contiguous.  m n, m k and n k are at most 2^34. */
 typedef struct {
-    uint64_t m;            /* 0 .. 2^31 - 1                                       */
+    uint64_t m;            /* 0 .. 2^27                                           */
     uint64_t n, k;         /* 1 .. 2^24                                           */
     uint64_t x_ld, w_ld;   /* elements between rows, here and below: at least the
                               columns, at most 2^31                               */
@@ -190,8 +190,11 @@ typedef struct {
  * products and sums in fp32 (z is not rounded before act).  All of `type`
  * (HC_T_F32, HC_T_BF16, HC_T_F16).  z (NULL: not wanted) is what the gradient of
  * an activation asks for.  Sums are taken in an order that depends on the shape
- * and strides alone: two calls agree bit for bit.  Infinities in x or w may give
- * NaN where fp32 matrices are wide.  y may be residual (same address and stride).
+ * and strides alone: two calls agree bit for bit.  Large fp32 products run as three
+ * of fp16 parts with fp32 sums: an element of x or w keeps 22 bits if it is no
+ * smaller than 2^-29 of the largest in its row, fewer below, none below 2^-51 of it;
+ * small ones are fp32 products.  An infinity may come out as NaN.  y may be residual
+ * (same address and stride).
  * The workspace does for fewer rows of the same n, k and strides too. */
 hc_status hc_linear_bytes(const hc_linear_params *p, hc_type type, size_t *bytes);
 hc_status hc_linear(const hc_linear_params *p, hc_type type, const void *x, const void *w,
@@ -210,7 +213,8 @@ hc_status hc_linear(const hc_linear_params *p, hc_type type, const void *x, cons
  * HC_T_F32 or HC_T_I32 takes it in three bf16 parts (24 bits) or two fp16 ones
  * (22 bits), three or two times the products.  Without activation and dropout dz
  * is dy.  db takes dz unrounded.
- *   m = 0 gives zeros.  Order and infinities as in hc_linear. */
+ *   m = 0 gives zeros.  Order, fp32 parts (there by the rows of dz and the columns
+ * of w, the columns of dz and of x) and infinities as in hc_linear. */
 hc_status hc_linear_grad_bytes(const hc_linear_params *p, hc_type type, size_t *bytes);
 hc_status hc_linear_grad(const hc_linear_params *p, hc_type type, const void *dy, const void *x,
                          const void *w, const void *z, void *dx, hc_type g_type, void *dw,

@@ -15,6 +15,8 @@ typedef float f8 __attribute__((ext_vector_type(8)));
 
 enum Kind { FORWARD, DX, DW };
 
+constexpr uint32_t kCus = 256;  // of the gfx950
+
 // What a forward product's sums become.
 struct Forward {
     const void *bias, *residual;
@@ -42,26 +44,27 @@ __device__ __forceinline__ void finish_forward(const Forward& f, const Masks& ma
 
 // An operand may be a sum of planes, and a product the sum of some products of
 // planes: pass s takes plane p_planes >> 4 s of P and q_planes >> 4 s of Q.  The
-// small ones come first; the first pass's sums are multiplied by `factor`.
+// small ones come first; the sums of the first `small` are multiplied by `factor`.
 struct Passes {
-    uint32_t count, p_planes, q_planes;
+    uint32_t count, p_planes, q_planes, small;
     float factor;
 };
-constexpr Passes kOnePass = {1, 0, 0, 1.0f};
+constexpr Passes kOnePass = {1, 0, 0, 0, 1.0f};
 // dz in three bf16 parts that follow each other; in an fp16 part and 2^11 times the
 // rest, which as it is would lose bits below fp16's normal range
 constexpr float kRestUnit = 0x1p11f;
-constexpr Passes kRestBf16 = {3, 0x012, 0x000, 1.0f};
-constexpr Passes kRestF16 = {2, 0x01, 0x00, 1.0f / kRestUnit};
-// Three bf16 planes each, of 8 bits that follow each other: products down to 2^-16
-// of the largest.  What is left out is below 2^-23 of a product of two fp32 values.
-constexpr Passes kThreePlanes = {6, 0x010120, 0x001102, 1.0f};
+constexpr Passes kRestBf16 = {3, 0x012, 0x000, 0, 1.0f};
+constexpr Passes kRestF16 = {2, 0x01, 0x00, 1, 1.0f / kRestUnit};
+// fp32 in an fp16 part and 2^11 times the rest, 22 bits: high x rest, rest x high,
+// high x high.  The product of the rests is below 2^-22 of the whole.
+constexpr Passes kTwoPlanes = {3, 0x010, 0x001, 2, 1.0f / kRestUnit};
 
 struct Product {
     const void *p, *q;       // operands
     uint64_t p_ld, q_ld;
     uint64_t p_cols, q_cols;    // stored elements of a row: its columns, or with zeros behind
     uint64_t p_plane, q_plane;  // elements between planes
+    const float *p_most, *q_most;  // planes of fp32: the largest element of each row
     Passes passes;
     uint64_t rows, inner;    // of D; length of l
     uint32_t cols;
@@ -202,7 +205,7 @@ __global__ __launch_bounds__(256) void direct_kernel(Product g) {
 #pragma unroll
                 for (int v = 0; v < 2; v++) acc[u][v] = product16(fq[v], fp[u], acc[u][v]);
         }
-        if (pass == 0 && g.passes.count > 1)
+        if (pass + 1 == g.passes.small)
 #pragma unroll
             for (int u = 0; u < 2; u++)
 #pragma unroll
@@ -306,7 +309,7 @@ __device__ __forceinline__ void split_tile(const Product& g, uint32_t tile, floa
                 acc = product16(b, a, acc);
             }
         }
-        if (pass == 0 && g.passes.count > 1) acc *= g.passes.factor;
+        if (pass + 1 == g.passes.small) acc *= g.passes.factor;
     }
     *reinterpret_cast<f4*>(&s_sum[wave][lane & 15][(lane >> 4) * 4]) = acc;
     __syncthreads();
@@ -557,12 +560,28 @@ template <int END, int STEP, int I = 0, typename F> __device__ __forceinline__ v
 
 // Columns col .. col + 7 of FM rows 16 apart become results.  What is read for them
 // is asked for before the first is stored: a load behind a store would wait for it.
+// The power of two that an fp32 row's planes are scaled by: its largest element is
+// brought to 2^14 .. 2^15.
+__device__ __forceinline__ int scale_of(float most) {
+    return most == 0.0f ? 0 : 15 - __builtin_amdgcn_frexp_expf(most);
+}
+
 template <Kind KIND, typename T, int FIRST, int FM, int FN>
 __device__ __forceinline__ void finish_rows(const Product& g, const Masks& masks, uint64_t row0, uint32_t col,
                                             const f4 (&acc)[FM][FN]) {
     constexpr int N = FM <= 4 ? FM : sizeof(T) == 4 ? 2 : 4;  // rows at a time
     // every lane takes part in the exchange, also those behind the last column
     const uint32_t count = col < g.cols ? g.cols - col : 0;
+    // fp32: back from the rows' scales
+    float most[8];
+    if constexpr (sizeof(T) == 4) load8(g.q_most + col, count, most);
+    auto unscale = [&](uint64_t row, float (&v)[8]) __attribute__((always_inline)) {
+        if constexpr (sizeof(T) == 4) {
+            const int down = row < g.rows ? -scale_of(g.p_most[row]) : 0;
+#pragma unroll
+            for (int e = 0; e < 8; e++) v[e] = __builtin_ldexpf(v[e], down - scale_of(most[e]));
+        }
+    };
     if constexpr (KIND == FORWARD) {
         const Forward& f = g.forward;
         float bias[8] = {};
@@ -577,6 +596,7 @@ __device__ __forceinline__ void finish_rows(const Product& g, const Masks& masks
             unrolled<N, 1>([&](auto u) __attribute__((always_inline)) {
                 float v[8];
                 pair_up(acc[u0 + u][FIRST], acc[u0 + u][FIRST + 1], v);
+                unscale(row0 + 16 * (u0 + u), v);
                 finish_forward<T>(f, masks, row0 + 16 * (u0 + u), g.rows, col, count, bias, residual[u], v);
             });
         });
@@ -585,6 +605,7 @@ __device__ __forceinline__ void finish_rows(const Product& g, const Masks& masks
             float v[8];
             pair_up(acc[u][FIRST], acc[u][FIRST + 1], v);
             const uint64_t row = row0 + 16 * u;
+            unscale(row, v);
             if (row >= g.rows || count == 0) return;
             if constexpr (KIND == DX) store8(static_cast<T*>(g.gradient.out) + row * g.gradient.ld + col, count, v);
             else store_gradient(g.gradient, row, col, count, v);
@@ -615,7 +636,9 @@ __global__ __launch_bounds__(S::kThreads, kWavesOfSimd<S>) void tiled_kernel(Pro
     const uint32_t all = g.whole + g.cut * g.pieces;
     const uint32_t lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     const uint32_t wi = wave / (S::BN / S::WN) * S::WM, wj = wave % (S::BN / S::WN) * S::WN;
-    const float factor = KIND == DW ? g.passes.factor : 1.0f;
+    constexpr bool kScaled = KIND == DW || sizeof(T) == 4;
+    const float factor = g.passes.factor;
+    const uint32_t small = kScaled ? g.passes.small * ((uint32_t)(g.inner + 63) / 64) : 0;  // steps
     Feed<KIND, V, S> feed(g, s_mem, wave, lane);
     uint32_t i = blockIdx.x;
     Work w = work_at(g, i, steps);
@@ -630,15 +653,15 @@ __global__ __launch_bounds__(S::kThreads, kWavesOfSimd<S>) void tiled_kernel(Pro
             for (int v = 0; v < FN; v++) acc[u][v] = f4{zero, zero, zero, zero};
         auto run = [&](uint32_t n) {
             auto fetch = [&](uint32_t, uint32_t buf) { feed.fetch(buf); };
-            if constexpr (S::kStages == 2 && S::kWaves == 8)
+            if constexpr (S::kWaves == 8)
                 main_loop_paired<1, S, V, typename R::P, typename R::Q>(acc, fetch, s_mem, n, wi, wj, lane, wave);
             else
                 main_loop<1, S, V, typename R::P, typename R::Q>(acc, fetch, s_mem, n, wi, wj, lane);
             __syncthreads();
         };
         uint32_t s0 = w.s0;
-        if (KIND == DW && factor != 1.0f && s0 < feed.lines) {
-            const uint32_t stop = min(w.s1, feed.lines);
+        if (kScaled && s0 < small) {
+            const uint32_t stop = min(w.s1, small);
             run(stop - s0);
 #pragma unroll
             for (int u = 0; u < FM; u++)
@@ -710,23 +733,6 @@ template <Kind KIND, typename T, typename S> __global__ __launch_bounds__(256) v
 
 // ---- operands as the tiles take them --------------------------------------------------
 
-// v = the sum of three bf16 values, exactly where v is no smaller than 2^-110.  The
-// first is cut off, so that none becomes infinite, or rounded, where it is also used
-// alone; the others are rounded.  Infinity leaves nothing, NaN is NaN in all.
-template <bool ROUND> __device__ __forceinline__ void split3(float v, __bf16 (&w)[3]) {
-    float first;
-    if constexpr (ROUND) {
-        w[0] = (__bf16)v;
-        first = (float)w[0];
-    } else {
-        first = __uint_as_float(__float_as_uint(v) & 0xffff0000u);
-        w[0] = __builtin_bit_cast(__bf16, (uint16_t)(__float_as_uint(v) >> 16));
-    }
-    const float r = fabsf(first) == __builtin_inff() && v == v ? 0.0f : v - first;
-    w[1] = (__bf16)r;
-    w[2] = (__bf16)(r - (float)w[1]);
-}
-
 struct PackArgs {
     const void* in;
     void* out;
@@ -734,26 +740,8 @@ struct PackArgs {
     uint32_t cols;
 };
 
-template <typename T, bool ROUND = false>
-__device__ __forceinline__ void store_planes(const PackArgs& a, uint64_t at, const float (&v)[8]) {
-    if constexpr (sizeof(T) == 4) {
-        b8 w[3];
-#pragma unroll
-        for (int e = 0; e < 8; e++) {
-            __bf16 s[3];
-            split3<ROUND>(v[e], s);
-#pragma unroll
-            for (int k = 0; k < 3; k++) w[k][e] = s[k];
-        }
-#pragma unroll
-        for (int k = 0; k < 3; k++) *reinterpret_cast<b8*>(static_cast<__bf16*>(a.out) + k * a.plane + at) = w[k];
-    } else {
-        store8(static_cast<T*>(a.out) + at, 8, v);
-    }
-}
-
-// A matrix of any stride and alignment as rows of a multiple of 64 values with
-// zeros behind them: 16-bit types as they are, fp32 in three planes.
+// A 16-bit matrix of any stride and alignment as rows of a multiple of 64 values
+// with zeros behind them.
 template <typename T> __global__ __launch_bounds__(256) void pack_kernel(PackArgs a) {
     const uint32_t groups = (uint32_t)(a.out_ld / 8);
     const uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x, row = at / groups;
@@ -761,7 +749,139 @@ template <typename T> __global__ __launch_bounds__(256) void pack_kernel(PackArg
     const uint32_t col = (uint32_t)(at - row * groups) * 8;
     float v[8];
     load8(static_cast<const T*>(a.in) + row * a.in_ld + (col < a.cols ? col : 0), col < a.cols ? a.cols - col : 0, v);
-    store_planes<T>(a, row * a.out_ld + col, v);
+    store8(static_cast<T*>(a.out) + row * a.out_ld + col, 8, v);
+}
+
+// fp32 matrices go in two fp16 planes, scaled by a power of two for each row of the
+// product's operand, which leaves the sums by 2^-(both) at the end.  That way 22 bits
+// of every element down to 2^-29 of its row's largest are kept, and nothing is lost
+// above 2^-51 of it; three products of fp16 then take half the time of six of bf16
+// planes, which would need no scale (33278 x 1500 x 700: 427 us).  The largest is
+// taken over finite elements; infinity leaves no rest, NaN is NaN in both.
+__device__ __forceinline__ void split2(float v, int scale, _Float16& high, _Float16& rest) {
+    const float s = __builtin_ldexpf(v, scale);
+    high = (_Float16)s;
+    const float r = s - (float)high;
+    rest = (_Float16)(r - r == 0.0f || s != s ? r * kRestUnit : 0.0f);
+}
+
+__device__ __forceinline__ void store_two(void* out, uint64_t plane, uint64_t at, const float (&v)[8],
+                                          const int (&scale)[8]) {
+    h8 high, rest;
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+        _Float16 a, b;
+        split2(v[e], scale[e], a, b);
+        high[e] = a;
+        rest[e] = b;
+    }
+    *reinterpret_cast<h8*>(static_cast<_Float16*>(out) + at) = high;
+    *reinterpret_cast<h8*>(static_cast<_Float16*>(out) + plane + at) = rest;
+}
+
+// |v| where v is finite, else 0.
+__device__ __forceinline__ float finite_size(float v) {
+    const float a = fabsf(v);
+    return a < __builtin_inff() ? a : 0.0f;
+}
+
+// A workgroup a stored row, which is a row of the operand: its largest element, then
+// its planes.  cols_out: the same matrix again by its columns' scales (dz is P along
+// its rows for dx and across them for dw).
+struct SplitRowsArgs {
+    PackArgs pack;
+    float* most;             // of each row
+    void* cols_out;          // or null
+    const float* cols_most;
+};
+
+__global__ __launch_bounds__(256) void split_rows_kernel(SplitRowsArgs a) {
+    __shared__ float s_most[4];
+    const uint32_t groups = (uint32_t)(a.pack.out_ld / 8), cols = a.pack.cols;
+    for (uint64_t row = blockIdx.x; row < a.pack.rows; row += gridDim.x) {
+        const float* in = static_cast<const float*>(a.pack.in) + row * a.pack.in_ld;
+        float v[8], most = 0.0f;
+        auto load = [&](uint32_t g) {
+            load8(in + (g * 8 < cols ? g * 8 : 0), g * 8 < cols ? cols - g * 8 : 0, v);
+        };
+        for (uint32_t g = threadIdx.x; g < groups; g += 256) {
+            load(g);
+#pragma unroll
+            for (int e = 0; e < 8; e++) most = fmaxf(most, finite_size(v[e]));
+        }
+        for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
+        __syncthreads();  // the row before is done with
+        if ((threadIdx.x & 63) == 0) s_most[threadIdx.x >> 6] = most;
+        __syncthreads();
+        most = fmaxf(fmaxf(s_most[0], s_most[1]), fmaxf(s_most[2], s_most[3]));
+        if (threadIdx.x == 0) a.most[row] = most;
+        const int mine = scale_of(most), all[8] = {mine, mine, mine, mine, mine, mine, mine, mine};
+        for (uint32_t g = threadIdx.x; g < groups; g += 256) {
+            if (groups > 256) load(g);  // otherwise it is still there
+            const uint64_t at = row * a.pack.out_ld + g * 8;
+            store_two(a.pack.out, a.pack.plane, at, v, all);
+            if (!a.cols_out) continue;
+            float by[8];
+            int scale[8];
+            load8(a.cols_most + g * 8, 8, by);
+#pragma unroll
+            for (int e = 0; e < 8; e++) scale[e] = scale_of(by[e]);
+            store_two(a.cols_out, a.pack.plane, at, v, scale);
+        }
+    }
+}
+
+// The largest element of each column, into zeros.  Sizes are compared as the whole
+// numbers that their bits are, so that no order of the atomics matters.
+__device__ __forceinline__ void columns_most(float* s_most, uint32_t width, uint32_t step, const float (&most)[8],
+                                             uint32_t first, uint32_t cols, float* out) {
+#pragma unroll
+    for (int e = 0; e < 8; e++) s_most[threadIdx.x * 8 + e] = most[e];
+    __syncthreads();
+    for (uint32_t c = threadIdx.x; c < width * 8; c += 256) {
+        float t = 0.0f;
+        for (uint32_t r = 0; r < step; r++) t = fmaxf(t, s_most[r * width * 8 + c]);
+        if (first + c < cols) atomicMax(reinterpret_cast<uint32_t*>(out) + first + c, __float_as_uint(t));
+    }
+}
+
+__global__ __launch_bounds__(256) void most_kernel(PackArgs a, uint64_t per, float* __restrict__ out) {
+    __shared__ float s_most[256 * 8];
+    const uint32_t col = (blockIdx.x * 64 + (threadIdx.x & 63)) * 8;
+    const uint64_t end = min((uint64_t)(blockIdx.y + 1) * per, a.rows);
+    float most[8] = {};
+    if (col < a.cols)
+        for (uint64_t row = (uint64_t)blockIdx.y * per + (threadIdx.x >> 6); row < end; row += 4) {
+            float v[8];
+            load8(static_cast<const float*>(a.in) + row * a.in_ld + col, a.cols - col, v);
+#pragma unroll
+            for (int e = 0; e < 8; e++) most[e] = fmaxf(most[e], finite_size(v[e]));
+        }
+    columns_most(s_most, 64, 4, most, blockIdx.x * 512, a.cols, out);
+}
+
+// A matrix whose columns are the operand's rows, by their scales.
+__global__ __launch_bounds__(256) void split_columns_kernel(PackArgs a, const float* __restrict__ most) {
+    const uint32_t groups = (uint32_t)(a.out_ld / 8);
+    const uint64_t at = (uint64_t)blockIdx.x * 256 + threadIdx.x, row = at / groups;
+    if (row >= a.rows) return;
+    const uint32_t col = (uint32_t)(at - row * groups) * 8;
+    float v[8], by[8];
+    int scale[8];
+    load8(static_cast<const float*>(a.in) + row * a.in_ld + (col < a.cols ? col : 0), col < a.cols ? a.cols - col : 0, v);
+    load8(most + col, 8, by);
+#pragma unroll
+    for (int e = 0; e < 8; e++) scale[e] = scale_of(by[e]);
+    store_two(a.out, a.plane, row * a.out_ld + col, v, scale);
+}
+
+// v = the sum of three bf16 values, exactly where v is no smaller than 2^-110.
+// Infinity leaves nothing, NaN is NaN in all.
+__device__ __forceinline__ void split3(float v, __bf16 (&w)[3]) {
+    w[0] = (__bf16)v;
+    const float first = (float)w[0], r = fabsf(first) == __builtin_inff() && v == v ? 0.0f : v - first;
+    w[1] = (__bf16)r;
+    w[2] = (__bf16)(r - (float)w[1]);
 }
 
 // ---- dz and the bias's gradient ----------------------------------------------------
@@ -776,6 +896,7 @@ struct DzArgs {
     Dropout drop;
     PackArgs dz;       // where it goes (out: or null), zeros behind its columns
     uint32_t planes;   // 1: in its own type; 2: and 2^11 times the rest; 3: bf16 parts
+    float* most;       // fp32: the largest of each column, or null
     float* part;       // the workgroups' sums, [blocks][n], or null
     Gradient db;       // one workgroup along the rows: the sums themselves
 };
@@ -787,7 +908,7 @@ template <typename T> __global__ __launch_bounds__(256) void dz_kernel(DzArgs a)
     const uint32_t lane = threadIdx.x % a.width, sub = threadIdx.x / a.width, step = 256 / a.width;
     const uint32_t group = blockIdx.x * a.width + lane, col = group * 8;
     const uint64_t end = min((uint64_t)(blockIdx.y + 1) * a.per, a.m);
-    float sum[8] = {};
+    float sum[8] = {}, most[8] = {};
     if (group < a.groups && sub < step) {
         const uint32_t count = col < a.n ? a.n - col : 0;
         for (uint64_t row = (uint64_t)blockIdx.y * a.per + sub; row < end; row += step) {
@@ -804,10 +925,23 @@ template <typename T> __global__ __launch_bounds__(256) void dz_kernel(DzArgs a)
                 for (int e = 0; e < 8; e++) v[e] = (uint32_t)e < count ? v[e] : 0.0f;
 #pragma unroll
             for (int e = 0; e < 8; e++) sum[e] += v[e];
+            if (sizeof(T) == 4 && a.most)
+#pragma unroll
+                for (int e = 0; e < 8; e++) most[e] = fmaxf(most[e], finite_size(v[e]));
             if (!a.dz.out) continue;
             const uint64_t at = row * a.dz.out_ld + col;
             if (a.planes == 3) {
-                store_planes<float, sizeof(T) == 2>(a.dz, at, v);
+                b8 w[3];
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    __bf16 s[3];
+                    split3(v[e], s);
+#pragma unroll
+                    for (int k = 0; k < 3; k++) w[k][e] = s[k];
+                }
+#pragma unroll
+                for (int k = 0; k < 3; k++)
+                    *reinterpret_cast<b8*>(static_cast<__bf16*>(a.dz.out) + k * a.dz.plane + at) = w[k];
             } else {
                 store8(static_cast<T*>(a.dz.out) + at, 8, v);
                 if (a.planes == 2) {
@@ -821,6 +955,10 @@ template <typename T> __global__ __launch_bounds__(256) void dz_kernel(DzArgs a)
                 }
             }
         }
+    }
+    if (sizeof(T) == 4 && a.most) {
+        columns_most(s_sum, a.width, step, most, blockIdx.x * a.width * 8, a.n, a.most);
+        __syncthreads();
     }
     if (!a.part) return;
 #pragma unroll
@@ -861,7 +999,6 @@ __global__ __launch_bounds__(1024) void bias_kernel(const float* __restrict__ pa
 
 // ---- layout and launches ------------------------------------------------------------
 
-constexpr int kCus = 256;                // of the gfx950
 constexpr uint64_t kDzGroups = 2048;     // workgroups of dz
 constexpr uint64_t kSplitBias = 2048;    // rows whose db a small layer's launch sums too
 constexpr uint64_t kDzAlone = 32;        // rows that one workgroup takes, without a launch for db
@@ -890,10 +1027,9 @@ template <Kind KIND, typename T> hipError_t direct(Product g, hipStream_t s) {
 }
 
 typedef Shape<256, 256, 128, 64, 2> Large;
-typedef Shape<256, 128, 64, 64, 3> Tall;
 typedef Shape<128, 128, 64, 64, 2> Medium;
 typedef Shape<64, 64, 32, 32, 3> Small;
-constexpr int kShapes = 4;
+constexpr int kShapes = 3;
 
 // Estimated times in us: a step takes a workgroup `alone` on its CU, or `shared` by
 // as many as fit; a tile's first loads and its results take `ends`, a piece's with
@@ -903,9 +1039,8 @@ struct TileCost {
     double alone, shared, ends, piece_ends;
 };
 constexpr TileCost kTileCosts[kShapes] = {
-    {256, 256, 1, 1.50, 1.50, 9.0, 8.0},
-    {256, 128, 1, 0.80, 0.80, 6.0, 5.0},
-    {128, 128, 2, 0.50, 0.86, 6.0, 5.0},
+    {256, 256, 1, 1.50, 1.50, 16.0, 10.0},
+    {128, 128, 2, 0.60, 0.86, 7.0, 6.0},
     {64, 64, 3, 0.35, 0.70, 5.0, 4.0},
 };
 constexpr uint64_t kLeastSteps = 4;      // of a piece
@@ -920,11 +1055,7 @@ struct TilePlan {
 double rounds(const TileCost& c, uint64_t groups, double steps, double ends) {
     const uint64_t slots = kCus * c.resident, full = groups / slots, rest = groups % slots;
     double t = (double)full * (steps * c.shared + ends);
-    if (rest) {
-        const double filled = c.resident == 1 || rest <= (uint64_t)kCus
-                                  ? 0.0 : (double)(rest - kCus) / (double)(slots - kCus);
-        t += steps * (c.alone + filled * (c.shared - c.alone)) + ends;
-    }
+    if (rest) t += steps * (rest <= kCus ? c.alone : c.shared) + ends;
     return t;
 }
 
@@ -985,15 +1116,14 @@ template <Kind KIND, typename T, typename V> hipError_t tiled(Product g, hipStre
     g.stripe = (uint32_t)(stripe < p.tiles_j ? stripe : p.tiles_j);
     const uint64_t resident = c.resident;
     if (p.shape == 0) return tiled_shape<KIND, T, V, Large>(g, resident, s);
-    if (p.shape == 1) return tiled_shape<KIND, T, V, Tall>(g, resident, s);
-    if (p.shape == 2) return tiled_shape<KIND, T, V, Medium>(g, resident, s);
+    if (p.shape == 1) return tiled_shape<KIND, T, V, Medium>(g, resident, s);
     return tiled_shape<KIND, T, V, Small>(g, resident, s);
 }
 
 // Estimated time of a small product: its tiles' rows come from L2 again and again.
 double split_cost(uint64_t rows, uint64_t cols, uint64_t inner, uint32_t passes, hc_type type) {
     const double tiles = (double)up(rows, kSplitTile) * (double)up(cols, kSplitTile);
-    return 2.5 + tiles * passes * (double)inner * (2 * kSplitTile) * (type == HC_T_F32 ? 4 : 2) / 6e6;
+    return 2.5 + tiles * passes * (double)inner * (2 * kSplitTile) * (type == HC_T_F32 ? 4 : 2) / 4e6;
 }
 
 // How a product runs: operands as the tiles take them (fp32 in three planes) or as
@@ -1032,7 +1162,7 @@ template <typename T> hipError_t split_grad(SplitGrad g, hipStream_t s) {
 
 template <Kind KIND> hipError_t product(const Product& g, hc_type type, Way way, hipStream_t s) {
     if (way == TILED) {
-        if (type == HC_T_F32) return tiled<KIND, float, b8>(g, s);
+        if (type == HC_T_F32) return tiled<KIND, float, h8>(g, s);
         if (type == HC_T_BF16) return tiled<KIND, __bf16, b8>(g, s);
         return tiled<KIND, _Float16, h8>(g, s);
     }
@@ -1068,17 +1198,23 @@ bool tile_rows(const void* p, uint64_t cols, uint64_t ld) {
 // Whether operands that the tiles cannot take as they are (fp32: all) are copied
 // for them, rather than multiplied directly: by estimated times that are linear in
 // m, so that what is copied for m rows is room for fewer.  Direct products reach 75
-// TFLOP/s in fp32 and 170 to 400 in 16 bits; tiles a sixth of 1000 and 1000.
-bool worth_packing(const hc_linear_params& p, hc_type type, double products) {
-    const double flops = 2.0 * (double)p.m * (double)p.n * (double)p.k * products;
-    const double bytes = (type == HC_T_F32 ? 16.0 : 4.0) *
-                         ((double)p.m * p.k + (double)p.n * p.k + (products > 1 ? (double)p.m * p.n : 0.0));
-    const double gain = type == HC_T_F32 ? 1.0 / 75e6 - 6.0 / 1000e6 : 1.0 / 280e6 - 1.0 / 1000e6;
-    return p.k <= kMostTileLd && p.n <= kMostTileLd && flops * gain > bytes / 4e6 + 15.0;
+// TFLOP/s in fp32 and 170 to 400 in 16 bits; tiles a third of 1000 and 1000.
+bool worth_packing(const hc_linear_params& p, hc_type type, bool grad) {
+    const bool fp32 = type == HC_T_F32;
+    const double mk = (double)p.m * p.k, nk = (double)p.n * p.k, mn = (double)p.m * p.n;
+    const double flops = 2.0 * mn * p.k * (grad ? 2.0 : 1.0);
+    // what packing moves, and its launches
+    const double bytes = !fp32 ? 4.0 * (mk + nk + (grad ? mn : 0.0)) : grad ? 12.0 * (mk + nk) + 24.0 * mn : 8.0 * (mk + nk);
+    const double launches = !fp32 ? 15.0 : grad ? 40.0 : 15.0;
+    const double gain = fp32 ? 1.0 / 75e6 - 3.0 / 1000e6 : 1.0 / 280e6 - 1.0 / 1000e6;
+    return p.k <= kMostTileLd && p.n <= kMostTileLd && flops * gain > bytes / 4e6 + launches;
 }
 
 struct Layout {
     size_t x, w, dz, bias, part, bytes;
+    size_t dz_rows, dz_cols;          // fp32: its planes by rows and by columns
+    size_t row_most, col_most;        // the largest elements: forward of x and w; of dz,
+    uint64_t x_most, w_most, most;    // and of dz, x and w by columns, from here and in all
     uint64_t k_ld, n_ld;  // of packed rows
     uint64_t per, blocks;
     uint32_t width;
@@ -1093,12 +1229,12 @@ size_t take(size_t& at, size_t bytes) {
 
 // Copies of x and w: where they are worth it, and they may be needed (a pointer's
 // alignment is not known here; one that is off by itself goes the direct way).
-void take_packed(const hc_linear_params& p, hc_type type, double products, size_t& at, Layout* L) {
-    const size_t size = type == HC_T_F32 ? 6 : 2;
+void take_packed(const hc_linear_params& p, hc_type type, bool grad, size_t& at, Layout* L) {
+    const size_t size = type == HC_T_F32 ? 4 : 2;
     L->k_ld = up(p.k, 64) * 64;
     L->n_ld = up(p.n, 64) * 64;
     L->pack = (type == HC_T_F32 || p.k % 8 || p.x_ld % 8 || p.w_ld % 8 || p.x_ld > kMostTileLd ||
-               p.w_ld > kMostTileLd) && worth_packing(p, type, products);
+               p.w_ld > kMostTileLd) && worth_packing(p, type, grad);
     L->x = take(at, L->pack ? p.m * L->k_ld * size : 0);
     L->w = take(at, L->pack ? p.n * L->k_ld * size : 0);
 }
@@ -1106,7 +1242,10 @@ void take_packed(const hc_linear_params& p, hc_type type, double products, size_
 Layout linear_layout(const hc_linear_params& p, hc_type type) {
     Layout L = {};
     size_t at = 0;
-    take_packed(p, type, 1.0, at, &L);
+    take_packed(p, type, false, at, &L);
+    const bool planes = L.pack && type == HC_T_F32;
+    L.row_most = take(at, planes ? p.m * 4 : 0);
+    L.col_most = take(at, planes ? L.n_ld * 4 : 0);
     L.part = take(at, most_part_bytes(p.m, p.n));
     L.bytes = at;
     return L;
@@ -1115,7 +1254,7 @@ Layout linear_layout(const hc_linear_params& p, hc_type type) {
 Layout grad_layout(const hc_linear_params& p, hc_type type) {
     Layout L = {};
     size_t at = 0;
-    take_packed(p, type, 2.0, at, &L);
+    take_packed(p, type, true, at, &L);
     const uint64_t groups = L.n_ld / 8;
     // as few column blocks of up to 64 lanes as there can be, evenly wide
     const uint64_t across = up(groups, 64);
@@ -1123,7 +1262,15 @@ Layout grad_layout(const hc_linear_params& p, hc_type type) {
     const uint64_t step = 256 / L.width, most = across < kDzGroups ? kDzGroups / across : 1;
     L.per = p.m <= kDzAlone ? kDzAlone : up(up(p.m, most), step) * step;
     L.blocks = p.m ? up(p.m, L.per) : 0;
-    L.dz = take(at, p.m * L.n_ld * (type == HC_T_F32 ? (L.pack ? 6 : 4) : type == HC_T_BF16 ? 6 : 4));
+    L.dz = take(at, p.m * L.n_ld * (type == HC_T_BF16 ? 6 : 4));
+    const bool planes = L.pack && type == HC_T_F32;
+    L.dz_rows = take(at, planes ? p.m * L.n_ld * 4 : 0);
+    L.dz_cols = take(at, planes ? p.m * L.n_ld * 4 : 0);
+    L.row_most = take(at, planes ? p.m * 4 : 0);
+    L.x_most = L.n_ld;
+    L.w_most = L.n_ld + L.k_ld;
+    L.most = L.n_ld + 2 * L.k_ld;
+    L.col_most = take(at, planes ? L.most * 4 : 0);
     L.bias = take(at, (p.m < most ? p.m : most) * p.n * 4);
     const size_t a = most_part_bytes(p.m, p.k), b = most_part_bytes(p.n, p.k);
     L.part = take(at, a > b ? a : b);
@@ -1136,7 +1283,7 @@ struct Operand {
     uint64_t ld, cols, plane;
 };
 
-// rows x cols of an operand in tiles' form: where it is, or packed into `to`.
+// rows x cols of a 16-bit operand in tiles' form: where it is, or packed into `to`.
 hipError_t packed(hc_type type, bool pack, const void* p, uint64_t rows, uint64_t cols, uint64_t ld, void* to,
                   uint64_t to_ld, Operand* out, hipStream_t s) {
     *out = {p, ld, cols, 0};
@@ -1144,9 +1291,31 @@ hipError_t packed(hc_type type, bool pack, const void* p, uint64_t rows, uint64_
     const PackArgs a = {p, to, rows, ld, to_ld, rows * to_ld, (uint32_t)cols};
     *out = {to, to_ld, to_ld, a.plane};
     const dim3 grid((uint32_t)up(rows * (to_ld / 8), 256));
-    if (type == HC_T_F32) hipLaunchKernelGGL(pack_kernel<float>, grid, dim3(256), 0, s, a);
-    else if (type == HC_T_BF16) hipLaunchKernelGGL(pack_kernel<__bf16>, grid, dim3(256), 0, s, a);
+    if (type == HC_T_BF16) hipLaunchKernelGGL(pack_kernel<__bf16>, grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL(pack_kernel<_Float16>, grid, dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+// An fp32 operand in planes, scaled by its rows (and again by its columns into
+// cols_out), or by its columns, whose largest elements are taken first if `find`.
+hipError_t split_rows(const void* p, uint64_t rows, uint64_t cols, uint64_t ld, void* to, uint64_t to_ld, float* most,
+                      void* cols_out, const float* cols_most, Operand* out, hipStream_t s) {
+    const SplitRowsArgs a = {{p, to, rows, ld, to_ld, rows * to_ld, (uint32_t)cols}, most, cols_out, cols_most};
+    *out = {to, to_ld, to_ld, a.pack.plane};
+    hipLaunchKernelGGL(split_rows_kernel, dim3((uint32_t)(rows < 65536 ? rows : 65536)), dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+hipError_t split_columns(const void* p, uint64_t rows, uint64_t cols, uint64_t ld, void* to, uint64_t to_ld,
+                         float* most, bool find, Operand* out, hipStream_t s) {
+    const PackArgs a = {p, to, rows, ld, to_ld, rows * to_ld, (uint32_t)cols};
+    *out = {to, to_ld, to_ld, a.plane};
+    if (find) {
+        const uint64_t per = rows > 32 * 1024 ? up(rows, 1024) : 32;
+        hipLaunchKernelGGL(most_kernel, dim3((uint32_t)up(cols, 512), (uint32_t)up(rows, per)), dim3(256), 0, s, a, per,
+                           most);
+    }
+    hipLaunchKernelGGL(split_columns_kernel, dim3((uint32_t)up(rows * (to_ld / 8), 256)), dim3(256), 0, s, a, most);
     return hipGetLastError();
 }
 
@@ -1173,19 +1342,30 @@ hipError_t launch_linear(const hc_linear_params& p, const Dropout& d, hc_type ty
     const bool fp32 = type == HC_T_F32;
     const bool x_fits = !fp32 && tile_rows(x, p.k, p.x_ld), w_fits = !fp32 && tile_rows(w, p.k, p.w_ld);
     const bool in_tiles = L.pack || (x_fits && w_fits);
-    Operand ox, ow;
-    hipError_t e = packed(type, L.pack && !x_fits, x, p.m, p.k, p.x_ld, ws + L.x, L.k_ld, &ox, s);
-    if (e != hipSuccess) return e;
-    e = packed(type, L.pack && !w_fits, w, p.n, p.k, p.w_ld, ws + L.w, L.k_ld, &ow, s);
-    if (e != hipSuccess) return e;
     Product g = {};
-    set(&g, ox, ow);
-    g.passes = fp32 && in_tiles ? kThreePlanes : kOnePass;
+    g.passes = kOnePass;
     g.rows = p.m;
     g.cols = (uint32_t)p.n;
     g.inner = p.k;
     g.part = reinterpret_cast<float*>(ws + L.part);
     g.forward = {bias, residual, y, z, p.residual_ld, p.y_ld, p.z_ld, p.act, d};
+    Operand ox, ow;
+    hipError_t e;
+    if (fp32 && in_tiles) {
+        float *x_most = reinterpret_cast<float*>(ws + L.row_most), *w_most = reinterpret_cast<float*>(ws + L.col_most);
+        e = split_rows(x, p.m, p.k, p.x_ld, ws + L.x, L.k_ld, x_most, nullptr, nullptr, &ox, s);
+        if (e == hipSuccess) e = split_rows(w, p.n, p.k, p.w_ld, ws + L.w, L.k_ld, w_most, nullptr, nullptr, &ow, s);
+        if (e != hipSuccess) return e;
+        g.passes = kTwoPlanes;
+        g.p_most = x_most;
+        g.q_most = w_most;
+        set(&g, ox, ow);
+        return product<FORWARD>(g, type, TILED, s);
+    }
+    e = packed(type, L.pack && !x_fits, x, p.m, p.k, p.x_ld, ws + L.x, L.k_ld, &ox, s);
+    if (e == hipSuccess) e = packed(type, L.pack && !w_fits, w, p.n, p.k, p.w_ld, ws + L.w, L.k_ld, &ow, s);
+    if (e != hipSuccess) return e;
+    set(&g, ox, ow);
     const Way way = way_of(g, type, in_tiles);
     if (way != SPLIT) return product<FORWARD>(g, type, way, s);
     if (type == HC_T_F32) return split_forward<float>(g, s);
@@ -1201,12 +1381,13 @@ hipError_t launch_linear_grad(const hc_linear_params& p, const Dropout& d, hc_ty
     char* ws = static_cast<char*>(ws_);
     const bool fp32 = type == HC_T_F32, plain = p.act == HC_ACT_NONE && d.limit == 0;
     const bool x_fits = !fp32 && tile_rows(q.x, p.k, p.x_ld), w_fits = !fp32 && tile_rows(q.w, p.k, p.w_ld);
-    const bool in_tiles = L.pack || ((!q.dw || x_fits) && (!q.dx || w_fits));
+    const bool in_tiles = L.pack || ((!q.dw || x_fits) && (!q.dx || w_fits) && p.n <= kMostTileLd && !fp32);
     const bool rest = !plain && q.dw && !fp32 && (q.g_type == HC_T_F32 || q.g_type == HC_T_I32);
     Product dx = {}, dw = {};
     dx.part = dw.part = reinterpret_cast<float*>(ws + L.part);
     dx.cols = dw.cols = (uint32_t)p.k;
-    dx.passes = dw.passes = fp32 && in_tiles ? kThreePlanes : kOnePass;
+    const bool planes = fp32 && in_tiles;
+    dx.passes = dw.passes = planes ? kTwoPlanes : kOnePass;
     dx.rows = dw.inner = p.m;
     dx.inner = dw.rows = p.n;
     if (rest) dw.passes = type == HC_T_BF16 ? kRestBf16 : kRestF16;
@@ -1222,13 +1403,18 @@ hipError_t launch_linear_grad(const hc_linear_params& p, const Dropout& d, hc_ty
     db.out = q.db;
     const Way dx_way = way_of(dx, type, in_tiles), dw_way = way_of(dw, type, in_tiles);
     // small layers go in one launch, where nothing is packed for it; db too if dz is dy
-    const bool together = !(fp32 && in_tiles) && (!dx.gradient.out || dx_way == SPLIT) && (!q.dw || dw_way == SPLIT);
+    const bool together = !planes && (!dx.gradient.out || dx_way == SPLIT) && (!q.dw || dw_way == SPLIT);
     // dz is dy itself where nothing changes it and the products can take it
-    const bool dy_fits = plain && (in_tiles && !together ? !fp32 && tile_rows(q.dy, p.n, p.y_ld) : true);
+    const bool dy_fits = plain && (planes || together || !in_tiles || tile_rows(q.dy, p.n, p.y_ld));
     const bool dz = !dy_fits && (q.dx || q.dw), db_together = together && plain && p.m <= kSplitBias;
     hipError_t e = hipSuccess;
     Operand oz = {q.dy, p.y_ld, p.n, 0};
-    if ((dz || (q.db && !db_together)) && p.m) {
+    float* col_most = reinterpret_cast<float*>(ws + L.col_most);
+    if (planes && p.m) {
+        e = launch_fill_u32(reinterpret_cast<uint32_t*>(col_most), L.most, 0, s);
+        if (e != hipSuccess) return e;
+    }
+    if ((dz || (q.db && !db_together) || (planes && q.dw)) && p.m) {
         DzArgs a = {};
         a.dy = q.dy;
         a.z = q.z;
@@ -1245,9 +1431,10 @@ hipError_t launch_linear_grad(const hc_linear_params& p, const Dropout& d, hc_ty
             a.dz.out = ws + L.dz;
             a.dz.out_ld = L.n_ld;
             a.dz.plane = p.m * L.n_ld;
-            a.planes = fp32 ? (in_tiles ? 3 : 1) : !rest ? 1 : type == HC_T_BF16 ? 3 : 2;
+            a.planes = !rest ? 1 : type == HC_T_BF16 ? 3 : 2;
             oz = {a.dz.out, L.n_ld, L.n_ld, a.dz.plane};
         }
+        a.most = planes && q.dw ? col_most : nullptr;
         a.part = q.db && !db_together ? reinterpret_cast<float*>(ws + L.bias) : nullptr;
         a.db = db;
         const dim3 grid((uint32_t)up(a.groups, L.width), (uint32_t)L.blocks);
@@ -1279,6 +1466,35 @@ hipError_t launch_linear_grad(const hc_linear_params& p, const Dropout& d, hc_ty
         if (fp32) return split_grad<float>(g, s);
         if (type == HC_T_BF16) return split_grad<__bf16>(g, s);
         return split_grad<_Float16>(g, s);
+    }
+    if (planes && p.m) {
+        float* row_most = reinterpret_cast<float*>(ws + L.row_most);
+        Operand by_rows, by_cols, ox, ow;
+        by_cols = {ws + L.dz_cols, L.n_ld, L.n_ld, p.m * L.n_ld};
+        if (q.dx)
+            e = split_rows(oz.p, p.m, p.n, oz.ld, ws + L.dz_rows, L.n_ld, row_most,
+                           q.dw ? ws + L.dz_cols : nullptr, col_most, &by_rows, s);
+        else if (q.dw)
+            e = split_columns(oz.p, p.m, p.n, oz.ld, ws + L.dz_cols, L.n_ld, col_most, false, &by_cols, s);
+        if (e != hipSuccess) return e;
+        if (q.dx) {
+            e = split_columns(q.w, p.n, p.k, p.w_ld, ws + L.w, L.k_ld, col_most + L.w_most, true, &ow, s);
+            if (e != hipSuccess) return e;
+            set(&dx, by_rows, ow);
+            dx.p_most = row_most;
+            dx.q_most = col_most + L.w_most;
+            e = product<DX>(dx, type, TILED, s);
+            if (e != hipSuccess) return e;
+        }
+        if (q.dw) {
+            e = split_columns(q.x, p.m, p.k, p.x_ld, ws + L.x, L.k_ld, col_most + L.x_most, true, &ox, s);
+            if (e != hipSuccess) return e;
+            set(&dw, by_cols, ox);
+            dw.p_most = col_most;
+            dw.q_most = col_most + L.x_most;
+            e = product<DW>(dw, type, TILED, s);
+        }
+        return e;
     }
     if (dx.gradient.out) {
         Operand ow;

@@ -135,7 +135,9 @@ hc_status check_ortho(const hc_orthogonalise_params* p, OrthoStep* steps) {
 
 // ---- layers ----------------------------------------------------------------------
 
-constexpr uint64_t kMostElements = 1ull << 38, kMostStride = 1ull << 31;
+// A launch has fewer than 2^32 lanes: of dropout one for 32 elements, of a layer's
+// copies one for 8 with their padding.
+constexpr uint64_t kMostElements = 1ull << 35, kMostLayer = 1ull << 34, kMostStride = 1ull << 31;
 
 hc_status check_drop(float p) {
     return p >= 0.0f && p <= 1.0f ? HC_OK : fail(HC_EINVAL, "p must be in [0, 1]");
@@ -151,7 +153,7 @@ hc_status check_dropout(const hc_dropout_params* p) {
     if (p == nullptr) return fail(HC_EINVAL, "params is NULL");
     if (p->rows > 0x7fffffffull) return fail(HC_EINVAL, "rows must be at most 2^31 - 1");
     if (p->cols < 1 || p->cols > 0x7fffffffull) return fail(HC_EINVAL, "cols must be in [1, 2^31 - 1]");
-    if (p->rows * p->cols > kMostElements) return fail(HC_EINVAL, "at most 2^38 elements");
+    if (p->rows * p->cols > kMostElements) return fail(HC_EINVAL, "at most 2^35 elements");
     if (p->reserved != 0) return fail(HC_EINVAL, "reserved must be 0");
     return check_drop(p->p);
 }
@@ -162,11 +164,11 @@ bool bad_stride(uint64_t ld, uint64_t cols) { return ld < cols || ld > kMostStri
 hc_status check_linear(const hc_linear_params* p, uint32_t type) {
     if (p == nullptr) return fail(HC_EINVAL, "params is NULL");
     if (!float_type(type)) return fail(HC_EINVAL, "unknown type");
-    if (p->m > 0x7fffffffull) return fail(HC_EINVAL, "m must be at most 2^31 - 1");
+    if (p->m > (1ull << 27)) return fail(HC_EINVAL, "m must be at most 2^27");
     if (p->n < 1 || p->k < 1 || p->n > (1ull << 24) || p->k > (1ull << 24))
         return fail(HC_EINVAL, "n and k must be in [1, 2^24]");
-    if (p->m * p->n > kMostElements || p->m * p->k > kMostElements || p->n * p->k > kMostElements)
-        return fail(HC_EINVAL, "matrices have at most 2^38 elements");
+    if (p->m * p->n > kMostLayer || p->m * p->k > kMostLayer || p->n * p->k > kMostLayer)
+        return fail(HC_EINVAL, "matrices have at most 2^34 elements");
     if (bad_stride(p->x_ld, p->k) || bad_stride(p->w_ld, p->k) || bad_stride(p->y_ld, p->n))
         return fail(HC_EINVAL, "row strides must be at least the columns and at most 2^31");
     if (p->act > HC_ACT_SIGMOID) return fail(HC_EINVAL, "unknown act");

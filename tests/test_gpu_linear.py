@@ -1,8 +1,9 @@
 """The linear layer and its gradient against their definition in 64 bits.
 
 Tolerances, from the arithmetic.  A sum of t products in fp32, in any grouping, is within (t + 2)
-2^-24 of the sum S of its terms' magnitudes (products of 16-bit values are exact; three bf16 parts
-of an fp32 value leave 2^-23 of a product).  An activation's slope is at most 1.13, and its own
+2^-24 of the sum S of its terms' magnitudes (products of 16-bit values are exact; fp32 in two fp16
+parts is 2^-22 off, and a product of two leaves the rests' out: 3 2^-22; below 2^-29 of a row's largest
+2^-51 of that).  An activation's slope is at most 1.13, and its own
 error is layer_reference.FUNCTION relative to its factors.  Dropout's factor and a residual are 3
 roundings.  The result is rounded by half a unit.  In the gradient of 16-bit types dz is rounded by
 half a unit h before the products; where the gradient is wider bf16 takes three parts (2^-24) and
@@ -16,6 +17,7 @@ pytestmark = pytest.mark.gpu
 
 TYPES = ["float32", "bfloat16", "float16"]
 SLOPE = 1.13
+PARTS, FAR = 3 * 2.0**-22, 2.0**-50   # FAR: 2^-51 of either side
 
 
 def _hc():
@@ -69,7 +71,9 @@ def check_linear(torch, L, got_y, got_z, act, p, seed, draw, bias, residual):
     x, w = L.x.cpu().double(), L.w.cpu().double()
     k = x.shape[1]
     z = x @ w.t()
-    off = (x.abs() @ w.abs().t()) * ((k + 2) * ref.UNIT + (2**-23 if d == "float32" else 0))
+    off = (x.abs() @ w.abs().t()) * ((k + 2) * ref.UNIT + (PARTS if d == "float32" else 0))
+    if d == "float32":
+        off += k * FAR * x.abs().amax(1)[:, None] * w.abs().amax(1)[None, :]
     if bias:
         b = L.bias.cpu().double()
         z, off = z + b, off + 2 * ref.UNIT * (z.abs() + b.abs())
@@ -101,11 +105,13 @@ def check_grad(torch, L, act, p, seed, draw, dx, dw, db, out, old=None, fixed=No
         slope_off = slope_off * SLOPE + dz.abs() * size * (0 if act == "relu" else 2 * ref.FUNCTION[d])
         dz = dz * slope
     plain = act == "none" and not p
-    part = 2**-23 if d == "float32" else 0
+    part = PARTS if d == "float32" else 0
     one = slope_off if plain or d == "float32" else slope_off + h * dz.abs() + ref.FLOOR[d]
     if dx is not None:
         want, size = dz @ w, dz.abs() @ w.abs()
         off = one @ w.abs() + size * ((n + 2) * ref.UNIT + part) * (1 + h)
+        if d == "float32":
+            off += n * FAR * dz.abs().amax(1)[:, None] * w.abs().amax(0)[None, :]
         _within(dx, want, off + h * (want.abs() + off) + ref.FLOOR[d], "dx")
 
     def widened(want, off, name, got):
@@ -126,7 +132,10 @@ def check_grad(torch, L, act, p, seed, draw, dx, dw, db, out, old=None, fixed=No
             wide = slope_off + h * h * dz.abs() * (1 if d == "float16" else h) + ref.FLOOR[d] * 2**-11
             terms = (2 if d == "float16" else 3) * m
         want, size = dz.t() @ x, dz.abs().t() @ x.abs()
-        widened(want, wide.t() @ x.abs() + size * ((terms + 2) * ref.UNIT + part) * (1 + h), "dw", dw)
+        off = wide.t() @ x.abs() + size * ((terms + 2) * ref.UNIT + part) * (1 + h)
+        if d == "float32":
+            off += m * FAR * dz.abs().amax(0)[:, None] * x.abs().amax(0)[None, :]
+        widened(want, off, "dw", dw)
     if db is not None:
         widened(dz.sum(0), slope_off.sum(0) + dz.abs().sum(0) * (m + 2) * ref.UNIT, "db", db)
 
@@ -512,3 +521,54 @@ def test_tiles(m, n, k, dtype):
         ws = hc.alloc_linear_grad_workspace(L.x, L.w).fill_(0xFF)
         hc.hc_linear_grad(L.dy, ws, x=L.x, w=L.w, z=L.z, dx=dx, dw=dw, db=db, act=act, p=p, seed=m, draw=n)
         check_grad(torch, L, act, p, m, n, dx, dw, db, out)
+
+
+def test_fp32_rows_and_columns_of_far_sizes():
+    """Rows and columns between 1e-30 and 1e30: fp32 products in parts keep their accuracy in each."""
+    torch, hc = _hc()
+    m, n, k = 1100, 1000, 1300
+    gen = torch.Generator().manual_seed(5)
+
+    def sizes(count):
+        return 10.0 ** torch.randint(-15, 16, (count,), generator=gen).float()
+
+    L = Layer(torch, m, n, k, "float32")
+    L.x.mul_(sizes(m)[:, None].cuda())
+    L.w.mul_(sizes(n)[:, None].cuda())
+    y = torch.empty(m, n, device="cuda")
+    hc.hc_linear(L.x, L.w, y, hc.alloc_linear_workspace(L.x, L.w))
+    L.bias.zero_()
+    check_linear(torch, L, y, None, "none", 0.0, 0, 0, False, False)
+    # dx sees rows of dy and columns of w, dw columns of dy and of x
+    L = Layer(torch, m, n, k, "float32")
+    dx, dw = torch.empty_like(L.x), torch.empty_like(L.w)
+    ws = hc.alloc_linear_grad_workspace(L.x, L.w)
+    L.dy.mul_(sizes(m)[:, None].cuda())
+    L.w.mul_(sizes(k)[None, :].cuda())
+    hc.hc_linear_grad(L.dy, ws, w=L.w, dx=dx)
+    check_grad(torch, L, "none", 0.0, 0, 0, dx, None, None, "float32")
+    L.dy.copy_(torch.randn(m, n, generator=gen)).mul_(sizes(n)[None, :].cuda())
+    L.x.mul_(sizes(k)[None, :].cuda())
+    hc.hc_linear_grad(L.dy, ws, x=L.x, dw=dw)
+    check_grad(torch, L, "none", 0.0, 0, 0, None, dw, None, "float32")
+
+
+def test_fp32_zeros_subnormals_and_nan_in_parts():
+    torch, hc = _hc()
+    m, n, k = 1100, 1000, 1300
+    L = Layer(torch, m, n, k, "float32")
+    L.x[3] = 0
+    L.x[4] = 2.0**-149
+    L.x[5, 7] = float("nan")
+    L.w[6] = 0
+    L.w[8] = 3.0e38
+    y = torch.empty(m, n, device="cuda")
+    hc.hc_linear(L.x, L.w, y, hc.alloc_linear_workspace(L.x, L.w))
+    y = y.cpu()
+    assert bool((y[3, :6] == 0).all()) and bool(torch.isnan(y[5]).all())
+    rest = torch.cat([y[:5], y[6:]])
+    assert bool((rest[:, 6] == 0).all()) and not bool(torch.isnan(rest).any())
+    want = L.x[:3].cpu().double().sum(1) * float(L.w[8, 0])
+    tol = L.x[:3].cpu().double().abs().sum(1) * 3.0e38 * ((k + 2) * ref.UNIT + PARTS)
+    inside = want.abs() + tol < 3.4e38
+    assert bool(((rest[:3, 8].double() - want).abs() <= tol)[inside].all())

@@ -177,7 +177,7 @@ __global__ __launch_bounds__(256) void direct_kernel(Product g) {
     const uint64_t first = piece * all / g.pieces, end = (piece + 1) * all / g.pieces;
     const T* q = static_cast<const T*>(g.q);
     f4 acc[2][2] = {};
-    T rp[8], rq[8];
+    T rp[8], rq[8];  // of the next step: more would cost workgroups of a CU (65536 x 64 x 128 fp32: 17 us, 20 with four)
     for (uint64_t s = first; s < end;) {
         const uint32_t pass = (uint32_t)(s / lines);
         const uint64_t stop = min(end, (pass + 1) * lines);
@@ -287,6 +287,18 @@ __device__ __forceinline__ void split_tile(const Product& g, uint32_t tile, floa
     const uint64_t row0 = (uint64_t)ti * kSplitTile;
     const uint32_t col0 = tj * kSplitTile, inner = (uint32_t)g.inner;
     const uint32_t lines = (inner + kStep - 1) / kStep;
+    // the lanes that store results ask for what is added to them first
+    const uint32_t i = threadIdx.x / 2 % 16, j = threadIdx.x % 2 * 8, col = col0 + j;
+    const bool finishes = threadIdx.x < 32 && row0 + i < g.rows && col < g.cols;
+    float bias[8] = {};
+    T residual[8];
+    if constexpr (KIND == FORWARD)
+        if (finishes) {
+            const Forward& f = g.forward;
+            if (f.bias) load8(static_cast<const T*>(f.bias) + col, g.cols - col, bias);
+            if (f.residual)
+                load8_raw(static_cast<const T*>(f.residual) + (row0 + i) * f.residual_ld + col, g.cols - col, residual);
+        }
     f4 acc = {};
     for (uint32_t pass = 0; pass < g.passes.count; pass++) {
         const T* p = static_cast<const T*>(g.p) + (g.passes.p_planes >> 4 * pass & 15u) * g.p_plane;
@@ -313,16 +325,15 @@ __device__ __forceinline__ void split_tile(const Product& g, uint32_t tile, floa
     }
     *reinterpret_cast<f4*>(&s_sum[wave][lane & 15][(lane >> 4) * 4]) = acc;
     __syncthreads();
-    if (threadIdx.x < 32) {
-        const uint32_t i = threadIdx.x / 2, j = threadIdx.x % 2 * 8;
-        float v[8] = {};
-        for (uint32_t w = 0; w < kSplitWaves; w++)
+    if (!finishes) return;
+    float v[8] = {};
+    for (uint32_t w = 0; w < kSplitWaves; w++)
 #pragma unroll
-            for (int e = 0; e < 8; e++) v[e] += s_sum[w][i][j + e];
-        Masks masks = {};
-        if constexpr (KIND == FORWARD) masks = masks_of(g.forward.drop);
-        if (row0 + i < g.rows && col0 + j < g.cols) finish8<KIND, T>(g, masks, row0 + i, col0 + j, v);
-    }
+        for (int e = 0; e < 8; e++) v[e] += s_sum[w][i][j + e];
+    if constexpr (KIND == FORWARD)
+        finish_forward<T>(g.forward, masks_of(g.forward.drop), row0 + i, g.rows, col, g.cols - col, bias, residual, v);
+    else
+        finish8<KIND, T>(g, Masks{}, row0 + i, col, v);
 }
 
 template <typename T> __global__ __launch_bounds__(512) void split_forward_kernel(Product g) {
@@ -1120,10 +1131,12 @@ template <Kind KIND, typename T, typename V> hipError_t tiled(Product g, hipStre
     return tiled_shape<KIND, T, V, Small>(g, resident, s);
 }
 
-// Estimated time of a small product: its tiles' rows come from L2 again and again.
+// Estimated time of a small product: its tiles' rows come from L2 again and again, and
+// four workgroups on a CU take 4 us at least.
 double split_cost(uint64_t rows, uint64_t cols, uint64_t inner, uint32_t passes, hc_type type) {
     const double tiles = (double)up(rows, kSplitTile) * (double)up(cols, kSplitTile);
-    return 2.5 + tiles * passes * (double)inner * (2 * kSplitTile) * (type == HC_T_F32 ? 4 : 2) / 4e6;
+    return 2.5 + tiles * passes * (double)inner * (2 * kSplitTile) * (type == HC_T_F32 ? 4 : 2) / 4e6 +
+           tiles / (4 * kCus) * 4.0;
 }
 
 // How a product runs: operands as the tiles take them (fp32 in three planes) or as

@@ -572,3 +572,18 @@ def test_fp32_zeros_subnormals_and_nan_in_parts():
     tol = L.x[:3].cpu().double().abs().sum(1) * 3.0e38 * ((k + 2) * ref.UNIT + PARTS)
     inside = want.abs() + tol < 3.4e38
     assert bool(((rest[:3, 8].double() - want).abs() <= tol)[inside].all())
+
+
+@pytest.mark.parametrize("m,n,k", [(16384, 64, 128), (20001, 40, 24), (33000, 7, 250), (17000, 64, 256)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_many_rows_through_a_small_matrix(m, n, k, dtype):
+    torch, hc = _hc()
+    dt = getattr(torch, dtype)
+    for (a, b), gap in (((n, k), 0), ((k, n), 3)):   # the forward pass's and dx's
+        L = Layer(torch, m, a, b, dtype, gap)
+        y, dx = torch.empty(m, a, device="cuda", dtype=dt), torch.empty(m, b, device="cuda", dtype=dt)
+        hc.hc_linear(L.x, L.w, y, hc.alloc_linear_workspace(L.x, L.w), bias=L.bias, residual=L.residual, act="silu",
+                     p=0.1, seed=m)
+        check_linear(torch, L, y, None, "silu", 0.1, m, 0, True, True)
+        hc.hc_linear_grad(L.dy, hc.alloc_linear_grad_workspace(L.x, L.w), w=L.w, dx=dx)
+        check_grad(torch, L, "none", 0.0, 0, 0, dx, None, None, dtype)

@@ -1,10 +1,11 @@
 """Data-parallel training steps with compressed gradients, end to end on one GPU.
 
 A bag-of-words classifier: token ids are looked up in a scaled embedding table
-(hc_embed), the mean of a sequence's rows goes through one weight matrix, and a
-cross entropy is taken.  Every simulated worker has its own batch.  Its gradient
-is one flat int32 vector in fixed point, the table's part summed by token id
-(hc_embed_grad) and the matrix's part behind it.  Workers encode their vectors
+(hc_embed), the mean of a sequence's rows goes through dropout (hc_dropout) and
+one layer (hc_linear), and a cross entropy is taken.  Every simulated worker has
+its own batch.  Its gradient is one flat int32 vector in fixed point, the table's
+part summed by token id (hc_embed_grad) and the layer's matrix (hc_linear_grad)
+behind it.  Workers encode their vectors
 (hc_encode), the sketches are summed and the indexes OR-ed (hc_aggregate), and
 the exact sum is recovered (hc_decode).  The recovered sum updates the table
 directly, and the matrix through its momentum made orthogonal
@@ -25,7 +26,7 @@ import torch  # noqa: E402
 import paper_2402_07529_amd as hc  # noqa: E402
 
 VOCAB, DIM, CLASSES, WORDS, BATCH = 20000, 64, 96, 24, 256
-SCALE = DIM**0.5
+SCALE, DROP = DIM**0.5, 0.1
 
 
 def batch(gen, meaning):
@@ -35,6 +36,40 @@ def batch(gen, meaning):
     ids = meaning[label].gather(1, pick)
     pad = torch.rand(BATCH, WORDS, device="cuda", generator=gen) < 0.125
     return torch.where(pad, -1, ids).to(torch.int32), label
+
+
+class Worker:
+    """What one worker keeps: its buffers and workspaces."""
+
+    def __init__(self, seed):
+        def empty(*shape):
+            return torch.empty(shape, device="cuda")
+
+        self.seed = seed
+        self.rows, self.mean, self.kept = empty(BATCH, WORDS, DIM), empty(BATCH, DIM), empty(BATCH, DIM)
+        self.logits, self.d_kept = empty(BATCH, CLASSES), empty(BATCH, DIM)
+        weight = empty(CLASSES, DIM)
+        self.layer_ws = hc.alloc_linear_workspace(self.kept, weight)
+        self.layer_grad_ws = hc.alloc_linear_grad_workspace(self.kept, weight)
+        self.table_ws = hc.alloc_embed_workspace(VOCAB, DIM, BATCH * WORDS)
+
+    def gradient(self, table, weight, ids, label, draw, flat):
+        """The gradient of the batch's mean loss, in fixed point, into flat; returns the loss."""
+        hc.hc_embed(table, ids, self.rows, scale=SCALE)
+        torch.mean(self.rows, 1, out=self.mean)
+        hc.hc_dropout(self.mean, self.kept, DROP, self.seed, draw)
+        hc.hc_linear(self.kept, weight, self.logits, self.layer_ws)
+        loss = torch.nn.functional.cross_entropy(self.logits, label)
+        d_logits = torch.softmax(self.logits, 1)
+        d_logits[torch.arange(BATCH, device="cuda"), label] -= 1.0
+        d_logits /= BATCH
+        n_table = VOCAB * DIM
+        hc.hc_linear_grad(d_logits, self.layer_grad_ws, x=self.kept, w=weight, dx=self.d_kept,
+                          dw=flat[n_table:].view(CLASSES, DIM))
+        hc.hc_dropout(self.d_kept, self.d_kept, DROP, self.seed, draw)  # the same mask
+        d_rows = (self.d_kept / WORDS)[:, None].expand(BATCH, WORDS, DIM).contiguous()
+        hc.hc_embed_grad(d_rows, ids, flat[:n_table].view(VOCAB, DIM), self.table_ws, scale=SCALE)
+        return loss
 
 
 def main(steps=20, workers=4, seed=0, table_lr=20.0, matrix_lr=0.1, momentum=0.9):
@@ -59,23 +94,15 @@ def main(steps=20, workers=4, seed=0, table_lr=20.0, matrix_lr=0.1, momentum=0.9
     y_sum, b_sum = torch.empty_like(y[0]), torch.empty_like(b[0])
     total = torch.empty(n, device="cuda", dtype=torch.int32)
     info, ws = hc.alloc_info(), hc.alloc_workspace(p, most)
-    rows = torch.empty((BATCH, WORDS, DIM), device="cuda")
-    grad_ws = hc.alloc_embed_workspace(VOCAB, DIM, BATCH * WORDS)
+    worker = Worker(seed)
     ortho_ws, update = hc.alloc_orthogonalise_workspace(weight), torch.empty_like(weight)
 
     losses = []
-    for _ in range(steps):
+    for step in range(steps):
         loss = 0.0
         for w in range(workers):
             ids, label = batch(gen, meaning)
-            hc.hc_embed(table, ids, rows, scale=SCALE)
-            x = rows.detach().requires_grad_()
-            m = weight.detach().requires_grad_()
-            out = torch.nn.functional.cross_entropy(x.mean(1) @ m.t(), label)
-            out.backward()
-            loss += out.detach() / workers
-            hc.hc_embed_grad(x.grad, ids, flat[w, :n_table].view(VOCAB, DIM), grad_ws, scale=SCALE)
-            flat[w, n_table:] = torch.round(m.grad * hc.FIXED_POINT).to(torch.int32).view(-1)
+            loss += worker.gradient(table, weight, ids, label, step * workers + w, flat[w]) / workers
             hc.hc_encode(p, flat[w], y[w], b[w])
         hc.hc_aggregate(p, y, b, workers, y_sum, b_sum)
         hc.hc_decode(p, y_sum, b_sum, info, ws, x_out=total, max_support=most, plan=plan)

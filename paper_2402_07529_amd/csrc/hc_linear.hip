@@ -569,14 +569,15 @@ template <int END, int STEP, int I = 0, typename F> __device__ __forceinline__ v
     }
 }
 
-// Columns col .. col + 7 of FM rows 16 apart become results.  What is read for them
-// is asked for before the first is stored: a load behind a store would wait for it.
 // The power of two that an fp32 row's planes are scaled by: its largest element is
 // brought to 2^14 .. 2^15.
 __device__ __forceinline__ int scale_of(float most) {
     return most == 0.0f ? 0 : 15 - __builtin_amdgcn_frexp_expf(most);
 }
 
+// Columns col .. col + 7 of FM rows 16 apart become results.  What is read for some
+// rows is asked for before the first of them is stored: a load behind a store would
+// wait for it.
 template <Kind KIND, typename T, int FIRST, int FM, int FN>
 __device__ __forceinline__ void finish_rows(const Product& g, const Masks& masks, uint64_t row0, uint32_t col,
                                             const f4 (&acc)[FM][FN]) {
@@ -1020,13 +1021,17 @@ uint64_t up(uint64_t v, uint64_t to) { return (v + to - 1) / to; }
 constexpr uint64_t kSlots = 1024;
 constexpr uint64_t kMostPieces = 64;
 
+uint64_t direct_pieces(uint64_t tiles, uint64_t lines) {
+    uint64_t pieces = kSlots / tiles;
+    pieces = pieces > lines / 4 ? lines / 4 : pieces;
+    return pieces > kMostPieces ? kMostPieces : pieces < 1 ? 1 : pieces;
+}
+
 template <Kind KIND, typename T> hipError_t direct(Product g, hipStream_t s) {
     const uint64_t lines = up(g.inner, kStep) * g.passes.count;
     g.tiles_j = (uint32_t)up(g.cols, kDirect);
     const uint64_t tiles = up(g.rows, kDirect) * g.tiles_j;
-    uint64_t pieces = kSlots / tiles;
-    pieces = pieces > lines / 4 ? lines / 4 : pieces;
-    pieces = pieces > kMostPieces ? kMostPieces : pieces < 1 ? 1 : pieces;
+    const uint64_t pieces = direct_pieces(tiles, lines);
     g.cut = (uint32_t)tiles;
     g.pieces = (uint32_t)pieces;
     g.part_ld = (uint32_t)up(g.cols, 8) * 8;
@@ -1131,26 +1136,35 @@ template <Kind KIND, typename T, typename V> hipError_t tiled(Product g, hipStre
     return tiled_shape<KIND, T, V, Small>(g, resident, s);
 }
 
-// Estimated time of a small product: its tiles' rows come from L2 again and again, and
-// four workgroups on a CU take 4 us at least.
+// Estimated time of a small product: a wave's four steps take 1 us, its tiles' rows
+// come from L2 again and again, and four workgroups on a CU take 4 us at least.
 double split_cost(uint64_t rows, uint64_t cols, uint64_t inner, uint32_t passes, hc_type type) {
     const double tiles = (double)up(rows, kSplitTile) * (double)up(cols, kSplitTile);
-    return 2.5 + tiles * passes * (double)inner * (2 * kSplitTile) * (type == HC_T_F32 ? 4 : 2) / 4e6 +
-           tiles / (4 * kCus) * 4.0;
+    const uint64_t lines = up(inner, kStep) * passes;
+    const uint64_t live = (rows < kSplitTile ? rows : kSplitTile) + (cols < kSplitTile ? cols : kSplitTile);
+    return 1.5 + 1.0 * (double)up(lines, kSplitWaves * kSplitAhead) + tiles / (4 * kCus) * 4.0 +
+           tiles * passes * (double)inner * (double)live * (type == HC_T_F32 ? 4 : 2) / 9e6;
 }
 
-// How a product runs: operands as the tiles take them (fp32 in three planes) or as
+// And of a direct one: a step of 32 takes 0.8 us.
+double direct_cost(uint64_t rows, uint64_t cols, uint64_t inner, uint32_t passes, hc_type type) {
+    const uint64_t lines = up(inner, kStep) * passes, pieces = direct_pieces(up(rows, kDirect) * up(cols, kDirect), lines);
+    return 3.0 + 0.8 * (double)up(lines, pieces) + (pieces > 1 ? 4.0 : 0.0) +
+           2.0 * (double)(up(rows, kDirect) * kDirect) * (double)(up(cols, kDirect) * kDirect) * (double)inner * passes /
+               (type == HC_T_F32 ? 75e6 : 280e6);
+}
+
+// How a product runs: operands as the tiles take them (fp32 in two planes) or as
 // they are, and then in small tiles or not.
 enum Way { SPLIT, DIRECT, TILED };
 
 Way way_of(const Product& g, hc_type type, bool in_tiles) {
-    if (g.inner == 0) return DIRECT;
+    if (g.inner == 0 || g.rows == 0) return DIRECT;
     if (in_tiles && type == HC_T_F32) return TILED;
-    const double split = split_cost(g.rows, g.cols, g.inner, g.passes.count, type);
-    // a direct product takes 0.8 us a step of 32, cut into up to 64 pieces
-    const double other = in_tiles ? tile_plan(g.rows, g.cols, up(g.inner, 64) * g.passes.count).us
-                                  : 3.0 + 0.8 * (double)up(up(g.inner, kStep), 4) +
-                                        (double)g.rows * g.cols * g.inner * 2 / (type == HC_T_F32 ? 75e6 : 280e6);
+    const uint32_t passes = g.passes.count;
+    const double split = split_cost(g.rows, g.cols, g.inner, passes, type);
+    const double other = in_tiles ? tile_plan(g.rows, g.cols, up(g.inner, 64) * passes).us
+                                  : direct_cost(g.rows, g.cols, g.inner, passes, type);
     return split < other ? SPLIT : in_tiles ? TILED : DIRECT;
 }
 

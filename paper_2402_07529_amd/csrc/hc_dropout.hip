@@ -1,4 +1,9 @@
 // hc_dropout.hip -- dropout and its gradient (include/hc_train.h).
+//
+// A lane takes eight elements of a row, one call of the generator, four times 256
+// groups apart.  Memory bounds it: 393216 x 512 (fp16) 141 us, 5.7 TB/s of reads and
+// writes; 32768 x 768 (bf16) with a residual 29, 5.1 TB/s (a plain copy 4.4 to 4.8).
+// The generator alone would take 86 and 11 us of the vector units.
 #include "hc_layer.h"
 
 namespace hc {
@@ -18,6 +23,7 @@ struct DropoutArgs {
     Dropout drop;
 };
 
+// Rows and groups are found by one division a workgroup and steps of 256 groups.
 template <typename T, bool RESIDUAL>
 __global__ __launch_bounds__(kBlock) void dropout_kernel(DropoutArgs a) {
     const Masks masks = masks_of(a.drop);

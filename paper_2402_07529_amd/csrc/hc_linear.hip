@@ -3,6 +3,28 @@
 //   forward   D = y,  D[i][j] = sum over l of x[i][l] w[j][l]
 //   dx        D = dx, D[i][j] = sum over l of dz[i][l] w[l][j]
 //   dw        D = dw, D[i][j] = sum over l of dz[l][i] x[l][j]
+//
+// Bias, activation, dropout and residual are applied to the sums before they leave
+// the registers; dz = act'(z) mask dy is made in a pass of its own, which leaves the
+// column sums (db) too, since both products read it.
+//
+// Precision.  Products of 16-bit types are exact and summed in fp32; dz is rounded to
+// the type for dx and for a 16-bit dw, and taken in two or three parts for a wider one.
+// fp32: large products as three of fp16 parts (22 bits), others by fp32 matrix
+// instructions.  Sums are taken in an order that the shape fixes; partial sums of a
+// tile's pieces are joined in order.
+//
+// Three ways.  Tiles of 256, 128 or 64 fed from memory to LDS directly, which need
+// rows that are read 16 bytes at a time (others are copied where that pays); small
+// tiles whose eight waves share l, for products that are a chain of latencies; and
+// 64-tiles through registers, which take anything.  Host estimates pick one.
+//
+// What bounds it (MI355X, a library product of 8192^3 reaches 1.29 to 1.37 PFLOP/s).
+// Large products the matrix cores: 4096 x 4096 x 25088 in bf16 takes 665 us without
+// epilogue (1.27 PFLOP/s), its dx and dw 675.  With l of a few hundred the tiles'
+// way through L2: 32768 x 768 x 768 (bf16) 57 us in 128-tiles, 40 of them products
+// (600 MB from L2) and 17 results, hardly overlapped; 256-tiles read half of that but
+// are one round and a half of the CUs.
 #include "hc_internal.h"
 #include "hc_layer.h"
 #include "hc_tiles.h"
@@ -161,7 +183,8 @@ __device__ __forceinline__ void direct_store(T* s, const T (&v)[8]) {
 
 // A 64 x 64 tile, or a piece of one, a workgroup of four waves, each 32 x 32 of
 // it.  Loads go through registers, which takes any stride, alignment and length,
-// zeros where a matrix ends.
+// zeros where a matrix ends.  fp32: 75 TFLOP/s of the matrix instructions' 157, and
+// 65536 x 64 x 128 in 17 us, whose memory takes 10.
 template <Kind KIND, typename T>
 __global__ __launch_bounds__(256) void direct_kernel(Product g) {
     constexpr bool PS = KIND == DW, QS = KIND != FORWARD;
@@ -261,7 +284,8 @@ __global__ __launch_bounds__(256) void direct_join_kernel(Product g) {
 // A tile of 16 x 16 a workgroup, whose eight waves share l: what bounds a small
 // product is a chain of latencies, so a wave asks for the fragments of four steps at
 // once, from memory to registers, and the waves' sums are added up in LDS in order.
-// 16 tokens through 768 x 768 (bf16): one launch of 2.6 us, in 64-tiles 5.
+// 16 tokens through 768 x 768 (bf16): one launch of 5.4 us, in 64-tiles 8; 16 x 4096 x
+// 4096 in fp32 15, directly 27.
 constexpr uint32_t kSplitTile = 16, kSplitWaves = 8, kSplitAhead = 4;
 
 // 8 values of l of an operand's row, zeros behind its ends.
@@ -497,18 +521,21 @@ __device__ __forceinline__ Work work_at(const Product& g, uint32_t i, uint32_t s
     return w;
 }
 
-// Brings the steps of a tile to LDS, one after the other.
+// Brings the steps of a tile to LDS, one after the other: a pass after the other, or,
+// where no factor comes between them (dz in three parts), all passes of a step of l,
+// so that x comes from memory once (32768 x 768 x 768: 235 MB read, 340 otherwise).
 template <Kind KIND, typename V, typename S> struct Feed {
     static constexpr bool PA = kPAcross<KIND>, QA = kQAcross<KIND>;
     typedef typename Reads<KIND, V, S>::InLds InLds;
     Loads<PA, S::BM, S::kWaves> lp;
     Loads<QA, S::BN, S::kWaves> lq;
     char* s_mem;
-    uint32_t inner, wave, lines, pass, l, p_planes, q_planes;
+    uint32_t inner, wave, lines, pass, l, p_planes, q_planes, mixed;
 
     __device__ __forceinline__ Feed(const Product& g, char* s_mem_, uint32_t wave_, uint32_t lane)
         : s_mem(s_mem_), inner((uint32_t)g.inner), wave(wave_), lines((uint32_t)((g.inner + 63) / 64)),
-          p_planes(g.passes.p_planes), q_planes(g.passes.q_planes) {
+          p_planes(g.passes.p_planes), q_planes(g.passes.q_planes),
+          mixed(KIND == DW && g.passes.small == 0 && g.passes.count > 1 ? g.passes.count : 0) {
         lp.init(g.p_ld, g.p_plane, wave, lane);
         lq.init(g.q_ld, g.q_plane, wave, lane);
     }
@@ -520,8 +547,13 @@ template <Kind KIND, typename V, typename S> struct Feed {
     __device__ __forceinline__ void begin(const Product& g, const Work& w) {
         lp.tile(g.p, g.p_cols, PA ? g.inner : g.rows, (uint64_t)w.ti * S::BM);
         lq.tile(g.q, g.q_cols, QA ? g.inner : g.cols, (uint64_t)w.tj * S::BN);
-        pass = w.s0 / lines;
-        l = w.s0 - pass * lines;
+        if (KIND == DW && mixed) {
+            l = w.s0 / mixed;
+            pass = w.s0 - l * mixed;
+        } else {
+            pass = w.s0 / lines;
+            l = w.s0 - pass * lines;
+        }
         seek();
         fetch(0);
     }
@@ -530,7 +562,13 @@ template <Kind KIND, typename V, typename S> struct Feed {
         const uint32_t left = inner - l * 64;
         lp.fetch(base, wave, left);
         lq.fetch(base + InLds::kQ, wave, left);
-        if (++l == lines) {
+        if (KIND == DW && mixed) {
+            if (++pass == mixed) {
+                pass = 0;
+                l++;
+            }
+            seek();
+        } else if (++l == lines) {
             l = 0;
             pass++;
             seek();
@@ -913,7 +951,10 @@ struct DzArgs {
     Gradient db;       // one workgroup along the rows: the sums themselves
 };
 
-// dz = act'(z) mask dy, and each workgroup's sums of its rows.
+// dz = act'(z) mask dy, and each workgroup's sums of its rows.  Memory bounds it: 32768
+// x 768 in bf16 through GELU and dropout into three parts, 250 MB, 53 us (115 with 512
+// workgroups of columns in powers of two, and a first part that was checked for
+// overflow).
 template <typename T> __global__ __launch_bounds__(256) void dz_kernel(DzArgs a) {
     __shared__ float s_sum[256 * 8];
     const Masks masks = masks_of(a.drop);
@@ -1049,7 +1090,8 @@ constexpr int kShapes = 3;
 
 // Estimated times in us: a step takes a workgroup `alone` on its CU, or `shared` by
 // as many as fit; a tile's first loads and its results take `ends`, a piece's with
-// the tile of sums that it writes `piece_ends`.
+// the tile of sums that it writes `piece_ends`.  From measured products whose inputs
+// come from memory.
 struct TileCost {
     uint64_t bm, bn, resident;
     double alone, shared, ends, piece_ends;
@@ -1076,7 +1118,9 @@ double rounds(const TileCost& c, uint64_t groups, double steps, double ends) {
 }
 
 // The tile's size, and how many tiles are cut into how many pieces: none, all, or
-// those left after whole rounds of the CUs.
+// those left after whole rounds of the CUs.  (bf16, us: 4096 x 25088 x 4096 in 256-tiles
+// 710 whole, 672 with the 32 left after six rounds in 8 pieces each; 2048 x 2048 x 2048
+// 68 in 256-tiles, 37 in 128; 1024 x 1024 x 1024 36, 21 and 12 in 256, 128 and 64.)
 TilePlan tile_plan(uint64_t rows, uint64_t cols, uint64_t steps) {
     TilePlan best = {};
     double least = 1e300;

@@ -11,7 +11,10 @@ namespace hc {
 namespace {
 
 constexpr int kBlock = 256;
-constexpr uint32_t kPer = 4;  // groups of a lane
+// Groups of a lane: four, or one where that leaves CUs without a workgroup (700 x 1500
+// in fp32: 129 workgroups of four).
+constexpr uint32_t kPer = 4;
+constexpr uint64_t kFewGroups = 1024ull * kBlock;
 
 struct DropoutArgs {
     const void *x, *residual;
@@ -24,16 +27,16 @@ struct DropoutArgs {
 };
 
 // Rows and groups are found by one division a workgroup and steps of 256 groups.
-template <typename T, bool RESIDUAL>
+template <typename T, bool RESIDUAL, uint32_t PER>
 __global__ __launch_bounds__(kBlock) void dropout_kernel(DropoutArgs a) {
     const Masks masks = masks_of(a.drop);
-    const uint64_t first = (uint64_t)blockIdx.x * (kBlock * kPer);
+    const uint64_t first = (uint64_t)blockIdx.x * (kBlock * PER);
     uint64_t row = first / a.groups;
     uint32_t group = (uint32_t)(first - row * a.groups) + threadIdx.x;
     row += group / a.groups;
     group %= a.groups;
 #pragma unroll
-    for (uint32_t k = 0; k < kPer; k++) {
+    for (uint32_t k = 0; k < PER; k++) {
         if (row < a.rows) {
             const uint32_t col = group * 8, count = a.cols - col;
             float v[8], r[8];
@@ -55,13 +58,19 @@ __global__ __launch_bounds__(kBlock) void dropout_kernel(DropoutArgs a) {
     }
 }
 
-template <typename T> hipError_t launch_typed(const DropoutArgs& a, hipStream_t s) {
-    const uint64_t per = (uint64_t)kBlock * kPer, blocks = (a.rows * a.groups + per - 1) / per;
-    if (a.residual)
-        hipLaunchKernelGGL((dropout_kernel<T, true>), dim3((uint32_t)blocks), dim3(kBlock), 0, s, a);
+template <typename T, bool RESIDUAL> hipError_t launch_typed(const DropoutArgs& a, hipStream_t s) {
+    const uint64_t groups = a.rows * a.groups;
+    if (groups <= kFewGroups)
+        hipLaunchKernelGGL((dropout_kernel<T, RESIDUAL, 1>), dim3((uint32_t)((groups + kBlock - 1) / kBlock)),
+                           dim3(kBlock), 0, s, a);
     else
-        hipLaunchKernelGGL((dropout_kernel<T, false>), dim3((uint32_t)blocks), dim3(kBlock), 0, s, a);
+        hipLaunchKernelGGL((dropout_kernel<T, RESIDUAL, kPer>),
+                           dim3((uint32_t)((groups + kBlock * kPer - 1) / (kBlock * kPer))), dim3(kBlock), 0, s, a);
     return hipGetLastError();
+}
+
+template <typename T> hipError_t launch_type(const DropoutArgs& a, hipStream_t s) {
+    return a.residual ? launch_typed<T, true>(a, s) : launch_typed<T, false>(a, s);
 }
 
 }  // namespace
@@ -81,9 +90,9 @@ hipError_t launch_dropout(const hc_dropout_params& p, const Dropout& d, hc_type 
     a.step_rows = kBlock / a.groups;
     a.step_groups = kBlock % a.groups;
     a.drop = d;
-    if (type == HC_T_F32) return launch_typed<float>(a, s);
-    if (type == HC_T_BF16) return launch_typed<__bf16>(a, s);
-    return launch_typed<_Float16>(a, s);
+    if (type == HC_T_F32) return launch_type<float>(a, s);
+    if (type == HC_T_BF16) return launch_type<__bf16>(a, s);
+    return launch_type<_Float16>(a, s);
 }
 
 }  // namespace hc

@@ -271,43 +271,72 @@ def hc_orthogonalise(x, out, ws, steps: int = 5, coeffs=MUON, eps: float = 1e-7,
                                  _stream(stream)), "hc_orthogonalise")
 
 
-_current_device = None
+_device = _UINT8 = None     # the current device's number, torch's byte; filled by the first call
 
 
-def _on_device(*tensors):
-    """Refuses tensors of another device than the current one, whose stream is used."""
-    global _current_device
-    if _current_device is None:
+def _current():
+    """The current device, whose stream the layer operators use and whose tensors they take."""
+    global _device, _UINT8
+    if _device is None:
         import torch
-        _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
-    current = _current_device()
-    for t in tensors:
-        if t is not None and t.get_device() != current:
-            raise ValueError(f"a tensor is on device {t.device}, the current one is cuda:{current}")
+        _UINT8 = torch.uint8
+        _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    return _device()
 
 
-def _counter(t):
-    if t is None:
-        return None
-    import torch
-    types = (torch.int64, torch.uint64) if hasattr(torch, "uint64") else (torch.int64,)
-    return _ptr(t, "counter", types, 1)
+def _here(t, name, device):
+    if t.get_device() != device:    # -1: not a device tensor
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{device}")
 
 
-def _like(t, name, x, rows, cols):
+def _matrix(t, name, device):
+    """(device pointer, rows, columns, row stride), as _rows'."""
+    if t.get_device() != device:
+        _here(t, name, device)
+    shape = t.shape
+    if len(shape) == 2 and t.is_contiguous():
+        rows, cols = shape
+        return t.data_ptr(), rows, cols, cols
+    return _rows(t, name)
+
+
+def _like(t, name, x, rows, cols, device):
     """(pointer, row stride) of a [rows, cols] tensor of x's type; None: none."""
     if t is None:
         return None, 0
     if t.dtype != x.dtype:
         raise ValueError(f"{name} is {t.dtype}, expected {x.dtype}")
-    p, r, c, ld = _rows(t, name)
+    p, r, c, ld = _matrix(t, name, device)
     if r != rows or c != cols:
         raise ValueError(f"{name} is {r} x {c}, expected {rows} x {cols}")
     return p, ld
 
 
-def _uint64(v):
-    return v & (2**64 - 1)
+def _vector(t, name, dtype, n, device):
+    """Pointer of n contiguous elements; None: none."""
+    if t is None:
+        return None
+    if t.get_device() != device:
+        _here(t, name, device)
+    if t.dtype != dtype or t.numel() < n or not t.is_contiguous():
+        raise ValueError(f"{name} must be {n} contiguous elements of {dtype}, not {t.dtype} {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _workspace(ws, device):
+    """(pointer, bytes)"""
+    n = ws.numel()
+    return _vector(ws, "ws", _UINT8, n, device), n
+
+
+def _counter(t, device):
+    if t is None:
+        return None
+    import torch
+    return _vector(t, "counter", torch.uint64 if t.dtype == getattr(torch, "uint64", None) else torch.int64, 1, device)
+
+
+_LOW = 2**64 - 1
 
 
 def hc_dropout(x, out, p: float, seed: int, draw: int = 0, residual=None, counter=None, stream=None):
@@ -316,12 +345,12 @@ def hc_dropout(x, out, p: float, seed: int, draw: int = 0, residual=None, counte
     bfloat16 or float16; out may be x or residual.  The mask depends on seed, draw and an
     element's row and column alone: the same call on an output gradient is the backward pass.
     counter (int64, one element, on the device) is added to draw when the kernel runs."""
-    px, rows, cols, x_ld = _rows(x, "x")
-    po, out_ld = _like(out, "out", x, rows, cols)
-    pr, r_ld = _like(residual, "residual", x, rows, cols)
-    _on_device(x, out, residual, counter)
-    q = hc_dropout_params(rows, cols, x_ld, r_ld, out_ld, _uint64(seed), _uint64(draw), p, 0)
-    _check(_lib.hc_dropout(ctypes.byref(q), _type(x, "x"), px, pr, po, _counter(counter),
+    device = _current()
+    px, rows, cols, x_ld = _matrix(x, "x", device)
+    po, out_ld = _like(out, "out", x, rows, cols, device)
+    pr, r_ld = _like(residual, "residual", x, rows, cols, device)
+    q = hc_dropout_params(rows, cols, x_ld, r_ld, out_ld, seed & _LOW, draw & _LOW, p, 0)
+    _check(_lib.hc_dropout(ctypes.byref(q), _type(x, "x"), px, pr, po, _counter(counter, device),
                            _stream(stream)), "hc_dropout")
 
 
@@ -334,8 +363,8 @@ def _act(act):
 
 def _layer(m, n, k, x_ld, w_ld, y_ld, z_ld=0, residual_ld=0, dx_ld=0, dw_ld=0, seed=0, draw=0, p=0.0,
            act="none", fixed=1.0):
-    return hc_linear_params(m, n, k, x_ld, w_ld, y_ld, z_ld, residual_ld, dx_ld, dw_ld, _uint64(seed),
-                            _uint64(draw), p, _act(act), fixed, 0)
+    return hc_linear_params(m, n, k, x_ld, w_ld, y_ld, z_ld, residual_ld, dx_ld, dw_ld, seed & _LOW,
+                            draw & _LOW, p, _act(act), fixed, 0)
 
 
 def _layer_bytes(call, where, x, w):
@@ -364,17 +393,19 @@ def hc_linear(x, w, y, ws, bias=None, residual=None, z=None, act: str = "none", 
     p > 0.  x [.., k], w [n, k], bias [n], residual, y and z [.., n], all float32, bfloat16 or
     float16; act "none", "relu", "gelu" (by erf), "silu", "tanh" or "sigmoid".  z, where given,
     gets x w^T + bias: hc_linear_grad reads it.  y may be residual."""
-    px, m, k, x_ld = _rows(x, "x")
-    pw, n, kw, w_ld = _rows(w, "w")
-    if kw != k or w.dtype != x.dtype:
-        raise ValueError(f"w is {w.dtype} with {kw} columns, x {x.dtype} with {k}")
-    py, y_ld = _like(y, "y", x, m, n)
-    pz, z_ld = _like(z, "z", x, m, n)
-    pr, r_ld = _like(residual, "residual", x, m, n)
-    _on_device(x, w, y, ws, bias, residual, z, counter)
+    device = _current()
+    px, m, k, x_ld = _matrix(x, "x", device)
+    pw, n, kw, w_ld = _matrix(w, "w", device)
+    dtype = x.dtype
+    if kw != k or w.dtype != dtype:
+        raise ValueError(f"w is {w.dtype} with {kw} columns, x {dtype} with {k}")
+    py, y_ld = _like(y, "y", x, m, n, device)
+    pz, z_ld = _like(z, "z", x, m, n, device)
+    pr, r_ld = _like(residual, "residual", x, m, n, device)
+    pws, ws_bytes = _workspace(ws, device)
     q = _layer(m, n, k, x_ld, w_ld, y_ld, z_ld, r_ld, 0, 0, seed, draw, p, act)
-    _check(_lib.hc_linear(ctypes.byref(q), _type(x, "x"), px, pw, _ptr(bias, "bias", (x.dtype,), n),
-                          pr, py, pz, _counter(counter), _bytes(ws), ws.numel(), _stream(stream)),
+    _check(_lib.hc_linear(ctypes.byref(q), _type(x, "x"), px, pw, _vector(bias, "bias", dtype, n, device),
+                          pr, py, pz, _counter(counter, device), pws, ws_bytes, _stream(stream)),
            "hc_linear")
 
 
@@ -396,31 +427,34 @@ def hc_linear_grad(dy, ws, x=None, w=None, z=None, dx=None, dw=None, db=None, ac
     needs x, an activation needs z; dy, x, w, z and dx are of one type.  dw [n, k] and db [n] are
     both float32, bfloat16, float16, or int32: fixed point with `fixed` units per 1.0; accumulate
     adds to them.  The residual's gradient is dy itself."""
-    py, m, n, y_ld = _rows(dy, "dy")
-    for t, name, needs, what in ((dx, "dx", w, "w"), (dw, "dw", x, "x")):
-        if t is not None and needs is None:
-            raise ValueError(f"{name} needs {what}")
+    device = _current()
+    py, m, n, y_ld = _matrix(dy, "dy", device)
+    if dx is not None and w is None:
+        raise ValueError("dx needs w")
+    if dw is not None and x is None:
+        raise ValueError("dw needs x")
     if act != "none" and z is None:
         raise ValueError(f"the gradient of {act} needs z")
-    k = next((t.shape[-1] for t in (x, w, dx, dw) if t is not None), 1)
-    px, x_ld = _like(x, "x", dy, m, k)
-    pw, w_ld = _like(w, "w", dy, n, k)
-    pz, z_ld = _like(z, "z", dy, m, n)
-    pdx, dx_ld = _like(dx, "dx", dy, m, k)
-    pdw, dw_ld, g_type = None, 0, HC_T_F32
+    k = 1
+    for t in (x, w, dx, dw):
+        if t is not None:
+            k = t.shape[-1]
+            break
+    px, x_ld = _like(x, "x", dy, m, k, device)
+    pw, w_ld = _like(w, "w", dy, n, k, device)
+    pz, z_ld = _like(z, "z", dy, m, n, device)
+    pdx, dx_ld = _like(dx, "dx", dy, m, k, device)
+    pdw, dw_ld, g_type, pdb = None, 0, HC_T_F32, None
     if dw is not None:
-        pdw, rows, cols, dw_ld = _rows(dw, "dw")
+        pdw, rows, cols, dw_ld = _matrix(dw, "dw", device)
         g_type = _type(dw, "dw")
         if rows != n or cols != k:
             raise ValueError(f"dw is {rows} x {cols}, expected {n} x {k}")
     if db is not None:
-        if dw is not None and db.dtype != dw.dtype:
-            raise ValueError(f"db is {db.dtype}, dw {dw.dtype}")
+        pdb = _vector(db, "db", db.dtype if dw is None else dw.dtype, n, device)
         g_type = _type(db, "db")
-    _on_device(dy, ws, x, w, z, dx, dw, db, counter)
-    q = _layer(m, n, k, x_ld if x is not None else k, w_ld if w is not None else k, y_ld, z_ld, 0, dx_ld,
-               dw_ld, seed, draw, p, act, fixed)
-    pdb = None if db is None else _ptr(db, "db", (db.dtype,), n)
+    pws, ws_bytes = _workspace(ws, device)
+    q = _layer(m, n, k, x_ld or k, w_ld or k, y_ld, z_ld, 0, dx_ld, dw_ld, seed, draw, p, act, fixed)
     _check(_lib.hc_linear_grad(ctypes.byref(q), _type(dy, "dy"), py, px, pw, pz, pdx, g_type, pdw,
-                               pdb, 1 if accumulate else 0, _counter(counter), _bytes(ws), ws.numel(),
+                               pdb, 1 if accumulate else 0, _counter(counter, device), pws, ws_bytes,
                                _stream(stream)), "hc_linear_grad")

@@ -587,3 +587,48 @@ def test_many_rows_through_a_small_matrix(m, n, k, dtype):
         check_linear(torch, L, y, None, "silu", 0.1, m, 0, True, True)
         hc.hc_linear_grad(L.dy, hc.alloc_linear_grad_workspace(L.x, L.w), w=L.w, dx=dx)
         check_grad(torch, L, "none", 0.0, 0, 0, dx, None, None, dtype)
+
+
+@pytest.mark.parametrize("dtype,act", [("float32", "none"), ("float32", "gelu"), ("bfloat16", "gelu"), ("float16", "silu")])
+def test_large_gradients_captured_replayed_and_on_two_streams(dtype, act):
+    """Packed, cut and joined products in a graph, against eager calls, and two calls at once."""
+    torch, hc = _hc()
+    m, n, k = 1100, 1000, 1300
+    L = [Layer(torch, m, n, k, dtype, seed=s) for s in (1, 2)]
+    p = 0.0 if act == "none" else 0.2
+
+    def outs():
+        dt = L[0].x.dtype
+        return [torch.full((m, k), 9.0, device="cuda", dtype=dt), torch.full((n, k), 9.0, device="cuda"),
+                torch.full((n,), 9.0, device="cuda"), torch.full((m, n), 9.0, device="cuda", dtype=dt)]
+
+    ws = [(hc.alloc_linear_workspace(l.x, l.w), hc.alloc_linear_grad_workspace(l.x, l.w)) for l in L]
+
+    def run(i, o):
+        l = L[i]
+        hc.hc_linear(l.x, l.w, o[3], ws[i][0], bias=l.bias, residual=l.residual, act=act, p=p, seed=i)
+        hc.hc_linear_grad(l.dy, ws[i][1], x=l.x, w=l.w, z=l.z, dx=o[0], dw=o[1], db=o[2], act=act, p=p, seed=i)
+
+    want = [outs(), outs()]
+    for i in (0, 1):
+        run(i, want[i])
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], [outs(), outs()]
+    torch.cuda.synchronize()
+    for i in (0, 1, 0, 1):
+        with torch.cuda.stream(streams[i]):
+            run(i, got[i])
+    torch.cuda.synchronize()
+    for i in (0, 1):
+        assert all(torch.equal(a, b) for a, b in zip(got[i], want[i]))
+    graph, o = torch.cuda.CUDAGraph(), outs()
+    with torch.cuda.graph(graph, stream=streams[0]):
+        run(0, o)
+    for _ in range(3):
+        for t in o:
+            t.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(o, want[0]))
+        L[0].dy.mul_(1.0)          # eager work between the replays
+        torch.cuda.synchronize()

@@ -1039,6 +1039,7 @@ __global__ __launch_bounds__(1024) void bias_kernel(const float* __restrict__ pa
     const uint32_t lane = threadIdx.x & 15, share = threadIdx.x >> 4, col = blockIdx.x * 16 + lane;
     float t = 0.0f;
     if (col < n)
+#pragma unroll 8
         for (uint32_t b = blocks * share / 64; b < blocks * (share + 1) / 64; b++) t += part[(uint64_t)b * n + col];
     s_sum[share][lane] = t;
     __syncthreads();

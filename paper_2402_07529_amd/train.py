@@ -280,13 +280,15 @@ def _current():
     if _device is None:
         import torch
         _UINT8 = torch.uint8
+        if not torch.cuda.is_available():
+            return None             # no tensor is on it
         _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
     return _device()
 
 
 def _here(t, name, device):
     if t.get_device() != device:    # -1: not a device tensor
-        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{device}")
+        raise ValueError(f"{name} must be a device tensor of the current device ({device}), not of {t.device}")
 
 
 def _matrix(t, name, device):

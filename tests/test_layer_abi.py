@@ -135,3 +135,18 @@ def test_a_workspace_does_for_fewer_rows(n, k, t):
             assert call(ctypes.byref(p), t, ctypes.byref(size)) == hc.HC_OK
             assert size.value >= last, m
             last = size.value
+
+
+def test_binding_refuses_host_tensors_and_unknown_names():
+    torch = pytest.importorskip("torch")
+    import paper_2402_07529_amd as hc
+    x, w, y, ws = torch.zeros(4, 8), torch.zeros(6, 8), torch.zeros(4, 6), torch.zeros(512, dtype=torch.uint8)
+    with pytest.raises(ValueError, match="device tensor"):
+        hc.hc_dropout(x, x.clone(), 0.5, 1)
+    with pytest.raises(ValueError, match="device tensor"):
+        hc.hc_linear(x, w, y, ws)
+    with pytest.raises(ValueError, match="device tensor"):
+        hc.hc_linear_grad(y, ws, x=x, dw=w)
+    with pytest.raises(ValueError, match="device tensor"):
+        hc.alloc_linear_workspace(x, w)
+    assert set(hc.ACTIVATIONS) == {"none", "relu", "gelu", "silu", "tanh", "sigmoid"}

@@ -230,6 +230,18 @@ template <typename T> __device__ __forceinline__ void store8(T* p, uint32_t coun
     }
 }
 
+// Past the caches.
+template <typename T> __device__ __forceinline__ void stream8(T* p, uint32_t count, const float (&v)[8]) {
+    if (count >= 8) {
+        typename Eight<T>::V t;
+#pragma unroll
+        for (int e = 0; e < 8; e++) t[e] = (T)v[e];
+        __builtin_nontemporal_store(t, reinterpret_cast<typename Eight<T>::V*>(p));
+    } else {
+        store8(p, count, v);
+    }
+}
+
 // Fixed point: the nearest whole number, ties to even, saturating at +-(2^31 - 1)
 // (NaN: 0).
 __device__ __forceinline__ int32_t to_fixed(float v, float fixed) {

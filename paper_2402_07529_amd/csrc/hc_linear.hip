@@ -45,8 +45,15 @@ struct Forward {
     void *y, *z;
     uint64_t residual_ld, y_ld, z_ld;
     uint32_t act;
+    uint32_t stream;  // results pass the caches by
     Dropout drop;
 };
+
+template <typename T>
+__device__ __forceinline__ void put8(const Forward& f, T* p, uint32_t count, const float (&v)[8]) {
+    if (f.stream) stream8(p, count, v);
+    else store8(p, count, v);
+}
 
 template <typename T>
 __device__ __forceinline__ void finish_forward(const Forward& f, const Masks& masks, uint64_t row, uint64_t rows,
@@ -55,13 +62,13 @@ __device__ __forceinline__ void finish_forward(const Forward& f, const Masks& ma
     if (row >= rows || count == 0) return;
 #pragma unroll
     for (int e = 0; e < 8; e++) v[e] += bias[e];
-    if (f.z) store8(static_cast<T*>(f.z) + row * f.z_ld + col, count, v);
+    if (f.z) put8(f, static_cast<T*>(f.z) + row * f.z_ld + col, count, v);
     activate8<T>(f.act, v);
     if (masks.limit) drop8(masks, (uint32_t)row, col / 8, v);
     if (f.residual)
 #pragma unroll
         for (int e = 0; e < 8; e++) v[e] += (float)residual[e];
-    store8(static_cast<T*>(f.y) + row * f.y_ld + col, count, v);
+    put8(f, static_cast<T*>(f.y) + row * f.y_ld + col, count, v);
 }
 
 // An operand may be a sum of planes, and a product the sum of some products of
@@ -1260,6 +1267,7 @@ size_t most_part_bytes(uint64_t rows, uint64_t cols) {
 
 // ---- which way a call goes --------------------------------------------------------------
 
+constexpr uint64_t kStreamBytes = 32ull << 20;  // of all eight L2s
 constexpr uint64_t kMostTileLd = 1ull << 22;  // a tile's rows within 2^31 bytes
 
 // A 16-bit operand whose rows the tiles can take where they are.
@@ -1420,7 +1428,10 @@ hipError_t launch_linear(const hc_linear_params& p, const Dropout& d, hc_type ty
     g.cols = (uint32_t)p.n;
     g.inner = p.k;
     g.part = reinterpret_cast<float*>(ws + L.part);
-    g.forward = {bias, residual, y, z, p.residual_ld, p.y_ld, p.z_ld, p.act, d};
+    // results that the L2s cannot keep leave them to the operands: 16384 x 2048 x 512 (bf16)
+    // 58 -> 46 us, 4096 x 4096 x 4096 126 -> 121 (dx 32768 x 768 x 768 56 -> 60: not there)
+    const bool stream = p.m * p.n * (fp32 ? 4 : 2) > kStreamBytes;
+    g.forward = {bias, residual, y, z, p.residual_ld, p.y_ld, p.z_ld, p.act, stream, d};
     Operand ox, ow;
     hipError_t e;
     if (fp32 && in_tiles) {

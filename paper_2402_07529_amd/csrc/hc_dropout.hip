@@ -1,8 +1,8 @@
 // hc_dropout.hip -- dropout and its gradient (include/hc_train.h).
 //
 // A lane takes eight elements of a row, one call of the generator, four times 256
-// groups apart.  Memory bounds it: 393216 x 512 (fp16) 141 us, 5.7 TB/s of reads and
-// writes; 32768 x 768 (bf16) with a residual 29, 5.1 TB/s (a plain copy 4.4 to 4.8).
+// groups apart.  Memory bounds it: 393216 x 512 (fp16) 137 us, 5.9 TB/s of reads and
+// writes; 32768 x 768 (bf16) with a residual 25, 6.0 TB/s (a plain copy 4.4 to 4.8).
 // The generator alone would take 86 and 11 us of the vector units.
 #include "hc_layer.h"
 
@@ -15,6 +15,9 @@ constexpr int kBlock = 256;
 // in fp32: 129 workgroups of four).
 constexpr uint32_t kPer = 4;
 constexpr uint64_t kFewGroups = 1024ull * kBlock;
+// Results that the L2s cannot keep pass them by, and so does what is read for them:
+// 32768 x 768 (bf16) with a residual 29.5 -> 25 us, 393216 x 512 (fp16) 141 -> 137.
+constexpr uint64_t kPastBytes = 32ull << 20;
 
 struct DropoutArgs {
     const void *x, *residual;
@@ -27,7 +30,7 @@ struct DropoutArgs {
 };
 
 // Rows and groups are found by one division a workgroup and steps of 256 groups.
-template <typename T, bool RESIDUAL, uint32_t PER>
+template <typename T, bool RESIDUAL, uint32_t PER, bool PAST>
 __global__ __launch_bounds__(kBlock) void dropout_kernel(DropoutArgs a) {
     const Masks masks = masks_of(a.drop);
     const uint64_t first = (uint64_t)blockIdx.x * (kBlock * PER);
@@ -40,14 +43,20 @@ __global__ __launch_bounds__(kBlock) void dropout_kernel(DropoutArgs a) {
         if (row < a.rows) {
             const uint32_t col = group * 8, count = a.cols - col;
             float v[8], r[8];
-            load8(static_cast<const T*>(a.x) + row * a.x_ld + col, count, v);
-            if constexpr (RESIDUAL)
-                load8(static_cast<const T*>(a.residual) + row * a.residual_ld + col, count, r);
+            auto load = [&](const void* p, uint64_t ld, float (&w)[8]) {
+                const T* at = static_cast<const T*>(p) + row * ld + col;
+                if constexpr (PAST) load8_past(at, count, w);
+                else load8(at, count, w);
+            };
+            load(a.x, a.x_ld, v);
+            if constexpr (RESIDUAL) load(a.residual, a.residual_ld, r);
             if (masks.limit) drop8(masks, (uint32_t)row, group, v);
             if constexpr (RESIDUAL)
 #pragma unroll
                 for (int e = 0; e < 8; e++) v[e] += r[e];
-            store8(static_cast<T*>(a.out) + row * a.out_ld + col, count, v);
+            T* out = static_cast<T*>(a.out) + row * a.out_ld + col;
+            if constexpr (PAST) store8_past(out, count, v);
+            else store8(out, count, v);
         }
         row += a.step_rows;
         group += a.step_groups;
@@ -58,15 +67,17 @@ __global__ __launch_bounds__(kBlock) void dropout_kernel(DropoutArgs a) {
     }
 }
 
-template <typename T, bool RESIDUAL> hipError_t launch_typed(const DropoutArgs& a, hipStream_t s) {
-    const uint64_t groups = a.rows * a.groups;
-    if (groups <= kFewGroups)
-        hipLaunchKernelGGL((dropout_kernel<T, RESIDUAL, 1>), dim3((uint32_t)((groups + kBlock - 1) / kBlock)),
-                           dim3(kBlock), 0, s, a);
-    else
-        hipLaunchKernelGGL((dropout_kernel<T, RESIDUAL, kPer>),
-                           dim3((uint32_t)((groups + kBlock * kPer - 1) / (kBlock * kPer))), dim3(kBlock), 0, s, a);
+template <typename T, bool RESIDUAL, uint32_t PER, bool PAST>
+hipError_t launch_variant(const DropoutArgs& a, hipStream_t s) {
+    const uint64_t per = (uint64_t)kBlock * PER, blocks = (a.rows * a.groups + per - 1) / per;
+    hipLaunchKernelGGL((dropout_kernel<T, RESIDUAL, PER, PAST>), dim3((uint32_t)blocks), dim3(kBlock), 0, s, a);
     return hipGetLastError();
+}
+
+template <typename T, bool RESIDUAL> hipError_t launch_typed(const DropoutArgs& a, hipStream_t s) {
+    if (a.rows * a.groups <= kFewGroups) return launch_variant<T, RESIDUAL, 1, false>(a, s);
+    if (a.rows * a.cols * sizeof(T) <= kPastBytes) return launch_variant<T, RESIDUAL, kPer, false>(a, s);
+    return launch_variant<T, RESIDUAL, kPer, true>(a, s);
 }
 
 template <typename T> hipError_t launch_type(const DropoutArgs& a, hipStream_t s) {

@@ -230,8 +230,20 @@ template <typename T> __device__ __forceinline__ void store8(T* p, uint32_t coun
     }
 }
 
-// Past the caches.
-template <typename T> __device__ __forceinline__ void stream8(T* p, uint32_t count, const float (&v)[8]) {
+// The same past the caches, for what is read or written once.
+template <typename T>
+__device__ __forceinline__ void load8_past(const T* __restrict__ p, uint32_t count, float (&v)[8]) {
+    if (count >= 8) {
+        typedef typename Eight<T>::V V;
+        const V t = __builtin_nontemporal_load(reinterpret_cast<const V*>(p));
+#pragma unroll
+        for (int e = 0; e < 8; e++) v[e] = (float)t[e];
+    } else {
+        load8(p, count, v);
+    }
+}
+
+template <typename T> __device__ __forceinline__ void store8_past(T* p, uint32_t count, const float (&v)[8]) {
     if (count >= 8) {
         typename Eight<T>::V t;
 #pragma unroll

@@ -51,7 +51,7 @@ struct Forward {
 
 template <typename T>
 __device__ __forceinline__ void put8(const Forward& f, T* p, uint32_t count, const float (&v)[8]) {
-    if (f.stream) stream8(p, count, v);
+    if (f.stream) store8_past(p, count, v);
     else store8(p, count, v);
 }
 

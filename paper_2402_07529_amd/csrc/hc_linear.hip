@@ -23,7 +23,7 @@
 // Large products the matrix cores: 4096 x 4096 x 25088 in bf16 takes 665 us without
 // epilogue (1.27 PFLOP/s), its dx and dw 675.  With l of a few hundred the tiles'
 // way through L2: 32768 x 768 x 768 (bf16) 57 us in 128-tiles, 40 of them products
-// (600 MB from L2) and 17 results, hardly overlapped (67 with dropout and residual); 256-tiles read half of that but
+// (600 MB from L2) and 17 results, hardly overlapped; 256-tiles read half of that but
 // are one round and a half of the CUs.
 #include "hc_internal.h"
 #include "hc_layer.h"
@@ -45,7 +45,7 @@ struct Forward {
     void *y, *z;
     uint64_t residual_ld, y_ld, z_ld;
     uint32_t act;
-    uint32_t stream;  // results and the residual pass the caches by
+    uint32_t stream;  // results pass the caches by
     Dropout drop;
 };
 
@@ -647,20 +647,9 @@ __device__ __forceinline__ void finish_rows(const Product& g, const Masks& masks
             T residual[N][8];
             if (f.residual)
 #pragma unroll
-                for (int u = 0; u < N; u++) {
-                    const T* at = static_cast<const T*>(f.residual) + (row0 + 16 * (u0 + u)) * f.residual_ld + col;
-                    const uint32_t here = row0 + 16 * (u0 + u) < g.rows ? count : 0;
-                    // One condition for both keeps the group's loads together: 32768 x 768 x 768
-                    // (bf16) 66.7 us; with the count asked below it 75, through the caches 72.
-                    if (f.stream && here >= 8) {
-                        typedef typename Eight<T>::V V;
-                        const V t = __builtin_nontemporal_load(reinterpret_cast<const V*>(at));
-#pragma unroll
-                        for (int e = 0; e < 8; e++) residual[u][e] = t[e];
-                    } else {
-                        load8_raw(at, here, residual[u]);
-                    }
-                }
+                for (int u = 0; u < N; u++)
+                    load8_raw(static_cast<const T*>(f.residual) + (row0 + 16 * (u0 + u)) * f.residual_ld + col,
+                              row0 + 16 * (u0 + u) < g.rows ? count : 0, residual[u]);
             unrolled<N, 1>([&](auto u) __attribute__((always_inline)) {
                 float v[8];
                 pair_up(acc[u0 + u][FIRST], acc[u0 + u][FIRST + 1], v);

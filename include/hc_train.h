@@ -189,8 +189,11 @@ typedef struct {
 /* z = x w^T + bias (NULL: none), y = residual (NULL: none) + mask * act(z), with
  * products and sums in fp32 (z is not rounded before act).  All of `type`
  * (HC_T_F32, HC_T_BF16, HC_T_F16).  z (NULL: not wanted) is what the gradient of
- * an activation asks for.  Sums are taken in an order that depends on the shape
- * and strides alone: two calls agree bit for bit.  Large fp32 products run as three
+ * an activation asks for.  Sums are taken in an order that depends on the shape, the
+ * type, the strides and, in 16-bit types, on whether x and w begin at multiples of 16
+ * bytes, and on nothing else: two calls agree bit for bit.  (A 16-bit x or w that does
+ * not, though its stride is a multiple of 8, is multiplied by a slower way: 170 to 400
+ * TFLOP/s.)  Large fp32 products run as three
  * of fp16 parts with fp32 sums: an element of x or w keeps 22 bits if it is no
  * smaller than 2^-29 of the largest in its row, fewer below, none below 2^-51 of it;
  * small ones are fp32 products.  An infinity may come out as NaN.  y may be residual
@@ -214,7 +217,9 @@ hc_status hc_linear(const hc_linear_params *p, hc_type type, const void *x, cons
  * (22 bits), three or two times the products.  Without activation and dropout dz
  * is dy.  db takes dz unrounded.
  *   m = 0 gives zeros.  Order, fp32 parts (there by the rows of dz and the columns
- * of w, the columns of dz and of x) and infinities as in hc_linear. */
+ * of w, the columns of dz and of x) and infinities as in hc_linear; dx goes by w's
+ * stride and address, dw by x's and by g_type, db by neither, all by whether dz is dy,
+ * and none by what else is wanted. */
 hc_status hc_linear_grad_bytes(const hc_linear_params *p, hc_type type, size_t *bytes);
 hc_status hc_linear_grad(const hc_linear_params *p, hc_type type, const void *dy, const void *x,
                          const void *w, const void *z, void *dx, hc_type g_type, void *dw,

@@ -396,6 +396,7 @@ template <typename T> __global__ __launch_bounds__(512) void split_grad_kernel(S
         const T* dy = static_cast<const T*>(g.dy);
         float t = 0.0f;
         if (col < g.n)
+#pragma unroll 8
             for (uint64_t row = g.m * wave / kSplitWaves; row < g.m * (wave + 1) / kSplitWaves; row++)
                 t += (float)dy[row * g.dy_ld + col];
         sums[wave * 64 + lane] = t;
@@ -1061,7 +1062,11 @@ __global__ __launch_bounds__(1024) void bias_kernel(const float* __restrict__ pa
 // ---- layout and launches ------------------------------------------------------------
 
 constexpr uint64_t kDzGroups = 2048;     // workgroups of dz
-constexpr uint64_t kSplitBias = 2048;    // rows whose db a small layer's launch sums too
+// db of a dz that is dy, up to these rows and elements, is summed in the launch of small products, or
+// alone in such a one: 512 x 512 (fp32) 3.8 us, 2048 x 64 6.8, where dz's pass and its join take 6.2.
+// More elements take those as long (2048 x 1500: 11.7 and 11.9), and fp32 planes need dz's pass anyway
+// (2048 x 512 x 512 57 us, 61 with db apart).  By m and n alone, since db is asked for without x and w too.
+constexpr uint64_t kSplitBias = 2048, kSplitBiasElements = 1ull << 19;
 constexpr uint64_t kDzAlone = 32;        // rows that one workgroup takes, without a launch for db
 
 uint64_t up(uint64_t v, uint64_t to) { return (v + to - 1) / to; }
@@ -1189,13 +1194,16 @@ template <Kind KIND, typename T, typename V> hipError_t tiled(Product g, hipStre
 }
 
 // Estimated time of a small product: a wave's four steps take 1 us, its tiles' rows
-// come from L2 again and again, and four workgroups on a CU take 4 us at least.
-double split_cost(uint64_t rows, uint64_t cols, uint64_t inner, uint32_t passes, hc_type type) {
+// come from L2 again and again, and four workgroups on a CU take 4 us at least.  Of an
+// operand across its rows a tile reads 16 columns, and with them the 128 bytes that they
+// are in: dx of 1 x 4096 x 4096 (bf16) 23 us, in tiles 12.5.
+double split_cost(Kind kind, uint64_t rows, uint64_t cols, uint64_t inner, uint32_t passes, hc_type type) {
     const double tiles = (double)up(rows, kSplitTile) * (double)up(cols, kSplitTile);
-    const uint64_t lines = up(inner, kStep) * passes;
-    const uint64_t live = (rows < kSplitTile ? rows : kSplitTile) + (cols < kSplitTile ? cols : kSplitTile);
+    const uint64_t lines = up(inner, kStep) * passes, along = type == HC_T_F32 ? 4 : 2, across = 128 / kSplitTile;
+    const uint64_t live = (rows < kSplitTile ? rows : kSplitTile) * (kind == DW ? across : along) +
+                          (cols < kSplitTile ? cols : kSplitTile) * (kind == FORWARD ? along : across);
     return 1.5 + 1.0 * (double)up(lines, kSplitWaves * kSplitAhead) + tiles / (4 * kCus) * 4.0 +
-           tiles * passes * (double)inner * (double)live * (type == HC_T_F32 ? 4 : 2) / 9e6;
+           tiles * passes * (double)inner * (double)live / 9e6;
 }
 
 // And of a direct one: a step of 32 takes 0.8 us.
@@ -1210,11 +1218,11 @@ double direct_cost(uint64_t rows, uint64_t cols, uint64_t inner, uint32_t passes
 // they are, and then in small tiles or not.
 enum Way { SPLIT, DIRECT, TILED };
 
-Way way_of(const Product& g, hc_type type, bool in_tiles) {
+Way way_of(Kind kind, const Product& g, hc_type type, bool in_tiles) {
     if (g.inner == 0 || g.rows == 0) return DIRECT;
     if (in_tiles && type == HC_T_F32) return TILED;
     const uint32_t passes = g.passes.count;
-    const double split = split_cost(g.rows, g.cols, g.inner, passes, type);
+    const double split = split_cost(kind, g.rows, g.cols, g.inner, passes, type);
     const double other = in_tiles ? tile_plan(g.rows, g.cols, up(g.inner, 64) * passes).us
                                   : direct_cost(g.rows, g.cols, g.inner, passes, type);
     return split < other ? SPLIT : in_tiles ? TILED : DIRECT;
@@ -1298,7 +1306,7 @@ struct Layout {
     uint64_t k_ld, n_ld;  // of packed rows
     uint64_t per, blocks;
     uint32_t width;
-    bool pack;            // x and w
+    bool pack_x, pack_w;  // whether they are copied; fp32: both or none
 };
 
 size_t take(size_t& at, size_t bytes) {
@@ -1308,22 +1316,26 @@ size_t take(size_t& at, size_t bytes) {
 }
 
 // Copies of x and w: where they are worth it, and they may be needed (a pointer's
-// alignment is not known here; one that is off by itself goes the direct way).
+// alignment is not known here; one that is off by itself goes the direct way).  The
+// gradient has them each by its own strides, since dx is the same whether x is there
+// or not, and dw whether w is.
 void take_packed(const hc_linear_params& p, hc_type type, bool grad, size_t& at, Layout* L) {
     const size_t size = type == HC_T_F32 ? 4 : 2;
     L->k_ld = up(p.k, 64) * 64;
     L->n_ld = up(p.n, 64) * 64;
-    L->pack = (type == HC_T_F32 || p.k % 8 || p.x_ld % 8 || p.w_ld % 8 || p.x_ld > kMostTileLd ||
-               p.w_ld > kMostTileLd) && worth_packing(p, type, grad);
-    L->x = take(at, L->pack ? p.m * L->k_ld * size : 0);
-    L->w = take(at, L->pack ? p.n * L->k_ld * size : 0);
+    const bool worth = worth_packing(p, type, grad);
+    auto needed = [&](uint64_t ld) { return type == HC_T_F32 || p.k % 8 || ld % 8 || ld > kMostTileLd; };
+    L->pack_x = worth && (needed(p.x_ld) || (!grad && needed(p.w_ld)));
+    L->pack_w = worth && (needed(p.w_ld) || (!grad && needed(p.x_ld)));
+    L->x = take(at, L->pack_x ? p.m * L->k_ld * size : 0);
+    L->w = take(at, L->pack_w ? p.n * L->k_ld * size : 0);
 }
 
 Layout linear_layout(const hc_linear_params& p, hc_type type) {
     Layout L = {};
     size_t at = 0;
     take_packed(p, type, false, at, &L);
-    const bool planes = L.pack && type == HC_T_F32;
+    const bool planes = L.pack_x && type == HC_T_F32;
     L.row_most = take(at, planes ? p.m * 4 : 0);
     L.col_most = take(at, planes ? L.n_ld * 4 : 0);
     L.part = take(at, most_part_bytes(p.m, p.n));
@@ -1343,7 +1355,7 @@ Layout grad_layout(const hc_linear_params& p, hc_type type) {
     L.per = p.m <= kDzAlone ? kDzAlone : up(up(p.m, most), step) * step;
     L.blocks = p.m ? up(p.m, L.per) : 0;
     L.dz = take(at, p.m * L.n_ld * (type == HC_T_BF16 ? 6 : 4));
-    const bool planes = L.pack && type == HC_T_F32;
+    const bool planes = L.pack_x && type == HC_T_F32;
     L.dz_rows = take(at, planes ? p.m * L.n_ld * 4 : 0);
     L.dz_cols = take(at, planes ? p.m * L.n_ld * 4 : 0);
     L.row_most = take(at, planes ? p.m * 4 : 0);
@@ -1421,7 +1433,7 @@ hipError_t launch_linear(const hc_linear_params& p, const Dropout& d, hc_type ty
     char* ws = static_cast<char*>(ws_);
     const bool fp32 = type == HC_T_F32;
     const bool x_fits = !fp32 && tile_rows(x, p.k, p.x_ld), w_fits = !fp32 && tile_rows(w, p.k, p.w_ld);
-    const bool in_tiles = L.pack || (x_fits && w_fits);
+    const bool in_tiles = L.pack_x || (x_fits && w_fits);
     Product g = {};
     g.passes = kOnePass;
     g.rows = p.m;
@@ -1445,11 +1457,11 @@ hipError_t launch_linear(const hc_linear_params& p, const Dropout& d, hc_type ty
         set(&g, ox, ow);
         return product<FORWARD>(g, type, TILED, s);
     }
-    e = packed(type, L.pack && !x_fits, x, p.m, p.k, p.x_ld, ws + L.x, L.k_ld, &ox, s);
-    if (e == hipSuccess) e = packed(type, L.pack && !w_fits, w, p.n, p.k, p.w_ld, ws + L.w, L.k_ld, &ow, s);
+    e = packed(type, L.pack_x && !x_fits, x, p.m, p.k, p.x_ld, ws + L.x, L.k_ld, &ox, s);
+    if (e == hipSuccess) e = packed(type, L.pack_w && !w_fits, w, p.n, p.k, p.w_ld, ws + L.w, L.k_ld, &ow, s);
     if (e != hipSuccess) return e;
     set(&g, ox, ow);
-    const Way way = way_of(g, type, in_tiles);
+    const Way way = way_of(FORWARD, g, type, in_tiles);
     if (way != SPLIT) return product<FORWARD>(g, type, way, s);
     if (type == HC_T_F32) return split_forward<float>(g, s);
     if (type == HC_T_BF16) return split_forward<__bf16>(g, s);
@@ -1464,12 +1476,14 @@ hipError_t launch_linear_grad(const hc_linear_params& p, const Dropout& d, hc_ty
     char* ws = static_cast<char*>(ws_);
     const bool fp32 = type == HC_T_F32, plain = p.act == HC_ACT_NONE && d.limit == 0;
     const bool x_fits = !fp32 && tile_rows(q.x, p.k, p.x_ld), w_fits = !fp32 && tile_rows(q.w, p.k, p.w_ld);
-    const bool in_tiles = L.pack || ((!q.dw || x_fits) && (!q.dx || w_fits) && p.n <= kMostTileLd && !fp32);
+    // dx goes by w, dw by x and db by dy: what else is wanted changes none of them
+    const bool dz_fits = p.n <= kMostTileLd;
+    const bool dx_in_tiles = L.pack_w || (w_fits && dz_fits), dw_in_tiles = L.pack_x || (x_fits && dz_fits);
     const bool rest = !plain && q.dw && !fp32 && (q.g_type == HC_T_F32 || q.g_type == HC_T_I32);
     Product dx = {}, dw = {};
     dx.part = dw.part = reinterpret_cast<float*>(ws + L.part);
     dx.cols = dw.cols = (uint32_t)p.k;
-    const bool planes = fp32 && in_tiles;
+    const bool planes = fp32 && L.pack_x;
     dx.passes = dw.passes = planes ? kTwoPlanes : kOnePass;
     dx.rows = dw.inner = p.m;
     dx.inner = dw.rows = p.n;
@@ -1484,12 +1498,14 @@ hipError_t launch_linear_grad(const hc_linear_params& p, const Dropout& d, hc_ty
     dw.gradient.ld = p.dw_ld;
     Gradient db = gradient;
     db.out = q.db;
-    const Way dx_way = way_of(dx, type, in_tiles), dw_way = way_of(dw, type, in_tiles);
-    // small layers go in one launch, where nothing is packed for it; db too if dz is dy
-    const bool together = !planes && (!dx.gradient.out || dx_way == SPLIT) && (!q.dw || dw_way == SPLIT);
+    const Way dx_way = way_of(DX, dx, type, dx_in_tiles), dw_way = way_of(DW, dw, type, dw_in_tiles);
+    // small products go in one launch, where nothing is packed for them; db too if dz is dy
+    const bool dx_split = dx.gradient.out && dx_way == SPLIT, dw_split = q.dw && dw_way == SPLIT;
+    const bool db_split = q.db && plain && p.m <= kSplitBias && p.m * p.n <= kSplitBiasElements;
     // dz is dy itself where nothing changes it and the products can take it
-    const bool dy_fits = plain && (planes || together || !in_tiles || tile_rows(q.dy, p.n, p.y_ld));
-    const bool dz = !dy_fits && (q.dx || q.dw), db_together = together && plain && p.m <= kSplitBias;
+    const bool tiles = !planes && ((dx.gradient.out && dx_way == TILED) || (q.dw && dw_way == TILED));
+    const bool dy_fits = plain && (!tiles || tile_rows(q.dy, p.n, p.y_ld));
+    const bool dz = !dy_fits && (q.dx || q.dw), db_pass = q.db && !db_split;
     hipError_t e = hipSuccess;
     Operand oz = {q.dy, p.y_ld, p.n, 0};
     float* col_most = reinterpret_cast<float*>(ws + L.col_most);
@@ -1497,7 +1513,7 @@ hipError_t launch_linear_grad(const hc_linear_params& p, const Dropout& d, hc_ty
         e = launch_fill_u32(reinterpret_cast<uint32_t*>(col_most), L.most, 0, s);
         if (e != hipSuccess) return e;
     }
-    if ((dz || (q.db && !db_together) || (planes && q.dw)) && p.m) {
+    if ((dz || db_pass || (planes && q.dw)) && p.m) {
         DzArgs a = {};
         a.dy = q.dy;
         a.z = q.z;
@@ -1518,7 +1534,7 @@ hipError_t launch_linear_grad(const hc_linear_params& p, const Dropout& d, hc_ty
             oz = {a.dz.out, L.n_ld, L.n_ld, a.dz.plane};
         }
         a.most = planes && q.dw ? col_most : nullptr;
-        a.part = q.db && !db_together ? reinterpret_cast<float*>(ws + L.bias) : nullptr;
+        a.part = db_pass ? reinterpret_cast<float*>(ws + L.bias) : nullptr;
         a.db = db;
         const dim3 grid((uint32_t)up(a.groups, L.width), (uint32_t)L.blocks);
         if (fp32) hipLaunchKernelGGL(dz_kernel<float>, grid, dim3(256), 0, s, a);
@@ -1527,28 +1543,31 @@ hipError_t launch_linear_grad(const hc_linear_params& p, const Dropout& d, hc_ty
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (q.db && !db_together && L.blocks != 1) {
+    if (db_pass && L.blocks != 1) {
         hipLaunchKernelGGL(bias_kernel, dim3((uint32_t)up(p.n, 16)), dim3(1024), 0, s,
                            reinterpret_cast<const float*>(ws + L.bias), (uint32_t)L.blocks, (uint32_t)p.n, db);
         e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (together) {
-        set(&dx, oz, {q.w, p.w_ld, p.k, 0});
-        set(&dw, oz, {q.x, p.x_ld, p.k, 0});
+    if (dx_split || dw_split || db_split) {
         SplitGrad g = {};
-        g.dx = dx;
-        g.dw = dw;
-        if (db_together && q.db) {
+        if (dx_split) {
+            g.dx = dx;
+            set(&g.dx, oz, {q.w, p.w_ld, p.k, 0});
+        }
+        if (dw_split) {
+            g.dw = dw;
+            set(&g.dw, oz, {q.x, p.x_ld, p.k, 0});
+        }
+        if (db_split) {
             g.dy = p.m ? q.dy : ws;  // not read without rows
             g.dy_ld = p.y_ld;
             g.m = p.m;
             g.n = (uint32_t)p.n;
             g.db = db;
         }
-        if (fp32) return split_grad<float>(g, s);
-        if (type == HC_T_BF16) return split_grad<__bf16>(g, s);
-        return split_grad<_Float16>(g, s);
+        e = fp32 ? split_grad<float>(g, s) : type == HC_T_BF16 ? split_grad<__bf16>(g, s) : split_grad<_Float16>(g, s);
+        if (e != hipSuccess) return e;
     }
     if (planes && p.m) {
         float* row_most = reinterpret_cast<float*>(ws + L.row_most);
@@ -1579,20 +1598,20 @@ hipError_t launch_linear_grad(const hc_linear_params& p, const Dropout& d, hc_ty
         }
         return e;
     }
-    if (dx.gradient.out) {
+    if (dx.gradient.out && !dx_split) {
         Operand ow;
-        e = packed(type, L.pack && !w_fits, q.w, p.n, p.k, p.w_ld, ws + L.w, L.k_ld, &ow, s);
+        e = packed(type, dx_way == TILED && !w_fits, q.w, p.n, p.k, p.w_ld, ws + L.w, L.k_ld, &ow, s);
         if (e != hipSuccess) return e;
         set(&dx, oz, ow);
-        e = product<DX>(dx, type, dx_way == SPLIT ? (in_tiles ? TILED : DIRECT) : dx_way, s);
+        e = product<DX>(dx, type, dx_way, s);
         if (e != hipSuccess) return e;
     }
-    if (q.dw) {
+    if (q.dw && !dw_split) {
         Operand ox;
-        e = packed(type, L.pack && !x_fits && p.m, q.x, p.m, p.k, p.x_ld, ws + L.x, L.k_ld, &ox, s);
+        e = packed(type, dw_way == TILED && !x_fits, q.x, p.m, p.k, p.x_ld, ws + L.x, L.k_ld, &ox, s);
         if (e != hipSuccess) return e;
         set(&dw, oz, ox);
-        return product<DW>(dw, type, dw_way == SPLIT ? (in_tiles ? TILED : DIRECT) : dw_way, s);
+        return product<DW>(dw, type, dw_way, s);
     }
     return hipSuccess;
 }

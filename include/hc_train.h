@@ -214,8 +214,11 @@ hc_status hc_linear(const hc_linear_params *p, hc_type type, const void *x, cons
  * (NaN: 0).  accumulate != 0 adds them to what dw and db hold (int32 saturating).
  *   16-bit types: dx, and a 16-bit dw, take dz rounded to `type`; a dw of
  * HC_T_F32 or HC_T_I32 takes it in three bf16 parts (24 bits) or two fp16 ones
- * (22 bits), three or two times the products.  Without activation and dropout dz
- * is dy.  db takes dz unrounded.
+ * (22 bits), three or two times the products.  An fp16 dz is held in units of 2^e, the
+ * smallest power of two, 1 or more, that dropout's scale times the largest slope (1.13
+ * for GELU and SiLU, 1 otherwise) does not exceed: it does not overflow, and below its
+ * normal range it is up to 2^(e - 25) off, in two parts 2^(e - 36).  Without activation
+ * and dropout dz is dy.  db takes dz unrounded.
  *   m = 0 gives zeros.  Order, fp32 parts (there by the rows of dz and the columns
  * of w, the columns of dz and of x) and infinities as in hc_linear; dx goes by w's
  * stride and address, dw by x's and by g_type, db by neither, all by whether dz is dy,

@@ -268,6 +268,7 @@ struct Gradient {
     uint32_t type;  // hc_type
     uint32_t accumulate;
     float fixed;
+    float unit;     // of a product with an fp16 dz: what its sums are multiplied by
 };
 
 template <typename T>

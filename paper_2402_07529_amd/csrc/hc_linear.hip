@@ -106,6 +106,13 @@ struct Product {
     Gradient gradient;
 };
 
+// Sums of a product with dz, back from the units that an fp16 dz is held in.
+template <typename T> __device__ __forceinline__ void from_units(const Gradient& g, float (&v)[8]) {
+    if constexpr (std::is_same<T, _Float16>::value)
+#pragma unroll
+        for (int e = 0; e < 8; e++) v[e] *= g.unit;
+}
+
 template <Kind KIND, typename T>
 __device__ __forceinline__ void finish8(const Product& g, const Masks& masks, uint64_t row, uint32_t col,
                                         float (&v)[8]) {
@@ -117,10 +124,10 @@ __device__ __forceinline__ void finish8(const Product& g, const Masks& masks, ui
         if (f.bias) load8(static_cast<const T*>(f.bias) + col, count, bias);
         if (f.residual) load8_raw(static_cast<const T*>(f.residual) + row * f.residual_ld + col, count, residual);
         finish_forward<T>(f, masks, row, g.rows, col, count, bias, residual, v);
-    } else if constexpr (KIND == DX) {
-        store8(static_cast<T*>(g.gradient.out) + row * g.gradient.ld + col, count, v);
     } else {
-        store_gradient(g.gradient, row, col, count, v);
+        from_units<T>(g.gradient, v);
+        if constexpr (KIND == DX) store8(static_cast<T*>(g.gradient.out) + row * g.gradient.ld + col, count, v);
+        else store_gradient(g.gradient, row, col, count, v);
     }
 }
 
@@ -665,6 +672,7 @@ __device__ __forceinline__ void finish_rows(const Product& g, const Masks& masks
             const uint64_t row = row0 + 16 * u;
             unscale(row, v);
             if (row >= g.rows || count == 0) return;
+            from_units<T>(g.gradient, v);
             if constexpr (KIND == DX) store8(static_cast<T*>(g.gradient.out) + row * g.gradient.ld + col, count, v);
             else store_gradient(g.gradient, row, col, count, v);
         });
@@ -933,6 +941,17 @@ __global__ __launch_bounds__(256) void split_columns_kernel(PackArgs a, const fl
     store_two(a.out, a.plane, row * a.out_ld + col, v, scale);
 }
 
+// An fp16 dz, up to 65504 times dropout's scale and the largest slope, is held in units of
+// the power of two that takes both in, so that it does not overflow: that costs nothing
+// in its normal range, and what is lost below it, 2^-25 units, is less than twice what dy,
+// off by 2^-25 itself, brings along.  The sums are multiplied by the unit.
+float dz_unit(uint32_t act, const Dropout& d) {
+    const float slope = act == HC_ACT_GELU || act == HC_ACT_SILU ? 1.13f : 1.0f;
+    float unit = 1.0f;
+    while (unit < d.scale * slope) unit *= 2.0f;
+    return unit;
+}
+
 // v = the sum of three bf16 values, exactly where v is no smaller than 2^-110.
 // Infinity leaves nothing, NaN is NaN in all.
 __device__ __forceinline__ void split3(float v, __bf16 (&w)[3]) {
@@ -954,6 +973,7 @@ struct DzArgs {
     Dropout drop;
     PackArgs dz;       // where it goes (out: or null), zeros behind its columns
     uint32_t planes;   // 1: in its own type; 2: and 2^11 times the rest; 3: bf16 parts
+    float per_unit;    // fp16: dz is multiplied by it, 1 / its unit
     float* most;       // fp32: the largest of each column, or null
     float* part;       // the workgroups' sums, [blocks][n], or null
     Gradient db;       // one workgroup along the rows: the sums themselves
@@ -1004,6 +1024,9 @@ template <typename T> __global__ __launch_bounds__(256) void dz_kernel(DzArgs a)
                 for (int k = 0; k < 3; k++)
                     *reinterpret_cast<b8*>(static_cast<__bf16*>(a.dz.out) + k * a.dz.plane + at) = w[k];
             } else {
+                if constexpr (std::is_same<T, _Float16>::value)
+#pragma unroll
+                    for (int e = 0; e < 8; e++) v[e] *= a.per_unit;
                 store8(static_cast<T*>(a.dz.out) + at, 8, v);
                 if (a.planes == 2) {
                     // infinity and NaN leave nothing
@@ -1488,10 +1511,12 @@ hipError_t launch_linear_grad(const hc_linear_params& p, const Dropout& d, hc_ty
     dx.rows = dw.inner = p.m;
     dx.inner = dw.rows = p.n;
     if (rest) dw.passes = type == HC_T_BF16 ? kRestBf16 : kRestF16;
-    const Gradient gradient = {nullptr, 0, (uint32_t)q.g_type, q.accumulate ? 1u : 0u, p.fixed};
+    const float unit = dz_unit(p.act, d);
+    const Gradient gradient = {nullptr, 0, (uint32_t)q.g_type, q.accumulate ? 1u : 0u, p.fixed, unit};
     dw.gradient = gradient;
     if (p.m) {
         dx.gradient.out = q.dx;
+        dx.gradient.unit = unit;
         dx.gradient.ld = p.dx_ld;
     }
     dw.gradient.out = q.dw;
@@ -1530,6 +1555,7 @@ hipError_t launch_linear_grad(const hc_linear_params& p, const Dropout& d, hc_ty
             a.dz.out = ws + L.dz;
             a.dz.out_ld = L.n_ld;
             a.dz.plane = p.m * L.n_ld;
+            a.per_unit = 1.0f / unit;
             a.planes = !rest ? 1 : type == HC_T_BF16 ? 3 : 2;
             oz = {a.dz.out, L.n_ld, L.n_ld, a.dz.plane};
         }

@@ -207,6 +207,7 @@ hc_status hc_linear(const hc_linear_params *p, hc_type type, const void *x, cons
 /* dz = act'(z) * mask * dy, then dx = dz w, dw = dz^T x and db = the sum of dz's
  * rows; each may be NULL (not wanted), and x, w, z where nothing wanted reads
  * them (w: dx; x: dw; z: an activation).  The residual's gradient is dy itself.
+ * A dropped element's dz is 0, whatever dy and z hold there.
  * dy, x, w, z and dx: `type`.  z holds what hc_linear wrote there (for HC_ACT_RELU
  * y itself does where there is neither dropout nor residual).
  *   dw and db: g_type, fp32 sums rounded once, or HC_T_I32: a sum times `fixed`,

@@ -995,12 +995,21 @@ template <typename T> __global__ __launch_bounds__(256) void dz_kernel(DzArgs a)
         for (uint64_t row = (uint64_t)blockIdx.y * a.per + sub; row < end; row += step) {
             float v[8];
             load8(static_cast<const T*>(a.dy) + row * a.dy_ld + col, count, v);
-            if (masks.limit) drop8(masks, (uint32_t)row, group, v);
+            MaskBits bits = {};
+            if (masks.limit) {
+                bits = mask_bits(masks, (uint32_t)row, group);
+#pragma unroll
+                for (int e = 0; e < 8; e++) v[e] *= masks.scale;
+            }
             if (a.act != HC_ACT_NONE) {
                 float z[8];
                 load8(static_cast<const T*>(a.z) + row * a.z_ld + col, count, z);
                 backward8<T>(a.act, z, v);
             }
+            // after the slope, which may be NaN: a dropped element is 0 whatever z was
+            if (masks.limit)
+#pragma unroll
+                for (int e = 0; e < 8; e++) v[e] = bits.kept(e, masks.limit) ? v[e] : 0.0f;
             if (count < 8)
 #pragma unroll
                 for (int e = 0; e < 8; e++) v[e] = (uint32_t)e < count ? v[e] : 0.0f;

@@ -1,4 +1,5 @@
-"""The linear layer's gradient at the ends of fp16: output gradients near its largest and smallest values.
+"""The linear layer's gradient at the ends of fp16, output gradients near its largest and smallest values; and
+what stands in places that dropout drops.
 
 fp16: dz is held in units of 2^e, the smallest power of two no less than dropout's scale times the largest
 slope (1.13 for gelu and silu, else 1), at least 1.  So none overflows, and what fp16 holds below its normal
@@ -8,7 +9,7 @@ import math
 import pytest
 
 import layer_reference as ref
-from test_gpu_linear import SLOPE, Layer, _f, _hc, _within
+from test_gpu_linear import SLOPE, TYPES, Layer, _f, _hc, _within
 
 pytestmark = pytest.mark.gpu
 
@@ -93,3 +94,32 @@ def test_fp16_output_gradients_near_the_smallest(m, n, k, act, p, out):
     sizes = 2.0 ** -torch.randint(8, 25, (m, n), generator=torch.Generator().manual_seed(n)).float()
     L.dy.mul_(sizes.cuda())
     _run(torch, hc, L, act, p, out, 1.0)
+
+
+@pytest.mark.parametrize("m,n,k", [(90, 80, 70), (1030, 1000, 520)])
+@pytest.mark.parametrize("act", ["relu", "gelu", "silu", "tanh", "sigmoid"])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_a_dropped_element_has_no_gradient_whatever_z_holds(m, n, k, act, dtype):
+    torch, hc = _hc()
+    L = Layer(torch, m, n, k, dtype, seed=6)
+    dropped = (torch.from_numpy(ref.factors(m, n, 0.5, 8, 9)) == 0).cuda()
+    ws = hc.alloc_linear_grad_workspace(L.x, L.w)
+
+    def grads(z):
+        dx, dw = torch.empty_like(L.x), torch.empty(n, k, device="cuda")
+        db = torch.empty(n, device="cuda")
+        hc.hc_linear_grad(L.dy, ws, x=L.x, w=L.w, z=z, dx=dx, dw=dw, db=db, act=act, p=0.5, seed=8, draw=9)
+        return dx, dw, db
+
+    want = grads(L.z)
+    for bad in (float("nan"), float("inf"), float("-inf")):
+        got = grads(torch.where(dropped, bad, L.z))
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), bad
+    # one that is kept stays: in its row of dx and dw, and in db
+    i, j = (int(v) for v in (~dropped).nonzero()[37])
+    z = L.z.clone()
+    z[i, j] = float("nan")
+    dx, dw, db = grads(z)
+    for t, rows in ((dx, i), (dw, j), (db, j)):
+        bad = torch.isnan(t).reshape(t.shape[0], -1)
+        assert bool(bad[rows].all()) and int(bad.any(1).sum()) == 1

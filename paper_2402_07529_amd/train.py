@@ -320,7 +320,7 @@ def _vector(t, name, dtype, n, device):
         return None
     if t.get_device() != device:
         _here(t, name, device)
-    if t.dtype != dtype or t.numel() < n or not t.is_contiguous():
+    if t.dtype != dtype or t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{name} must be {n} contiguous elements of {dtype}, not {t.dtype} {tuple(t.shape)}")
     return t.data_ptr()
 
@@ -332,10 +332,12 @@ def _workspace(ws, device):
 
 
 def _counter(t, device):
+    """Pointer of the counter, the first element where there are more."""
     if t is None:
         return None
     import torch
-    return _vector(t, "counter", torch.uint64 if t.dtype == getattr(torch, "uint64", None) else torch.int64, 1, device)
+    dtype = torch.uint64 if t.dtype == getattr(torch, "uint64", None) else torch.int64
+    return _vector(t, "counter", dtype, max(1, t.numel()), device)
 
 
 _LOW = 2**64 - 1

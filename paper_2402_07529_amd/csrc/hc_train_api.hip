@@ -318,7 +318,7 @@ hc_status hc_linear(const hc_linear_params* p, hc_type type, const void* x, cons
         return fail(HC_EINVAL, "buffers must be aligned to their elements");
     if (y == residual && p->y_ld != p->residual_ld)
         return fail(HC_EINVAL, "in place the strides must be the same");
-    if (y == x || y == w || z == y || (z && (z == x || z == w || z == residual)))
+    if (y == x || y == w || y == bias || z == y || (z && (z == x || z == w || z == bias || z == residual)))
         return fail(HC_EINVAL, "outputs overlap inputs or each other");
     if (!aligned(ws, 256)) return fail(HC_EINVAL, "ws must be 256-byte aligned");
     if (ws_bytes < linear_bytes(*p, type))
@@ -359,6 +359,9 @@ hc_status hc_linear_grad(const hc_linear_params* p, hc_type type, const void* dy
     for (const void* out : {(const void*)dx, (const void*)dw, (const void*)db})
         if (out && (out == dy || out == x || out == w || (out == z && p->act != HC_ACT_NONE)))
             return fail(HC_EINVAL, "outputs overlap inputs");
+    // without rows there is no dx
+    if ((dw && dw == db) || (dx && p->m != 0 && (dx == dw || dx == db)))
+        return fail(HC_EINVAL, "outputs overlap each other");
     if (!aligned(ws, 256)) return fail(HC_EINVAL, "ws must be 256-byte aligned");
     if (ws_bytes < linear_grad_bytes(*p, type))
         return fail(HC_EWORKSPACE, "workspace smaller than hc_linear_grad_bytes reports");

@@ -1,8 +1,8 @@
 // hc_dropout.hip -- dropout and its gradient (include/hc_train.h).
 //
 // A lane takes eight elements of a row, one call of the generator, four times 256
-// groups apart.  Memory bounds it: 393216 x 512 (fp16) 137 us, 5.9 TB/s of reads and
-// writes; 32768 x 768 (bf16) with a residual 25, 6.0 TB/s (a plain copy 4.4 to 4.8).
+// groups apart.  Memory bounds it: a call for 393216 x 512 (fp16) takes 137 us, 5.9 TB/s
+// of reads and writes; for 32768 x 768 (bf16) with a residual 26, 5.7 (a plain copy 4.4 to 4.8).
 // The generator alone would take 86 and 11 us of the vector units.
 #include "hc_layer.h"
 
@@ -16,7 +16,7 @@ constexpr int kBlock = 256;
 constexpr uint32_t kPer = 4;
 constexpr uint64_t kFewGroups = 1024ull * kBlock;
 // Results that the L2s cannot keep pass them by, and so does what is read for them:
-// 32768 x 768 (bf16) with a residual 29.5 -> 25 us, 393216 x 512 (fp16) 141 -> 137.
+// 32768 x 768 (bf16) with a residual 29.5 -> 26 us, 393216 x 512 (fp16) 141 -> 137.
 constexpr uint64_t kPastBytes = 32ull << 20;
 
 struct DropoutArgs {

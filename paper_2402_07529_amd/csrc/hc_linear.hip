@@ -9,19 +9,22 @@
 // column sums (db) too, since both products read it.
 //
 // Precision.  Products of 16-bit types are exact and summed in fp32; dz is rounded to
-// the type for dx and for a 16-bit dw, and taken in two or three parts for a wider one.
-// fp32: large products as three of fp16 parts (22 bits), others by fp32 matrix
-// instructions.  Sums are taken in an order that the shape fixes; partial sums of a
-// tile's pieces are joined in order.
+// the type for dx and for a 16-bit dw, whose results are rounded to it too (bf16: 2.3e-3
+// off in all, 1.7e-3 by the result alone; each further part of dz is another product),
+// and taken in two or three parts for a wider one.  fp32: large products as three of
+// fp16 parts (22 bits), others by fp32 matrix instructions.  Sums are taken in an order
+// that shape, type, strides and the 16-byte alignment of 16-bit operands fix; partial
+// sums of a tile's pieces are joined in order.
 //
 // Three ways.  Tiles of 256, 128 or 64 fed from memory to LDS directly, which need
 // rows that are read 16 bytes at a time (others are copied where that pays); small
 // tiles whose eight waves share l, for products that are a chain of latencies; and
-// 64-tiles through registers, which take anything.  Host estimates pick one.
+// 64-tiles through registers, which take anything.  Host estimates pick one for each
+// product by itself.
 //
 // What bounds it (MI355X, a library product of 8192^3 reaches 1.29 to 1.37 PFLOP/s).
-// Large products the matrix cores: 4096 x 4096 x 25088 in bf16 takes 665 us without
-// epilogue (1.27 PFLOP/s), its dx and dw 675.  With l of a few hundred the tiles'
+// Large products the matrix cores: 4096 x 4096 x 25088 in bf16 takes 666 us without
+// epilogue (1.26 PFLOP/s), its dx and dw 683 and 695.  With l of a few hundred the tiles'
 // way through L2: 32768 x 768 x 768 (bf16) 57 us in 128-tiles, 40 of them products
 // (600 MB from L2) and 17 results, hardly overlapped; 256-tiles read half of that but
 // are one round and a half of the CUs.
@@ -198,7 +201,7 @@ __device__ __forceinline__ void direct_store(T* s, const T (&v)[8]) {
 // A 64 x 64 tile, or a piece of one, a workgroup of four waves, each 32 x 32 of
 // it.  Loads go through registers, which takes any stride, alignment and length,
 // zeros where a matrix ends.  fp32: 75 TFLOP/s of the matrix instructions' 157, and
-// 65536 x 64 x 128 in 17 us, whose memory takes 10.
+// 65536 x 64 x 128 in 17 us, whose memory takes 8 to 10.
 template <Kind KIND, typename T>
 __global__ __launch_bounds__(256) void direct_kernel(Product g) {
     constexpr bool PS = KIND == DW, QS = KIND != FORWARD;

@@ -53,3 +53,33 @@ def test_a_gradient_is_the_same_alone(m, n, k, dtype, act):
             assert torch.equal(dx, ax) and torch.equal(dx, bx), ("dx", where)
             assert torch.equal(dw, aw) and torch.equal(dw, bw), ("dw", where)
             assert torch.equal(db, ab) and torch.equal(db, bb), ("db", where)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("act", ["none", "gelu"])
+def test_small_and_large_products_of_a_call_captured_and_replayed(dtype, act):
+    """dx and db small beside a dw in tiles, in a graph, against the eager call."""
+    torch, hc = _hc()
+    L = Layer(torch, 16, 768, 768, dtype)
+    ws = hc.alloc_linear_grad_workspace(L.x, L.w)
+    kw = dict(x=L.x, w=L.w, z=L.z if act != "none" else None, act=act, p=0.2 if act == "gelu" else 0.0, seed=3)
+
+    def outs():
+        return dict(dx=torch.empty_like(L.x), dw=torch.empty(768, 768, device="cuda"),
+                    db=torch.empty(768, device="cuda"))
+
+    got, want, side, graph = outs(), outs(), torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    hc.hc_linear_grad(L.dy, ws, **kw, **got)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        hc.hc_linear_grad(L.dy, ws, **kw, **got)
+    for _ in range(3):
+        L.dy.mul_(0.5)         # eager work between the replays
+        for t in got.values():
+            t.fill_(float("nan"))
+        ws.fill_(0xFF)
+        graph.replay()
+        torch.cuda.synchronize()
+        hc.hc_linear_grad(L.dy, ws, **kw, **want)
+        assert all(torch.equal(got[name], want[name]) for name in got)
+        torch.cuda.synchronize()
